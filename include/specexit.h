@@ -139,9 +139,29 @@ typedef struct {
   const int32_t *page_table_d;  /* [batch, max_pages] */
   int32_t max_pages;
   int32_t num_pages;            /* physical pages in k_pages_d / v_pages_d */
-  void *k_pages_d;              /* [num_pages, n_kv, page_size, head_dim] bf16 */
+  void *k_pages_d;              /* [num_pages, n_kv, page_size, head_dim] bf16, or e4m3 codes (dtype) */
   void *v_pages_d;
+  int32_t dtype;                /* SX_KV_BF16 (0) or SX_KV_E4M3 */
+  int32_t n_groups;             /* SX_KV_E4M3: groups of sequences that share a prefix; 0: none (see sx_attention) */
+  uint8_t *k_scale_d;           /* SX_KV_E4M3: [num_pages, n_kv, page_size] exponent bytes of the rows; 16-byte aligned */
+  uint8_t *v_scale_d;
+  const int32_t *group_start_d; /* [n_groups + 1] ascending from 0 to batch: group g is the sequences
+                                   group_start_d[g] .. group_start_d[g + 1] - 1 */
+  const int32_t *prefix_len_d;  /* [n_groups] slots that the members of the group have in common */
 } sx_kv;
+
+/* Element type of the cache.  SX_KV_E4M3 keeps a row (one token of one KV head) as e4m3 codes with one power-of-two
+ * scale 2^e, e = ceil(log2(max |x| / 448)) held to [-64, 120] (0 for a row of zeros), stored as the byte e + 127;
+ * code = e4m3(x * 2^-e), round to nearest even.  x * 2^-e and code * 2^e are exact, so the rounding to 4
+ * significand bits is all that is lost (values below 2^-10 of a row's largest keep fewer).  A row with a value
+ * that is not finite has the byte 255 and codes of zero, and reads as NaN.  Half the bytes of bf16 and one byte
+ * per row.  Needs a page size that is a multiple of 16; the draft step also needs head_dim 64 or 128. */
+enum { SX_KV_BF16 = 0, SX_KV_E4M3 = 1 };
+
+/* Shape of a cache for the calls that take no context. */
+typedef struct {
+  int32_t n_q_heads, n_kv_heads, head_dim, page_size;
+} sx_kv_shape;
 
 typedef struct {
   int32_t mode;        /* SX_MODE_CHAIN | SX_MODE_TREE */
@@ -275,6 +295,50 @@ sx_status sx_tile_weight(const void *src_d, int32_t N, int32_t K, void *dst_d, v
  * state, read when a call is issued. */
 enum { SX_ATTN_AUTO = 0, SX_ATTN_SPLIT = 1, SX_ATTN_TC = 2 };
 sx_status sx_set_attention(sx_ctx *ctx, int32_t kernel);
+
+/* Rows into an 8-bit cache (kv->dtype == SX_KV_E4M3; no context needed): the keys and values of new tokens, for a
+ * prompt, a decode step of a batch, or both.  The rows of sequence b are row_start_d[b] .. row_start_d[b + 1] - 1
+ * of the buffers (row_start_d [batch + 1], ascending; a sequence may have none; rows behind the last sequence, up to
+ * T, are padding and ignored) and go to its slots pos_start_d[b], pos_start_d[b] + 1, ... (pos_start_d = NULL:
+ * cache_len_d[b]).  cache_len_d is not advanced.  K as the attention wants it (rotated).
+ *   k_d, v_d   [T, n_kv, head_dim] bf16, k_stride / v_stride elements from row to row (a multiple of 8, at least
+ *              n_kv * head_dim: the projection's output can be given as it is); head_dim 16, 32, 64 or 128
+ * A row whose page does not exist is skipped and reported as SX_ERR_CAPACITY, as are starts that do not ascend.
+ * Two sequences must not write one slot in the same call (a shared page belongs to the prefix, which is written
+ * through one of them). */
+sx_status sx_kv_append(const sx_kv_shape *shape, const sx_kv *kv, int32_t T, const int32_t *row_start_d,
+                       const int32_t *pos_start_d, const void *k_d, int64_t k_stride, const void *v_d, int64_t v_stride,
+                       int32_t *status_d, void *stream);
+
+/* The way back: slots pos_start_d[b] .. of every sequence to bf16 rows (exact), arguments as above with the buffers
+ * written; pos_start_d is needed.  Rows behind the last sequence, and rows that are reported, stay as they are. */
+sx_status sx_kv_read(const sx_kv_shape *shape, const sx_kv *kv, int32_t T, const int32_t *row_start_d,
+                     const int32_t *pos_start_d, void *k_d, int64_t k_stride, void *v_d, int64_t v_stride,
+                     int32_t *status_d, void *stream);
+
+/* Decode attention over an 8-bit cache (no context needed; the draft step runs the same kernels when it is given such a
+ * cache).  Sequence b has `rows` query rows (1..64), row r = b * rows + j, each with n_q_heads heads; a row sees the
+ * slots [0, cache_len_d[b]) and, of the `drafted` (0..64) slots behind them, those whose bit is set in row_mask_d[r]
+ * (NULL: all).  Softmax of scale * q.k; an output row that sees no slot is zero.  What a slot holds that a row
+ * does not see never reaches that row, whatever it is.
+ *   q_d [batch * rows, n_q_heads, head_dim] bf16, q_stride elements from row to row (a multiple of 8)
+ *   o_d [batch * rows, n_q_heads, head_dim] bf16
+ * head_dim 64 or 128; n_q_heads a multiple of n_kv_heads; batch + n_groups <= 1024, batch * rows <= 65535.
+ *
+ * Shared prefix (kv->n_groups > 0): the members of a group hold the same keys and values in their first
+ * prefix_len_d[g] slots - sampled answers to one question.  Those slots are read once, through the page table of
+ * the group's first member, for the queries of all members together; every member's own slots follow from its own
+ * table.  Whether the tables share the pages makes no difference to the result.  prefix_len_d[g] may end inside a page
+ * and may be 0.  A prefix longer than a member's cache_len, or groups that do not cover the batch in order, are
+ * reported as SX_ERR_CAPACITY and the sequences concerned read their own tables.
+ *
+ * kernel: SX_ATTN_AUTO, or SX_ATTN_SPLIT / SX_ATTN_TC to force one (see sx_set_attention; SX_ATTN_TC needs
+ * head_dim 128).  Workspace (256-byte aligned, not shared by calls that may overlap): sx_attention_ws_bytes for the
+ * current device, or 0 for a shape that cannot be. */
+size_t sx_attention_ws_bytes(const sx_kv_shape *shape, int32_t batch, int32_t rows, int32_t n_groups);
+sx_status sx_attention(const sx_kv_shape *shape, const sx_kv *kv, int32_t rows, int32_t drafted, const void *q_d,
+                       int64_t q_stride, const uint64_t *row_mask_d, float scale, int32_t kernel, void *o_d, void *ws_d,
+                       size_t ws_bytes, int32_t *status_d, void *stream);
 
 /* Stochastic acceptance: speculative sampling, the acceptance rule of the speculative-decoding
  * scheme the method builds on (Section 2, background on speculative decoding; Algorithm 1,

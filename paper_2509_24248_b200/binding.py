@@ -24,13 +24,15 @@ ACT_SIGMOID, ACT_EXPM1, ACT_IDENTITY = 0, 1, 2
 DIR_GT, DIR_LT = 0, 1
 EMA_VERIFIED_CONTEXT, EMA_FIRST_ONLY = 0, 1
 ATTN_AUTO, ATTN_SPLIT, ATTN_TC = 0, 1, 2
+KV_BF16, KV_E4M3 = 0, 1
 SMOOTH_EWMA, SMOOTH_NONE, SMOOTH_WINDOW, SMOOTH_MOMENTUM, SMOOTH_PARAGRAPH = 0, 1, 2, 3, 4
 HIST = 16
 
 EXPORTS = ["sx_create", "sx_destroy", "sx_workspace_bytes", "sx_strerror", "sx_launch_count",
            "sx_draft_step", "sx_verify", "sx_exit_update", "sx_spec_exit_iter",
            "sx_spec_exit_iter_host", "sx_profile_begin", "sx_profile_end", "sx_verify_noalloc", "sx_commit",
-           "sx_set_sampling", "sx_tiled_weight_bytes", "sx_tile_weight", "sx_selftest_bounded_wait", "sx_set_attention"]
+           "sx_set_sampling", "sx_tiled_weight_bytes", "sx_tile_weight", "sx_selftest_bounded_wait", "sx_set_attention",
+           "sx_kv_append", "sx_kv_read", "sx_attention", "sx_attention_ws_bytes"]
 PROF_CLASSES = ["head_draft", "head_verify", "gemm_fc", "gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down",
                 "attention"]
 
@@ -56,7 +58,13 @@ class Weights(C.Structure):
 class KV(C.Structure):
     _fields_ = [("batch", C.c_int32), ("cache_len_d", C.c_void_p), ("page_table_d", C.c_void_p),
                 ("max_pages", C.c_int32), ("num_pages", C.c_int32), ("k_pages_d", C.c_void_p),
-                ("v_pages_d", C.c_void_p)]
+                ("v_pages_d", C.c_void_p), ("dtype", C.c_int32), ("n_groups", C.c_int32),
+                ("k_scale_d", C.c_void_p), ("v_scale_d", C.c_void_p), ("group_start_d", C.c_void_p),
+                ("prefix_len_d", C.c_void_p)]
+
+
+class KVShape(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32)]
 
 
 class DraftCfg(C.Structure):
@@ -139,6 +147,15 @@ def load_library() -> C.CDLL:
     lib.sx_set_attention.argtypes = [vp, i32]
     lib.sx_selftest_bounded_wait.restype = i32
     lib.sx_selftest_bounded_wait.argtypes = [C.c_uint32, i32, vp, vp, vp]
+    i64 = C.c_int64
+    lib.sx_kv_append.restype = lib.sx_kv_read.restype = i32
+    lib.sx_kv_append.argtypes = lib.sx_kv_read.argtypes = [C.POINTER(KVShape), C.POINTER(KV), i32, vp, vp, vp, i64, vp,
+                                                           i64, vp, vp]
+    lib.sx_attention_ws_bytes.restype = sz
+    lib.sx_attention_ws_bytes.argtypes = [C.POINTER(KVShape), i32, i32, i32]
+    lib.sx_attention.restype = i32
+    lib.sx_attention.argtypes = [C.POINTER(KVShape), C.POINTER(KV), i32, i32, vp, i64, vp, C.c_float, i32, vp, vp, sz,
+                                 vp, vp]
     lib.sx_verify_noalloc.restype = i32
     lib.sx_verify_noalloc.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
     _lib = lib
@@ -216,6 +233,156 @@ def sx_verify_noalloc(target_head: torch.Tensor, target_hidden: torch.Tensor, ca
                                  _p(parent), out["target_tok"].data_ptr(), out["accept_len"].data_ptr(),
                                  out["path"].data_ptr(), int(out["path"].shape[1]), out["recover_tok"].data_ptr(),
                                  status.data_ptr(), torch.cuda.current_stream().cuda_stream), "sx_verify_noalloc")
+
+
+_CACHE_NAMES = ("k_pages", "v_pages", "k_scale", "v_scale", "page_table", "cache_len", "group_start", "prefix_len")
+
+
+def _kv_struct(kv: Dict[str, torch.Tensor], n_kv: int, page: int, d: int) -> KV:
+    """Argument block of a paged cache; an 8-bit one (codes in one byte per value) carries its exponent bytes and, if
+    it has them, its groups.  Checks what the C side cannot see: types, shapes, contiguity, one device."""
+    dev = kv["k_pages"].device
+    for name in _CACHE_NAMES:
+        t = kv.get(name)
+        if t is not None and (not t.is_cuda or t.device != dev or not t.is_contiguous()):
+            raise SxError(f"{name} must be contiguous on {dev}")
+    for name in ("page_table", "cache_len", "group_start", "prefix_len"):
+        if kv.get(name) is not None and kv[name].dtype != torch.int32:
+            raise SxError(f"{name} must be int32")
+    pool = tuple(kv["k_pages"].shape)
+    if len(pool) != 4 or pool[1:] != (n_kv, page, d) or tuple(kv["v_pages"].shape) != pool:
+        raise SxError(f"k_pages and v_pages must be [num_pages, {n_kv}, {page}, {d}]")
+    B = int(kv["cache_len"].numel())
+    if kv["page_table"].dim() != 2 or int(kv["page_table"].shape[0]) != B:
+        raise SxError("page_table must be [batch, max_pages], one row per cache_len")
+    st = KV(B, kv["cache_len"].data_ptr(), kv["page_table"].data_ptr(), int(kv["page_table"].shape[1]), pool[0],
+            kv["k_pages"].data_ptr(), kv["v_pages"].data_ptr())
+    if kv["k_pages"].element_size() != 1:
+        if kv["k_pages"].dtype != torch.bfloat16 or kv["v_pages"].dtype != torch.bfloat16:
+            raise SxError("pages must be bf16, or 8-bit codes (uint8 or float8_e4m3fn)")
+        if kv.get("group_start") is not None or kv.get("k_scale") is not None:
+            raise SxError("groups and exponent bytes belong to an 8-bit cache")
+        return st
+    for name in ("k_pages", "v_pages"):
+        if kv[name].dtype not in (torch.uint8, torch.float8_e4m3fn):
+            raise SxError(f"{name} must be uint8 or float8_e4m3fn")
+    for name in ("k_scale", "v_scale"):
+        t = kv.get(name)
+        if t is None or t.dtype != torch.uint8 or tuple(t.shape) != pool[:3]:
+            raise SxError(f"{name} must be uint8 [num_pages, {n_kv}, {page}]")
+    st.dtype = KV_E4M3
+    st.k_scale_d, st.v_scale_d = kv["k_scale"].data_ptr(), kv["v_scale"].data_ptr()
+    if kv.get("group_start") is not None:
+        n = int(kv["group_start"].numel()) - 1
+        if n < 1 or kv.get("prefix_len") is None or int(kv["prefix_len"].numel()) != n:
+            raise SxError("group_start must be [n_groups + 1] and prefix_len [n_groups]")
+        st.n_groups = n
+        st.group_start_d, st.prefix_len_d = kv["group_start"].data_ptr(), kv["prefix_len"].data_ptr()
+    return st
+
+
+class KV8:
+    """An 8-bit paged cache and the operators over it (no draft model needed).
+
+    ``kv`` holds ``k_pages`` / ``v_pages`` (uint8 or float8_e4m3fn ``[num_pages, n_kv, page, d]``), ``k_scale`` /
+    ``v_scale`` (uint8 ``[num_pages, n_kv, page]``), ``page_table`` (int32 ``[B, max_pages]``), ``cache_len`` (int32
+    ``[B]``) and, for sequences that share a prefix, ``group_start`` (int32 ``[n_groups + 1]``) with ``prefix_len``
+    (int32 ``[n_groups]``).  The tensors are borrowed; what they hold may change between calls.  Work goes to the
+    current stream of their device.  The object owns the attention's workspace: use one per stream."""
+
+    def __init__(self, kv: Dict[str, torch.Tensor]):
+        self.lib = load_library()
+        self.kv = {n: kv[n] for n in _CACHE_NAMES if kv.get(n) is not None}
+        if kv["k_pages"].dim() != 4 or kv["k_pages"].element_size() != 1:
+            raise SxError("k_pages must be 8-bit codes [num_pages, n_kv, page, d]")
+        self.n_kv, self.page, self.d = (int(v) for v in kv["k_pages"].shape[1:])
+        self.dev = kv["k_pages"].device
+        self._kv = _kv_struct(self.kv, self.n_kv, self.page, self.d)
+        self._kv_ref = C.byref(self._kv)
+        self.B = int(self._kv.batch)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.dev)
+        self._shape = KVShape(self.n_kv, self.n_kv, self.d, self.page)
+        self._shape_ref = C.byref(self._shape)
+        self._ws, self._ws_at, self._ws_bytes, self._ws_for = None, 0, 0, None
+
+    def check_status(self, what: str = "device") -> None:
+        code = int(self.status.item())
+        if code != 0:
+            self.status.zero_()
+            _check(code, what)
+
+    def _rows(self, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, pos_start: Optional[torch.Tensor]) -> int:
+        for name, t in (("k", k), ("v", v)):
+            if (t.dtype != torch.bfloat16 or t.device != self.dev or t.dim() != 3 or t.shape[1:] != (self.n_kv, self.d)
+                    or t.stride(2) != 1 or t.stride(1) != self.d):
+                raise SxError(f"{name} must be bf16 [T, {self.n_kv}, {self.d}] on {self.dev}, rows of heads contiguous")
+        if k.shape[0] != v.shape[0]:
+            raise SxError("k and v must have the same number of rows")
+        for name, t, n in (("row_start", row_start, self.B + 1), ("pos_start", pos_start, self.B)):
+            if t is not None and (t.dtype != torch.int32 or t.device != self.dev or t.numel() != n or not t.is_contiguous()):
+                raise SxError(f"{name} must be int32 [{n}] on {self.dev}")
+        return int(k.shape[0])
+
+    def _stride(self, t: torch.Tensor) -> int:
+        return t.stride(0) if t.shape[0] > 1 else self.n_kv * self.d
+
+    def sx_kv_append(self, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor,
+                     pos_start: Optional[torch.Tensor] = None) -> None:
+        """Quantises rows ``k`` / ``v`` (bf16 ``[T, n_kv, d]``, any row stride that is a multiple of 8) into the cache:
+        rows ``row_start[b] .. row_start[b + 1] - 1`` become slots ``pos_start[b] ..`` of sequence ``b`` (default: behind
+        ``cache_len``, which is not advanced)."""
+        T = self._rows(k, v, row_start, pos_start)
+        if T == 0:
+            return
+        with torch.cuda.device(self.dev):
+            _check(self.lib.sx_kv_append(self._shape_ref, self._kv_ref, T, row_start.data_ptr(), _p(pos_start),
+                                         k.data_ptr(), self._stride(k), v.data_ptr(), self._stride(v),
+                                         self.status.data_ptr(), torch.cuda.current_stream().cuda_stream), "sx_kv_append")
+
+    def sx_kv_read(self, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, pos_start: torch.Tensor) -> None:
+        """Reads slots ``pos_start[b] ..`` of every sequence back into rows ``row_start[b] .. row_start[b + 1] - 1`` of
+        ``k`` / ``v`` (bf16 ``[T, n_kv, d]``); rows behind the last sequence stay as they are."""
+        T = self._rows(k, v, row_start, pos_start)
+        if T == 0:
+            return
+        with torch.cuda.device(self.dev):
+            _check(self.lib.sx_kv_read(self._shape_ref, self._kv_ref, T, row_start.data_ptr(), _p(pos_start),
+                                       k.data_ptr(), self._stride(k), v.data_ptr(), self._stride(v),
+                                       self.status.data_ptr(), torch.cuda.current_stream().cuda_stream), "sx_kv_read")
+
+    def sx_attention(self, q: torch.Tensor, drafted: int = 0, row_mask: Optional[torch.Tensor] = None,
+                     scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                     kernel: int = ATTN_AUTO) -> torch.Tensor:
+        """Decode attention of ``q`` (bf16 ``[B, rows, n_q, d]``; a slice of a projection's output will do) over the
+        cached slots and, by ``row_mask`` (int64 ``[B, rows]``, bit i = drafted slot i; default all), the ``drafted``
+        slots behind them.  ``scale`` defaults to ``1 / sqrt(d)``.  Returns bf16 ``[B, rows, n_q, d]``."""
+        if q.dtype != torch.bfloat16 or q.device != self.dev or q.dim() != 4 or q.shape[0] != self.B or q.shape[3] != self.d:
+            raise SxError(f"q must be bf16 [{self.B}, rows, n_q, {self.d}] on {self.dev}")
+        rows, nq = int(q.shape[1]), int(q.shape[2])
+        stride = q.stride(1) if rows > 1 else (q.stride(0) if self.B > 1 else nq * self.d)
+        if q.stride(3) != 1 or q.stride(2) != self.d or (self.B > 1 and q.stride(0) != rows * stride):
+            raise SxError("the heads of a row of q must be contiguous and its rows evenly spaced")
+        if row_mask is not None and (row_mask.dtype != torch.int64 or row_mask.device != self.dev
+                                     or row_mask.numel() != self.B * rows or not row_mask.is_contiguous()):
+            raise SxError(f"row_mask must be int64 [{self.B}, {rows}] on {self.dev}")
+        if out is None:
+            out = torch.empty(self.B, rows, nq, self.d, dtype=torch.bfloat16, device=self.dev)
+        elif out.dtype != torch.bfloat16 or out.device != self.dev or out.shape != q.shape or not out.is_contiguous():
+            raise SxError("out must be contiguous bf16 of q's shape")
+        with torch.cuda.device(self.dev):
+            self._shape.n_q_heads = nq
+            if self._ws_for != (rows, nq):
+                need = int(self.lib.sx_attention_ws_bytes(self._shape_ref, self.B, rows, int(self._kv.n_groups)))
+                if need > self._ws_bytes:
+                    self._ws = torch.empty(need + 256, dtype=torch.uint8, device=self.dev)
+                    self._ws_at = self._ws.data_ptr() + (-self._ws.data_ptr()) % 256
+                    self._ws_bytes = need
+                self._ws_for = (rows, nq)
+            _check(self.lib.sx_attention(self._shape_ref, self._kv_ref, rows, drafted, q.data_ptr(), stride, _p(row_mask),
+                                         self.d ** -0.5 if scale is None else scale, kernel, out.data_ptr(), self._ws_at,
+                                         self._ws_bytes, self.status.data_ptr(), torch.cuda.current_stream().cuda_stream),
+                   "sx_attention")
+        return out
 
 
 class SpecExit:

@@ -1,0 +1,490 @@
+// Decode attention over the 8-bit paged KV cache: the warp-level kernel, the merge of partial results and the
+// choice between the warp-level and the tensor-memory kernel (sx_attn8_tc.cu).
+//
+//   o_r = sum_s w_rs V_s / sum_s w_rs,   w_rs = exp(scale * q_r . K_s),   over the slots s that row r sees
+//   K_s = kc_s 2^(ek_s), V_s = vc_s 2^(ev_s)    (e4m3 codes, one exponent per slot and KV head)
+//
+// The warp-level kernel: a warp streams its run of 16-slot steps (sx_attn8.cuh) through a ring of its own in shared
+// memory - cp.async, 512 contiguous bytes per instruction, XOR-swizzled - and needs no other warp.  e4m3 codes
+// are exact in fp16, so both products run as mma.sync m16n8k16 (fp16 in, fp32 out) with the slots (then the head
+// dimension) on the 16-row side and 8 queries on the 8-column side:
+//     S^T[slot][q] = sum_d kc[slot][d] Q[q][d]         O^T[d][q] += sum_slot vc[slot][d] P[slot][q]
+// Codes go from shared memory to fragments as bytes: ldmatrix moves pairs of codes, cvt.f16x2.e4m3x2 widens them, and
+// the order that results (four codes of a row per lane) is undone for free by ordering Q the same way; for V
+// ldmatrix.trans delivers [slot][pair of d], one byte permute splits the pair into two rows of the product, whose
+// order is undone where O is stored.  Queries are scaled by a power of two per row, so that bf16 fits fp16.
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <math.h>
+
+#include "sx_attn8.cuh"
+#include "sx_kernels.cuh"
+#include "sx_launch.cuh"
+
+#define A8S_WARPS 4
+#define A8S_CTAS 3                       // per SM: 12 warps with rings of about 16 KB each
+
+__device__ __forceinline__ float a8_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void a8_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                       uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t a8_transpose(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// two codes (low half, high half of the register) to fp16 pairs
+__device__ __forceinline__ void a8_widen(uint32_t x, uint32_t &lo, uint32_t &hi) {
+  asm("{\n\t.reg .b16 a, b;\n\t"
+      "mov.b32 {a, b}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(x));
+}
+// the codes of slots that no query may see can be anything; a code that is not a number must not meet a weight of 0
+__device__ __forceinline__ uint32_t a8_finite(uint32_t x) {
+  const __half2 top = __float2half2_rn(448.f);
+  __half2 v = __hmin2(*reinterpret_cast<__half2 *>(&x), top);
+  return *reinterpret_cast<uint32_t *>(&v);
+}
+__device__ __forceinline__ void a8_cp16(uint32_t dst, const void *src, bool valid) {
+  const uint32_t bytes = valid ? 16u : 0u;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void a8_cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void a8_cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void a8_ldm4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void a8_ldm4t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// 16-byte chunk position of a staged row (D bytes), so that eight rows of an ldmatrix phase fall into different banks
+template <int D>
+__device__ __forceinline__ int a8_swz(int row, int c) { return c ^ (D >= 128 ? (row & 7) : ((row >> 1) & 3)); }
+
+template <int D, int NQT> struct A8S {
+  static constexpr int STAGES = D == 128 ? 4 : 8;        // 16 KB of codes per warp
+  static constexpr int BLK = 16 * D;                     // bytes of the K (or V) codes of a step
+  static constexpr int WARP_BYTES = STAGES * 2 * BLK;
+  static constexpr int CODES = A8S_WARPS * WARP_BYTES;
+  static constexpr int SCALES = A8S_WARPS * STAGES * 32;
+};
+
+template <bool PRE, int D, int NQT>
+__global__ void __launch_bounds__(A8S_WARPS * 32, A8S_CTAS) sx_attn8_split_kernel(const __grid_constant__ SxA8 p) {
+  using C = A8S<D, NQT>;
+  constexpr int ST = C::STAGES, BLK = C::BLK, CPR = D / 16;
+  extern __shared__ __align__(16) uint8_t a8_smem[];
+  a8_enter<PRE>(p);
+  const SxA8List &ls = PRE ? p.pre : p.own;
+  A8Plan pl;
+  a8_plan<PRE, A8S_WARPS * 32>(p, ls, A8_SPLIT_STEP, a8_smem + C::CODES + C::SCALES, pl);
+  a8_planned<PRE>(p);
+  a8_publish<PRE, A8S_WARPS * 32>(p, pl, ls, A8_SPLIT_STEP);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int run = blockIdx.x * A8S_WARPS + warp;
+  const int64_t total = pl.cum[pl.units], xb = min(total, (int64_t)run * pl.per), xe = min(total, xb + pl.per);
+  if (xb >= xe) { a8_leave<PRE>(p); return; }
+  const uint32_t codes = (uint32_t)__cvta_generic_to_shared(a8_smem) + warp * C::WARP_BYTES;
+  uint8_t *scale_sh = a8_smem + C::CODES + warp * ST * 32;
+  const uint32_t scales = (uint32_t)__cvta_generic_to_shared(scale_sh);
+
+  // ---- loader: requests the step at list position lx into ring stage `st` ---------------------------------
+  int64_t lx = xb, l_x1 = xb;
+  int l_slot = 0, l_end = 0, l_b0 = 0, l_h = 0, l_pp = -1;
+  bool bad = false;
+  auto page_of = [&](int b0, int slot) -> int {
+    const int lp = slot / p.page;
+    return lp < p.max_pages ? p.page_table[(int64_t)b0 * p.max_pages + lp] : -1;
+  };
+  auto request = [&](int st) {
+    if (lx < xe) {
+      if (lx == l_x1) {
+        const A8Seg s = a8_seek<PRE>(p, pl, ls, A8_SPLIT_STEP, lx);
+        l_x1 = s.x1; l_slot = s.first + (int)(lx - s.x0) * 16; l_end = s.end; l_b0 = s.b0; l_h = s.h;
+        l_pp = page_of(l_b0, l_slot);
+      }
+      const bool ok = l_pp >= 0 && l_pp < p.num_pages;
+      bad |= !ok;
+      const int off = l_slot % p.page, rows = ok ? min(16, l_end - l_slot) : 0;
+      const int64_t row0 = ok ? ((int64_t)l_pp * p.nkv + l_h) * p.page + off : 0;
+      const uint32_t dst = codes + st * 2 * BLK;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const int e = i * 32 + lane, row = e / CPR, c = e - row * CPR;
+        const uint32_t at = (uint32_t)(row * D + a8_swz<D>(row, c) * 16);
+        const int64_t src = row < rows ? row0 * D + e * 16 : 0;
+        a8_cp16(dst + at, p.k + src, row < rows);
+        a8_cp16(dst + BLK + at, p.v + src, row < rows);
+      }
+      if (lane < 2) a8_cp16(scales + st * 32 + lane * 16, (lane ? p.vs : p.ks) + row0, ok);
+      ++lx;
+      l_slot += 16;
+      if (lx < l_x1) l_pp = page_of(l_b0, l_slot);       // looked up a step ahead
+    }
+    a8_cp_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < ST - 1; ++i) request(i);
+
+  A8Seg seg;
+  seg.x1 = xb;
+  uint32_t qf[NQT][CPR][2];
+  float qs[NQT][2], M[NQT][2], L[NQT][2], O[NQT][CPR][4];
+  uint64_t vis[NQT][2];
+  int st = 0;
+  for (int64_t x = xb; x < xe; ++x) {
+    if (x == seg.x1) {
+      // ---- a new (unit, head, tile): its queries, scaled to fp16 --------------------------------------------
+      seg = a8_seek<PRE>(p, pl, ls, A8_SPLIT_STEP, x);
+#pragma unroll
+      for (int i = 0; i < NQT; ++i) {
+        const int col = i * 8 + g, qi = seg.tile * ls.qt + col, j = qi / p.G;
+        const bool live = col < seg.cols;
+        const bf16 *src = p.q + (int64_t)(seg.r0 + j) * p.q_stride + (int64_t)(seg.h * p.G + qi - j * p.G) * D + t * 4;
+        uint2 raw[CPR];
+        uint32_t top = 0;
+#pragma unroll
+        for (int c = 0; c < CPR; ++c) {
+          raw[c] = live ? *reinterpret_cast<const uint2 *>(src + c * 16) : make_uint2(0, 0);
+          top = __vmaxu2(top, __vmaxu2(raw[c].x & 0x7fff7fffu, raw[c].y & 0x7fff7fffu));
+        }
+        top = max(top & 0xffffu, top >> 16);
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // 2^-e brings the largest magnitude into [2^10, 2^11): values down to 2^-24 of it keep all their bits
+        int ex = (int)(top >> 7);
+        ex = (ex == 0 || ex == 255) ? 0 : ex - 137;
+        const float up = __uint_as_float((uint32_t)(127 - max(-126, min(126, ex))) << 23);
+        ex = max(-126, min(126, ex));
+#pragma unroll
+        for (int c = 0; c < CPR; ++c) {
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t w = k ? raw[c].y : raw[c].x;
+            __half2 h = __floats2half2_rn(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up);
+            qf[i][c][k] = *reinterpret_cast<uint32_t *>(&h);
+          }
+        }
+        const float mine = __uint_as_float((uint32_t)(127 + ex) << 23) * p.scale_log2;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          qs[i][k] = __shfl_sync(0xffffffffu, mine, (2 * t + k) * 4);
+          M[i][k] = -INFINITY;
+          L[i][k] = 0.f;
+          if (!PRE) {
+            const int cq = i * 8 + 2 * t + k, qq = seg.tile * ls.qt + min(cq, seg.cols - 1);
+            vis[i][k] = p.row_mask ? p.row_mask[seg.r0 + qq / p.G] : ~0ull;
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < CPR; ++c)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) O[i][c][k] = 0.f;
+      }
+    }
+    a8_cp_wait<ST - 2>();
+    __syncwarp();
+    request((st + ST - 1) % ST);               // the stage of the step before, which every lane has left
+    const int slot0 = seg.first + (int)(x - seg.x0) * 16;
+    const bool whole = PRE ? slot0 + 16 <= seg.end : (slot0 >= seg.lo && slot0 + 16 <= seg.len);
+    const uint32_t kb = codes + st * 2 * BLK, vb = kb + BLK;
+    const uint8_t *sb = scale_sh + st * 32;
+    // ---- S^T: lane (g, t) holds slots g and g + 8, queries 2t and 2t + 1 ---------------------------------------
+    float S[NQT][4];
+#pragma unroll
+    for (int i = 0; i < NQT; ++i) S[i][0] = S[i][1] = S[i][2] = S[i][3] = 0.f;
+    const int lrow = (lane & 7) + ((lane >> 3) & 1) * 8, lc = lane >> 4;
+#pragma unroll
+    for (int c = 0; c < CPR; c += 2) {
+      uint32_t r[4], a[8];
+      a8_ldm4(kb + lrow * D + a8_swz<D>(lrow, c + lc) * 16, r);
+      a8_widen(r[0], a[0], a[2]);
+      a8_widen(r[1], a[1], a[3]);
+      a8_widen(r[2], a[4], a[6]);
+      a8_widen(r[3], a[5], a[7]);
+#pragma unroll
+      for (int i = 0; i < NQT; ++i) {
+        a8_mma(S[i], a[0], a[1], a[2], a[3], qf[i][c][0], qf[i][c][1]);
+        a8_mma(S[i], a[4], a[5], a[6], a[7], qf[i][c + 1][0], qf[i][c + 1][1]);
+      }
+    }
+    float kscale[2], ev[2], inv[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int kbyte = sb[g + r * 8], vbyte = sb[16 + g + r * 8];
+      kscale[r] = a8_pow2(kbyte);
+      ev[r] = a8_exponent(vbyte);
+      inv[r] = a8_pow2_inv(vbyte);
+    }
+    bool up = false;
+#pragma unroll
+    for (int i = 0; i < NQT; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) S[i][k] = fmaf(S[i][k] * qs[i][k & 1], kscale[k >> 1], ev[k >> 1]);
+    if (!whole) {
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int slot = slot0 + g + r * 8, dr = slot - seg.len;
+#pragma unroll
+        for (int i = 0; i < NQT; ++i)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const bool seen = slot >= seg.lo && slot < seg.end && (PRE || dr < 0 || ((vis[i][k] >> dr) & 1ull));
+            if (!seen) S[i][r * 2 + k] = -INFINITY;
+          }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NQT; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) up |= S[i][k] > M[i][k & 1] + 8.f;
+    if (__any_sync(0xffffffffu, up)) {
+      // a reference moves: it only has to keep the weights in range, so this is rare behind the first steps
+#pragma unroll
+      for (int i = 0; i < NQT; ++i)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float bm = fmaxf(S[i][k], S[i][k + 2]);
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, o));
+          if (bm > M[i][k] + 8.f) {
+            const float w = a8_ex2(M[i][k] - bm);              // 0 for the first one
+            M[i][k] = bm;
+            L[i][k] *= w;
+#pragma unroll
+            for (int c = 0; c < CPR; ++c) { O[i][c][k] *= w; O[i][c][k + 2] *= w; }
+          }
+        }
+    }
+    // ---- weights (below 2^8), their sums without the value scale, P^T as fp16 -----------------------------------
+    uint32_t pb[NQT][2];
+#pragma unroll
+    for (int i = 0; i < NQT; ++i) {
+      float w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float m = M[i][k & 1];
+        w[k] = a8_ex2(S[i][k] - (m == -INFINITY ? 0.f : m));
+        L[i][k & 1] += (!whole && w[k] == 0.f) ? 0.f : w[k] * inv[k >> 1];
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        __half2 h = __floats2half2_rn(w[2 * r], w[2 * r + 1]);
+        pb[i][r] = a8_transpose(*reinterpret_cast<uint32_t *>(&h));
+      }
+    }
+    // ---- O^T: rows 2g and 2g + 1 of each 16-row chunk of the head dimension ---------------------------------------
+#pragma unroll
+    for (int c = 0; c < CPR; c += 2) {
+      uint32_t r[4], a[8];
+      a8_ldm4t(vb + lrow * D + a8_swz<D>(lrow, c + lc) * 16, r);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) r[k] = __byte_perm(r[k], 0, 0x3120);     // slots side by side, per row of d
+      a8_widen(r[0], a[0], a[1]);
+      a8_widen(r[1], a[2], a[3]);
+      a8_widen(r[2], a[4], a[5]);
+      a8_widen(r[3], a[6], a[7]);
+      if (!whole) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) a[k] = a8_finite(a[k]);
+      }
+#pragma unroll
+      for (int i = 0; i < NQT; ++i) {
+        a8_mma(O[i][c], a[0], a[1], a[2], a[3], pb[i][0], pb[i][1]);
+        a8_mma(O[i][c + 1], a[4], a[5], a[6], a[7], pb[i][0], pb[i][1]);
+      }
+    }
+    st = (st + 1) % ST;
+    if (x + 1 == seg.x1 || x + 1 == xe) {
+      // ---- leave the segment: the partial result of this run ------------------------------------------------------
+      const int64_t row = seg.base + (int64_t)ls.qt * run;
+#pragma unroll
+      for (int i = 0; i < NQT; ++i)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float l = L[i][k];
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+          const int col = i * 8 + 2 * t + k;
+          if (col < seg.cols) {
+            if (g == 0) ls.ml[row + col] = make_float2(M[i][k], l);
+            float *o = ls.o + (row + col) * D + 2 * g;
+#pragma unroll
+            for (int c = 0; c < CPR; ++c)
+              *reinterpret_cast<float2 *>(o + c * 16) = make_float2(O[i][c][k], O[i][c][k + 2]);
+          }
+        }
+    }
+  }
+  if (__any_sync(0xffffffffu, bad) && lane == 0) sx_set_status(p.status, SX_ERR_CAPACITY);
+  a8_leave<PRE>(p);
+}
+
+// ---- merge -------------------------------------------------------------------------------------------------------
+// o[row, head] = sum over the partial results of 2^(ref - max ref) O, over the same sum of l; zero when no slot is
+// seen.  One CTA per (row, query head); its eight warps share the partial results, a lane owns D / 32 columns.
+template <int D>
+__global__ void __launch_bounds__(A8_MERGE_THREADS) sx_attn8_merge_kernel(const __grid_constant__ SxA8 p) {
+  constexpr int V = D / 32, W = A8_MERGE_THREADS / 32;
+  __shared__ float2 ml_sh[W];
+  __shared__ float o_sh[W][D];
+  sx_pdl_launch_dependents();
+  const int r = blockIdx.y, hq = blockIdx.x, b = r / p.rows, j = r - b * p.rows, h = hq / p.G;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  sx_pdl_wait();
+  float M = -INFINITY, L = 0.f, acc[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) acc[i] = 0.f;
+  auto take = [&](const SxA8List &ls, int u, int nq, int q, int64_t row0) {
+    const int steps = ls.steps[u];
+    if (steps == 0) return;
+    const int64_t total = ls.total[0];
+    int64_t per = (total + ls.runs - 1) / ls.runs;
+    if (per < ls.min_per) per = ls.min_per;
+    const int nt = (nq + ls.qt - 1) / ls.qt;
+    const int64_t x0 = ls.cum[u] + ((int64_t)h * nt + q / ls.qt) * steps;
+    const int64_t c0 = x0 / per, c1 = (x0 + steps - 1) / per;
+    const int64_t base = row0 + (int64_t)h * nq + q;
+    for (int64_t c = c0 + warp; c <= c1; c += 4 * W) {
+      float2 ml[4];
+      float v[4][V];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const bool on = c + k * W <= c1;
+        const int64_t at = base + (int64_t)ls.qt * (on ? c + k * W : c);
+        ml[k] = ls.ml[at];
+        if (!on) ml[k] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[k][i] = ls.o[at * D + lane * V + i];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (ml[k].x == -INFINITY && ml[k].y == 0.f) continue;         // nothing seen there
+        const float m = fmaxf(M, ml[k].x), a = (M == -INFINITY) ? 0.f : exp2f(M - m), w = exp2f(ml[k].x - m);
+        M = m;
+        L = L * a + ml[k].y * w;
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] = acc[i] * a + v[k][i] * w;
+      }
+    }
+  };
+  const int gq = hq - h * p.G;
+  take(p.own, b, p.rows * p.G, j * p.G + gq, (int64_t)b * p.rows * p.G * p.nkv);
+  if (p.n_groups > 0) {
+    const int g = p.seq_group[b];
+    if (g >= 0) {
+      const int s = p.group_start[g], nq = a8_members(p, g) * p.rows * p.G;
+      take(p.pre, g, nq, ((b - s) * p.rows + j) * p.G + gq, (int64_t)s * p.rows * p.G * p.nkv);
+    }
+  }
+  if (lane == 0) ml_sh[warp] = make_float2(M, L);
+#pragma unroll
+  for (int i = 0; i < V; ++i) o_sh[warp][lane * V + i] = acc[i];
+  __syncthreads();
+  if (threadIdx.x < D) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < W; ++w) m = fmaxf(m, ml_sh[w].x);
+    float l = 0.f, o = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float2 v = ml_sh[w];
+      if (v.x == -INFINITY && v.y == 0.f) continue;
+      const float f = exp2f(v.x - m);
+      l += v.y * f;
+      o += o_sh[w][threadIdx.x] * f;
+    }
+    p.o_out[((int64_t)r * p.nq + hq) * D + threadIdx.x] = __float2bfloat16_rn(l == 0.f ? 0.f : o / l);
+  }
+}
+
+// ---- host side -------------------------------------------------------------------------------------------------------
+static int split_runs(int sm_count) { return sm_count * A8S_CTAS * A8S_WARPS; }
+
+template <bool PRE, int D, int NQT>
+static sx_status launch_split(const SxA8 &p, int sm_count, cudaStream_t st) {
+  using C = A8S<D, NQT>;
+  const size_t smem = C::CODES + C::SCALES + a8_plan_bytes(p.B, p.n_groups);
+  static_assert(C::CODES + C::SCALES + 48 * 1024 < 200 * 1024, "ring and the largest plan fit one SM");
+  // set on every call: the attribute belongs to the current device, and setting it costs less than remembering it
+  SX_TRY(sx_rc(cudaFuncSetAttribute(sx_attn8_split_kernel<PRE, D, NQT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)));
+  return sx_rc(sx_launch(sx_attn8_split_kernel<PRE, D, NQT>, dim3(sm_count * A8S_CTAS), dim3(A8S_WARPS * 32), smem, st, p));
+}
+
+// one list with the warp-level kernel
+template <bool PRE>
+static sx_status split_list(SxA8 &p, int sm_count, cudaStream_t st) {
+  if (p.d == 128)
+    return (PRE ? p.pre : p.own).qt == 8 ? launch_split<PRE, 128, 1>(p, sm_count, st) : launch_split<PRE, 128, 2>(p, sm_count, st);
+  return (PRE ? p.pre : p.own).qt == 8 ? launch_split<PRE, 64, 1>(p, sm_count, st) : launch_split<PRE, 64, 2>(p, sm_count, st);
+}
+
+static size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+// rows of partial results that any variant of a list may use
+static size_t list_rows(int nq, int B, int rows, int sm_count) {
+  const size_t split = (size_t)16 * split_runs(sm_count), tc = (size_t)128 * sm_count;
+  return (split > tc ? split : tc) + (size_t)B * rows * nq;
+}
+static size_t list_bytes(int nq, int d, int B, int rows, int units, int sm_count) {
+  return up256((size_t)units * 8) + up256((size_t)units * 4) + 256 +
+         up256(list_rows(nq, B, rows, sm_count) * 8) + up256(list_rows(nq, B, rows, sm_count) * d * 4);
+}
+
+size_t sx_attn8_ws_bytes(int nq, int nkv, int d, int B, int rows, int groups, int sm_count) {
+  (void)nkv;
+  return up256((size_t)B * 4) + list_bytes(nq, d, B, rows, B, sm_count) +
+         (groups > 0 ? list_bytes(nq, d, B, rows, groups, sm_count) : 0);
+}
+
+sx_status sx_launch_attn8(SxA8 p, int kernel, char *ws, int sm_count, cudaStream_t st) {
+  if ((p.d != 64 && p.d != 128) || p.page % A8_SPLIT_STEP || p.B + p.n_groups > A8_MAX_UNITS) return SX_ERR_UNSUPPORTED;
+  size_t o = 0;
+  auto take = [&](size_t bytes) { char *at = ws + o; o += up256(bytes); return at; };
+  p.seq_group = (int32_t *)take((size_t)p.B * 4);
+  auto place = [&](SxA8List &ls, int units) {
+    ls.cum = (int64_t *)take((size_t)units * 8);
+    ls.steps = (int32_t *)take((size_t)units * 4);
+    ls.total = (int64_t *)take(8);
+    ls.ml = (float2 *)take(list_rows(p.nq, p.B, p.rows, sm_count) * 8);
+    ls.o = (float *)take(list_rows(p.nq, p.B, p.rows, sm_count) * p.d * 4);
+  };
+  place(p.own, p.B);
+  if (p.n_groups > 0) place(p.pre, p.n_groups);
+  const int own_q = p.rows * p.G;
+  // a group has at most this many queries per KV head (the host does not know the groups)
+  const int pre_q = p.n_groups > 0 ? (p.B - p.n_groups + 1 > 1 ? p.B - p.n_groups + 1 : 2) * own_q : 0;
+  auto choose = [&](SxA8List &ls, int q) -> bool {
+    const bool tc = false;
+    (void)kernel;
+    ls.step = tc ? A8_TC_STEP : A8_SPLIT_STEP;
+    ls.qt = q <= 8 ? 8 : 16;
+    ls.runs = split_runs(sm_count);
+    ls.min_per = 4;
+    return tc;
+  };
+  choose(p.own, own_q);
+  if (p.n_groups > 0) {
+    choose(p.pre, pre_q);
+    p.after_prefix = 1;
+    SX_TRY(split_list<true>(p, sm_count, st));
+  }
+  SX_TRY(split_list<false>(p, sm_count, st));
+  const dim3 grid(p.nq, p.B * p.rows);
+  if (p.d == 128) return sx_rc(sx_launch(sx_attn8_merge_kernel<128>, grid, dim3(A8_MERGE_THREADS), 0, st, p));
+  return sx_rc(sx_launch(sx_attn8_merge_kernel<64>, grid, dim3(A8_MERGE_THREADS), 0, st, p));
+}
