@@ -22,7 +22,6 @@
 #include "sx_launch.cuh"
 
 #define A8S_WARPS 4
-#define A8S_CTAS 3                       // per SM: 12 warps with rings of about 16 KB each
 
 __device__ __forceinline__ float a8_ex2(float x) {
   float y;
@@ -77,7 +76,8 @@ template <int D>
 __device__ __forceinline__ int a8_swz(int row, int c) { return c ^ (D >= 128 ? (row & 7) : ((row >> 1) & 3)); }
 
 template <int D, int NQT> struct A8S {
-  static constexpr int STAGES = D == 128 ? 4 : 8;        // 16 KB of codes per warp
+  static constexpr int CTAS = 3;                         // per SM: 12 warps with rings of 16 KB each
+  static constexpr int STAGES = D == 128 ? 4 : 8;
   static constexpr int BLK = 16 * D;                     // bytes of the K (or V) codes of a step
   static constexpr int WARP_BYTES = STAGES * 2 * BLK;
   static constexpr int CODES = A8S_WARPS * WARP_BYTES;
@@ -85,7 +85,7 @@ template <int D, int NQT> struct A8S {
 };
 
 template <bool PRE, int D, int NQT>
-__global__ void __launch_bounds__(A8S_WARPS * 32, A8S_CTAS) sx_attn8_split_kernel(const __grid_constant__ SxA8 p) {
+__global__ void __launch_bounds__(A8S_WARPS * 32, (A8S<D, NQT>::CTAS)) sx_attn8_split_kernel(const __grid_constant__ SxA8 p) {
   using C = A8S<D, NQT>;
   constexpr int ST = C::STAGES, BLK = C::BLK, CPR = D / 16;
   extern __shared__ __align__(16) uint8_t a8_smem[];
@@ -94,17 +94,17 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, A8S_CTAS) sx_attn8_split_kerne
   A8Plan pl;
   a8_plan<PRE, A8S_WARPS * 32>(p, ls, A8_SPLIT_STEP, a8_smem + C::CODES + C::SCALES, pl);
   a8_planned<PRE>(p);
-  a8_publish<PRE, A8S_WARPS * 32>(p, pl, ls, A8_SPLIT_STEP);
+  a8_publish<PRE, A8S_WARPS * 32>(p, pl, ls);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int run = blockIdx.x * A8S_WARPS + warp;
-  const int64_t total = pl.cum[pl.units], xb = min(total, (int64_t)run * pl.per), xe = min(total, xb + pl.per);
+  const int total = pl.cum[pl.units], xb = (int)min((int64_t)total, (int64_t)run * pl.per), xe = min(total - xb, pl.per) + xb;
   if (xb >= xe) { a8_leave<PRE>(p); return; }
   const uint32_t codes = (uint32_t)__cvta_generic_to_shared(a8_smem) + warp * C::WARP_BYTES;
   uint8_t *scale_sh = a8_smem + C::CODES + warp * ST * 32;
   const uint32_t scales = (uint32_t)__cvta_generic_to_shared(scale_sh);
 
   // ---- loader: requests the step at list position lx into ring stage `st` ---------------------------------
-  int64_t lx = xb, l_x1 = xb;
+  int lx = xb, l_x1 = xb;
   int l_slot = 0, l_end = 0, l_b0 = 0, l_h = 0, l_pp = -1;
   bool bad = false;
   auto page_of = [&](int b0, int slot) -> int {
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, A8S_CTAS) sx_attn8_split_kerne
     if (lx < xe) {
       if (lx == l_x1) {
         const A8Seg s = a8_seek<PRE>(p, pl, ls, A8_SPLIT_STEP, lx);
-        l_x1 = s.x1; l_slot = s.first + (int)(lx - s.x0) * 16; l_end = s.end; l_b0 = s.b0; l_h = s.h;
+        l_x1 = s.x1; l_slot = s.first + (lx - s.x0) * 16; l_end = s.end; l_b0 = s.b0; l_h = s.h;
         l_pp = page_of(l_b0, l_slot);
       }
       const bool ok = l_pp >= 0 && l_pp < p.num_pages;
@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, A8S_CTAS) sx_attn8_split_kerne
     }
     a8_cp_commit();
   };
-#pragma unroll
+#pragma unroll 1
   for (int i = 0; i < ST - 1; ++i) request(i);
 
   A8Seg seg;
@@ -147,7 +147,8 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, A8S_CTAS) sx_attn8_split_kerne
   float qs[NQT][2], M[NQT][2], L[NQT][2], O[NQT][CPR][4];
   uint64_t vis[NQT][2];
   int st = 0;
-  for (int64_t x = xb; x < xe; ++x) {
+#pragma unroll 1
+  for (int x = xb; x < xe; ++x) {
     if (x == seg.x1) {
       // ---- a new (unit, head, tile): its queries, scaled to fp16 --------------------------------------------
       seg = a8_seek<PRE>(p, pl, ls, A8_SPLIT_STEP, x);
@@ -200,7 +201,7 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, A8S_CTAS) sx_attn8_split_kerne
     a8_cp_wait<ST - 2>();
     __syncwarp();
     request((st + ST - 1) % ST);               // the stage of the step before, which every lane has left
-    const int slot0 = seg.first + (int)(x - seg.x0) * 16;
+    const int slot0 = seg.first + (x - seg.x0) * 16;
     const bool whole = PRE ? slot0 + 16 <= seg.end : (slot0 >= seg.lo && slot0 + 16 <= seg.len);
     const uint32_t kb = codes + st * 2 * BLK, vb = kb + BLK;
     const uint8_t *sb = scale_sh + st * 32;
@@ -238,21 +239,18 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, A8S_CTAS) sx_attn8_split_kerne
       for (int k = 0; k < 4; ++k) S[i][k] = fmaf(S[i][k] * qs[i][k & 1], kscale[k >> 1], ev[k >> 1]);
     if (!whole) {
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int slot = slot0 + g + r * 8, dr = slot - seg.len;
+      for (int i = 0; i < NQT; ++i)
 #pragma unroll
-        for (int i = 0; i < NQT; ++i)
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const bool seen = slot >= seg.lo && slot < seg.end && (PRE || dr < 0 || ((vis[i][k] >> dr) & 1ull));
-            if (!seen) S[i][r * 2 + k] = -INFINITY;
-          }
-      }
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t seen = a8_visible<PRE>(seg, vis[i][k], slot0, 16) >> g;
+          if (!(seen & 1u)) S[i][k] = -INFINITY;
+          if (!(seen & 256u)) S[i][2 + k] = -INFINITY;
+        }
     }
 #pragma unroll
     for (int i = 0; i < NQT; ++i)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) up |= S[i][k] > M[i][k & 1] + 8.f;
+      for (int k = 0; k < 4; ++k) up |= S[i][k] > M[i][k & 1] + A8_SLACK;
     if (__any_sync(0xffffffffu, up)) {
       // a reference moves: it only has to keep the weights in range, so this is rare behind the first steps
 #pragma unroll
@@ -262,7 +260,7 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, A8S_CTAS) sx_attn8_split_kerne
           float bm = fmaxf(S[i][k], S[i][k + 2]);
 #pragma unroll
           for (int o = 4; o < 32; o <<= 1) bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, o));
-          if (bm > M[i][k] + 8.f) {
+          if (bm > M[i][k] + A8_SLACK) {
             const float w = a8_ex2(M[i][k] - bm);              // 0 for the first one
             M[i][k] = bm;
             L[i][k] *= w;
@@ -271,7 +269,7 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, A8S_CTAS) sx_attn8_split_kerne
           }
         }
     }
-    // ---- weights (below 2^8), their sums without the value scale, P^T as fp16 -----------------------------------
+    // ---- weights (below 2^14), their sums without the value scale, P^T as fp16 -----------------------------------
     uint32_t pb[NQT][2];
 #pragma unroll
     for (int i = 0; i < NQT; ++i) {
@@ -337,36 +335,45 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, A8S_CTAS) sx_attn8_split_kerne
 
 // ---- merge -------------------------------------------------------------------------------------------------------
 // o[row, head] = sum over the partial results of 2^(ref - max ref) O, over the same sum of l; zero when no slot is
-// seen.  One CTA per (row, query head); its eight warps share the partial results, a lane owns D / 32 columns.
-template <int D>
+// seen.  W warps share the partial results of a (row, query head), a lane owns D / 32 columns; a CTA has 8 / W of them.
+template <int D, int W>
 __global__ void __launch_bounds__(A8_MERGE_THREADS) sx_attn8_merge_kernel(const __grid_constant__ SxA8 p) {
-  constexpr int V = D / 32, W = A8_MERGE_THREADS / 32;
-  __shared__ float2 ml_sh[W];
-  __shared__ float o_sh[W][D];
+  constexpr int V = D / 32, PER = A8_MERGE_THREADS / 32 / W;
+  __shared__ float2 ml_sh[PER][W];
+  __shared__ float o_sh[PER][W][D];
   sx_pdl_launch_dependents();
-  const int r = blockIdx.y, hq = blockIdx.x, b = r / p.rows, j = r - b * p.rows, h = hq / p.G;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % W, mine = warp / W;
+  const int64_t at0 = (int64_t)blockIdx.x * PER + mine;
+  const bool live = at0 < (int64_t)p.B * p.rows * p.nq;
+  const int r = live ? (int)(at0 / p.nq) : 0, hq = live ? (int)(at0 - (int64_t)r * p.nq) : 0, b = r / p.rows, j = r - b * p.rows, h = hq / p.G;
   sx_pdl_wait();
   float M = -INFINITY, L = 0.f, acc[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) acc[i] = 0.f;
-  auto take = [&](const SxA8List &ls, int u, int nq, int q, int64_t row0) {
-    const int steps = ls.steps[u];
-    if (steps == 0) return;
-    const int64_t total = ls.total[0];
-    int64_t per = (total + ls.runs - 1) / ls.runs;
-    if (per < ls.min_per) per = ls.min_per;
-    const int nt = (nq + ls.qt - 1) / ls.qt;
-    const int64_t x0 = ls.cum[u] + ((int64_t)h * nt + q / ls.qt) * steps;
-    const int64_t c0 = x0 / per, c1 = (x0 + steps - 1) / per;
-    const int64_t base = row0 + (int64_t)h * nq + q;
-    for (int64_t c = c0 + warp; c <= c1; c += 4 * W) {
+  const int gq = hq - h * p.G, grp = p.n_groups > 0 ? p.seq_group[b] : -1;
+#pragma unroll 1
+  for (int list = 0; list < (grp >= 0 ? 2 : 1); ++list) {
+    // the own list, then the prefix list: unit, queries of the unit, which of them, first row of the unit
+    const SxA8List &ls = list ? p.pre : p.own;
+    const int s = list ? p.group_start[grp] : b, u = list ? grp : b;
+    const int nq = (list ? a8_members(p, grp) : 1) * p.rows * p.G, q = ((b - s) * p.rows + j) * p.G + gq;
+    const int steps = ls.steps[u], cum = ls.cum[u];
+    const uint32_t per = (uint32_t)a8_per(ls.total[0], ls);
+    if (steps == 0) continue;
+    const uint32_t x0 = (uint32_t)(cum + (h * a8_tiles(nq, ls.qt_shift) + (q >> ls.qt_shift)) * steps);
+    // partial k of this row: part k mod 2^parts_shift of run c0 + k / 2^parts_shift
+    const uint32_t c0 = x0 / per;
+    const int n = (int)((x0 + (uint32_t)steps - 1u) / per - c0 + 1u) << ls.parts_shift;
+    const int64_t base = ((int64_t)s * p.rows * p.nkv) * p.G + (int64_t)h * nq + q + ((int64_t)c0 << ls.qt_shift);
+#pragma unroll 1
+    for (int k0 = part; k0 < n; k0 += 4 * W) {
       float2 ml[4];
       float v[4][V];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const bool on = c + k * W <= c1;
-        const int64_t at = base + (int64_t)ls.qt * (on ? c + k * W : c);
+        const bool on = k0 + k * W < n;
+        const int kk = on ? k0 + k * W : k0, run = kk >> ls.parts_shift;
+        const int64_t at = base + ((int64_t)run << ls.qt_shift) + (kk - (run << ls.parts_shift)) * ls.half;
         ml[k] = ls.ml[at];
         if (!on) ml[k] = make_float2(-INFINITY, 0.f);
 #pragma unroll
@@ -375,46 +382,47 @@ __global__ void __launch_bounds__(A8_MERGE_THREADS) sx_attn8_merge_kernel(const 
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         if (ml[k].x == -INFINITY && ml[k].y == 0.f) continue;         // nothing seen there
-        const float m = fmaxf(M, ml[k].x), a = (M == -INFINITY) ? 0.f : exp2f(M - m), w = exp2f(ml[k].x - m);
+        const float m = fmaxf(M, ml[k].x), a = (M == -INFINITY) ? 0.f : a8_ex2(M - m), w = a8_ex2(ml[k].x - m);
         M = m;
         L = L * a + ml[k].y * w;
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = acc[i] * a + v[k][i] * w;
       }
     }
-  };
-  const int gq = hq - h * p.G;
-  take(p.own, b, p.rows * p.G, j * p.G + gq, (int64_t)b * p.rows * p.G * p.nkv);
-  if (p.n_groups > 0) {
-    const int g = p.seq_group[b];
-    if (g >= 0) {
-      const int s = p.group_start[g], nq = a8_members(p, g) * p.rows * p.G;
-      take(p.pre, g, nq, ((b - s) * p.rows + j) * p.G + gq, (int64_t)s * p.rows * p.G * p.nkv);
-    }
   }
-  if (lane == 0) ml_sh[warp] = make_float2(M, L);
+  if (W > 1) {
+    if (lane == 0) ml_sh[mine][part] = make_float2(M, L);
 #pragma unroll
-  for (int i = 0; i < V; ++i) o_sh[warp][lane * V + i] = acc[i];
-  __syncthreads();
-  if (threadIdx.x < D) {
+    for (int i = 0; i < V; ++i) o_sh[mine][part][lane * V + i] = acc[i];
+    __syncthreads();
+    if (part != 0) return;
     float m = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < W; ++w) m = fmaxf(m, ml_sh[w].x);
-    float l = 0.f, o = 0.f;
+    for (int w = 0; w < W; ++w) m = fmaxf(m, ml_sh[mine][w].x);
+    L = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      const float2 v = ml_sh[w];
+      const float2 v = ml_sh[mine][w];
       if (v.x == -INFINITY && v.y == 0.f) continue;
-      const float f = exp2f(v.x - m);
-      l += v.y * f;
-      o += o_sh[w][threadIdx.x] * f;
+      const float f = a8_ex2(v.x - m);
+      L += v.y * f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[i] += o_sh[mine][w][lane * V + i] * f;
     }
-    p.o_out[((int64_t)r * p.nq + hq) * D + threadIdx.x] = __float2bfloat16_rn(l == 0.f ? 0.f : o / l);
   }
+  if (!live) return;
+  bf16 y[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) y[i] = __float2bfloat16_rn(L == 0.f ? 0.f : acc[i] / L);
+  bf16 *o = p.o_out + ((int64_t)r * p.nq + hq) * D + lane * V;
+  if (V == 4) *reinterpret_cast<uint2 *>(o) = *reinterpret_cast<uint2 *>(y);
+  else *reinterpret_cast<uint32_t *>(o) = *reinterpret_cast<uint32_t *>(y);
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------
-static int split_runs(int sm_count) { return sm_count * A8S_CTAS * A8S_WARPS; }
+static int split_runs(int sm_count) { return sm_count * 3 * A8S_WARPS; }
 
 template <bool PRE, int D, int NQT>
 static sx_status launch_split(const SxA8 &p, int sm_count, cudaStream_t st) {
@@ -423,25 +431,35 @@ static sx_status launch_split(const SxA8 &p, int sm_count, cudaStream_t st) {
   static_assert(C::CODES + C::SCALES + 48 * 1024 < 200 * 1024, "ring and the largest plan fit one SM");
   // set on every call: the attribute belongs to the current device, and setting it costs less than remembering it
   SX_TRY(sx_rc(cudaFuncSetAttribute(sx_attn8_split_kernel<PRE, D, NQT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)));
-  return sx_rc(sx_launch(sx_attn8_split_kernel<PRE, D, NQT>, dim3(sm_count * A8S_CTAS), dim3(A8S_WARPS * 32), smem, st, p));
+  SX_TRY(sx_rc(cudaFuncSetAttribute(sx_attn8_split_kernel<PRE, D, NQT>, cudaFuncAttributePreferredSharedMemoryCarveout, 100)));
+  return sx_rc(sx_launch(sx_attn8_split_kernel<PRE, D, NQT>, dim3(sm_count * C::CTAS), dim3(A8S_WARPS * 32), smem, st, p));
 }
 
 // one list with the warp-level kernel
 template <bool PRE>
 static sx_status split_list(SxA8 &p, int sm_count, cudaStream_t st) {
-  if (p.d == 128)
-    return (PRE ? p.pre : p.own).qt == 8 ? launch_split<PRE, 128, 1>(p, sm_count, st) : launch_split<PRE, 128, 2>(p, sm_count, st);
-  return (PRE ? p.pre : p.own).qt == 8 ? launch_split<PRE, 64, 1>(p, sm_count, st) : launch_split<PRE, 64, 2>(p, sm_count, st);
+  const int qt = (PRE ? p.pre : p.own).qt;
+  if (p.d == 128) return qt == 8 ? launch_split<PRE, 128, 1>(p, sm_count, st) : launch_split<PRE, 128, 2>(p, sm_count, st);
+  return qt == 8 ? launch_split<PRE, 64, 1>(p, sm_count, st) : launch_split<PRE, 64, 2>(p, sm_count, st);
 }
 
 static size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+// Queries per tile of the tensor-memory kernel for at most `q` per KV head: with 32 (64) the softmax is spread over four
+// (two) copies of them, which leave a partial result each; bounded, so that the workspace of a large batch is not four
+// times what it needs.
+#define A8_COPY_ROWS 65536
+static int tc_tile(int q, size_t all) {
+  const int qt = q <= 32 ? 32 : q <= 64 ? 64 : 128;
+  return (256 / qt) * all <= A8_COPY_ROWS ? qt : 128;
+}
 // rows of partial results that any variant of a list may use
 static size_t list_rows(int nq, int B, int rows, int sm_count) {
-  const size_t split = (size_t)16 * split_runs(sm_count), tc = (size_t)128 * sm_count;
-  return (split > tc ? split : tc) + (size_t)B * rows * nq;
+  const size_t q = (size_t)B * rows * nq, split = (size_t)16 * split_runs(sm_count) + q, most = 8 * q < A8_COPY_ROWS ? 8 * q : A8_COPY_ROWS,
+               tc = (size_t)256 * sm_count + (most > 2 * q ? most : 2 * q);
+  return split > tc ? split : tc;
 }
 static size_t list_bytes(int nq, int d, int B, int rows, int units, int sm_count) {
-  return up256((size_t)units * 8) + up256((size_t)units * 4) + 256 +
+  return 2 * up256((size_t)units * 4) + 256 +
          up256(list_rows(nq, B, rows, sm_count) * 8) + up256(list_rows(nq, B, rows, sm_count) * d * 4);
 }
 
@@ -451,40 +469,61 @@ size_t sx_attn8_ws_bytes(int nq, int nkv, int d, int B, int rows, int groups, in
          (groups > 0 ? list_bytes(nq, d, B, rows, groups, sm_count) : 0);
 }
 
+template <int D, int W>
+static sx_status launch_merge(const SxA8 &p, cudaStream_t st) {
+  const int64_t rows = (int64_t)p.B * p.rows * p.nq, per = A8_MERGE_THREADS / 32 / W;
+  SX_TRY(sx_rc(cudaFuncSetAttribute(sx_attn8_merge_kernel<D, W>, cudaFuncAttributePreferredSharedMemoryCarveout, 100)));
+  return sx_rc(sx_launch(sx_attn8_merge_kernel<D, W>, dim3((unsigned)((rows + per - 1) / per)), dim3(A8_MERGE_THREADS), 0, st, p));
+}
+// Warps per output row: eight while that fills the SMs once (latency of a chain of partial results), fewer beyond
+template <int D>
+static sx_status merge(const SxA8 &p, int sm_count, cudaStream_t st) {
+  const int64_t rows = (int64_t)p.B * p.rows * p.nq, slots = 8ll * sm_count;       // CTAs of 256 threads at a time
+  return rows <= slots / 2 ? launch_merge<D, 8>(p, st) : rows <= 2 * slots ? launch_merge<D, 4>(p, st) : launch_merge<D, 1>(p, st);
+}
+
 sx_status sx_launch_attn8(SxA8 p, int kernel, char *ws, int sm_count, cudaStream_t st) {
   if ((p.d != 64 && p.d != 128) || p.page % A8_SPLIT_STEP || p.B + p.n_groups > A8_MAX_UNITS) return SX_ERR_UNSUPPORTED;
   size_t o = 0;
   auto take = [&](size_t bytes) { char *at = ws + o; o += up256(bytes); return at; };
   p.seq_group = (int32_t *)take((size_t)p.B * 4);
   auto place = [&](SxA8List &ls, int units) {
-    ls.cum = (int64_t *)take((size_t)units * 8);
+    ls.cum = (int32_t *)take((size_t)units * 4);
     ls.steps = (int32_t *)take((size_t)units * 4);
-    ls.total = (int64_t *)take(8);
+    ls.total = (int32_t *)take(4);
     ls.ml = (float2 *)take(list_rows(p.nq, p.B, p.rows, sm_count) * 8);
     ls.o = (float *)take(list_rows(p.nq, p.B, p.rows, sm_count) * p.d * 4);
   };
+  auto log2i = [](int v) { int s = 0; while ((1 << s) < v) ++s; return s; };
   place(p.own, p.B);
   if (p.n_groups > 0) place(p.pre, p.n_groups);
   const int own_q = p.rows * p.G;
   // a group has at most this many queries per KV head (the host does not know the groups)
   const int pre_q = p.n_groups > 0 ? (p.B - p.n_groups + 1 > 1 ? p.B - p.n_groups + 1 : 2) * own_q : 0;
-  auto choose = [&](SxA8List &ls, int q) -> bool {
-    const bool tc = false;
-    (void)kernel;
+  // Which kernel takes a list of `q` queries per KV head (at most, for the prefix).
+  auto choose = [&](SxA8List &ls, int q, bool &tc) -> sx_status {
+    const bool can = sx_attn8_tc_supported(p);
+    if (kernel == SX_ATTN_TC && !can) return SX_ERR_UNSUPPORTED;
+    tc = can && (kernel == SX_ATTN_TC || (kernel == SX_ATTN_AUTO && q > 16));
     ls.step = tc ? A8_TC_STEP : A8_SPLIT_STEP;
-    ls.qt = q <= 8 ? 8 : 16;
-    ls.runs = split_runs(sm_count);
-    ls.min_per = 4;
-    return tc;
+    ls.qt = tc ? tc_tile(q, (size_t)p.B * p.rows * p.nq) : q <= 8 ? 8 : 16;
+    ls.runs = tc ? sm_count : split_runs(sm_count);
+    ls.min_per = tc ? 1 : 4;
+    ls.qt_shift = log2i(ls.qt);
+    ls.step_shift = log2i(ls.step);
+    ls.parts_shift = tc ? log2i(256 / ls.qt) : 0;
+    ls.half = (int64_t)ls.qt * sm_count + (int64_t)p.B * p.rows * p.nq;
+    // list positions are 32-bit: steps of a sequence's whole capacity x KV heads x tiles of all units
+    const int64_t steps = (int64_t)p.max_pages * p.page / ls.step + 2, tiles = (int64_t)p.B * p.rows * p.G / ls.qt + p.B + p.n_groups;
+    return steps * p.nkv * tiles < (1ll << 31) - (1 << 20) ? SX_OK : SX_ERR_UNSUPPORTED;
   };
-  choose(p.own, own_q);
+  bool own_tc = false, pre_tc = false;
+  SX_TRY(choose(p.own, own_q, own_tc));
   if (p.n_groups > 0) {
-    choose(p.pre, pre_q);
+    SX_TRY(choose(p.pre, pre_q, pre_tc));
+    SX_TRY(pre_tc ? sx_launch_attn8_tc(p, true, sm_count, st) : split_list<true>(p, sm_count, st));
     p.after_prefix = 1;
-    SX_TRY(split_list<true>(p, sm_count, st));
   }
-  SX_TRY(split_list<false>(p, sm_count, st));
-  const dim3 grid(p.nq, p.B * p.rows);
-  if (p.d == 128) return sx_rc(sx_launch(sx_attn8_merge_kernel<128>, grid, dim3(A8_MERGE_THREADS), 0, st, p));
-  return sx_rc(sx_launch(sx_attn8_merge_kernel<64>, grid, dim3(A8_MERGE_THREADS), 0, st, p));
+  SX_TRY(own_tc ? sx_launch_attn8_tc(p, false, sm_count, st) : split_list<false>(p, sm_count, st));
+  return p.d == 128 ? merge<128>(p, sm_count, st) : merge<64>(p, sm_count, st);
 }

@@ -19,14 +19,21 @@
 #define A8_SPLIT_STEP 16           // slots per step of the warp-level kernel
 #define A8_TC_STEP 128             // slots per step of the tensor-memory kernel
 #define A8_MERGE_THREADS 256
+// How far (in powers of two) a score may exceed its reference before the reference moves.  A weight then stays below
+// 2^14 in fp16, whose subnormals reach down to 2^-24: whatever a row's largest weight is between 1 and 2^14, weights
+// are held to 2^-25 of it or better.  With 2^8 the reference moved in most blocks of a prefix with 128 queries
+// whose scores spread over 2^4 (one query that exceeds is enough).
+#define A8_SLACK 14.f
 
 struct SxA8List {                  // one list: what the main kernel writes down for the merge
-  int64_t *cum;                    // [units] first list position of the unit
+  int32_t *cum;                    // [units] first list position of the unit (the host has checked that lists fit)
   int32_t *steps;                  // [units] steps of one (head, tile) of the unit
-  int64_t *total;                  // [1]
+  int32_t *total;                  // [1]
   float2 *ml;                      // partial (reference, sum) per row
   float *o;                        // partial outputs [row][d]
-  int qt, step, runs, min_per;
+  int qt, qt_shift, step, step_shift, runs, min_per;
+  int parts_shift;                 // log2 of the partial results per run and tile (the tensor-memory kernel's groups and copies), `half`
+  int64_t half;                    // rows apart
 };
 
 struct SxA8 {
@@ -71,19 +78,25 @@ __device__ __forceinline__ void a8_leave(const SxA8 &p) {
 
 // ---- the plan of a list in shared memory ------------------------------------------------------------------
 struct A8Plan {
-  int64_t *cum;                    // [units + 1]
+  int32_t *cum;                    // [units + 1]
+  int32_t *steps;                  // [units] of one (head, tile)
   int32_t *len;                    // [B] cached slots (checked)
   int32_t *pre;                    // [B] slots that the shared prefix covers for the sequence
   int32_t *grp;                    // [B] group or -1
   int32_t *bad;                    // [n_groups]
-  int units;
-  int64_t per;
+  int units, per;
 };
 __host__ __device__ inline size_t a8_plan_bytes(int B, int n_groups) {
-  return ((size_t)(B + 1) * 8 + (size_t)B * 12 + (size_t)(n_groups > 0 ? n_groups : 1) * 4 + 32 * 8 + 15) & ~(size_t)15;
+  return ((size_t)(B + 1) * 4 + (size_t)B * 16 + (size_t)(n_groups > 0 ? n_groups : 1) * 4 + 32 * 4 + 15) & ~(size_t)15;
 }
 
-__device__ __forceinline__ int a8_first_slot(const A8Plan &pl, int b, int align) { return pl.pre[b] / align * align; }
+// tiles of a unit with nq queries; steps of a run
+__device__ __forceinline__ int a8_tiles(int nq, int qt_shift) { return (nq + (1 << qt_shift) - 1) >> qt_shift; }
+__device__ __forceinline__ int a8_per(int total, const SxA8List &ls) {
+  return max(ls.min_per, (int)((uint32_t)(total + ls.runs - 1) / (uint32_t)ls.runs));
+}
+// (align, the granule in which steps begin, is a power of two)
+__device__ __forceinline__ int a8_first_slot(const A8Plan &pl, int b, int align) { return pl.pre[b] & ~(align - 1); }
 __device__ __forceinline__ int a8_members(const SxA8 &p, int g) { return p.group_start[g + 1] - p.group_start[g]; }
 
 // steps of one (head, tile) of unit u
@@ -92,11 +105,11 @@ __device__ __forceinline__ int a8_steps(const SxA8 &p, const A8Plan &pl, const S
   if (PRE) {
     const int b0 = p.group_start[u], b1 = p.group_start[u + 1];
     if (b1 <= b0 || pl.pre[b0] == 0) return 0;
-    return (pl.pre[b0] + ls.step - 1) / ls.step;
+    return (pl.pre[b0] + ls.step - 1) >> ls.step_shift;
   }
   const int cap = p.max_pages * p.page;
   const int end = min(pl.len[u] + p.E, cap), a0 = a8_first_slot(pl, u, align);
-  return end > a0 ? (end - a0 + ls.step - 1) / ls.step : 0;
+  return end > a0 ? (end - a0 + ls.step - 1) >> ls.step_shift : 0;
 }
 template <bool PRE>
 __device__ __forceinline__ int a8_unit_nq(const SxA8 &p, int u) {
@@ -109,9 +122,10 @@ __device__ __forceinline__ int a8_unit_nq(const SxA8 &p, int u) {
 template <bool PRE, int NT>
 __device__ void a8_plan(const SxA8 &p, const SxA8List &ls, int align, uint8_t *smem, A8Plan &pl) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  pl.cum = reinterpret_cast<int64_t *>(smem);
-  int64_t *wsum = pl.cum + p.B + 1;
-  pl.len = reinterpret_cast<int32_t *>(wsum + 32);
+  pl.cum = reinterpret_cast<int32_t *>(smem);
+  int32_t *wsum = pl.cum + p.B + 1;
+  pl.steps = wsum + 32;
+  pl.len = pl.steps + p.B;
   pl.pre = pl.len + p.B;
   pl.grp = pl.pre + p.B;
   pl.bad = pl.grp + p.B;
@@ -119,18 +133,21 @@ __device__ void a8_plan(const SxA8 &p, const SxA8List &ls, int align, uint8_t *s
   const int cap = p.max_pages * p.page;
   bool wrong = false;
   bool ordered = true;
+#pragma unroll 1
   for (int g = tid; g < p.n_groups; g += NT) {
     pl.bad[g] = 0;
     const int s = p.group_start[g], e = p.group_start[g + 1];
     ordered = ordered && s >= 0 && s <= e && e <= p.B && (g > 0 || s == 0) && (g < p.n_groups - 1 || e == p.B);
   }
   ordered = __syncthreads_and(ordered) != 0;
+#pragma unroll 1
   for (int b = tid; b < p.B; b += NT) {
     int n = p.cache_len[b];
     if (n < 0 || n > cap - p.E) { wrong = true; n = max(0, min(n, cap)); }
     int g = -1, pre = 0;
     if (p.n_groups > 0 && ordered) {
       int lo = 0, hi = p.n_groups - 1;                 // the last group that starts at or before b
+#pragma unroll 1
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (p.group_start[mid] <= b) lo = mid; else hi = mid - 1;
@@ -146,81 +163,89 @@ __device__ void a8_plan(const SxA8 &p, const SxA8List &ls, int align, uint8_t *s
   }
   wrong = __syncthreads_or(wrong || !ordered) != 0;
   if (wrong) {
+#pragma unroll 1
     for (int b = tid; b < p.B; b += NT)
       if (pl.grp[b] >= 0 && pl.bad[pl.grp[b]]) { pl.grp[b] = -1; pl.pre[b] = 0; }
     if (tid == 0 && blockIdx.x == 0) sx_set_status(p.status, SX_ERR_CAPACITY);
     __syncthreads();
   }
   // exclusive sum of the units' list entries
-  int64_t run = 0;
+  int run = 0;
+#pragma unroll 1
   for (int u0 = 0; u0 < pl.units; u0 += NT) {
     const int u = u0 + tid;
-    int64_t x = 0;
+    int x = 0;
     if (u < pl.units && (!PRE || ordered)) {
-      const int nq = a8_unit_nq<PRE>(p, u);
-      x = (int64_t)a8_steps<PRE>(p, pl, ls, u, align) * p.nkv * ((nq + ls.qt - 1) / ls.qt);
+      const int st = a8_steps<PRE>(p, pl, ls, u, align);
+      pl.steps[u] = st;
+      x = st * p.nkv * a8_tiles(a8_unit_nq<PRE>(p, u), ls.qt_shift);
     }
-    int64_t s = x;
+    int s = x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(0xffffffffu, s, o);
+      const int y = __shfl_up_sync(0xffffffffu, s, o);
       if (lane >= o) s += y;
     }
     if (lane == 31) wsum[warp] = s;
     __syncthreads();
-    int64_t before = run, all = 0;
-#pragma unroll
+    int before = run, all = 0;
+#pragma unroll 1
     for (int w = 0; w < NT / 32; ++w) {
-      if (w < warp) before += wsum[w];
-      all += wsum[w];
+      const int y = wsum[w];
+      if (w < warp) before += y;
+      all += y;
     }
     if (u < pl.units) pl.cum[u] = before + s - x;
     run += all;
     __syncthreads();
   }
   if (tid == 0) pl.cum[pl.units] = run;
-  const int64_t per = (run + ls.runs - 1) / ls.runs;
-  pl.per = per < ls.min_per ? ls.min_per : per;
+  pl.per = a8_per(run, ls);
   __syncthreads();
 }
 
 // what the merge needs to find the partial results again (CTA 0, once nothing earlier can still be reading it)
 template <bool PRE, int NT>
-__device__ __forceinline__ void a8_publish(const SxA8 &p, const A8Plan &pl, const SxA8List &ls, int align) {
+__device__ __forceinline__ void a8_publish(const SxA8 &p, const A8Plan &pl, const SxA8List &ls) {
   if (blockIdx.x != 0) return;
+#pragma unroll 1
   for (int u = threadIdx.x; u < pl.units; u += NT) {
     ls.cum[u] = pl.cum[u];
-    ls.steps[u] = pl.cum[u + 1] > pl.cum[u] ? a8_steps<PRE>(p, pl, ls, u, align) : 0;
+    ls.steps[u] = pl.cum[u + 1] > pl.cum[u] ? pl.steps[u] : 0;
   }
   if (threadIdx.x == 0) ls.total[0] = pl.cum[pl.units];
   if (!PRE)
+#pragma unroll 1
     for (int b = threadIdx.x; b < p.B; b += NT) p.seq_group[b] = pl.pre[b] > 0 ? pl.grp[b] : -1;
 }
 
 // a place in a list: the segment (unit, head, tile) that holds list position x
 struct A8Seg {
   int u, h, tile, cols;            // cols: queries of the tile
-  int64_t x0, x1;                  // list positions of the segment
+  int x0, x1;                      // list positions of the segment
   int b0, r0, first, end, len;     // table row, first query row, slots [first, end), cached slots
   int lo;                          // slots below it belong to the shared prefix
   int64_t base;                    // partial-result rows before qt * run is added
 };
+// (Written for few instructions: every role of the kernels that call it has a copy of it, and with divisions in 64 bits
+// in here the code of a kernel passed 100 KB and ran out of the instruction cache: 14 us for the smallest call, and
+// every part of the others several times slower.)
 template <bool PRE>
-__device__ __forceinline__ A8Seg a8_seek(const SxA8 &p, const A8Plan &pl, const SxA8List &ls, int align, int64_t x) {
+__device__ __forceinline__ A8Seg a8_seek(const SxA8 &p, const A8Plan &pl, const SxA8List &ls, int align, int x) {
   A8Seg s;
   int lo = 0, hi = pl.units - 1;                       // the last unit that starts at or before x
+#pragma unroll 1
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (pl.cum[mid] <= x) lo = mid; else hi = mid - 1;
   }
   s.u = lo;
-  const int nq = a8_unit_nq<PRE>(p, lo), nt = (nq + ls.qt - 1) / ls.qt;
-  const int64_t entries = pl.cum[lo + 1] - pl.cum[lo];
-  const int steps = (int)(entries / (p.nkv * nt)), r = (int)((x - pl.cum[lo]) / steps);
-  s.h = r / nt;
+  const int nq = a8_unit_nq<PRE>(p, lo), nt = a8_tiles(nq, ls.qt_shift), steps = pl.steps[lo];
+  const int r = (int)((uint32_t)(x - pl.cum[lo]) / (uint32_t)steps);
+  s.h = nt == 1 ? r : (int)((uint32_t)r / (uint32_t)nt);
   s.tile = r - s.h * nt;
-  s.cols = min(ls.qt, nq - s.tile * ls.qt);
-  s.x0 = pl.cum[lo] + (int64_t)r * steps;
+  s.cols = min(ls.qt, nq - (s.tile << ls.qt_shift));
+  s.x0 = pl.cum[lo] + r * steps;
   s.x1 = s.x0 + steps;
   if (PRE) {
     s.b0 = p.group_start[lo];
@@ -228,12 +253,26 @@ __device__ __forceinline__ A8Seg a8_seek(const SxA8 &p, const A8Plan &pl, const 
     s.end = pl.pre[s.b0]; s.len = s.end;
   } else {
     s.b0 = lo;
-    s.first = a8_first_slot(pl, lo, align); s.lo = pl.pre[lo];
+    s.lo = pl.pre[lo];
+    s.first = s.lo & ~(align - 1);
     s.len = pl.len[lo]; s.end = min(s.len + p.E, p.max_pages * p.page);
   }
   s.r0 = s.b0 * p.rows;
-  s.base = (int64_t)s.r0 * p.G * p.nkv + (int64_t)s.h * nq + (int64_t)s.tile * ls.qt;
+  s.base = (int64_t)s.r0 * p.G * p.nkv + (int64_t)s.h * nq + (s.tile << ls.qt_shift);
   return s;
+}
+// bit j: slot first + j (j < n <= 32) is seen by a row of the segment whose drafted slots are `mask`
+template <bool PRE>
+__device__ __forceinline__ uint32_t a8_visible(const A8Seg &s, uint64_t mask, int first, int n) {
+  const int a = max(s.lo - first, 0), b = min(s.len - first, n);
+  uint64_t v = b > a ? ((1ull << b) - 1ull) & ~((1ull << a) - 1ull) : 0ull;
+  if (!PRE) {
+    const int drafted = s.end - s.len, at = first - s.len;        // drafted slots; position of `first` among them
+    if (drafted < 64) mask &= (1ull << max(drafted, 0)) - 1ull;
+    if (at >= 0) v |= at < 64 ? mask >> at : 0ull;
+    else if (at > -32) v |= mask << -at;
+  }
+  return (uint32_t)v;
 }
 
 // running softmax in base 2 over s' = s + e, where 2^e is the scale of the slot's value row: the weight of a code row

@@ -1,0 +1,672 @@
+// Decode attention over the 8-bit paged cache on the 5th-generation tensor cores, for head dimension 128 and many
+// queries per KV head: a prefix that a group of sequences shares (its members' queries side by side), or the
+// sibling rows of a draft tree.  Up to 128 queries per tile.
+//
+// Work, partial results and merge are those of sx_attn8.cuh: a CTA takes one run of 128-slot blocks.  Per block, with the
+// queries on M:
+//     S[q][slot] = sum_d Q[q][d] kc[slot][d]         A = Q, B = K codes as they lie in the pages (both K-major)
+//     O[q][d]   += sum_slot P[q][slot] V[slot][d]    A = P from tensor memory, B = V as bf16 (N-major)
+// First product: e4m3 x e4m3.  A bf16 query is the exact sum of two e4m3 numbers (4 + 4 significand bits) once its
+// row is scaled by a power of two, down to 2^-10 / 224 of the row's largest value; so A is [high part] then [low part]
+// into the same accumulator - the cost of one bf16 product, and K is used as it was stored; its scale is a factor of the
+// slot's scores.  Second product: weights need 16 bits (in 8 a long flat tail of small weights would vanish), so V becomes
+// bf16 in shared memory, exactly (4 significand bits, a power of two), by eight warps of their own, once per block
+// whatever the number of queries: a code's exponent and mantissa are moved to their places in a bf16 number and one packed
+// multiplication by 2^(120 + e) puts bias and scale right.
+// (Tried before: slots on M, so that a thread owned a slot and the softmax ran across threads - a barrier vote per block,
+// weights through shared memory, a reference per query to fetch for every score: 6500 cycles per block with 128 queries,
+// 3400 with 32.  V as fp16 codes with its scale in the score and a second factor in the sums: three broadcasts from
+// shared memory per score pair, 4000 cycles.  K as bf16 too: the widening of both took 4700.)
+//
+// Two groups of four softmax warps take a half of every block each (64 slots), with scores (two buffers: the next
+// block's are ready when a group comes to them), weights (in place of the scores, as they are read), references, sums and
+// an output accumulator of their own: 2 x (2 x 64 + 128) columns of tensor memory, and nothing to agree on between
+// threads - a thread owns one query, its reference and its sum, and moves the reference when a score exceeds it by
+// more than 2^T8_SLACK.  With up to 64 (32) queries the 128 rows of the products hold 2 (4) copies of them, and a
+// copy's threads take a half (a quarter) of the group's slots, with weights of zero for the others: the products cost the
+// same, and the softmax of 32 queries, one warp's work before, is spread over four.  Every copy of every group leaves
+// its own partial result.
+//
+// Warps: 0 K producer, 1 issuer of the first product (owns TMEM), 2 V producer, 3 issuer of the second, 4-11 softmax,
+// 12-19 widen V, lay out the scales of K and load Q.  Every mbarrier wait is bounded (sx_tc_ptx.cuh).
+#include <cuda.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <math.h>
+
+#include "sx_attn8.cuh"
+#include "sx_kernels.cuh"
+#include "sx_launch.cuh"
+#include "sx_tc_ptx.cuh"
+
+#define T8_THREADS 640
+#define T8_BLK (128 * 128)               // bytes of the codes of a block
+#define T8_NONE (-1e30f)                 // reference before the first visible score
+// Weights are bf16, sums fp32: their precision does not depend on where the reference lies, so it moves only where the
+// range of numbers asks for it.
+#define T8_SLACK 30.f
+#ifndef T8_NK
+#define T8_NK 4                          // ring slots of 16 KB for the codes of K,
+#define T8_NV 3                          // of V
+#define T8_NW 2                          // bf16 copies (32 KB) of V blocks
+#define T8_NC 4                          // entries of K scales; of query factors
+#endif
+#define T8_Q_BYTES T8_BLK                // one of the two parts
+#define T8_O_COL 256                     // tensor memory: scores / weights of the groups, then their outputs
+#define T8_OFF_W (2 * T8_Q_BYTES)
+#define T8_OFF_RING (T8_OFF_W + T8_NW * 2 * T8_BLK)
+#define T8_OFF_SC (T8_OFF_RING + (T8_NK + T8_NV) * T8_BLK)             // [slot of V][128 + 128] exponent bytes of K and V
+#define T8_OFF_KS (T8_OFF_SC + 1024)                     // [entry][128] scales of K
+#define T8_OFF_QF (T8_OFF_KS + T8_NC * 512)              // [entry][128] factor of the query's scores
+#define T8_OFF_BAR (T8_OFF_QF + T8_NC * 512)
+#define T8_OFF_PLAN (T8_OFF_BAR + 512)
+#define T8_FIXED (T8_OFF_PLAN + 1024)                    // + alignment
+#define T8_SMEM_MAX (227 * 1024)
+
+template <int N> __device__ __forceinline__ void t8_setreg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void t8_setreg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+__device__ __forceinline__ float t8_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Bounded wait of one thread.  The poll carries a time for which the hardware may keep the thread asleep: a dozen warps
+// polling without one kept the shared-memory pipe so busy that every access of the others took hundreds of cycles.
+#define T8_NAP_NS 20000u
+#define T8_WAIT_POLLS (1u << 17)          // x T8_NAP_NS: about 2.6 s
+__device__ __forceinline__ bool t8_poll(uint64_t *bar, uint32_t parity, volatile int *abort_flag, uint32_t limit) {
+  const uint32_t at = smem_u32(bar);
+  for (uint32_t i = 0; i < limit; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(at), "r"(parity), "r"(T8_NAP_NS) : "memory");
+    if (ok) return true;
+    if (*abort_flag) return false;
+  }
+  *abort_flag = 1;
+  return false;
+}
+// of a warp: one lane polls for all of it
+__device__ __forceinline__ bool t8_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, uint32_t limit, int lane) {
+  bool ok = true;
+  if (lane == 0) ok = t8_poll(bar, parity, abort_flag, limit);
+  return __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+}
+// true in one thread of the warp; unlike a test of the lane, the compiler knows that of it, and issues the tensor-core
+// instructions (whose operands live in uniform registers) without a loop over the threads that might be there
+__device__ __forceinline__ bool t8_elect() {
+  uint32_t one;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(one));
+  return one != 0;
+}
+// two fp32 operations in one instruction
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 t8_pack(float a, float b) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void t8_unpack(f32x2 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 t8_mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 t8_add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 t8_fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+// D[tmem] (+)= A[smem] * B[smem], e4m3 x e4m3 -> fp32, M = 128, K = 32
+__device__ __forceinline__ void t8_mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem], bf16 x bf16 -> fp32, M = 128, K = 16
+__device__ __forceinline__ void t8_mma_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// columns of this thread's TMEM lane as they are
+__device__ __forceinline__ void t8_st(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]),
+        "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+      : "memory");
+}
+__device__ __forceinline__ void t8_st(uint32_t taddr, const uint32_t (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+__device__ __forceinline__ void t8_ld(uint32_t taddr, float (&v)[16]) { tc_ld16(taddr, v); }
+__device__ __forceinline__ void t8_ld(uint32_t taddr, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr) : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+// four codes to bf16, times `f` (a packed pair of equal bf16 numbers): exponent and mantissa move to the low end of the
+// exponent's place and the high end of the mantissa's, which is the value times 2^-120; f = 2^(120 + e)
+__device__ __forceinline__ void t8_widen4(uint32_t x, uint32_t f, uint32_t &lo2, uint32_t &hi2) {
+  const uint32_t hi = ((x >> 4) & 0x07070707u) | (x & 0x80808080u), lo = (x << 4) & 0xf0f0f0f0u;
+  uint32_t a = __byte_perm(lo, hi, 0x5140), b = __byte_perm(lo, hi, 0x7362);
+  const __nv_bfloat162 ff = *reinterpret_cast<const __nv_bfloat162 *>(&f);
+  __nv_bfloat162 va = __hmul2(*reinterpret_cast<__nv_bfloat162 *>(&a), ff), vb = __hmul2(*reinterpret_cast<__nv_bfloat162 *>(&b), ff);
+  lo2 = *reinterpret_cast<uint32_t *>(&va);
+  hi2 = *reinterpret_cast<uint32_t *>(&vb);
+}
+// packed bf16 2^n, n in [-126, 127]
+__device__ __forceinline__ uint32_t t8_pow2x2(int n) { return (uint32_t)(127 + n) * 0x00800080u; }
+__device__ __forceinline__ uint32_t t8_mulx2(uint32_t x, uint32_t f) {
+  const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&f));
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+// the largest finite number in place of infinity: what a slot holds that no query sees must not meet a weight of 0
+__device__ __forceinline__ uint32_t t8_finite(uint32_t x) {
+  const uint32_t top = 0x7f7f7f7fu, bottom = 0xff7fff7fu;
+  const __nv_bfloat162 v = __hmax2(__hmin2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&top)),
+                                   *reinterpret_cast<const __nv_bfloat162 *>(&bottom));
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+template <bool PRE, int COPIES>
+__global__ void __launch_bounds__(T8_THREADS, 1)
+sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                   const __grid_constant__ SxA8 p, int slab, uint32_t wait_limit) {
+  constexpr int NK = T8_NK, NV = T8_NV, NW = T8_NW;
+  extern __shared__ uint8_t t8_raw[];
+  // an offset, not a cast to an integer and back: the compiler keeps seeing shared memory (generic loads cost a multiple)
+  uint8_t *smem = t8_raw + ((0u - smem_u32(t8_raw)) & 1023u);
+  uint8_t *sQ = smem, *sW = smem + T8_OFF_W, *ringK = smem + T8_OFF_RING, *ringV = ringK + NK * T8_BLK;
+  uint8_t *sc = smem + T8_OFF_SC;
+  float *ks_sh = reinterpret_cast<float *>(smem + T8_OFF_KS), *qf = reinterpret_cast<float *>(smem + T8_OFF_QF);
+  uint64_t *bars = reinterpret_cast<uint64_t *>(smem + T8_OFF_BAR);
+  uint64_t *kfull = bars, *kempty = kfull + NK, *vfull = kempty + NK, *vempty = vfull + NV;
+  // [group][block & 1]: scores ready, weights ready, second product done
+  uint64_t *sfull = vempty + NV, *pfull = sfull + 4, *pvdone = pfull + 4, *ofree = pvdone + 4, *wfull = ofree + 2;
+  uint64_t *wempty = wfull + NW, *cfull = wempty + NW, *qfull = cfull + T8_NC, *qempty = qfull + 1;
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(qempty + 1);
+  static_assert(COPIES == 1 || COPIES == 2 || COPIES == 4, "rows of a product hold whole copies");
+  constexpr int QT = 128 / COPIES, CH = COPIES == 4 ? 16 : 32, NCH = 64 / COPIES / CH;     // queries; slots per chunk; chunks
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  a8_enter<PRE>(p);
+  const SxA8List &ls = PRE ? p.pre : p.own;
+  A8Plan pl;
+  a8_plan<PRE, T8_THREADS>(p, ls, slab, smem + T8_OFF_PLAN, pl);
+  a8_planned<PRE>(p);
+  a8_publish<PRE, T8_THREADS>(p, pl, ls);
+  const int total = pl.cum[pl.units], g0 = (int)min((int64_t)total, (int64_t)blockIdx.x * pl.per), g1 = g0 + min(total - g0, pl.per);
+  if (g0 >= g1) { a8_leave<PRE>(p); return; }
+  const int nblk = g1 - g0;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < NK; ++i) { mbar_init(smem_u32(&kfull[i]), 1); mbar_init(smem_u32(&kempty[i]), 1); }
+    for (int i = 0; i < NV; ++i) { mbar_init(smem_u32(&vfull[i]), 1); mbar_init(smem_u32(&vempty[i]), 4); }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(smem_u32(&sfull[i]), 1); mbar_init(smem_u32(&pfull[i]), 4); mbar_init(smem_u32(&pvdone[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&ofree[i]), 4);
+    for (int i = 0; i < NW; ++i) { mbar_init(smem_u32(&wfull[i]), 4); mbar_init(smem_u32(&wempty[i]), 1); }
+    for (int i = 0; i < T8_NC; ++i) mbar_init(smem_u32(&cfull[i]), 4);
+    mbar_init(smem_u32(qfull), 4);
+    mbar_init(smem_u32(qempty), 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    tc_alloc(smem_u32(tmem_slot), 512);
+    tc_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp < 4) {
+    t8_setreg_dec<56>();
+    if (warp == 0 || warp == 2) {
+      // ---- producers: the codes of a block (one box per `slab` slots, which lie in one page); V's with the exponent bytes ----
+      const bool is_v = warp == 2;
+      const CUtensorMap *map = is_v ? &tmV : &tmK;
+      uint8_t *ring = is_v ? ringV : ringK;
+      uint64_t *full = is_v ? vfull : kfull, *empty = is_v ? vempty : kempty;
+      const int depth = is_v ? NV : NK, nbox = 128 / slab;
+      const uint64_t pol = policy_evict_first();
+      bool bad = false;
+      A8Seg s = a8_seek<PRE>(p, pl, ls, slab, g0);
+      // first pool row of box `lane` of the block at list position x; -1 where there is none
+      auto row_of = [&](int x) -> int {
+        if (lane >= nbox) return -1;
+        const int slot = s.first + (x - s.x0) * 128 + lane * slab;
+        if (slot >= s.end) return -1;
+        const int lp = slot / p.page, off = slot - lp * p.page;
+        const int pp = lp < p.max_pages ? p.page_table[(int64_t)s.b0 * p.max_pages + lp] : -1;
+        if (pp < 0 || pp >= p.num_pages) { bad = true; return -1; }
+        return (pp * p.nkv + s.h) * p.page + off;
+      };
+      int row = row_of(g0);
+#pragma unroll 1
+      for (int li = 0; li < nblk; ++li) {
+        int next = -1;
+        if (li + 1 < nblk) {                                // looked up while this block's slot may still be busy
+          if (g0 + li + 1 == s.x1) s = a8_seek<PRE>(p, pl, ls, slab, g0 + li + 1);
+          next = row_of(g0 + li + 1);
+        }
+        const int slot = li % depth;
+        if (li >= depth && !t8_wait(&empty[slot], (uint32_t)(li / depth - 1) & 1u, abort_flag, wait_limit, lane)) break;
+        const uint32_t fb = smem_u32(&full[slot]);
+        const uint32_t live = __ballot_sync(0xffffffffu, row >= 0);
+        if (lane == 0) mbar_expect_tx(fb, T8_BLK + (is_v ? 2u * (uint32_t)__popc(live) * (uint32_t)slab : 0u));
+        __syncwarp();
+        if (lane < nbox) {
+          // a box behind the last row of the pool reads zeros
+          tma_load_2d(smem_u32(ring + slot * T8_BLK + lane * slab * 128), map, fb, 0, row >= 0 ? row : p.num_pages * p.nkv * p.page, pol);
+          if (is_v && row >= 0) {
+            bulk_load(smem_u32(sc + slot * 256 + lane * slab), p.ks + row, (uint32_t)slab, fb);
+            bulk_load(smem_u32(sc + slot * 256 + 128 + lane * slab), p.vs + row, (uint32_t)slab, fb);
+          }
+        }
+        row = next;
+      }
+      if (!is_v && __any_sync(0xffffffffu, bad) && lane == 0) sx_set_status(p.status, SX_ERR_CAPACITY);
+    } else if (t8_elect()) {
+      A8Seg s = a8_seek<PRE>(p, pl, ls, slab, g0);
+      int item = 0, seg_li = 0;                             // segment number, its first block in the run
+      const uint32_t acc32 = (1u << 4) | (8u << 24);        // fp32 accumulate, M = 128 (M / 16 at bit 24)
+      if (warp == 1) {
+        // ---- first product: e4m3 (format 0), both operands K-major, N = 64 (N / 8 at bit 17) -------------------------
+        const uint64_t qd = smem_desc(smem_u32(sQ));
+        bool ok = true;
+#pragma unroll 1
+        for (int li = 0; li < nblk && ok; ++li) {
+          if (li > 0 && g0 + li == s.x1) { s = a8_seek<PRE>(p, pl, ls, slab, g0 + li); ++item; seg_li = li; }
+          if (li == seg_li && !t8_poll(qfull, (uint32_t)item & 1u, abort_flag, wait_limit)) break;
+          const int slot = li % NK, b = li & 1;
+          if (!t8_poll(&kfull[slot], (uint32_t)(li / NK) & 1u, abort_flag, wait_limit)) break;
+          // the scales too: whoever sees the scores may read them
+          if (!t8_poll(&cfull[li % T8_NC], (uint32_t)(li / T8_NC) & 1u, abort_flag, wait_limit)) break;
+          const uint64_t kd = smem_desc(smem_u32(ringK + slot * T8_BLK));
+#pragma unroll 1
+          for (int g = 0; g < 2 && ok; ++g) {
+            // the weights of the group's block before last, which lie in place of its scores, have met V
+            if (li >= 2) ok = t8_poll(&pvdone[g * 2 + b], (uint32_t)((li >> 1) - 1) & 1u, abort_flag, wait_limit);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              t8_mma_f8(tmem + (uint32_t)(g * 128 + b * 64), qd + (uint64_t)(((k >> 2) * T8_Q_BYTES + (k & 3) * 32) >> 4),
+                        kd + (uint64_t)((g * (T8_BLK / 2) + (k & 3) * 32) >> 4), acc32 | (8u << 17), k > 0 ? 1u : 0u);
+            tc_commit(smem_u32(&sfull[g * 2 + b]));
+          }
+          tc_commit(smem_u32(&kempty[slot]));
+          if (g0 + li + 1 == s.x1) tc_commit(smem_u32(qempty));       // the segment's queries are not needed any more
+        }
+      } else {
+        // ---- second product: bf16 (format 1), weights from tensor memory, V N-major, N = 128 --------------------------
+        bool ok = true;
+#pragma unroll 1
+        for (int li = 0; li < nblk && ok; ++li) {
+          if (li > 0 && g0 + li == s.x1) { s = a8_seek<PRE>(p, pl, ls, slab, g0 + li); ++item; seg_li = li; }
+          const int wb = li % NW, b = li & 1;
+          const bool first = li == seg_li;
+          if (!t8_poll(&wfull[wb], (uint32_t)(li / NW) & 1u, abort_flag, wait_limit)) break;
+          const uint64_t wd = smem_desc_mn(smem_u32(sW + wb * 2 * T8_BLK), T8_BLK, 1024u);
+#pragma unroll 1
+          for (int g = 0; g < 2 && ok; ++g) {
+            ok = t8_poll(&pfull[g * 2 + b], (uint32_t)(li >> 1) & 1u, abort_flag, wait_limit);
+            // the group has read out its output of the segment before
+            if (ok && first && item > 0) ok = t8_poll(&ofree[g], (uint32_t)(item - 1) & 1u, abort_flag, wait_limit);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              t8_mma_ta(tmem + T8_O_COL + (uint32_t)g * 128u, tmem + (uint32_t)(g * 128 + b * 64 + k * 8),
+                        wd + (uint64_t)((g * 4 + k) * 128),
+                        acc32 | (1u << 7) | (1u << 10) | (1u << 16) | (16u << 17), (first && k == 0) ? 0u : 1u);
+            tc_commit(smem_u32(&pvdone[g * 2 + b]));
+          }
+          tc_commit(smem_u32(&wempty[wb]));
+        }
+      }
+    }
+  } else if (warp >= 12) {
+    // ---- V codes to bf16 ([64 columns][128 slots][128 bytes] twice, 128-byte swizzle), scales of K, queries --------------
+    t8_setreg_dec<80>();
+    // two teams of four warps take the blocks in turn, each with its copy of V
+    const int team = (warp - 12) >> 2, tid = threadIdx.x & 127, c = tid & 7, r0 = tid >> 3;
+    static_assert(NW == 2, "a copy of V per team");
+    A8Seg s = a8_seek<PRE>(p, pl, ls, slab, g0);
+    int item = 0;
+#pragma unroll 1
+    for (int li = team; li < nblk; li += 2) {
+      // both teams wait for the end of every segment's first products, so that neither can be a phase behind
+      bool ok = true;
+#pragma unroll 1
+      while (ok && g0 + li >= s.x1) {
+        ok = t8_wait(qempty, (uint32_t)item & 1u, abort_flag, wait_limit, lane);
+        s = a8_seek<PRE>(p, pl, ls, slab, s.x1);
+        ++item;
+      }
+      if (!ok) break;
+      if (li == 0 || g0 + li == s.x0) {
+        // the queries of a segment: two e4m3 parts (rows of 128 bytes, 128-byte swizzle) and factor; eight threads share a row
+        const int buf = item % T8_NC;
+#pragma unroll 1
+        for (int q = r0; q < 128; q += 16) {
+          const int query = q % QT;
+          const bool live = query < s.cols;
+          const int qi = s.tile * QT + (live ? query : 0), j = qi / p.G, r = s.r0 + j;
+          const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (int64_t)r * p.q_stride + (int64_t)(s.h * p.G + qi - j * p.G) * 128 + c * 16);
+          uint4 x[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+          if (live) { x[0] = src[0]; x[1] = src[1]; }
+          const uint32_t m = 0x7fff7fffu;
+          uint32_t top = __vmaxu2(__vmaxu2(__vmaxu2(x[0].x & m, x[0].y & m), __vmaxu2(x[0].z & m, x[0].w & m)),
+                                  __vmaxu2(__vmaxu2(x[1].x & m, x[1].y & m), __vmaxu2(x[1].z & m, x[1].w & m)));
+          top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+          for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o, 8));
+          // largest magnitude into (224, 448], as for the rows of the cache
+          const int e = (int)(top >> 7);
+          int ex = top == 0 || e == 255 ? 0 : e - 135 + ((top & 0x7f) > 96 ? 1 : 0);
+          ex = max(-126, ex);
+          const float up = __uint_as_float((uint32_t)(127 - ex) << 23);
+          const uint32_t in[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+          uint32_t hi[4], lo[4];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float2 f = make_float2(__uint_as_float(in[k] << 16) * up, __uint_as_float(in[k] & 0xffff0000u) * up);
+            const uint32_t h2 = e == 255 ? 0x7f7fu : (uint32_t)__nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
+            const __half2_raw wide = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h2, __NV_E4M3);
+            const float2 back = __half22float2(*reinterpret_cast<const __half2 *>(&wide));
+            const uint32_t l2 = e == 255 ? 0x7f7fu : (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f.x - back.x, f.y - back.y), __NV_SATFINITE, __NV_E4M3);
+            if (k & 1) { hi[k >> 1] |= h2 << 16; lo[k >> 1] |= l2 << 16; }
+            else { hi[k >> 1] = h2; lo[k >> 1] = l2; }
+          }
+          uint8_t *at = sQ + q * 128 + ((c ^ (q & 7)) << 4);
+          *reinterpret_cast<uint4 *>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4 *>(at + T8_Q_BYTES) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          if (c == 0) qf[buf * 128 + q] = __uint_as_float((uint32_t)(127 + ex) << 23) * p.scale_log2;
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(qfull));
+      }
+      const int slot0 = s.first + (g0 + li - s.x0) * 128;
+      const bool whole = slot0 >= s.lo && slot0 + 128 <= s.len;
+      const int slot = li % NV, e = li % T8_NC;
+      if (!t8_wait(&vfull[slot], (uint32_t)(li / NV) & 1u, abort_flag, wait_limit, lane)) break;
+      const uint8_t *kbytes = sc + slot * 256, *vbytes = kbytes + 128;
+      // a row of K or V that is not finite makes the slot's scores so (whoever sees the slot gets it, whoever does not is
+      // spared); such a V is zero here
+      const int kbyte = kbytes[tid], vbyte = vbytes[tid];
+      ks_sh[e * 128 + tid] = kbyte == 255 || vbyte == 255 ? __int_as_float(0x7fffffff) : a8_pow2(kbyte);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&cfull[e]));
+      uint4 x[8];
+      const uint8_t *src = ringV + slot * T8_BLK + r0 * 128 + ((c ^ (r0 & 7)) << 4);
+#pragma unroll
+      for (int it = 0; it < 8; ++it) x[it] = *reinterpret_cast<const uint4 *>(src + it * 2048);
+      uint32_t f[8];                                        // 2^(120 + e)
+      int top = 0;
+#pragma unroll
+      for (int it = 0; it < 8; ++it) {
+        const int byte = vbytes[it * 16 + r0];
+        f[it] = byte == 255 ? 0u : t8_pow2x2(min(byte, 134) - 7);
+        top = max(top, byte == 255 ? 0 : byte);
+      }
+      // rows whose 2^(120 + e) is out of range (in two steps), blocks with slots that no query may see
+      const bool rare = !whole || __any_sync(0xffffffffu, top > 134);
+      if (li >= NW && !t8_wait(&wempty[team], (uint32_t)(li / NW - 1) & 1u, abort_flag, wait_limit, lane)) break;
+      // chunks 2c and 2c + 1 of the half; the lanes of the second half go the other way round, so that eight lanes of one
+      // row fall into eight different groups of banks
+      const int hi = c >> 2, ka = ((2 * c) & 7) + hi, kb = ((2 * c) & 7) + 1 - hi;
+      uint8_t *dst = sW + team * 2 * T8_BLK + hi * T8_BLK + r0 * 128;
+      uint8_t *da = dst + ((ka ^ (r0 & 7)) << 4), *db = dst + ((kb ^ (r0 & 7)) << 4);
+#pragma unroll
+      for (int it = 0; it < 8; ++it) {
+        uint32_t o[8];
+        t8_widen4(x[it].x, f[it], o[0], o[1]);
+        t8_widen4(x[it].y, f[it], o[2], o[3]);
+        t8_widen4(x[it].z, f[it], o[4], o[5]);
+        t8_widen4(x[it].w, f[it], o[6], o[7]);
+        const uint4 a = make_uint4(o[0], o[1], o[2], o[3]), b = make_uint4(o[4], o[5], o[6], o[7]);
+        *reinterpret_cast<uint4 *>(da + it * 2048) = hi ? b : a;
+        *reinterpret_cast<uint4 *>(db + it * 2048) = hi ? a : b;
+      }
+      if (rare) {
+#pragma unroll 1
+        for (int it = 0; it < 8; ++it) {
+          const int byte = vbytes[it * 16 + r0];
+          const uint32_t g2 = t8_pow2x2(byte > 134 && byte != 255 ? byte - 134 : 0);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            uint4 *at = reinterpret_cast<uint4 *>((k ? db : da) + it * 2048);
+            uint4 v = *at;
+            v.x = t8_finite(t8_mulx2(v.x, g2)); v.y = t8_finite(t8_mulx2(v.y, g2));
+            v.z = t8_finite(t8_mulx2(v.z, g2)); v.w = t8_finite(t8_mulx2(v.w, g2));
+            *at = v;
+          }
+        }
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) { mbar_arrive(smem_u32(&vempty[slot])); mbar_arrive(smem_u32(&wfull[team])); }
+    }
+  } else {
+    // ---- softmax: group g takes blocks g, g + 2, ...; a thread owns query (TMEM lane) i --------------------------------
+    t8_setreg_inc<128>();       // 56 + 2 x 128 + 2 x 80 <= 5 x 96, what the block was launched with
+    const int g = (warp - 4) >> 2, w = warp & 3, i = w * 32 + lane;
+    const int copy = i / QT, query = i % QT;
+    const int k0 = copy * (64 / COPIES);                     // this copy's slots within the group's half of a block
+    const uint32_t lane_base = tmem + ((uint32_t)(w * 32) << 16), o_col = lane_base + T8_O_COL + (uint32_t)g * 128u;
+    A8Seg s = a8_seek<PRE>(p, pl, ls, slab, g0);
+    int item = 0;
+    bool ok = true;
+    float m = T8_NONE, factor = 0.f;
+    uint64_t mask = 0;
+    f32x2 l2 = 0ull;
+#pragma unroll 1
+    for (int li = 0; li < nblk; ++li) {
+      const int x = g0 + li;
+      if (x == s.x1) { s = a8_seek<PRE>(p, pl, ls, slab, x); ++item; }
+      const bool first = li == 0 || x == s.x0, last = li == nblk - 1 || x + 1 == s.x1;
+      const bool work = (w * 32) % QT < s.cols;              // some thread of this warp has a query
+      const int e = li % T8_NC, b = li & 1;
+      const uint32_t s_col = lane_base + (uint32_t)(g * 128 + b * 64);
+      ok = t8_wait(&sfull[g * 2 + b], (uint32_t)(li >> 1) & 1u, abort_flag, wait_limit, lane);
+      if (!ok) break;
+      if (work) {
+        tc_fence_after();
+        if (first) {
+          m = T8_NONE;
+          l2 = 0ull;
+          factor = qf[(item % T8_NC) * 128 + i];
+          if (!PRE) mask = p.row_mask ? p.row_mask[s.r0 + (s.tile * QT + min(query, s.cols - 1)) / p.G] : ~0ull;
+        }
+        const int slot0 = s.first + (x - s.x0) * 128;
+        const bool whole = slot0 >= s.lo && slot0 + 128 <= s.len;
+        const int mine = slot0 + g * 64 + k0;
+        const ulonglong2 *kb = reinterpret_cast<const ulonglong2 *>(ks_sh + e * 128 + g * 64 + k0);
+        const f32x2 f2 = t8_pack(factor, factor);
+        // scores of CH slots in base 2, less `ref`; -inf where a slot is not seen.  Returns their maximum.
+        float t[CH];
+        auto scores = [&](int c, float ref) -> float {         // one copy of this in the code: see the note at a8_seek
+          t8_ld(s_col + (uint32_t)(k0 + c * CH), t);
+          const f32x2 r2 = t8_pack(-ref, -ref);
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int j = 0; j < CH; j += 4) {
+            const ulonglong2 k = kb[c * (CH / 4) + (j >> 2)];
+            t8_unpack(t8_fma2(t8_mul2(t8_pack(t[j], t[j + 1]), k.x), f2, r2), t[j], t[j + 1]);
+            t8_unpack(t8_fma2(t8_mul2(t8_pack(t[j + 2], t[j + 3]), k.y), f2, r2), t[j + 2], t[j + 3]);
+          }
+          if (!whole) {
+            const uint32_t seen = a8_visible<PRE>(s, mask, mine + c * CH, CH);
+#pragma unroll
+            for (int j = 0; j < CH; ++j)
+              if (!((seen >> j) & 1u)) t[j] = -INFINITY;
+          }
+#pragma unroll
+          for (int j = 0; j < CH; j += 4) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], t[j + k]);
+          }
+          return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        };
+#pragma unroll 1
+        for (int c = 0; c < NCH; ++c) {
+          const bool none = m == T8_NONE;
+          const float ref = none ? 0.f : m, top = scores(c, ref);
+          if (__any_sync(0xffffffffu, top > (none ? T8_NONE : T8_SLACK))) {
+            // ---- the reference moves to the largest of the chunk (from none: in a segment's first block; else rarely); what has
+            // been summed and weighted follows
+            const bool moves = top > (none ? T8_NONE : T8_SLACK);
+            if (moves) m = ref + top;
+            const float corr = !moves ? 1.f : none ? 0.f : t8_ex2(ref - m);
+            l2 = t8_mul2(l2, t8_pack(corr, corr));
+            if (!first) {
+              // O is at rest once the group's product before has completed
+              ok = t8_wait(&pvdone[g * 2 + (b ^ 1)], (uint32_t)((li - 1) >> 1) & 1u, abort_flag, wait_limit, lane);
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int k = 0; k < 8; ++k) {
+                float v[16];
+                tc_ld16(o_col + (uint32_t)k * 16u, v);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[j] *= corr;
+                tc_st16(o_col + (uint32_t)k * 16u, v);
+              }
+            }
+            if (c > 0) {                                     // the weights of this block so far (COPIES == 1, one chunk)
+              tc_wait_st();
+              float v[16];
+              uint32_t u[16];
+              tc_ld16(s_col, v);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const uint32_t y = __float_as_uint(v[j]);
+                const __nv_bfloat162 z = __floats2bfloat162_rn(__uint_as_float(y << 16) * corr, __uint_as_float(y & 0xffff0000u) * corr);
+                u[j] = *reinterpret_cast<const uint32_t *>(&z);
+              }
+              t8_st(s_col, u);
+            }
+#pragma unroll
+            for (int j = 0; j < CH; ++j) t[j] -= moves ? m - ref : 0.f;
+          }
+          // weights (below 2^T8_SLACK), their sum, bf16 in place of the scores that have been read
+          uint32_t u[CH / 2];
+          f32x2 sum[2] = {0ull, 0ull};
+#pragma unroll
+          for (int j = 0; j < CH; j += 2) {
+            const float a = t8_ex2(t[j]), d = t8_ex2(t[j + 1]);
+            sum[(j >> 1) & 1] = t8_add2(sum[(j >> 1) & 1], t8_pack(a, d));
+            const __nv_bfloat162 z = __floats2bfloat162_rn(a, d);
+            u[j >> 1] = *reinterpret_cast<const uint32_t *>(&z);
+          }
+          l2 = t8_add2(l2, t8_add2(sum[0], sum[1]));
+          t8_st(s_col + (uint32_t)(k0 / 2 + c * (CH / 2)), u);
+        }
+        if (!ok) break;
+        if (COPIES > 1) {                                    // the slots of the other copies
+          uint32_t zero[CH / 2];
+#pragma unroll
+          for (int j = 0; j < CH / 2; ++j) zero[j] = 0u;
+#pragma unroll
+          for (int k = 0; k < COPIES; ++k)
+            if (k != copy) t8_st(s_col + (uint32_t)(k * (CH / 2)), zero);
+        }
+        tc_wait_st();
+        tc_fence_before();
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&pfull[g * 2 + b]));
+      if (last) {
+        // ---- leave the segment: this copy's partial result ----------------------------------------------------------------
+        ok = t8_wait(&pvdone[g * 2 + b], (uint32_t)(li >> 1) & 1u, abort_flag, wait_limit, lane);
+        if (!ok) break;
+        if (work) {
+          const int64_t row = s.base + (int64_t)QT * blockIdx.x + (int64_t)(g * COPIES + copy) * ls.half + query;
+          tc_fence_after();
+          float la, lb;
+          t8_unpack(l2, la, lb);
+          if (query < s.cols) ls.ml[row] = make_float2(m, la + lb);
+#pragma unroll 1
+          for (int c = 0; c < 8; ++c) {
+            float v[16];
+            tc_ld16(o_col + (uint32_t)c * 16u, v);
+            if (query < s.cols) {
+              float4 *o = reinterpret_cast<float4 *>(ls.o + row * 128 + c * 16);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) o[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            }
+          }
+          tc_fence_before();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ofree[g]));
+      }
+    }
+  }
+  tc_teardown(abort_flag, p.status, tmem, 512);
+  a8_leave<PRE>(p);
+}
+
+// ---- host side -------------------------------------------------------------------------------------------------------
+static int t8_slab(int page) { return page % 128 == 0 ? 128 : page % 64 == 0 ? 64 : page % 32 == 0 ? 32 : 16; }
+static size_t t8_smem(const SxA8 &p) { return T8_FIXED + a8_plan_bytes(p.B, p.n_groups); }
+
+bool sx_attn8_tc_supported(const SxA8 &p) {
+  return p.d == 128 && (int64_t)p.num_pages * p.nkv * p.page < (1ll << 31) - 256 && t8_smem(p) <= T8_SMEM_MAX;
+}
+
+template <bool PRE, int COPIES>
+static sx_status launch_tc(const SxA8 &p, int sm_count, cudaStream_t st) {
+  const int slab = t8_slab(p.page);
+  const long long rows = (long long)p.num_pages * p.nkv * p.page;
+  CUtensorMap mk, mv;
+  if (!sx_tma_map_bytes(p.k, rows, 128, slab, &mk) || !sx_tma_map_bytes(p.v, rows, 128, slab, &mv)) return SX_ERR_CUDA;
+  const size_t smem = t8_smem(p);
+  SX_TRY(sx_rc(cudaFuncSetAttribute(sx_attn8_tc_kernel<PRE, COPIES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)));
+  return sx_rc(sx_launch(sx_attn8_tc_kernel<PRE, COPIES>, dim3(sm_count), dim3(T8_THREADS), smem, st, mk, mv, p, slab, T8_WAIT_POLLS));
+}
+
+sx_status sx_launch_attn8_tc(const SxA8 &p, bool prefix, int sm_count, cudaStream_t st) {
+  switch ((prefix ? p.pre : p.own).qt) {
+    case 32: return prefix ? launch_tc<true, 4>(p, sm_count, st) : launch_tc<false, 4>(p, sm_count, st);
+    case 64: return prefix ? launch_tc<true, 2>(p, sm_count, st) : launch_tc<false, 2>(p, sm_count, st);
+    default: return prefix ? launch_tc<true, 1>(p, sm_count, st) : launch_tc<false, 1>(p, sm_count, st);
+  }
+}

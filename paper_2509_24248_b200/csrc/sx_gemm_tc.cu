@@ -502,7 +502,8 @@ struct MapKeyHash {
 };
 static std::unordered_map<MapKey, CUtensorMap, MapKeyHash> g_maps;
 
-bool sx_tma_map_2d(const void *ptr, long long rows, int cols, int box_rows, CUtensorMap *out) {
+// elem: 2 = bf16, 1 = bytes; a box is 128 bytes wide (one swizzle row) and box_rows high
+static bool tma_map(const void *ptr, long long rows, int cols, int box_rows, int elem, CUtensorMap *out) {
   std::lock_guard<std::mutex> lk(g_mu);
   if (!g_encode) {
     void *fn = nullptr;
@@ -510,22 +511,28 @@ bool sx_tma_map_2d(const void *ptr, long long rows, int cols, int box_rows, CUte
     if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess || !fn) return false;
     g_encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
   }
-  MapKey key{ptr, rows, cols, box_rows};
+  MapKey key{ptr, rows, cols, box_rows * 4 + elem};
   auto it = g_maps.find(key);
   if (it != g_maps.end()) { *out = it->second; return true; }
   CUtensorMap m;
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-  cuuint64_t strides[1] = {(cuuint64_t)cols * 2};
-  cuuint32_t box[2] = {SX_BK, (cuuint32_t)box_rows};
+  cuuint64_t strides[1] = {(cuuint64_t)cols * elem};
+  cuuint32_t box[2] = {(cuuint32_t)(128 / elem), (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1, 1};
-  CUresult rc = g_encode(&m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(ptr), dims, strides, box, estr,
-                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  CUresult rc = g_encode(&m, elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2,
+                         const_cast<void *>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (rc != CUDA_SUCCESS) return false;
   if (g_maps.size() > 4096) g_maps.clear();
   g_maps.emplace(key, m);
   *out = m;
   return true;
+}
+bool sx_tma_map_2d(const void *ptr, long long rows, int cols, int box_rows, CUtensorMap *out) {
+  return tma_map(ptr, rows, cols, box_rows, 2, out);
+}
+bool sx_tma_map_bytes(const void *ptr, long long rows, int cols, int box_rows, CUtensorMap *out) {
+  return tma_map(ptr, rows, cols, box_rows, 1, out);
 }
 
 static int pow2_at_least(int v) { int p = 32; while (p < v) p <<= 1; return p; }

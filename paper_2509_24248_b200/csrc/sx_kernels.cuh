@@ -124,6 +124,8 @@ sx_status sx_gemm_init(int device);
 // cached 2-D tensor map of a bf16 matrix [rows, cols], box = box_rows x 64 columns, 128-byte swizzle
 struct CUtensorMap_st;
 bool sx_tma_map_2d(const void *ptr, long long rows, int cols, int box_rows, CUtensorMap_st *out);
+// the same for a matrix of bytes, box = box_rows x 128 columns
+bool sx_tma_map_bytes(const void *ptr, long long rows, int cols, int box_rows, CUtensorMap_st *out);
 // give-up path of the bounded mbarrier waits on its own (see sx_selftest_bounded_wait)
 sx_status sx_launch_wait_selftest(uint32_t limit, int ctas, int32_t *status, int32_t *reached, cudaStream_t st);
 // Sampled verification: with temp > 0 the plain-argmax head returns, per row, the arg max of

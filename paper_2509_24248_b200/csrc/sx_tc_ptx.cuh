@@ -174,6 +174,11 @@ __device__ __forceinline__ uint64_t smem_desc_mn(uint32_t addr, uint32_t mn_stri
   d |= (uint64_t)2 << 61;                                // SWIZZLE_128B
   return d;
 }
+// contiguous bytes (16-byte aligned, a multiple of 16) into shared memory, counted by an mbarrier
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 // writes made with ordinary stores to shared memory become visible to the tensor core / TMA ("async proxy")
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 

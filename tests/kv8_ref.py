@@ -55,18 +55,18 @@ def dequantise(codes: torch.Tensor, byte: torch.Tensor) -> np.ndarray:
     return VALUES[codes.numpy()] * s[..., None]
 
 
-def attention(kv, q: torch.Tensor, drafted: int, row_mask, scale: float):
-    """(output, bound) as float64 ``[B, rows, nq, d]``: the formula, and how far the kernels' fp32 sums, fp16 weights and
-    bf16 result may be from it.
+def attention(kv, q: torch.Tensor, drafted: int, row_mask, scale: float, weight: float = 2.0 ** -8):
+    """(output, bound) as float64 ``[B, rows, nq, d]``: the formula, and how far the kernels' fp32 sums, rounded weights
+    (``weight``: half a step of their type, 2^-11 for fp16, 2^-8 for bf16) and bf16 result may be from it.
 
-    With S the exact score of a slot and A = sum_s p_s |V_s|: a score is a sum of d products in fp32 of queries that
-    are held to 2^-18 of their row's largest value, so it is off by at most
-        delta = scale * max_s (d 2^-23 sum_i |q_i K_si| + 2^-18 max|q| sum_i |K_si|) + 2^-20 (1 + max |S|)
-    (the last term: the scaled score and the reference in fp32, and the exponential's own error of a few 2^-22); a
-    weight is then off by the factor e^(2 delta) (its own score and the sum's) and by 2^-11 (fp16), both sums of the
-    quotient by as much: |error| <= 2 (2 delta + 2^-11) A, and half a bf16 step, 2^-8, of the result.  A weight, which
-    stands for p_s 2^(e_s), is held to 2^-25 of the largest one at worst (fp16 below its normal range), and a code
-    is at most twice the largest of its row over 2^(e_s): n 2^-24 max_s(p_s max|V_s|) more."""
+    With S the exact score of a slot and A = sum_s p_s |V_s|: a score is a sum of d products in fp32, so it is off by at
+    most
+        delta = scale * max_s d 2^-23 sum_i |q_i K_si| + 2^-20 (1 + max |S|)
+    (the last term: the scaled score and the reference in fp32, and the exponential's own error of a few 2^-22).  Every
+    weight is then off by a factor of e^delta at most, in the numerator and in the sum of the weights, and those of the
+    numerator by their rounding: |error| <= (4 delta + weight) A, and half a bf16 step, 2^-8, of the result.  An fp16
+    weight, which stands for p_s 2^(e_s), is held to 2^-25 of the largest one at worst (below its normal range), and a
+    code is at most twice the largest of its row over 2^(e_s): n 2^-24 max_s(p_s max|V_s|) more."""
     B, rows, nq, d = q.shape
     page, n_kv = kv["k_pages"].shape[2], kv["k_pages"].shape[1]
     G = nq // n_kv
@@ -93,9 +93,8 @@ def attention(kv, q: torch.Tensor, drafted: int, row_mask, scale: float):
                 p /= p.sum()
                 out[b, j, h] = p @ Vh
                 A = p @ np.abs(Vh)
-                delta = abs(scale) * (d * 2.0 ** -23 * (np.abs(Kh) @ np.abs(x)).max()
-                                      + 2.0 ** -18 * np.abs(x).max() * np.abs(Kh).sum(1).max()) + 2.0 ** -20 * (1 + np.abs(S).max())
-                far = 2 * (2 * delta + 2.0 ** -11) * A + len(S) * 2.0 ** -24 * (p * np.abs(Vh).max(1)).max()
+                delta = abs(scale) * d * 2.0 ** -23 * (np.abs(Kh) @ np.abs(x)).max() + 2.0 ** -20 * (1 + np.abs(S).max())
+                far = (4 * delta + weight) * A + len(S) * 2.0 ** -24 * (p * np.abs(Vh).max(1)).max()
                 bound[b, j, h] = far + 2.0 ** -8 * (np.abs(out[b, j, h]) + far) + 1e-30
     return out, bound
 

@@ -132,10 +132,15 @@ def test_rows_without_a_place_are_skipped_and_reported(what):
 
 # ---- attention -----------------------------------------------------------------------------------------------------
 def check(kv, q, drafted, mask, scale=None, kernel=sx.ATTN_AUTO, cache=None):
+    if kernel == sx.ATTN_TC and q.shape[-1] != 128:
+        with pytest.raises(sx.SxError):
+            sx.KV8(to_dev(kv)).sx_attention(q.to(DEV), drafted, kernel=kernel)
+        kernel = sx.ATTN_AUTO
     c = cache or sx.KV8(to_dev(kv))
     got = c.sx_attention(q.to(DEV), drafted, None if mask is None else mask.to(DEV), scale, kernel=kernel)
     c.check_status()
-    want, bound = ref.attention(kv, q, drafted, mask, q.shape[-1] ** -0.5 if scale is None else scale)
+    want, bound = ref.attention(kv, q, drafted, mask, q.shape[-1] ** -0.5 if scale is None else scale,
+                                2.0 ** -11 if kernel == sx.ATTN_SPLIT else 2.0 ** -8)
     got = got.double().cpu().numpy()
     far = np.abs(got - want) / bound
     worst = float(far.max())
@@ -143,7 +148,7 @@ def check(kv, q, drafted, mask, scale=None, kernel=sx.ATTN_AUTO, cache=None):
     return got
 
 
-KERNELS = [sx.ATTN_AUTO, sx.ATTN_SPLIT]
+KERNELS = [sx.ATTN_SPLIT, sx.ATTN_TC]
 LENS = [[1], [16], [15, 17, 1], [127, 128, 129, 0], [1000, 3, 260], [65, 2049]]
 
 
