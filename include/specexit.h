@@ -155,7 +155,8 @@ typedef struct {
  * code = e4m3(x * 2^-e), round to nearest even.  x * 2^-e and code * 2^e are exact, so the rounding to 4
  * significand bits is all that is lost (values below 2^-10 of a row's largest keep fewer).  A row with a value
  * that is not finite has the byte 255 and codes of zero, and reads as NaN.  Half the bytes of bf16 and one byte
- * per row.  Needs a page size that is a multiple of 16; the draft step also needs head_dim 64 or 128. */
+ * per row.  Needs a page size that is a multiple of 16; attention (the draft step's too) needs head_dim 64 or 128.
+ * A draft call takes the kind of cache that sx_draft_cfg.kv_dtype names; fields behind v_pages_d are zero for bf16. */
 enum { SX_KV_BF16 = 0, SX_KV_E4M3 = 1 };
 
 /* Shape of a cache for the calls that take no context. */
@@ -170,6 +171,9 @@ typedef struct {
   int32_t max_nodes;   /* tree: nodes kept for verification, root excluded (< SX_MAX_VERIFY_SLOTS) */
   int32_t sample_drafts; /* 0 or 1: reserve workspace for sampled drafts (chain) / sampled children (tree), see
                             sx_set_sampling; needs the full draft vocabulary without an id map */
+  int32_t kv_dtype;      /* element type of the caches this context will be given: SX_KV_BF16 (0), or SX_KV_E4M3 (head_dim
+                            64 or 128, page size a multiple of 16), which reserves workspace for the attention over it
+                            and lets sequences share a prefix.  Calls with another kind of cache are refused. */
 } sx_draft_cfg;
 
 /* Exit rule.  Signal i passes when smoothed_i > thr[i] (SX_DIR_GT) or < thr[i] (SX_DIR_LT),

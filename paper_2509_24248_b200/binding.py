@@ -69,7 +69,7 @@ class KVShape(C.Structure):
 
 class DraftCfg(C.Structure):
     _fields_ = [("mode", C.c_int32), ("K", C.c_int32), ("topk", C.c_int32), ("max_nodes", C.c_int32),
-                ("sample_drafts", C.c_int32)]
+                ("sample_drafts", C.c_int32), ("kv_dtype", C.c_int32)]
 
 
 class ExitCfg(C.Structure):
@@ -391,7 +391,8 @@ class SpecExit:
     def __init__(self, shape: synth.ModelShape, weights: Dict[str, torch.Tensor], max_batch: int,
                  mode: int, K: int, topk: int = 1, max_nodes: int = 0,
                  act=(ACT_SIGMOID, ACT_SIGMOID, ACT_SIGMOID), device: str = "cuda:0",
-                 max_verify_rows: int = 0, sample_drafts: bool = False, tiled: bool = False):
+                 max_verify_rows: int = 0, sample_drafts: bool = False, tiled: bool = False,
+                 kv_dtype: int = KV_BF16):
         self.lib = load_library()
         if not torch.cuda.is_available():
             raise SxError("a CUDA device is required (there is no CPU fallback)")
@@ -427,7 +428,7 @@ class SpecExit:
                                                        "wgate_up", "wdown", "normf", "head", "target_head")],
                      d2t.data_ptr() if d2t is not None else None,
                      self.w["norm_e"].data_ptr() if "norm_e" in self.w else None)
-        dc = DraftCfg(mode, K, topk, max_nodes, 1 if sample_drafts else 0)
+        dc = DraftCfg(mode, K, topk, max_nodes, 1 if sample_drafts else 0, kv_dtype)
         h = C.c_void_p()
         _check(self.lib.sx_create(C.byref(mc), C.byref(ws), max_batch, C.byref(dc), max_verify_rows,
                                   C.byref(h)), "sx_create")
@@ -453,7 +454,14 @@ class SpecExit:
 
     # ---- buffers -------------------------------------------------------------------------
     def set_kv(self, kv: Dict[str, torch.Tensor]) -> None:
+        """``k_pages``, ``v_pages``, ``page_table``, ``cache_len``; with ``kv_dtype = KV_E4M3`` the tensors that
+        :class:`KV8` takes, shared prefixes included."""
         d = self.dev
+        if "k_scale" in kv:
+            self.kv = {n: kv[n].to(d).contiguous() for n in _CACHE_NAMES if kv.get(n) is not None}
+            self._kv_struct = _kv_struct(self.kv, self.shape.n_kv, self.shape.page, self.shape.d)
+            self.B = int(self._kv_struct.batch)
+            return
         self.kv = {"k_pages": kv["k_pages"].to(d), "v_pages": kv["v_pages"].to(d),
                    "page_table": kv["page_table"].to(d).contiguous(),
                    "cache_len": kv["cache_len"].to(d).contiguous()}

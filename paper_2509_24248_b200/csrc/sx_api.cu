@@ -2,6 +2,7 @@
 // speculative-exit iteration.  Nothing here synchronises or allocates device memory.
 #include <new>
 #include <vector>
+#include <math.h>
 #include <stdio.h>
 #include <string.h>
 
@@ -9,6 +10,7 @@
 
 #include <nvtx3/nvToolsExt.h>
 
+#include "sx_attn8.cuh"
 #include "sx_kernels.cuh"
 
 // Named ranges for timeline tools (the header-only NVTX v3: nothing is linked, and without a tool attached a
@@ -141,6 +143,8 @@ extern "C" sx_status sx_create(const sx_model_cfg *m, const sx_weights *w, int32
   if (m->arch == SX_ARCH_FUSED3 && (!w->norm_e_d || ((uintptr_t)w->norm_e_d & 15))) return SX_ERR_INVALID_ARG;
   if (dc->K < 1) return SX_ERR_INVALID_ARG;
   if (dc->sample_drafts != 0 && dc->sample_drafts != 1) return SX_ERR_INVALID_ARG;
+  if (dc->kv_dtype != SX_KV_BF16 && dc->kv_dtype != SX_KV_E4M3) return SX_ERR_INVALID_ARG;
+  if (dc->kv_dtype == SX_KV_E4M3 && ((m->head_dim != 64 && m->head_dim != 128) || m->page_size % 16)) return SX_ERR_UNSUPPORTED;
   if (dc->sample_drafts && (Vd != m->vocab || w->draft_to_token_d))
     return SX_ERR_UNSUPPORTED;        // sampled drafts: full draft vocabulary, no id map
   sx_ctx *c = new (std::nothrow) sx_ctx();
@@ -216,7 +220,12 @@ extern "C" sx_status sx_create(const sx_model_cfg *m, const sx_weights *w, int32
   c->off_part = take((size_t)c->max_splits * R * c->part_N * 4);
   {
     const size_t a = sx_attn_ws_bytes(s, max_batch, T, c->sm_count), b = sx_attn_tc_ws_bytes(s, max_batch, c->sm_count);
-    c->off_attn = take(a > b ? a : b);
+    size_t most = a > b ? a : b;
+    if (dc->kv_dtype == SX_KV_E4M3) {               // any number of groups, in every round
+      const size_t e = sx_attn8_ws_bytes(s.nq, s.nkv, s.d, max_batch, T, max_batch, c->sm_count);
+      most = most > e ? most : e;
+    }
+    c->off_attn = take(most);
   }
   c->off_hparts = take((size_t)c->head_G * c->head_rows * sizeof(SxHeadPartial));
   c->off_z = take((size_t)R * SX_MAX_SIGNALS * 4);
@@ -282,6 +291,11 @@ static sx_status check_kv(const sx_ctx *c, const sx_kv *kv) {
   if (!kv || !kv->cache_len_d || !kv->page_table_d || !kv->k_pages_d || !kv->v_pages_d) return SX_ERR_INVALID_ARG;
   if (kv->batch < 1 || kv->batch > c->max_batch || kv->max_pages < 1 || kv->num_pages < 1) return SX_ERR_INVALID_ARG;
   if (((uintptr_t)kv->k_pages_d & 15) || ((uintptr_t)kv->v_pages_d & 15)) return SX_ERR_INVALID_ARG;
+  if (kv->dtype != c->dc.kv_dtype) return SX_ERR_INVALID_ARG;
+  if (kv->dtype == SX_KV_BF16) return kv->n_groups == 0 ? SX_OK : SX_ERR_UNSUPPORTED;
+  SxA8 p;                                           // the checks of the 8-bit attention, before anything is launched
+  const sx_kv_shape sh = {c->sh.nq, c->sh.nkv, c->sh.d, c->sh.page};
+  SX_TRY(sx_attn8_params(sh, *kv, c->dc.mode == SX_MODE_TREE ? c->dc.topk : 1, 0, &p));
   return SX_OK;
 }
 
@@ -390,13 +404,27 @@ static sx_status draft_round(sx_ctx *c, const sx_kv *kv, int round, int R, const
   // Which attention kernel: the tensor-memory one for long caches with more than four queries per (sequence,
   // KV head); below a few blocks of keys per SM its set-up outweighs its stream, and with up to four queries
   // the split kernel's three small CTAs per SM keep more bytes in flight (the host knows capacities, not lengths).
-  bool tc = sx_attn_tc_supported(s, nr, *kv);
-  if (c->attn_kernel == SX_ATTN_SPLIT) tc = false;
+  const bool kv8 = kv->dtype == SX_KV_E4M3;         // a cache of codes has kernels of its own (sx_attn8.cu)
+  bool tc = !kv8 && sx_attn_tc_supported(s, nr, *kv);
+  if (kv8 || c->attn_kernel == SX_ATTN_SPLIT) tc = false;
   else if (c->attn_kernel == SX_ATTN_AUTO)
     tc = tc && nr * (s.nq / s.nkv) > 4 && (long long)B * s.nkv * ((kv->max_pages * s.page + 127) / 128) >= 4ll * c->sm_count;
   else if (!tc) return SX_ERR_UNSUPPORTED;
   prof_mark(c, SX_PROF_ATTENTION, true, st);
-  if (tc) {
+  if (kv8) {
+    SxA8 p;
+    const sx_kv_shape sh = {s.nq, s.nkv, s.d, s.page};
+    SX_TRY(sx_attn8_params(sh, *kv, nr, E, &p));
+    p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)s.d));
+    p.q = q;
+    p.q_stride = (int64_t)s.nq * s.d;
+    p.row_mask = (rm.mode == SX_MODE_TREE && round > 1) ? row_mask : nullptr;
+    p.o_out = o;
+    p.status = status;
+    p.early = 1;
+    SX_TRY(sx_launch_attn8(p, c->attn_kernel, ws + c->off_attn, c->sm_count, st));
+    if (p.n_groups > 0) c->launches += 1;
+  } else if (tc) {
     SX_TRY(sx_launch_attention_tc(s, rm, B, nr, E, q, *kv, (float *)(ws + c->off_attn), o, c->sm_count, status, st));
   } else {
     const int nsplit = sx_attn_splits(s, B, nr, kv->max_pages * s.page, c->sm_count);

@@ -76,6 +76,16 @@ __device__ __forceinline__ uint32_t sx_pack_index(unsigned long long p) {
   return 0xffffffffu - (uint32_t)(p & 0xffffffffu);
 }
 
+// 8-bit cache: exponent byte of a row whose largest magnitude has the bf16 bits `top` (448 = 1.75 * 2^8 is the largest
+// e4m3 value, so the exponent and the top of the mantissa decide), and two codes
+__device__ __forceinline__ int sx_kv8_scale_byte(uint32_t top) {
+  if (top == 0) return 127;
+  const int e = (int)(top >> 7);
+  if (e == 255) return 255;
+  return max(63, e - 8 + ((top & 0x7f) > 96 ? 1 : 0));
+}
+__device__ __forceinline__ float sx_kv8_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }   // 2^(127 - byte)
+
 __device__ __forceinline__ float sx_warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

@@ -3,6 +3,8 @@
 // head merge, greedy acceptance, the exit rule and the draft-tree bookkeeping.
 #include <math.h>
 
+#include <cuda_fp8.h>
+
 #include "sx_kernels.cuh"
 #include "sx_launch.cuh"
 
@@ -277,6 +279,25 @@ __global__ void sx_finish_qkv_rope_kernel(int nq, int nkv, int d, double theta, 
     return;
   }
   const int kh = (hh < nq + nkv) ? hh - nq : hh - nq - nkv;
+  if (kv.dtype == SX_KV_E4M3) {
+    // d is 64 or 128 here, so the d / 2 threads are one or two full warps; a row is quantised as sx_kv_append does it
+    __shared__ uint32_t top_sh[2];
+    const uint32_t b1 = __bfloat16_as_ushort(y1) & 0x7fffu, b2 = __bfloat16_as_ushort(y2) & 0x7fffu;
+    uint32_t top = __reduce_max_sync(0xffffffffu, max(b1, b2));
+    if (half > 32) {
+      if ((i & 31) == 0) top_sh[i >> 5] = top;
+      __syncthreads();
+      top = max(top_sh[0], top_sh[1]);
+    }
+    const int byte = sx_kv8_scale_byte(top);
+    const float up = sx_kv8_inverse(byte);
+    const size_t at = ((size_t)pp * nkv + kh) * page + off;
+    uint8_t *codes = reinterpret_cast<uint8_t *>(hh < nq + nkv ? kv.k_pages_d : kv.v_pages_d) + at * d;
+    codes[i] = byte == 255 ? 0 : __nv_cvt_float_to_fp8(__bfloat162float(y1) * up, __NV_SATFINITE, __NV_E4M3);
+    codes[i + half] = byte == 255 ? 0 : __nv_cvt_float_to_fp8(__bfloat162float(y2) * up, __NV_SATFINITE, __NV_E4M3);
+    if (i == 0) (hh < nq + nkv ? kv.k_scale_d : kv.v_scale_d)[at] = (uint8_t)byte;
+    return;
+  }
   bf16 *dst = reinterpret_cast<bf16 *>(hh < nq + nkv ? kv.k_pages_d : kv.v_pages_d) +
               (((size_t)pp * nkv + kh) * page + off) * d;
   dst[i] = y1;

@@ -49,13 +49,6 @@ __device__ __forceinline__ void kv8_places(const SxKv8Rows &p, int t0, int nt, i
   __syncthreads();
 }
 
-// exponent byte of a row whose largest magnitude has the bf16 bits `top`
-__device__ __forceinline__ int kv8_scale_byte(uint32_t top) {
-  if (top == 0) return 127;
-  const int e = (int)(top >> 7);
-  if (e == 255) return 255;
-  return max(63, e - 8 + ((top & 0x7f) > 96 ? 1 : 0));
-}
 __device__ __forceinline__ uint32_t kv8_codes4(uint32_t ab, uint32_t cd, float up) {
   const float2 x = make_float2(__uint_as_float(ab << 16) * up, __uint_as_float(ab & 0xffff0000u) * up);
   const float2 y = make_float2(__uint_as_float(cd << 16) * up, __uint_as_float(cd & 0xffff0000u) * up);
@@ -96,8 +89,8 @@ __global__ void __launch_bounds__(KV8_THREADS) sx_kv8_append_kernel(SxKv8Rows p,
       top = max(top & 0xffffu, top >> 16);
 #pragma unroll
       for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const int byte = kv8_scale_byte(top);
-      const float up = __uint_as_float((uint32_t)(254 - byte) << 23);
+      const int byte = sx_kv8_scale_byte(top);
+      const float up = sx_kv8_inverse(byte);
       uint2 c = make_uint2(0, 0);
       if (byte != 255) c = make_uint2(kv8_codes4(x[i].x, x[i].y, up), kv8_codes4(x[i].z, x[i].w, up));
       if (at[i] >= 0) {
