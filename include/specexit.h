@@ -156,7 +156,7 @@ typedef struct {
  * significand bits is all that is lost (values below 2^-10 of a row's largest keep fewer).  A row with a value
  * that is not finite has the byte 255 and codes of zero, and reads as NaN.  Half the bytes of bf16 and one byte
  * per row.  Needs a page size that is a multiple of 16; attention (the draft step's too) needs head_dim 64 or 128.
- * A draft call takes the kind of cache that sx_draft_cfg.kv_dtype names; fields behind v_pages_d are zero for bf16. */
+ * A draft call takes the kind of cache that sx_set_cache named; fields behind v_pages_d are zero for bf16. */
 enum { SX_KV_BF16 = 0, SX_KV_E4M3 = 1 };
 
 /* Shape of a cache for the calls that take no context. */
@@ -171,9 +171,6 @@ typedef struct {
   int32_t max_nodes;   /* tree: nodes kept for verification, root excluded (< SX_MAX_VERIFY_SLOTS) */
   int32_t sample_drafts; /* 0 or 1: reserve workspace for sampled drafts (chain) / sampled children (tree), see
                             sx_set_sampling; needs the full draft vocabulary without an id map */
-  int32_t kv_dtype;      /* element type of the caches this context will be given: SX_KV_BF16 (0), or SX_KV_E4M3 (head_dim
-                            64 or 128, page size a multiple of 16), which reserves workspace for the attention over it
-                            and lets sequences share a prefix.  Calls with another kind of cache are refused. */
 } sx_draft_cfg;
 
 /* Exit rule.  Signal i passes when smoothed_i > thr[i] (SX_DIR_GT) or < thr[i] (SX_DIR_LT),
@@ -299,6 +296,12 @@ sx_status sx_tile_weight(const void *src_d, int32_t N, int32_t K, void *dst_d, v
  * state, read when a call is issued. */
 enum { SX_ATTN_AUTO = 0, SX_ATTN_SPLIT = 1, SX_ATTN_TC = 2 };
 sx_status sx_set_attention(sx_ctx *ctx, int32_t kernel);
+
+/* Kind of cache that the context's calls (sx_draft_step, sx_spec_exit_iter, sx_commit) will be given from here on:
+ * SX_KV_BF16 (a new context) or SX_KV_E4M3, with which sequences may share prefixes (see sx_attention).  Changes what
+ * sx_workspace_bytes says: call it before asking.  SX_ERR_UNSUPPORTED where the shape does not allow an 8-bit cache
+ * (head_dim 64 or 128, page size a multiple of 16).  Host-side state; a call with a cache of another kind is refused. */
+sx_status sx_set_cache(sx_ctx *ctx, int32_t kv_dtype);
 
 /* Rows into an 8-bit cache (kv->dtype == SX_KV_E4M3; no context needed): the keys and values of new tokens, for a
  * prompt, a decode step of a batch, or both.  The rows of sequence b are row_start_d[b] .. row_start_d[b + 1] - 1

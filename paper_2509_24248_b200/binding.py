@@ -32,7 +32,7 @@ EXPORTS = ["sx_create", "sx_destroy", "sx_workspace_bytes", "sx_strerror", "sx_l
            "sx_draft_step", "sx_verify", "sx_exit_update", "sx_spec_exit_iter",
            "sx_spec_exit_iter_host", "sx_profile_begin", "sx_profile_end", "sx_verify_noalloc", "sx_commit",
            "sx_set_sampling", "sx_tiled_weight_bytes", "sx_tile_weight", "sx_selftest_bounded_wait", "sx_set_attention",
-           "sx_kv_append", "sx_kv_read", "sx_attention", "sx_attention_ws_bytes"]
+           "sx_set_cache", "sx_kv_append", "sx_kv_read", "sx_attention", "sx_attention_ws_bytes"]
 PROF_CLASSES = ["head_draft", "head_verify", "gemm_fc", "gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down",
                 "attention"]
 
@@ -69,7 +69,7 @@ class KVShape(C.Structure):
 
 class DraftCfg(C.Structure):
     _fields_ = [("mode", C.c_int32), ("K", C.c_int32), ("topk", C.c_int32), ("max_nodes", C.c_int32),
-                ("sample_drafts", C.c_int32), ("kv_dtype", C.c_int32)]
+                ("sample_drafts", C.c_int32)]
 
 
 class ExitCfg(C.Structure):
@@ -156,6 +156,8 @@ def load_library() -> C.CDLL:
     lib.sx_attention.restype = i32
     lib.sx_attention.argtypes = [C.POINTER(KVShape), C.POINTER(KV), i32, i32, vp, i64, vp, C.c_float, i32, vp, vp, sz,
                                  vp, vp]
+    lib.sx_set_cache.restype = i32
+    lib.sx_set_cache.argtypes = [vp, i32]
     lib.sx_verify_noalloc.restype = i32
     lib.sx_verify_noalloc.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
     _lib = lib
@@ -428,11 +430,12 @@ class SpecExit:
                                                        "wgate_up", "wdown", "normf", "head", "target_head")],
                      d2t.data_ptr() if d2t is not None else None,
                      self.w["norm_e"].data_ptr() if "norm_e" in self.w else None)
-        dc = DraftCfg(mode, K, topk, max_nodes, 1 if sample_drafts else 0, kv_dtype)
+        dc = DraftCfg(mode, K, topk, max_nodes, 1 if sample_drafts else 0)
         h = C.c_void_p()
         _check(self.lib.sx_create(C.byref(mc), C.byref(ws), max_batch, C.byref(dc), max_verify_rows,
                                   C.byref(h)), "sx_create")
         self.h = h
+        _check(self.lib.sx_set_cache(h, kv_dtype), "sx_set_cache")
         self.ws_bytes = int(self.lib.sx_workspace_bytes(h))
         self.ws = torch.empty(self.ws_bytes + 256, dtype=torch.uint8, device=self.dev)
         off = (-self.ws.data_ptr()) % 256

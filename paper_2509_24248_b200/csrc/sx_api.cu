@@ -41,6 +41,8 @@ struct sx_ctx {
       off_tok_rt, off_logp_rt, off_tree, off_cu, off_cn, off_cpart, off_cu2, off_ctok, off_dlogits, off_tlogits, off_spec, total;
   int commit_rows, commit_N;
   bool tiled;                    // GEMM weights are stored tile by tile (sx_tile_weight)
+  int kv_dtype;                  // SX_KV_* of the caches to come (sx_set_cache)
+  size_t off_attn8;              // workspace of the attention over an 8-bit cache, behind all the rest
   int attn_kernel;               // SX_ATTN_AUTO / _SPLIT / _TC (sx_set_attention)
   SxSample smp;                  // sampled verification (sx_set_sampling); temp == 0: greedy
   // set around a draft round whose head samples its token and leaves its logits (sampled drafts)
@@ -143,8 +145,6 @@ extern "C" sx_status sx_create(const sx_model_cfg *m, const sx_weights *w, int32
   if (m->arch == SX_ARCH_FUSED3 && (!w->norm_e_d || ((uintptr_t)w->norm_e_d & 15))) return SX_ERR_INVALID_ARG;
   if (dc->K < 1) return SX_ERR_INVALID_ARG;
   if (dc->sample_drafts != 0 && dc->sample_drafts != 1) return SX_ERR_INVALID_ARG;
-  if (dc->kv_dtype != SX_KV_BF16 && dc->kv_dtype != SX_KV_E4M3) return SX_ERR_INVALID_ARG;
-  if (dc->kv_dtype == SX_KV_E4M3 && ((m->head_dim != 64 && m->head_dim != 128) || m->page_size % 16)) return SX_ERR_UNSUPPORTED;
   if (dc->sample_drafts && (Vd != m->vocab || w->draft_to_token_d))
     return SX_ERR_UNSUPPORTED;        // sampled drafts: full draft vocabulary, no id map
   sx_ctx *c = new (std::nothrow) sx_ctx();
@@ -220,12 +220,7 @@ extern "C" sx_status sx_create(const sx_model_cfg *m, const sx_weights *w, int32
   c->off_part = take((size_t)c->max_splits * R * c->part_N * 4);
   {
     const size_t a = sx_attn_ws_bytes(s, max_batch, T, c->sm_count), b = sx_attn_tc_ws_bytes(s, max_batch, c->sm_count);
-    size_t most = a > b ? a : b;
-    if (dc->kv_dtype == SX_KV_E4M3) {               // any number of groups, in every round
-      const size_t e = sx_attn8_ws_bytes(s.nq, s.nkv, s.d, max_batch, T, max_batch, c->sm_count);
-      most = most > e ? most : e;
-    }
-    c->off_attn = take(most);
+    c->off_attn = take(a > b ? a : b);
   }
   c->off_hparts = take((size_t)c->head_G * c->head_rows * sizeof(SxHeadPartial));
   c->off_z = take((size_t)R * SX_MAX_SIGNALS * 4);
@@ -265,7 +260,7 @@ extern "C" sx_status sx_create(const sx_model_cfg *m, const sx_weights *w, int32
     c->t_nmask = take(B * T * 8) - base;
     c->t_rsig = take(B * rows * SX_MAX_SIGNALS * 4) - base;
   }
-  c->total = o;
+  c->total = c->off_attn8 = o;
   *out = c;
   return SX_OK;
 }
@@ -291,7 +286,7 @@ static sx_status check_kv(const sx_ctx *c, const sx_kv *kv) {
   if (!kv || !kv->cache_len_d || !kv->page_table_d || !kv->k_pages_d || !kv->v_pages_d) return SX_ERR_INVALID_ARG;
   if (kv->batch < 1 || kv->batch > c->max_batch || kv->max_pages < 1 || kv->num_pages < 1) return SX_ERR_INVALID_ARG;
   if (((uintptr_t)kv->k_pages_d & 15) || ((uintptr_t)kv->v_pages_d & 15)) return SX_ERR_INVALID_ARG;
-  if (kv->dtype != c->dc.kv_dtype) return SX_ERR_INVALID_ARG;
+  if (kv->dtype != c->kv_dtype) return SX_ERR_INVALID_ARG;
   if (kv->dtype == SX_KV_BF16) return kv->n_groups == 0 ? SX_OK : SX_ERR_UNSUPPORTED;
   SxA8 p;                                           // the checks of the 8-bit attention, before anything is launched
   const sx_kv_shape sh = {c->sh.nq, c->sh.nkv, c->sh.d, c->sh.page};
@@ -422,7 +417,7 @@ static sx_status draft_round(sx_ctx *c, const sx_kv *kv, int round, int R, const
     p.o_out = o;
     p.status = status;
     p.early = 1;
-    SX_TRY(sx_launch_attn8(p, c->attn_kernel, ws + c->off_attn, c->sm_count, st));
+    SX_TRY(sx_launch_attn8(p, c->attn_kernel, ws + c->off_attn8, c->sm_count, st));
     if (p.n_groups > 0) c->launches += 1;
   } else if (tc) {
     SX_TRY(sx_launch_attention_tc(s, rm, B, nr, E, q, *kv, (float *)(ws + c->off_attn), o, c->sm_count, status, st));
@@ -497,6 +492,20 @@ extern "C" sx_status sx_selftest_bounded_wait(uint32_t limit, int32_t ctas, int3
 extern "C" sx_status sx_set_attention(sx_ctx *c, int32_t kernel) {
   if (!c || kernel < SX_ATTN_AUTO || kernel > SX_ATTN_TC) return SX_ERR_INVALID_ARG;
   c->attn_kernel = kernel;
+  return SX_OK;
+}
+
+extern "C" sx_status sx_set_cache(sx_ctx *c, int32_t dtype) {
+  if (!c || (dtype != SX_KV_BF16 && dtype != SX_KV_E4M3)) return SX_ERR_INVALID_ARG;
+  size_t more = 0;
+  if (dtype == SX_KV_E4M3) {
+    const SxShape &s = c->sh;
+    if ((s.d != 64 && s.d != 128) || s.page % 16) return SX_ERR_UNSUPPORTED;
+    // any number of groups, in the round with the most rows
+    more = up256(sx_attn8_ws_bytes(s.nq, s.nkv, s.d, c->max_batch, c->dc.mode == SX_MODE_TREE ? c->dc.topk : 1, c->max_batch, c->sm_count));
+  }
+  c->kv_dtype = dtype;
+  c->total = c->off_attn8 + more;
   return SX_OK;
 }
 
