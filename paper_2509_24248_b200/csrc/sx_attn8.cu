@@ -5,14 +5,13 @@
 //   K_s = kc_s 2^(ek_s), V_s = vc_s 2^(ev_s)    (e4m3 codes, one exponent per slot and KV head)
 //
 // The warp-level kernel: a warp streams its run of 16-slot steps (sx_attn8.cuh) through a ring of its own in shared
-// memory - cp.async, 512 contiguous bytes per instruction, XOR-swizzled - and needs no other warp.  e4m3 codes
-// are exact in fp16, so both products run as mma.sync m16n8k16 (fp16 in, fp32 out) with the slots (then the head
-// dimension) on the 16-row side and 8 queries on the 8-column side:
-//     S^T[slot][q] = sum_d kc[slot][d] Q[q][d]         O^T[d][q] += sum_slot vc[slot][d] P[slot][q]
-// Codes go from shared memory to fragments as bytes: ldmatrix moves pairs of codes, cvt.f16x2.e4m3x2 widens them, and
-// the order that results (four codes of a row per lane) is undone for free by ordering Q the same way; for V
-// ldmatrix.trans delivers [slot][pair of d], one byte permute splits the pair into two rows of the product, whose
-// order is undone where O is stored.  Queries are scaled by a power of two per row, so that bf16 fits fp16.
+// memory - cp.async, 512 contiguous bytes per instruction, XOR-swizzled - and needs no other warp.  Both products
+// run as mma.sync with the slots (then the head dimension) on the 16-row side and 8 queries on the 8-column side:
+//     S^T[slot][q] = sum_d kc[slot][d] Q[q][d]         e4m3 x e4m3, m16n8k32; Q as the exact sum of two e4m3 numbers
+//     O^T[d][q] += sum_slot vc[slot][d] P[slot][q]     fp16 x fp16, m16n8k16; e4m3 codes are exact in fp16
+// K's fragments are the codes as ldmatrix delivers them.  For V ldmatrix.trans delivers [slot][pair of d]; one byte permute
+// splits the pair into two rows of the product, whose order is undone where O is stored, and cvt.f16x2.e4m3x2
+// widens them.  The scale of K is a factor of the slot's scores, that of V is added to the score.
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <math.h>
@@ -41,6 +40,14 @@ __device__ __forceinline__ uint32_t a8_transpose(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
+// e4m3 x e4m3 -> fp32, 16 x 8 x 32
+__device__ __forceinline__ void a8_mma_f8(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
 // two codes (low half, high half of the register) to fp16 pairs
 __device__ __forceinline__ void a8_widen(uint32_t x, uint32_t &lo, uint32_t &hi) {
   asm("{\n\t.reg .b16 a, b;\n\t"
@@ -56,7 +63,11 @@ __device__ __forceinline__ uint32_t a8_finite(uint32_t x) {
   __half2 v = __hmin2(*reinterpret_cast<__half2 *>(&x), top);
   return *reinterpret_cast<uint32_t *>(&v);
 }
-__device__ __forceinline__ void a8_cp16(uint32_t dst, const void *src, bool valid) {
+__device__ __forceinline__ void a8_cp16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+// reads nothing and writes zeros when !valid
+__device__ __forceinline__ void a8_cp16_if(uint32_t dst, const void *src, bool valid) {
   const uint32_t bytes = valid ? 16u : 0u;
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
@@ -104,37 +115,51 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, (A8S<D, NQT>::CTAS)) sx_attn8_
   const uint32_t scales = (uint32_t)__cvta_generic_to_shared(scale_sh);
 
   // ---- loader: requests the step at list position lx into ring stage `st` ---------------------------------
-  int lx = xb, l_x1 = xb;
-  int l_slot = 0, l_end = 0, l_b0 = 0, l_h = 0, l_pp = -1;
+  int lx = xb, l_x1 = xb, l_left = 0, l_off = 0, l_lp = 0, l_h = 0, l_pp = -1;      // slots left in the segment, place in the page
+  const int32_t *l_table = p.page_table;
   bool bad = false;
-  auto page_of = [&](int b0, int slot) -> int {
-    const int lp = slot / p.page;
-    return lp < p.max_pages ? p.page_table[(int64_t)b0 * p.max_pages + lp] : -1;
-  };
+  auto page_at = [&](int lp) -> int { return lp < p.max_pages ? l_table[lp] : -1; };
+  // where this lane's 16-byte pieces of a block of codes go; its source is 16 bytes of every 512
+  uint32_t at[D / 32];
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    const int e = i * 32 + lane, row = e / CPR, c = e - row * CPR;
+    at[i] = (uint32_t)(row * D + a8_swz<D>(row, c) * 16);
+  }
   auto request = [&](int st) {
     if (lx < xe) {
       if (lx == l_x1) {
         const A8Seg s = a8_seek<PRE>(p, pl, ls, A8_SPLIT_STEP, lx);
-        l_x1 = s.x1; l_slot = s.first + (lx - s.x0) * 16; l_end = s.end; l_b0 = s.b0; l_h = s.h;
-        l_pp = page_of(l_b0, l_slot);
+        const int slot = s.first + (lx - s.x0) * 16;
+        l_x1 = s.x1; l_left = s.end - slot; l_h = s.h;
+        l_table = p.page_table + (int64_t)s.b0 * p.max_pages;
+        l_lp = slot / p.page; l_off = slot - l_lp * p.page;
+        l_pp = page_at(l_lp);
       }
       const bool ok = l_pp >= 0 && l_pp < p.num_pages;
-      bad |= !ok;
-      const int off = l_slot % p.page, rows = ok ? min(16, l_end - l_slot) : 0;
-      const int64_t row0 = ok ? ((int64_t)l_pp * p.nkv + l_h) * p.page + off : 0;
+      const int64_t row0 = ok ? ((int64_t)l_pp * p.nkv + l_h) * p.page + l_off : 0;
       const uint32_t dst = codes + st * 2 * BLK;
+      const uint8_t *kp = p.k + row0 * D + lane * 16, *vp = p.v + row0 * D + lane * 16;
+      if (ok && l_left >= 16) {
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const int e = i * 32 + lane, row = e / CPR, c = e - row * CPR;
-        const uint32_t at = (uint32_t)(row * D + a8_swz<D>(row, c) * 16);
-        const int64_t src = row < rows ? row0 * D + e * 16 : 0;
-        a8_cp16(dst + at, p.k + src, row < rows);
-        a8_cp16(dst + BLK + at, p.v + src, row < rows);
+        for (int i = 0; i < D / 32; ++i) {
+          a8_cp16(dst + at[i], kp + i * 512);
+          a8_cp16(dst + BLK + at[i], vp + i * 512);
+        }
+      } else {                                           // the last slots of a sequence (or no page): zeros behind them
+        bad |= !ok;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          const bool on = ok && (i * 32 + lane) / CPR < l_left;
+          a8_cp16_if(dst + at[i], on ? kp + i * 512 : p.k, on);
+          a8_cp16_if(dst + BLK + at[i], on ? vp + i * 512 : p.v, on);
+        }
       }
-      if (lane < 2) a8_cp16(scales + st * 32 + lane * 16, (lane ? p.vs : p.ks) + row0, ok);
+      if (lane < 2) a8_cp16_if(scales + st * 32 + lane * 16, (lane ? p.vs : p.ks) + row0, ok);
       ++lx;
-      l_slot += 16;
-      if (lx < l_x1) l_pp = page_of(l_b0, l_slot);       // looked up a step ahead
+      l_left -= 16;
+      l_off += 16;
+      if (l_off == p.page && lx < l_x1) { l_off = 0; l_pp = page_at(++l_lp); }       // needed a step later
     }
     a8_cp_commit();
   };
@@ -167,19 +192,27 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, (A8S<D, NQT>::CTAS)) sx_attn8_
         top = max(top & 0xffffu, top >> 16);
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // 2^-e brings the largest magnitude into [2^10, 2^11): values down to 2^-24 of it keep all their bits
-        int ex = (int)(top >> 7);
-        ex = (ex == 0 || ex == 255) ? 0 : ex - 137;
-        const float up = __uint_as_float((uint32_t)(127 - max(-126, min(126, ex))) << 23);
-        ex = max(-126, min(126, ex));
+        // 2^-e brings the largest magnitude into (224, 448]; two e4m3 numbers then hold a bf16 number, exactly down to
+        // 2^-10
+        const int te = (int)(top >> 7);
+        const int ex = te == 0 || te == 255 ? 0 : max(-126, te - 135 + ((top & 0x7f) > 96 ? 1 : 0));
+        const float up = __uint_as_float((uint32_t)(127 - ex) << 23);
 #pragma unroll
         for (int c = 0; c < CPR; ++c) {
+          uint32_t hi = 0, lo = 0;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const uint32_t w = k ? raw[c].y : raw[c].x;
-            __half2 h = __floats2half2_rn(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up);
-            qf[i][c][k] = *reinterpret_cast<uint32_t *>(&h);
+            const float2 f = make_float2(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up);
+            const uint32_t h2 = te == 255 ? 0x7f7fu : (uint32_t)__nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
+            const __half2_raw wide = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h2, __NV_E4M3);
+            const float2 back = __half22float2(*reinterpret_cast<const __half2 *>(&wide));
+            const uint32_t l2 = te == 255 ? 0x7f7fu : (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f.x - back.x, f.y - back.y), __NV_SATFINITE, __NV_E4M3);
+            hi |= h2 << (16 * k);
+            lo |= l2 << (16 * k);
           }
+          qf[i][c][0] = hi;
+          qf[i][c][1] = lo;
         }
         const float mine = __uint_as_float((uint32_t)(127 + ex) << 23) * p.scale_log2;
 #pragma unroll
@@ -212,16 +245,12 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, (A8S<D, NQT>::CTAS)) sx_attn8_
     const int lrow = (lane & 7) + ((lane >> 3) & 1) * 8, lc = lane >> 4;
 #pragma unroll
     for (int c = 0; c < CPR; c += 2) {
-      uint32_t r[4], a[8];
+      uint32_t r[4];
       a8_ldm4(kb + lrow * D + a8_swz<D>(lrow, c + lc) * 16, r);
-      a8_widen(r[0], a[0], a[2]);
-      a8_widen(r[1], a[1], a[3]);
-      a8_widen(r[2], a[4], a[6]);
-      a8_widen(r[3], a[5], a[7]);
 #pragma unroll
       for (int i = 0; i < NQT; ++i) {
-        a8_mma(S[i], a[0], a[1], a[2], a[3], qf[i][c][0], qf[i][c][1]);
-        a8_mma(S[i], a[4], a[5], a[6], a[7], qf[i][c + 1][0], qf[i][c + 1][1]);
+        a8_mma_f8(S[i], r, qf[i][c][0], qf[i][c + 1][0]);
+        a8_mma_f8(S[i], r, qf[i][c][1], qf[i][c + 1][1]);
       }
     }
     float kscale[2], ev[2], inv[2];
@@ -450,12 +479,12 @@ static size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 #define A8_COPY_ROWS 65536
 static int tc_tile(int q, size_t all) {
   const int qt = q <= 32 ? 32 : q <= 64 ? 64 : 128;
-  return (256 / qt) * all <= A8_COPY_ROWS ? qt : 128;
+  return (128 / qt) * all <= A8_COPY_ROWS ? qt : 128;
 }
 // rows of partial results that any variant of a list may use
 static size_t list_rows(int nq, int B, int rows, int sm_count) {
-  const size_t q = (size_t)B * rows * nq, split = (size_t)16 * split_runs(sm_count) + q, most = 8 * q < A8_COPY_ROWS ? 8 * q : A8_COPY_ROWS,
-               tc = (size_t)256 * sm_count + (most > 2 * q ? most : 2 * q);
+  const size_t q = (size_t)B * rows * nq, split = (size_t)16 * split_runs(sm_count) + q, most = 4 * q < A8_COPY_ROWS ? 4 * q : A8_COPY_ROWS,
+               tc = (size_t)128 * sm_count + (most > q ? most : q);
   return split > tc ? split : tc;
 }
 static size_t list_bytes(int nq, int d, int B, int rows, int units, int sm_count) {
@@ -511,7 +540,7 @@ sx_status sx_launch_attn8(SxA8 p, int kernel, char *ws, int sm_count, cudaStream
     ls.min_per = tc ? 1 : 4;
     ls.qt_shift = log2i(ls.qt);
     ls.step_shift = log2i(ls.step);
-    ls.parts_shift = tc ? log2i(256 / ls.qt) : 0;
+    ls.parts_shift = tc ? log2i(128 / ls.qt) : 0;
     ls.half = (int64_t)ls.qt * sm_count + (int64_t)p.B * p.rows * p.nq;
     // list positions are 32-bit: steps of a sequence's whole capacity x KV heads x tiles of all units
     const int64_t steps = (int64_t)p.max_pages * p.page / ls.step + 2, tiles = (int64_t)p.B * p.rows * p.G / ls.qt + p.B + p.n_groups;

@@ -32,7 +32,7 @@ struct SxA8List {                  // one list: what the main kernel writes down
   float2 *ml;                      // partial (reference, sum) per row
   float *o;                        // partial outputs [row][d]
   int qt, qt_shift, step, step_shift, runs, min_per;
-  int parts_shift;                 // log2 of the partial results per run and tile (the tensor-memory kernel's groups and copies), `half`
+  int parts_shift;                 // log2 of the partial results per run and tile (the tensor-memory kernel's copies), `half`
   int64_t half;                    // rows apart
 };
 

@@ -24,8 +24,8 @@
 // threads - a thread owns one query, its reference and its sum, and moves the reference when a score exceeds it by
 // more than 2^T8_SLACK.  With up to 64 (32) queries the 128 rows of the products hold 2 (4) copies of them, and a
 // copy's threads take a half (a quarter) of the group's slots, with weights of zero for the others: the products cost the
-// same, and the softmax of 32 queries, one warp's work before, is spread over four.  Every copy of every group leaves
-// its own partial result.
+// same, and the softmax of 32 queries, one warp's work before, is spread over four.  At the end of a segment the groups'
+// results, which lie in the same rows of tensor memory, become one; every copy leaves its own.
 //
 // Warps: 0 K producer, 1 issuer of the first product (owns TMEM), 2 V producer, 3 issuer of the second, 4-11 softmax,
 // 12-19 widen V, lay out the scales of K and load Q.  Every mbarrier wait is bounded (sx_tc_ptx.cuh).
@@ -58,7 +58,8 @@
 #define T8_OFF_SC (T8_OFF_RING + (T8_NK + T8_NV) * T8_BLK)             // [slot of V][128 + 128] exponent bytes of K and V
 #define T8_OFF_KS (T8_OFF_SC + 1024)                     // [entry][128] scales of K
 #define T8_OFF_QF (T8_OFF_KS + T8_NC * 512)              // [entry][128] factor of the query's scores
-#define T8_OFF_BAR (T8_OFF_QF + T8_NC * 512)
+#define T8_OFF_ML (T8_OFF_QF + T8_NC * 512)              // [group][128] (reference, sum) at the end of a segment
+#define T8_OFF_BAR (T8_OFF_ML + 2048)
 #define T8_OFF_PLAN (T8_OFF_BAR + 512)
 #define T8_FIXED (T8_OFF_PLAN + 1024)                    // + alignment
 #define T8_SMEM_MAX (227 * 1024)
@@ -210,12 +211,13 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   uint8_t *sQ = smem, *sW = smem + T8_OFF_W, *ringK = smem + T8_OFF_RING, *ringV = ringK + NK * T8_BLK;
   uint8_t *sc = smem + T8_OFF_SC;
   float *ks_sh = reinterpret_cast<float *>(smem + T8_OFF_KS), *qf = reinterpret_cast<float *>(smem + T8_OFF_QF);
+  float2 *ml_sh = reinterpret_cast<float2 *>(smem + T8_OFF_ML);
   uint64_t *bars = reinterpret_cast<uint64_t *>(smem + T8_OFF_BAR);
   uint64_t *kfull = bars, *kempty = kfull + NK, *vfull = kempty + NK, *vempty = vfull + NV;
   // [group][block & 1]: scores ready, weights ready, second product done
   uint64_t *sfull = vempty + NV, *pfull = sfull + 4, *pvdone = pfull + 4, *ofree = pvdone + 4, *wfull = ofree + 2;
-  uint64_t *wempty = wfull + NW, *cfull = wempty + NW, *qfull = cfull + T8_NC, *qempty = qfull + 1;
-  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(qempty + 1);
+  uint64_t *wempty = wfull + NW, *cfull = wempty + NW, *qfull = cfull + T8_NC, *qempty = qfull + 1, *xfull = qempty + 1;
+  uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(xfull + 1);
   static_assert(COPIES == 1 || COPIES == 2 || COPIES == 4, "rows of a product hold whole copies");
   constexpr int QT = 128 / COPIES, CH = COPIES == 4 ? 16 : 32, NCH = 64 / COPIES / CH;     // queries; slots per chunk; chunks
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
@@ -237,11 +239,12 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     for (int i = 0; i < 4; ++i) {
       mbar_init(smem_u32(&sfull[i]), 1); mbar_init(smem_u32(&pfull[i]), 4); mbar_init(smem_u32(&pvdone[i]), 1);
     }
-    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&ofree[i]), 4);
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&ofree[i]), 8);
     for (int i = 0; i < NW; ++i) { mbar_init(smem_u32(&wfull[i]), 4); mbar_init(smem_u32(&wempty[i]), 1); }
     for (int i = 0; i < T8_NC; ++i) mbar_init(smem_u32(&cfull[i]), 4);
     mbar_init(smem_u32(qfull), 4);
     mbar_init(smem_u32(qempty), 1);
+    mbar_init(smem_u32(xfull), 8);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -384,13 +387,21 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         // the queries of a segment: two e4m3 parts (rows of 128 bytes, 128-byte swizzle) and factor; eight threads share a row
         const int buf = item % T8_NC;
 #pragma unroll 1
-        for (int q = r0; q < 128; q += 16) {
-          const int query = q % QT;
-          const bool live = query < s.cols;
-          const int qi = s.tile * QT + (live ? query : 0), j = qi / p.G, r = s.r0 + j;
-          const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (int64_t)r * p.q_stride + (int64_t)(s.h * p.G + qi - j * p.G) * 128 + c * 16);
-          uint4 x[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-          if (live) { x[0] = src[0]; x[1] = src[1]; }
+        for (int q0 = r0; q0 < 128; q0 += 64) {
+          uint4 xs[4][2];                                     // four rows on the way together
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int query = (q0 + k * 16) % QT;
+            const bool live = query < s.cols;
+            const int qi = s.tile * QT + (live ? query : 0), j = qi / p.G, r = s.r0 + j;
+            const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (int64_t)r * p.q_stride + (int64_t)(s.h * p.G + qi - j * p.G) * 128 + c * 16);
+            xs[k][0] = live ? src[0] : make_uint4(0, 0, 0, 0);
+            xs[k][1] = live ? src[1] : make_uint4(0, 0, 0, 0);
+          }
+#pragma unroll
+          for (int row = 0; row < 4; ++row) {
+          const int q = q0 + row * 16;
+          const uint4 *x = xs[row];
           const uint32_t m = 0x7fff7fffu;
           uint32_t top = __vmaxu2(__vmaxu2(__vmaxu2(x[0].x & m, x[0].y & m), __vmaxu2(x[0].z & m, x[0].w & m)),
                                   __vmaxu2(__vmaxu2(x[1].x & m, x[1].y & m), __vmaxu2(x[1].z & m, x[1].w & m)));
@@ -418,6 +429,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           *reinterpret_cast<uint4 *>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
           *reinterpret_cast<uint4 *>(at + T8_Q_BYTES) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
           if (c == 0) qf[buf * 128 + q] = __uint_as_float((uint32_t)(127 + ex) << 23) * p.scale_log2;
+          }
         }
         fence_async_smem();
         __syncwarp();
@@ -614,29 +626,39 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&pfull[g * 2 + b]));
       if (last) {
-        // ---- leave the segment: this copy's partial result ----------------------------------------------------------------
+        // ---- leave the segment: both groups' results become this copy's partial result, half of the columns each ------------
         ok = t8_wait(&pvdone[g * 2 + b], (uint32_t)(li >> 1) & 1u, abort_flag, wait_limit, lane);
         if (!ok) break;
+        float la, lb;
+        t8_unpack(l2, la, lb);
+        ml_sh[g * 128 + i] = make_float2(m, la + lb);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(xfull));
+        ok = t8_wait(xfull, (uint32_t)item & 1u, abort_flag, wait_limit, lane);
+        if (!ok) break;
         if (work) {
-          const int64_t row = s.base + (int64_t)QT * blockIdx.x + (int64_t)(g * COPIES + copy) * ls.half + query;
+          const int64_t row = s.base + (int64_t)QT * blockIdx.x + (int64_t)copy * ls.half + query;
           tc_fence_after();
-          float la, lb;
-          t8_unpack(l2, la, lb);
-          if (query < s.cols) ls.ml[row] = make_float2(m, la + lb);
+          const float2 r0 = ml_sh[i], r1 = ml_sh[128 + i];
+          const float top = fmaxf(r0.x, r1.x), w0 = t8_ex2(r0.x - top), w1 = t8_ex2(r1.x - top);
+          if (g == 0 && query < s.cols) ls.ml[row] = make_float2(top, r0.y * w0 + r1.y * w1);
 #pragma unroll 1
-          for (int c = 0; c < 8; ++c) {
-            float v[16];
-            tc_ld16(o_col + (uint32_t)c * 16u, v);
+          for (int c = g * 4; c < g * 4 + 4; ++c) {
+            float u[16], v[16];
+            tc_ld16(lane_base + T8_O_COL + (uint32_t)c * 16u, u);
+            tc_ld16(lane_base + T8_O_COL + 128u + (uint32_t)c * 16u, v);
             if (query < s.cols) {
               float4 *o = reinterpret_cast<float4 *>(ls.o + row * 128 + c * 16);
 #pragma unroll
-              for (int j = 0; j < 4; ++j) o[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+              for (int j = 0; j < 4; ++j)
+                o[j] = make_float4(u[4 * j] * w0 + v[4 * j] * w1, u[4 * j + 1] * w0 + v[4 * j + 1] * w1,
+                                   u[4 * j + 2] * w0 + v[4 * j + 2] * w1, u[4 * j + 3] * w0 + v[4 * j + 3] * w1);
             }
           }
           tc_fence_before();
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&ofree[g]));
+        if (lane == 0) { mbar_arrive(smem_u32(&ofree[0])); mbar_arrive(smem_u32(&ofree[1])); }
       }
     }
   }

@@ -20,7 +20,7 @@
 #include "sx_launch.cuh"
 
 #define KV8_THREADS 256
-#define KV8_MAX_TOKENS 16            // tokens per CTA
+#define KV8_MAX_TOKENS 64            // tokens per CTA
 
 struct SxKv8Rows {
   int B, T, nkv, d, page, max_pages, num_pages, tokens;      // tokens: per CTA
@@ -31,20 +31,30 @@ struct SxKv8Rows {
 };
 
 // First row of the pool (page * n_kv * page_size + offset, to which head * page_size is added) of the CTA's tokens, -1
-// where there is no token.  Every thread looks at some sequences and fills in the tokens that belong to them.
+// where there is no token.  Every thread looks at some sequences and names the tokens that belong to them; then a
+// thread per token finds its page.
 __device__ __forceinline__ void kv8_places(const SxKv8Rows &p, int t0, int nt, int64_t *place) {
-  for (int i = threadIdx.x; i < nt; i += KV8_THREADS) place[i] = -1;
+  __shared__ int seq[KV8_MAX_TOKENS];
+  for (int i = threadIdx.x; i < nt; i += KV8_THREADS) seq[i] = -1;
   __syncthreads();
+#pragma unroll 1
   for (int b = threadIdx.x; b < p.B; b += KV8_THREADS) {
     const int s = p.row_start[b], e = p.row_start[b + 1];
     if (blockIdx.x == 0 && (s < 0 || e < s || e > p.T)) sx_set_status(p.status, SX_ERR_CAPACITY);
-    for (int t = max(max(s, 0), t0); t < min(e, t0 + nt); ++t) {
-      const int64_t pos = (int64_t)p.pos_start[b] + (t - s), lp = pos < 0 ? -1 : pos / p.page;
+    for (int t = max(max(s, 0), t0); t < min(e, t0 + nt); ++t) seq[t - t0] = b;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < nt; i += KV8_THREADS) {
+    const int b = seq[i];
+    int64_t at = -1;
+    if (b >= 0) {
+      const int64_t pos = (int64_t)p.pos_start[b] + (t0 + i - p.row_start[b]), lp = pos < 0 ? -1 : pos / p.page;
       int pp = -1;
       if (lp >= 0 && lp < p.max_pages) pp = p.page_table[(int64_t)b * p.max_pages + lp];
       if (pp < 0 || pp >= p.num_pages) sx_set_status(p.status, SX_ERR_CAPACITY);
-      else place[t - t0] = (int64_t)pp * p.nkv * p.page + pos % p.page;
+      else at = (int64_t)pp * p.nkv * p.page + pos % p.page;
     }
+    place[i] = at;
   }
   __syncthreads();
 }
@@ -66,15 +76,20 @@ __global__ void __launch_bounds__(KV8_THREADS) sx_kv8_append_kernel(SxKv8Rows p,
   const int rows = nt * p.nkv * 2, lane = threadIdx.x % LPR;
   // row index: token, K or V, head.  Four rows per thread at a time, so that their loads are on the way together.
   constexpr int U = 4, RPC = KV8_THREADS / LPR;
-  for (int r0 = threadIdx.x / LPR; r0 - (int)(threadIdx.x / LPR) < rows; r0 += U * RPC) {
+  const int per = 2 * p.nkv;                 // rows of a token: its heads' keys, then their values
+  int t_at = (int)(threadIdx.x / LPR) / per, w_at = (int)(threadIdx.x / LPR) - t_at * per;
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows; r0 += U * RPC) {
     uint4 x[U];
     int64_t at[U];
     bool is_v[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int r = r0 + i * RPC, t = r / (2 * p.nkv), w = r - t * 2 * p.nkv, h = w % p.nkv;
-      is_v[i] = w >= p.nkv;
-      at[i] = r < rows ? place[t] : -1;
+      const int t = t_at, h = w_at < p.nkv ? w_at : w_at - p.nkv;
+      is_v[i] = w_at >= p.nkv;
+      at[i] = t < nt ? place[t] : -1;
+      w_at += RPC;
+      while (w_at >= per) { w_at -= per; ++t_at; }
       x[i] = make_uint4(0, 0, 0, 0);
       if (at[i] >= 0) {
         at[i] += (int64_t)h * p.page;
@@ -101,7 +116,9 @@ __global__ void __launch_bounds__(KV8_THREADS) sx_kv8_append_kernel(SxKv8Rows p,
   }
 }
 
-template <int D>
+// U rows per thread at a time: eight in large calls (172 us against 197 us for 140k tokens of 8 heads), four in small ones
+// (9.8 us against 13 us for 4096), where most of eight would not exist
+template <int D, int U>
 __global__ void __launch_bounds__(KV8_THREADS) sx_kv8_read_kernel(SxKv8Rows p, bf16 *__restrict__ k, bf16 *__restrict__ v) {
   constexpr int LPR = D / 16;
   __shared__ int64_t place[KV8_MAX_TOKENS];
@@ -109,17 +126,23 @@ __global__ void __launch_bounds__(KV8_THREADS) sx_kv8_read_kernel(SxKv8Rows p, b
   const int t0 = blockIdx.x * p.tokens, nt = min(p.tokens, p.T - t0);
   kv8_places(p, t0, nt, place);
   const int rows = nt * p.nkv * 2, lane = threadIdx.x % LPR;
-  constexpr int U = 4, RPC = KV8_THREADS / LPR;
-  for (int r0 = threadIdx.x / LPR; r0 < rows; r0 += U * RPC) {
+  constexpr int RPC = KV8_THREADS / LPR;
+  const int per = 2 * p.nkv;
+  int w_at = (int)(threadIdx.x / LPR) / nt, t_at = (int)(threadIdx.x / LPR) - w_at * nt;
+#pragma unroll 1
+  for (int r0 = 0; r0 < rows; r0 += U * RPC) {
     uint4 x[U];
     int byte[U];
     bf16 *dst[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int r = r0 + i * RPC, t = r / (2 * p.nkv), w = r - t * 2 * p.nkv, h = w % p.nkv;
-      const bool is_v = w >= p.nkv;
+      const int t = t_at, h = w_at < p.nkv ? w_at : w_at - p.nkv;
+      const bool is_v = w_at >= p.nkv;
       dst[i] = nullptr;
-      if (r < rows && place[t] >= 0) {
+      const bool on = w_at < per;
+      t_at += RPC;
+      while (t_at >= nt) { t_at -= nt; ++w_at; }
+      if (on && place[t] >= 0) {
         const int64_t at = place[t] + (int64_t)h * p.page;
         x[i] = *reinterpret_cast<const uint4 *>((is_v ? p.v : p.k) + at * D + lane * 16);
         byte[i] = (is_v ? p.vs : p.ks)[at];
@@ -159,6 +182,13 @@ static sx_status check_cache(const sx_kv_shape *sh, const sx_kv *kv) {
   return SX_OK;
 }
 
+static int sms_of_current_device() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    return 0;
+  return n;
+}
+
 static sx_status rows_call(const sx_kv_shape *sh, const sx_kv *kv, int32_t T, const int32_t *row_start_d,
                            const int32_t *pos_start_d, const void *k, const void *v, int64_t ks, int64_t vs,
                            int32_t *status_d, SxKv8Rows *out) {
@@ -176,8 +206,12 @@ static sx_status rows_call(const sx_kv_shape *sh, const sx_kv *kv, int32_t T, co
   p.k_stride = ks; p.v_stride = vs;
   p.k = (uint8_t *)kv->k_pages_d; p.v = (uint8_t *)kv->v_pages_d; p.ks = kv->k_scale_d; p.vs = kv->v_scale_d;
   p.status = status_d;
-  // few tokens: one per CTA; many: enough rows per CTA that finding the places is a small part
-  p.tokens = T <= 1024 ? 1 : 8;
+  // as many tokens per CTA as make one wave of about six CTAs per SM: finding the places is a chain of three dependent
+  // reads, which a CTA of few tokens spends half its time on
+  const int wave = 6 * sms_of_current_device();
+  p.tokens = wave ? (T + wave - 1) / wave : 1;
+  if (p.tokens > KV8_MAX_TOKENS) p.tokens = KV8_MAX_TOKENS;
+  if (p.tokens < 1) p.tokens = 1;
   *out = p;
   return SX_OK;
 }
@@ -199,6 +233,12 @@ extern "C" sx_status sx_kv_append(const sx_kv_shape *sh, const sx_kv *kv, int32_
   }
 }
 
+template <int D>
+static sx_status launch_read(const SxKv8Rows &p, dim3 grid, bf16 *k, bf16 *v, cudaStream_t st) {
+  if (p.tokens < 16) return sx_rc(sx_launch(sx_kv8_read_kernel<D, 4>, grid, dim3(KV8_THREADS), 0, st, p, k, v));
+  return sx_rc(sx_launch(sx_kv8_read_kernel<D, 8>, grid, dim3(KV8_THREADS), 0, st, p, k, v));
+}
+
 extern "C" sx_status sx_kv_read(const sx_kv_shape *sh, const sx_kv *kv, int32_t T, const int32_t *row_start_d,
                                 const int32_t *pos_start_d, void *k_d, int64_t k_stride, void *v_d, int64_t v_stride,
                                 int32_t *status_d, void *stream) {
@@ -210,18 +250,11 @@ extern "C" sx_status sx_kv_read(const sx_kv_shape *sh, const sx_kv *kv, int32_t 
   bf16 *k = (bf16 *)k_d, *v = (bf16 *)v_d;
   cudaStream_t st = (cudaStream_t)stream;
   switch (p.d) {
-    case 16: return sx_rc(sx_launch(sx_kv8_read_kernel<16>, grid, dim3(KV8_THREADS), 0, st, p, k, v));
-    case 32: return sx_rc(sx_launch(sx_kv8_read_kernel<32>, grid, dim3(KV8_THREADS), 0, st, p, k, v));
-    case 64: return sx_rc(sx_launch(sx_kv8_read_kernel<64>, grid, dim3(KV8_THREADS), 0, st, p, k, v));
-    default: return sx_rc(sx_launch(sx_kv8_read_kernel<128>, grid, dim3(KV8_THREADS), 0, st, p, k, v));
+    case 16: return launch_read<16>(p, grid, k, v, st);
+    case 32: return launch_read<32>(p, grid, k, v, st);
+    case 64: return launch_read<64>(p, grid, k, v, st);
+    default: return launch_read<128>(p, grid, k, v, st);
   }
-}
-
-static int sms_of_current_device() {
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return 0;
-  return n;
 }
 
 extern "C" size_t sx_attention_ws_bytes(const sx_kv_shape *sh, int32_t batch, int32_t rows, int32_t n_groups) {
