@@ -6,6 +6,7 @@ loaded, or a call returns an error, an exception is raised.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from dataclasses import dataclass
@@ -283,6 +284,9 @@ def _kv_struct(kv: Dict[str, torch.Tensor], n_kv: int, page: int, d: int) -> KV:
     return st
 
 
+_NO_GUARD = contextlib.nullcontext()
+
+
 class KV8:
     """An 8-bit paged cache and the operators over it (no draft model needed).
 
@@ -328,6 +332,11 @@ class KV8:
     def _stride(self, t: torch.Tensor) -> int:
         return t.stride(0) if t.shape[0] > 1 else self.n_kv * self.d
 
+    def _guard(self):
+        """The cache's device becomes the current one for a launch (entering a device costs more than the launch does, so
+        only where another one is current)."""
+        return _NO_GUARD if torch.cuda.current_device() == self.dev.index else torch.cuda.device(self.dev)
+
     def sx_kv_append(self, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor,
                      pos_start: Optional[torch.Tensor] = None) -> None:
         """Quantises rows ``k`` / ``v`` (bf16 ``[T, n_kv, d]``, any row stride that is a multiple of 8) into the cache:
@@ -336,10 +345,10 @@ class KV8:
         T = self._rows(k, v, row_start, pos_start)
         if T == 0:
             return
-        with torch.cuda.device(self.dev):
+        with self._guard():
             _check(self.lib.sx_kv_append(self._shape_ref, self._kv_ref, T, row_start.data_ptr(), _p(pos_start),
                                          k.data_ptr(), self._stride(k), v.data_ptr(), self._stride(v),
-                                         self.status.data_ptr(), torch.cuda.current_stream().cuda_stream), "sx_kv_append")
+                                         self.status.data_ptr(), torch.cuda.current_stream(self.dev).cuda_stream), "sx_kv_append")
 
     def sx_kv_read(self, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, pos_start: torch.Tensor) -> None:
         """Reads slots ``pos_start[b] ..`` of every sequence back into rows ``row_start[b] .. row_start[b + 1] - 1`` of
@@ -347,10 +356,10 @@ class KV8:
         T = self._rows(k, v, row_start, pos_start)
         if T == 0:
             return
-        with torch.cuda.device(self.dev):
+        with self._guard():
             _check(self.lib.sx_kv_read(self._shape_ref, self._kv_ref, T, row_start.data_ptr(), _p(pos_start),
                                        k.data_ptr(), self._stride(k), v.data_ptr(), self._stride(v),
-                                       self.status.data_ptr(), torch.cuda.current_stream().cuda_stream), "sx_kv_read")
+                                       self.status.data_ptr(), torch.cuda.current_stream(self.dev).cuda_stream), "sx_kv_read")
 
     def sx_attention(self, q: torch.Tensor, drafted: int = 0, row_mask: Optional[torch.Tensor] = None,
                      scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
@@ -371,7 +380,7 @@ class KV8:
             out = torch.empty(self.B, rows, nq, self.d, dtype=torch.bfloat16, device=self.dev)
         elif out.dtype != torch.bfloat16 or out.device != self.dev or out.shape != q.shape or not out.is_contiguous():
             raise SxError("out must be contiguous bf16 of q's shape")
-        with torch.cuda.device(self.dev):
+        with self._guard():
             self._shape.n_q_heads = nq
             if self._ws_for != (rows, nq):
                 need = int(self.lib.sx_attention_ws_bytes(self._shape_ref, self.B, rows, int(self._kv.n_groups)))
@@ -382,7 +391,7 @@ class KV8:
                 self._ws_for = (rows, nq)
             _check(self.lib.sx_attention(self._shape_ref, self._kv_ref, rows, drafted, q.data_ptr(), stride, _p(row_mask),
                                          self.d ** -0.5 if scale is None else scale, kernel, out.data_ptr(), self._ws_at,
-                                         self._ws_bytes, self.status.data_ptr(), torch.cuda.current_stream().cuda_stream),
+                                         self._ws_bytes, self.status.data_ptr(), torch.cuda.current_stream(self.dev).cuda_stream),
                    "sx_attention")
         return out
 

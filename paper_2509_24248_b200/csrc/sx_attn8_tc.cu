@@ -163,18 +163,36 @@ __device__ __forceinline__ void t8_st(uint32_t taddr, const uint32_t (&v)[8]) {
 }
 __device__ __forceinline__ void t8_ld(uint32_t taddr, float (&v)[16]) { tc_ld16(taddr, v); }
 __device__ __forceinline__ void t8_ld(uint32_t taddr, float (&v)[32]) {
-  uint32_t r[32];
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
-        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
-        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
+      "%22, %23, %24, %25, %26, %27, %28, %29, %30, %31 "
+      "}, [%32];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+        "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+        "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
       : "r"(taddr) : "memory");
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void t8_ld(uint32_t taddr, float (&v)[64]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
+      "%22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, "
+      "%42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, "
+      "%62, %63 "
+      "}, [%64];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+        "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+        "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]),
+        "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]),
+        "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]),
+        "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]),
+        "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63])
+      : "r"(taddr) : "memory");
 }
 // four codes to bf16, times `f` (a packed pair of equal bf16 numbers): exponent and mantissa move to the low end of the
 // exponent's place and the high end of the mantissa's, which is the value times 2^-120; f = 2^(120 + e)
@@ -219,7 +237,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   uint64_t *wempty = wfull + NW, *cfull = wempty + NW, *qfull = cfull + T8_NC, *qempty = qfull + 1, *xfull = qempty + 1;
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(xfull + 1);
   static_assert(COPIES == 1 || COPIES == 2 || COPIES == 4, "rows of a product hold whole copies");
-  constexpr int QT = 128 / COPIES, CH = COPIES == 4 ? 16 : 32, NCH = 64 / COPIES / CH;     // queries; slots per chunk; chunks
+  constexpr int QT = 128 / COPIES, CH = 64 / COPIES;       // queries of a copy; its slots of a group's half
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -242,7 +260,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&ofree[i]), 8);
     for (int i = 0; i < NW; ++i) { mbar_init(smem_u32(&wfull[i]), 4); mbar_init(smem_u32(&wempty[i]), 1); }
     for (int i = 0; i < T8_NC; ++i) mbar_init(smem_u32(&cfull[i]), 4);
-    mbar_init(smem_u32(qfull), 4);
+    mbar_init(smem_u32(qfull), 8);
     mbar_init(smem_u32(qempty), 1);
     mbar_init(smem_u32(xfull), 8);
     *abort_flag = 0;
@@ -367,27 +385,28 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   } else if (warp >= 12) {
     // ---- V codes to bf16 ([64 columns][128 slots][128 bytes] twice, 128-byte swizzle), scales of K, queries --------------
     t8_setreg_dec<80>();
-    // two teams of four warps take the blocks in turn, each with its copy of V
+    // Two teams of four warps take the blocks in turn, each with its copy of V; the queries of every segment are loaded by
+    // both, half of the rows each (a team alone, row after row, kept a segment's first block waiting for 4 us)
     const int team = (warp - 12) >> 2, tid = threadIdx.x & 127, c = tid & 7, r0 = tid >> 3;
     static_assert(NW == 2, "a copy of V per team");
     A8Seg s = a8_seek<PRE>(p, pl, ls, slab, g0);
-    int item = 0;
+    int item = -1;
+    bool ok = true;
 #pragma unroll 1
-    for (int li = team; li < nblk; li += 2) {
-      // both teams wait for the end of every segment's first products, so that neither can be a phase behind
-      bool ok = true;
+    for (int li = team;; li += 2) {
+      const int at_x = g0 + min(li, nblk - 1);
 #pragma unroll 1
-      while (ok && g0 + li >= s.x1) {
-        ok = t8_wait(qempty, (uint32_t)item & 1u, abort_flag, wait_limit, lane);
-        s = a8_seek<PRE>(p, pl, ls, slab, s.x1);
+      while (ok && (item < 0 || at_x >= s.x1)) {
+        // both teams wait for the end of every segment's first products, so that neither can be a phase behind
+        if (item >= 0) {
+          ok = t8_wait(qempty, (uint32_t)item & 1u, abort_flag, wait_limit, lane);
+          s = a8_seek<PRE>(p, pl, ls, slab, s.x1);
+        }
         ++item;
-      }
-      if (!ok) break;
-      if (li == 0 || g0 + li == s.x0) {
-        // the queries of a segment: two e4m3 parts (rows of 128 bytes, 128-byte swizzle) and factor; eight threads share a row
+        // two e4m3 parts (rows of 128 bytes, 128-byte swizzle) and factor; eight threads share a row
         const int buf = item % T8_NC;
-#pragma unroll 1
-        for (int q0 = r0; q0 < 128; q0 += 64) {
+        {
+          const int q0 = team * 64 + r0;
           uint4 xs[4][2];                                     // four rows on the way together
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -400,43 +419,42 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           }
 #pragma unroll
           for (int row = 0; row < 4; ++row) {
-          const int q = q0 + row * 16;
-          const uint4 *x = xs[row];
-          const uint32_t m = 0x7fff7fffu;
-          uint32_t top = __vmaxu2(__vmaxu2(__vmaxu2(x[0].x & m, x[0].y & m), __vmaxu2(x[0].z & m, x[0].w & m)),
-                                  __vmaxu2(__vmaxu2(x[1].x & m, x[1].y & m), __vmaxu2(x[1].z & m, x[1].w & m)));
-          top = max(top & 0xffffu, top >> 16);
+            const int q = q0 + row * 16;
+            const uint4 *x = xs[row];
+            const uint32_t m = 0x7fff7fffu;
+            uint32_t top = __vmaxu2(__vmaxu2(__vmaxu2(x[0].x & m, x[0].y & m), __vmaxu2(x[0].z & m, x[0].w & m)),
+                                    __vmaxu2(__vmaxu2(x[1].x & m, x[1].y & m), __vmaxu2(x[1].z & m, x[1].w & m)));
+            top = max(top & 0xffffu, top >> 16);
 #pragma unroll
-          for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o, 8));
-          // largest magnitude into (224, 448], as for the rows of the cache
-          const int e = (int)(top >> 7);
-          int ex = top == 0 || e == 255 ? 0 : e - 135 + ((top & 0x7f) > 96 ? 1 : 0);
-          ex = max(-126, ex);
-          const float up = __uint_as_float((uint32_t)(127 - ex) << 23);
-          const uint32_t in[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
-          uint32_t hi[4], lo[4];
+            for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o, 8));
+            // largest magnitude into (224, 448], as for the rows of the cache
+            const int e = (int)(top >> 7);
+            int ex = top == 0 || e == 255 ? 0 : e - 135 + ((top & 0x7f) > 96 ? 1 : 0);
+            ex = max(-126, ex);
+            const float up = __uint_as_float((uint32_t)(127 - ex) << 23);
+            const uint32_t in[8] = {x[0].x, x[0].y, x[0].z, x[0].w, x[1].x, x[1].y, x[1].z, x[1].w};
+            uint32_t hi[4], lo[4];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float2 f = make_float2(__uint_as_float(in[k] << 16) * up, __uint_as_float(in[k] & 0xffff0000u) * up);
-            const uint32_t h2 = e == 255 ? 0x7f7fu : (uint32_t)__nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
-            const __half2_raw wide = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h2, __NV_E4M3);
-            const float2 back = __half22float2(*reinterpret_cast<const __half2 *>(&wide));
-            const uint32_t l2 = e == 255 ? 0x7f7fu : (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f.x - back.x, f.y - back.y), __NV_SATFINITE, __NV_E4M3);
-            if (k & 1) { hi[k >> 1] |= h2 << 16; lo[k >> 1] |= l2 << 16; }
-            else { hi[k >> 1] = h2; lo[k >> 1] = l2; }
-          }
-          uint8_t *at = sQ + q * 128 + ((c ^ (q & 7)) << 4);
-          *reinterpret_cast<uint4 *>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4 *>(at + T8_Q_BYTES) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-          if (c == 0) qf[buf * 128 + q] = __uint_as_float((uint32_t)(127 + ex) << 23) * p.scale_log2;
+            for (int k = 0; k < 8; ++k) {
+              const float2 f = make_float2(__uint_as_float(in[k] << 16) * up, __uint_as_float(in[k] & 0xffff0000u) * up);
+              const uint32_t h2 = e == 255 ? 0x7f7fu : (uint32_t)__nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
+              const __half2_raw wide = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h2, __NV_E4M3);
+              const float2 back = __half22float2(*reinterpret_cast<const __half2 *>(&wide));
+              const uint32_t l2 = e == 255 ? 0x7f7fu : (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f.x - back.x, f.y - back.y), __NV_SATFINITE, __NV_E4M3);
+              if (k & 1) { hi[k >> 1] |= h2 << 16; lo[k >> 1] |= l2 << 16; }
+              else { hi[k >> 1] = h2; lo[k >> 1] = l2; }
+            }
+            uint8_t *at = sQ + q * 128 + ((c ^ (q & 7)) << 4);
+            *reinterpret_cast<uint4 *>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *reinterpret_cast<uint4 *>(at + T8_Q_BYTES) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            if (c == 0) qf[buf * 128 + q] = __uint_as_float((uint32_t)(127 + ex) << 23) * p.scale_log2;
           }
         }
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(qfull));
       }
-      const int slot0 = s.first + (g0 + li - s.x0) * 128;
-      const bool whole = slot0 >= s.lo && slot0 + 128 <= s.len;
+      if (!ok || li >= nblk) break;
       const int slot = li % NV, e = li % T8_NC;
       if (!t8_wait(&vfull[slot], (uint32_t)(li / NV) & 1u, abort_flag, wait_limit, lane)) break;
       const uint8_t *kbytes = sc + slot * 256, *vbytes = kbytes + 128;
@@ -458,8 +476,9 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         f[it] = byte == 255 ? 0u : t8_pow2x2(min(byte, 134) - 7);
         top = max(top, byte == 255 ? 0 : byte);
       }
-      // rows whose 2^(120 + e) is out of range (in two steps), blocks with slots that no query may see
-      const bool rare = !whole || __any_sync(0xffffffffu, top > 134);
+      // Rows whose 2^(120 + e) is out of range take two steps.  They alone can end as infinity (a slot that nobody may see can
+      // hold any byte), which must not meet a weight of 0.
+      const bool rare = __any_sync(0xffffffffu, top > 134);
       if (li >= NW && !t8_wait(&wempty[team], (uint32_t)(li / NW - 1) & 1u, abort_flag, wait_limit, lane)) break;
       // chunks 2c and 2c + 1 of the half; the lanes of the second half go the other way round, so that eight lanes of one
       // row fall into eight different groups of banks
@@ -532,87 +551,74 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const int mine = slot0 + g * 64 + k0;
         const ulonglong2 *kb = reinterpret_cast<const ulonglong2 *>(ks_sh + e * 128 + g * 64 + k0);
         const f32x2 f2 = t8_pack(factor, factor);
-        // scores of CH slots in base 2, less `ref`; -inf where a slot is not seen.  Returns their maximum.
+        // Scores in base 2, less the reference; -inf where a slot is not seen.  All of them at once: one wait for tensor
+        // memory and one vote per block (in chunks of 32, each with its own, two warps per scheduler could not hide them).
         float t[CH];
-        auto scores = [&](int c, float ref) -> float {         // one copy of this in the code: see the note at a8_seek
-          t8_ld(s_col + (uint32_t)(k0 + c * CH), t);
-          const f32x2 r2 = t8_pack(-ref, -ref);
-          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        t8_ld(s_col + (uint32_t)k0, t);
+        const bool none = m == T8_NONE;
+        const float ref = none ? 0.f : m;
+        const f32x2 r2 = t8_pack(-ref, -ref);
 #pragma unroll
-          for (int j = 0; j < CH; j += 4) {
-            const ulonglong2 k = kb[c * (CH / 4) + (j >> 2)];
-            t8_unpack(t8_fma2(t8_mul2(t8_pack(t[j], t[j + 1]), k.x), f2, r2), t[j], t[j + 1]);
-            t8_unpack(t8_fma2(t8_mul2(t8_pack(t[j + 2], t[j + 3]), k.y), f2, r2), t[j + 2], t[j + 3]);
+        for (int j = 0; j < CH; j += 4) {
+          const ulonglong2 k = kb[j >> 2];
+          t8_unpack(t8_fma2(t8_mul2(t8_pack(t[j], t[j + 1]), k.x), f2, r2), t[j], t[j + 1]);
+          t8_unpack(t8_fma2(t8_mul2(t8_pack(t[j + 2], t[j + 3]), k.y), f2, r2), t[j + 2], t[j + 3]);
+        }
+        if (!whole) {
+#pragma unroll
+          for (int j0 = 0; j0 < CH; j0 += 32) {
+            const uint32_t seen = a8_visible<PRE>(s, mask, mine + j0, CH < 32 ? CH : 32);
+#pragma unroll
+            for (int j = 0; j < (CH < 32 ? CH : 32); ++j)
+              if (!((seen >> j) & 1u)) t[j0 + j] = -INFINITY;
           }
-          if (!whole) {
-            const uint32_t seen = a8_visible<PRE>(s, mask, mine + c * CH, CH);
+        }
+        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int j = 0; j < CH; ++j)
-              if (!((seen >> j) & 1u)) t[j] = -INFINITY;
-          }
-#pragma unroll
-          for (int j = 0; j < CH; j += 4) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], t[j + k]);
-          }
-          return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-        };
+        for (int j = 0; j < CH; ++j) tops[j & 3] = fmaxf(tops[j & 3], t[j]);
+        const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        if (__any_sync(0xffffffffu, top > (none ? T8_NONE : T8_SLACK))) {
+          // ---- the reference moves to the largest (from none: in a segment's first block; else rarely); what has been summed
+          // and weighted follows
+          const bool moves = top > (none ? T8_NONE : T8_SLACK);
+          if (moves) m = ref + top;
+          const float corr = !moves ? 1.f : none ? 0.f : t8_ex2(ref - m);
+          l2 = t8_mul2(l2, t8_pack(corr, corr));
+          if (!first) {
+            // O is at rest once the group's product before has completed
+            ok = t8_wait(&pvdone[g * 2 + (b ^ 1)], (uint32_t)((li - 1) >> 1) & 1u, abort_flag, wait_limit, lane);
+            if (!ok) break;
+            tc_fence_after();
 #pragma unroll 1
-        for (int c = 0; c < NCH; ++c) {
-          const bool none = m == T8_NONE;
-          const float ref = none ? 0.f : m, top = scores(c, ref);
-          if (__any_sync(0xffffffffu, top > (none ? T8_NONE : T8_SLACK))) {
-            // ---- the reference moves to the largest of the chunk (from none: in a segment's first block; else rarely); what has
-            // been summed and weighted follows
-            const bool moves = top > (none ? T8_NONE : T8_SLACK);
-            if (moves) m = ref + top;
-            const float corr = !moves ? 1.f : none ? 0.f : t8_ex2(ref - m);
-            l2 = t8_mul2(l2, t8_pack(corr, corr));
-            if (!first) {
-              // O is at rest once the group's product before has completed
-              ok = t8_wait(&pvdone[g * 2 + (b ^ 1)], (uint32_t)((li - 1) >> 1) & 1u, abort_flag, wait_limit, lane);
-              if (!ok) break;
-              tc_fence_after();
-#pragma unroll 1
-              for (int k = 0; k < 8; ++k) {
-                float v[16];
-                tc_ld16(o_col + (uint32_t)k * 16u, v);
-#pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] *= corr;
-                tc_st16(o_col + (uint32_t)k * 16u, v);
-              }
-            }
-            if (c > 0) {                                     // the weights of this block so far (COPIES == 1, one chunk)
-              tc_wait_st();
+            for (int k = 0; k < 8; ++k) {
               float v[16];
-              uint32_t u[16];
-              tc_ld16(s_col, v);
+              tc_ld16(o_col + (uint32_t)k * 16u, v);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                const uint32_t y = __float_as_uint(v[j]);
-                const __nv_bfloat162 z = __floats2bfloat162_rn(__uint_as_float(y << 16) * corr, __uint_as_float(y & 0xffff0000u) * corr);
-                u[j] = *reinterpret_cast<const uint32_t *>(&z);
-              }
-              t8_st(s_col, u);
+              for (int j = 0; j < 16; ++j) v[j] *= corr;
+              tc_st16(o_col + (uint32_t)k * 16u, v);
             }
-#pragma unroll
-            for (int j = 0; j < CH; ++j) t[j] -= moves ? m - ref : 0.f;
           }
-          // weights (below 2^T8_SLACK), their sum, bf16 in place of the scores that have been read
-          uint32_t u[CH / 2];
-          f32x2 sum[2] = {0ull, 0ull};
+          const float by = moves ? m - ref : 0.f;
 #pragma unroll
-          for (int j = 0; j < CH; j += 2) {
-            const float a = t8_ex2(t[j]), d = t8_ex2(t[j + 1]);
+          for (int j = 0; j < CH; ++j) t[j] -= by;
+        }
+        // weights (below 2^T8_SLACK), their sum, bf16 in place of the scores that have been read
+        f32x2 sum[2] = {0ull, 0ull};
+        constexpr int CS = CH < 32 ? CH : 32;
+#pragma unroll
+        for (int j0 = 0; j0 < CH; j0 += CS) {
+          uint32_t u[CS / 2];
+#pragma unroll
+          for (int j = 0; j < CS; j += 2) {
+            const float a = t8_ex2(t[j0 + j]), d = t8_ex2(t[j0 + j + 1]);
             sum[(j >> 1) & 1] = t8_add2(sum[(j >> 1) & 1], t8_pack(a, d));
             const __nv_bfloat162 z = __floats2bfloat162_rn(a, d);
             u[j >> 1] = *reinterpret_cast<const uint32_t *>(&z);
           }
-          l2 = t8_add2(l2, t8_add2(sum[0], sum[1]));
-          t8_st(s_col + (uint32_t)(k0 / 2 + c * (CH / 2)), u);
+          t8_st(s_col + (uint32_t)((k0 + j0) / 2), u);
         }
-        if (!ok) break;
-        if (COPIES > 1) {                                    // the slots of the other copies
+        l2 = t8_add2(l2, t8_add2(sum[0], sum[1]));
+        if constexpr (COPIES > 1) {                          // the slots of the other copies
           uint32_t zero[CH / 2];
 #pragma unroll
           for (int j = 0; j < CH / 2; ++j) zero[j] = 0u;
