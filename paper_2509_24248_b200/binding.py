@@ -309,7 +309,8 @@ class KV8:
         self.status = torch.zeros(1, dtype=torch.int32, device=self.dev)
         self._shape = KVShape(self.n_kv, self.n_kv, self.d, self.page)
         self._shape_ref = C.byref(self._shape)
-        self._ws, self._ws_at, self._ws_bytes, self._ws_for = None, 0, 0, None
+        # a captured graph goes on using the workspace it was captured with, so one that became too small is kept
+        self._ws, self._ws_at, self._ws_bytes, self._ws_for = [], 0, 0, None
 
     def check_status(self, what: str = "device") -> None:
         code = int(self.status.item())
@@ -319,15 +320,16 @@ class KV8:
 
     def _rows(self, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, pos_start: Optional[torch.Tensor]) -> int:
         for name, t in (("k", k), ("v", v)):
-            if (t.dtype != torch.bfloat16 or t.device != self.dev or t.dim() != 3 or t.shape[1:] != (self.n_kv, self.d)
-                    or t.stride(2) != 1 or t.stride(1) != self.d):
+            shape, stride = t.shape, t.stride()
+            if (len(shape) != 3 or shape[1] != self.n_kv or shape[2] != self.d or stride[2] != 1 or stride[1] != self.d
+                    or t.dtype is not torch.bfloat16 or t.device != self.dev):
                 raise SxError(f"{name} must be bf16 [T, {self.n_kv}, {self.d}] on {self.dev}, rows of heads contiguous")
         if k.shape[0] != v.shape[0]:
             raise SxError("k and v must have the same number of rows")
         for name, t, n in (("row_start", row_start, self.B + 1), ("pos_start", pos_start, self.B)):
-            if t is not None and (t.dtype != torch.int32 or t.device != self.dev or t.numel() != n or not t.is_contiguous()):
+            if t is not None and (t.dtype is not torch.int32 or t.numel() != n or t.device != self.dev or not t.is_contiguous()):
                 raise SxError(f"{name} must be int32 [{n}] on {self.dev}")
-        return int(k.shape[0])
+        return k.shape[0]
 
     def _stride(self, t: torch.Tensor) -> int:
         return t.stride(0) if t.shape[0] > 1 else self.n_kv * self.d
@@ -385,8 +387,8 @@ class KV8:
             if self._ws_for != (rows, nq):
                 need = int(self.lib.sx_attention_ws_bytes(self._shape_ref, self.B, rows, int(self._kv.n_groups)))
                 if need > self._ws_bytes:
-                    self._ws = torch.empty(need + 256, dtype=torch.uint8, device=self.dev)
-                    self._ws_at = self._ws.data_ptr() + (-self._ws.data_ptr()) % 256
+                    self._ws.append(torch.empty(need + 256, dtype=torch.uint8, device=self.dev))
+                    self._ws_at = self._ws[-1].data_ptr() + (-self._ws[-1].data_ptr()) % 256
                     self._ws_bytes = need
                 self._ws_for = (rows, nq)
             _check(self.lib.sx_attention(self._shape_ref, self._kv_ref, rows, drafted, q.data_ptr(), stride, _p(row_mask),

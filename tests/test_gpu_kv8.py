@@ -255,6 +255,79 @@ def test_rows_that_are_not_finite_reach_those_who_see_them(kernel):
     assert (np.abs(got[~sees] - want[~sees]) <= bound[~sees]).all()
 
 
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("byte,code", [(254, 0x7e), (254, 0x7f), (255, 0xff), (0, 0x7f), (200, 0xfe)])
+def test_slots_that_nobody_sees_can_hold_anything(kernel, byte, code):
+    """Slots behind the last one, drafted slots outside every mask, and the slots in front of a sequence's own in a page that
+    the prefix ends in: any code and exponent byte there changes nothing."""
+    lens, drafted, rows = [200, 131, 150], 9, 2
+    kv = ref.make_cache(3, 2, 128, 64, lens, drafted, seed=24, groups=[0, 3], prefix=[100], share_pages=False)
+    mask = torch.tensor([[0b000000111, 0b010000001], [0b000000001, 0b000100000], [0, 1]])
+    q = ref.make_q(3, rows, 8, 128, 25)
+    before = sx.KV8(to_dev(kv)).sx_attention(q.to(DEV), drafted, mask.to(DEV), kernel=kernel)
+    for b in range(3):
+        dead = [lens[b] + i for i in range(drafted) if not any((int(m) >> i) & 1 for m in mask[b])]
+        dead += list(range(lens[b] + drafted, int(kv["page_table"].shape[1]) * 64))
+        if b:
+            dead += list(range(100))                          # the first member's table stands for the prefix
+        for s in dead:
+            pp, off = int(kv["page_table"][b, s // 64]), s % 64
+            for n in "kv":
+                kv[n + "_scale"][pp, :, off] = byte
+                kv[n + "_pages"][pp, :, off] = code
+    c = sx.KV8(to_dev(kv))
+    after = c.sx_attention(q.to(DEV), drafted, mask.to(DEV), kernel=kernel)
+    c.check_status()
+    assert torch.equal(before, after) and bool((after[2, 0] == 0).sum() == 0)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_a_query_that_is_not_finite_spoils_its_own_row_only(kernel):
+    kv = ref.make_cache(2, 2, 128, 64, [300, 70], 3, seed=26, groups=[0, 2], prefix=[64])
+    q = ref.make_q(2, 3, 8, 128, 27)
+    want, bound = ref.attention(kv, q, 3, None, 128 ** -0.5)
+    q[0, 1, 2, 5], q[1, 0, 7, 100] = math.nan, math.inf
+    c = sx.KV8(to_dev(kv))
+    got = c.sx_attention(q.to(DEV), 3, kernel=kernel).double().cpu().numpy()
+    c.check_status()
+    assert np.isnan(got[0, 1, 2]).all() and np.isnan(got[1, 0, 7]).all()
+    got[0, 1, 2], got[1, 0, 7] = want[0, 1, 2], want[1, 0, 7]
+    assert (np.abs(got - want) <= bound).all()
+
+
+@pytest.mark.parametrize("B,groups", [(300, None), (300, 7), (700, 3), (511, 511), (1023, 1)])
+def test_many_sequences(B, groups):
+    """More sequences than the tensor-memory kernel plans for fall to the other one; every group a sequence; the limit."""
+    g = torch.Generator().manual_seed(B)
+    start = None if groups is None else [B * i // groups for i in range(groups + 1)]
+    prefix = None if groups is None else [int(v) for v in torch.randint(0, 40, (groups,), generator=g)]
+    own = torch.randint(0, 60, (B,), generator=g).tolist()
+    of = None if groups is None else [next(i for i in range(groups) if b < start[i + 1]) for b in range(B)]
+    lens = own if groups is None else [n + prefix[of[b]] for b, n in enumerate(own)]
+    kv = ref.make_cache(B, 1, 128, 32, lens, 1, seed=B, groups=start, prefix=prefix)
+    check(kv, ref.make_q(B, 1, 2, 128, 28), 1, None)
+
+
+def test_a_graph_keeps_its_workspace():
+    """A larger call after a capture gets a workspace of its own; the replay goes on using the one it was captured with."""
+    kv = ref.make_cache(2, 2, 128, 64, [900, 400], 8, seed=29)
+    c = sx.KV8(to_dev(kv))
+    q1, q8 = ref.make_q(2, 1, 8, 128, 30), ref.make_q(2, 8, 64, 128, 31)
+    d1, out = q1.to(DEV), torch.empty(2, 1, 8, 128, dtype=torch.bfloat16, device=DEV)
+    want = c.sx_attention(d1, 8).clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.sx_attention(d1, 8, out=out)
+    for _ in range(3):
+        c.sx_attention(q8.to(DEV), 8)
+        fill = [torch.full((1 << 24,), 0x7f, dtype=torch.uint8, device=DEV) for _ in range(8)]
+        out.zero_()
+        graph.replay()
+        assert torch.equal(out, want)
+        assert all(int(f.min()) == 0x7f and int(f.max()) == 0x7f for f in fill)
+    c.check_status()
+
+
 def test_page_and_group_faults_are_reported():
     kv = ref.make_cache(3, 2, 128, 64, [200, 100, 70], 1, seed=6)
     q = ref.make_q(3, 1, 8, 128, 12)
