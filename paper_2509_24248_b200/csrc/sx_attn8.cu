@@ -538,6 +538,7 @@ sx_status sx_launch_attn8(SxA8 p, int kernel, char *ws, int sm_count, cudaStream
     ls.qt = tc ? tc_tile(q, (size_t)p.B * p.rows * p.nq) : q <= 8 ? 8 : 16;
     ls.runs = tc ? sm_count : split_runs(sm_count);
     ls.min_per = tc ? 1 : 4;
+    ls.spread = sm_count;
     ls.qt_shift = log2i(ls.qt);
     ls.step_shift = log2i(ls.step);
     ls.parts_shift = tc ? log2i(128 / ls.qt) : 0;
