@@ -473,9 +473,9 @@ static sx_status split_list(SxA8 &p, int sm_count, cudaStream_t st) {
 }
 
 static size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
-// Queries per tile of the tensor-memory kernel for at most `q` per KV head: with 32 (64) the softmax is spread over four
-// (two) copies of them, which leave a partial result each; bounded, so that the workspace of a large batch is not four
-// times what it needs.
+// Queries per tile of the tensor-memory kernel for `q` per KV head: with 32 (64) the softmax is spread over four
+// (two) copies of them, which leave a partial result each (eight prefixes of 4096 slots under 32 queries: 67 us, in a tile
+// of 128 for the same 32 71 us); bounded, so that the workspace of a large batch is not four times what it needs.
 #define A8_COPY_ROWS 65536
 static int tc_tile(int q, size_t all) {
   const int qt = q <= 32 ? 32 : q <= 64 ? 64 : 128;
@@ -504,7 +504,8 @@ static sx_status launch_merge(const SxA8 &p, cudaStream_t st) {
   SX_TRY(sx_rc(cudaFuncSetAttribute(sx_attn8_merge_kernel<D, W>, cudaFuncAttributePreferredSharedMemoryCarveout, 100)));
   return sx_rc(sx_launch(sx_attn8_merge_kernel<D, W>, dim3((unsigned)((rows + per - 1) / per)), dim3(A8_MERGE_THREADS), 0, st, p));
 }
-// Warps per output row: eight while that fills the SMs once (latency of a chain of partial results), fewer beyond
+// Warps per output row: as many as fill the SMs once (a row's partial results are a chain of loads: the merge of 32 x 32
+// rows takes 3 us with one warp each, 1.6 us with four), fewer where rows alone fill them
 template <int D>
 static sx_status merge(const SxA8 &p, int sm_count, cudaStream_t st) {
   const int64_t rows = (int64_t)p.B * p.rows * p.nq, slots = 8ll * sm_count;       // CTAs of 256 threads at a time
@@ -527,9 +528,16 @@ sx_status sx_launch_attn8(SxA8 p, int kernel, char *ws, int sm_count, cudaStream
   place(p.own, p.B);
   if (p.n_groups > 0) place(p.pre, p.n_groups);
   const int own_q = p.rows * p.G;
-  // a group has at most this many queries per KV head (the host does not know the groups)
-  const int pre_q = p.n_groups > 0 ? (p.B - p.n_groups + 1 > 1 ? p.B - p.n_groups + 1 : 2) * own_q : 0;
-  // Which kernel takes a list of `q` queries per KV head (at most, for the prefix).
+  // The host knows how many groups there are, not which; it takes them to be alike.  (A larger one becomes several tiles: a
+  // group of 29 sequences among four of 32 takes 48 us instead of 43 us with the tile that it needs, but sixteen pairs take
+  // 50 us instead of 87 us with the tile that one large group among them would need; prefixes of 4096 slots.)
+  const int pre_q = p.n_groups > 0 ? (p.B + p.n_groups - 1) / p.n_groups * own_q : 0;
+  // Which kernel takes a list of `q` queries per KV head.  The warp-level kernel reads a unit's slots once for every 16
+  // queries and is bound by bytes up to there; the tensor-memory kernel's time per block of slots hardly depends on the queries.
+  // Up to 16 queries the first is faster (one row of 4 heads over 32 x 4100 slots 57 against 107 us, two rows of 8 heads
+  // over 8 x 16384 slots 63 against 93 us, one of 4096 slots 15 against 27 us), beyond 16 the second (32 queries, 4 x 32768
+  // slots: 105 against 146 us; a prefix of 16384 slots under 128 queries: 51 against 92 us; 4 prefixes under 128: 95
+  // against 213 us).
   auto choose = [&](SxA8List &ls, int q, bool &tc) -> sx_status {
     const bool can = sx_attn8_tc_supported(p);
     if (kernel == SX_ATTN_TC && !can) return SX_ERR_UNSUPPORTED;

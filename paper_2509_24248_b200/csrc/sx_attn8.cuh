@@ -1,4 +1,4 @@
-// Shared pieces of the decode attention over the 8-bit paged cache (sx_attn8.cu, sx_attn8_tc.cu, sx_attn8_merge):
+// Shared pieces of the decode attention over the 8-bit paged cache (sx_attn8.cu, sx_attn8_tc.cu):
 // parameters, the list of work and the addressing of partial results.
 //
 // Work.  A "unit" is a set of query rows that read the same slots: in the OWN list unit b is sequence b with its
@@ -93,7 +93,8 @@ __host__ __device__ inline size_t a8_plan_bytes(int B, int n_groups) {
 // tiles of a unit with nq queries; steps of a run
 __device__ __forceinline__ int a8_tiles(int nq, int qt_shift) { return (nq + (1 << qt_shift) - 1) >> qt_shift; }
 // (at least min_per, what a run has in flight at once, as long as that leaves a run for every SM: three sequences of 129
-// slots take 9.4 us with two steps per run, 11.9 us with four; one of 4096 slots 17.2 us and 15.2 us)
+// slots take 7.8 us with a step per run, 9.4 us with two and 11.9 us with four; one of 4096 slots 17.2 us with two, 15.2 us
+// with four)
 __device__ __forceinline__ int a8_per(int total, const SxA8List &ls) {
   const int least = min(ls.min_per, (int)((uint32_t)(total + ls.spread - 1) / (uint32_t)ls.spread));
   return max(max(least, 1), (int)((uint32_t)(total + ls.runs - 1) / (uint32_t)ls.runs));

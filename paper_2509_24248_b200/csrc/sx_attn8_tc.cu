@@ -41,16 +41,14 @@
 
 #define T8_THREADS 640
 #define T8_BLK (128 * 128)               // bytes of the codes of a block
-#define T8_NONE (-1e30f)                 // reference before the first visible score
+#define T8_NONE (-3e38f)                 // reference before the first visible score
 // Weights are bf16, sums fp32: their precision does not depend on where the reference lies, so it moves only where the
 // range of numbers asks for it.
 #define T8_SLACK 30.f
-#ifndef T8_NK
 #define T8_NK 4                          // ring slots of 16 KB for the codes of K,
 #define T8_NV 3                          // of V
 #define T8_NW 2                          // bf16 copies (32 KB) of V blocks
 #define T8_NC 4                          // entries of K scales; of query factors
-#endif
 #define T8_Q_BYTES T8_BLK                // one of the two parts
 #define T8_O_COL 256                     // tensor memory: scores / weights of the groups, then their outputs
 #define T8_OFF_W (2 * T8_Q_BYTES)

@@ -282,6 +282,47 @@ def test_slots_that_nobody_sees_can_hold_anything(kernel, byte, code):
 
 
 @pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("groups", [None, [0, 2]])
+@pytest.mark.parametrize("power", [10, 55, 64])
+def test_scores_that_are_all_very_low(kernel, groups, power):
+    """Every key the same, every score -2^(57 + power): whatever that is, the weights are equal and the output is the mean
+    of the values (equal value scales: a power of two beside such a score is lost)."""
+    kv = ref.make_cache(2, 1, 128, 64, [300, 200], 2, seed=5, groups=groups, prefix=[150] if groups else None)
+    kv["k_pages"].fill_(0xb8)                                   # -1
+    kv["k_scale"].fill_(127 + power)
+    kv["v_scale"].fill_(127)
+    got = check_mean(kv, torch.full((2, 3, 4, 128), 2.0 ** 50, dtype=torch.bfloat16), kernel)
+    assert (got != 0).any()
+
+
+def check_mean(kv, q, kernel):
+    c = sx.KV8(to_dev(kv))
+    got = c.sx_attention(q.to(DEV), 2, scale=1.0, kernel=kernel).double().cpu().numpy()
+    c.check_status()
+    for b in range(q.shape[0]):
+        pos = np.arange(int(kv["cache_len"][b]) + 2)
+        pp = kv["page_table"][b].numpy()[pos // 64].astype(np.int64)
+        V = ref.dequantise(kv["v_pages"][pp, :, pos % 64], kv["v_scale"][pp, :, pos % 64])[:, 0]
+        # fp32 sums of a few hundred terms, one division, a bf16 result
+        far = len(pos) * 2.0 ** -23 * np.abs(V).mean(0)
+        want = V.mean(0)
+        assert (np.abs(got[b] - want) <= far + 2.0 ** -8 * (np.abs(want) + far)).all()
+    return got
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("groups,mine", [([0, 9, 10, 11, 12], 12), ([0, 1, 1, 40], 40), ([0, 0, 0, 33], 33)])
+def test_groups_that_are_not_alike(kernel, groups, mine):
+    """One group with most of the sequences (more queries than the tile that an average group would need), empty groups."""
+    prefix = [200] + [70] * (len(groups) - 2)
+    of = [max(g for g in range(len(prefix)) if groups[g] <= b and groups[g + 1] > b) for b in range(mine)]
+    lens = [prefix[g] + (b * 7) % 40 for b, g in enumerate(of)]
+    kv = ref.make_cache(mine, 1, 128, 32, lens, 1, seed=mine, groups=groups, prefix=prefix, fill=0xff)
+    check(kv, ref.make_q(mine, 1, 4, 128, 12), 1, None, kernel=kernel)
+    check(kv, ref.make_q(mine, 1, 4, 128, 12), 1, None)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
 def test_a_query_that_is_not_finite_spoils_its_own_row_only(kernel):
     kv = ref.make_cache(2, 2, 128, 64, [300, 70], 3, seed=26, groups=[0, 2], prefix=[64])
     q = ref.make_q(2, 3, 8, 128, 27)
