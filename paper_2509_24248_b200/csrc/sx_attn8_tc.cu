@@ -105,6 +105,11 @@ __device__ __forceinline__ bool t8_elect() {
       : "=r"(one));
   return one != 0;
 }
+__device__ __forceinline__ float t8_max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
 // two fp32 operations in one instruction
 typedef unsigned long long f32x2;
 __device__ __forceinline__ f32x2 t8_pack(float a, float b) {
@@ -462,10 +467,16 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       ks_sh[e * 128 + tid] = kbyte == 255 || vbyte == 255 ? __int_as_float(0x7fffffff) : a8_pow2(kbyte);
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&cfull[e]));
-      uint4 x[8];
+      // chunks 2c and 2c + 1 of the half; the lanes of the second half go the other way round, so that eight lanes of one
+      // row fall into eight different groups of banks
+      const int hi = c >> 2, ka = ((2 * c) & 7) + hi, kb = ((2 * c) & 7) + 1 - hi;
+      uint2 xa[8], xb[8];
       const uint8_t *src = ringV + slot * T8_BLK + r0 * 128 + ((c ^ (r0 & 7)) << 4);
 #pragma unroll
-      for (int it = 0; it < 8; ++it) x[it] = *reinterpret_cast<const uint4 *>(src + it * 2048);
+      for (int it = 0; it < 8; ++it) {
+        xa[it] = *reinterpret_cast<const uint2 *>(src + it * 2048 + hi * 8);
+        xb[it] = *reinterpret_cast<const uint2 *>(src + it * 2048 + 8 - hi * 8);
+      }
       uint32_t f[8];                                        // 2^(120 + e)
       int top = 0;
 #pragma unroll
@@ -478,21 +489,17 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       // hold any byte), which must not meet a weight of 0.
       const bool rare = __any_sync(0xffffffffu, top > 134);
       if (li >= NW && !t8_wait(&wempty[team], (uint32_t)(li / NW - 1) & 1u, abort_flag, wait_limit, lane)) break;
-      // chunks 2c and 2c + 1 of the half; the lanes of the second half go the other way round, so that eight lanes of one
-      // row fall into eight different groups of banks
-      const int hi = c >> 2, ka = ((2 * c) & 7) + hi, kb = ((2 * c) & 7) + 1 - hi;
       uint8_t *dst = sW + team * 2 * T8_BLK + hi * T8_BLK + r0 * 128;
       uint8_t *da = dst + ((ka ^ (r0 & 7)) << 4), *db = dst + ((kb ^ (r0 & 7)) << 4);
 #pragma unroll
       for (int it = 0; it < 8; ++it) {
-        uint32_t o[8];
-        t8_widen4(x[it].x, f[it], o[0], o[1]);
-        t8_widen4(x[it].y, f[it], o[2], o[3]);
-        t8_widen4(x[it].z, f[it], o[4], o[5]);
-        t8_widen4(x[it].w, f[it], o[6], o[7]);
-        const uint4 a = make_uint4(o[0], o[1], o[2], o[3]), b = make_uint4(o[4], o[5], o[6], o[7]);
-        *reinterpret_cast<uint4 *>(da + it * 2048) = hi ? b : a;
-        *reinterpret_cast<uint4 *>(db + it * 2048) = hi ? a : b;
+        uint4 a, b;
+        t8_widen4(xa[it].x, f[it], a.x, a.y);
+        t8_widen4(xa[it].y, f[it], a.z, a.w);
+        t8_widen4(xb[it].x, f[it], b.x, b.y);
+        t8_widen4(xb[it].y, f[it], b.z, b.w);
+        *reinterpret_cast<uint4 *>(da + it * 2048) = a;
+        *reinterpret_cast<uint4 *>(db + it * 2048) = b;
       }
       if (rare) {
 #pragma unroll 1
@@ -573,7 +580,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         }
         float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int j = 0; j < CH; ++j) tops[j & 3] = fmaxf(tops[j & 3], t[j]);
+        for (int j = 0; j < CH; j += 2) tops[(j >> 1) & 3] = t8_max3(tops[(j >> 1) & 3], t[j], t[j + 1]);
         const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
         if (__any_sync(0xffffffffu, top > (none ? T8_NONE : T8_SLACK))) {
           // ---- the reference moves to the largest (from none: in a segment's first block; else rarely); what has been summed
