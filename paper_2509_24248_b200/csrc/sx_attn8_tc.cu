@@ -27,6 +27,11 @@
 // same, and the softmax of 32 queries, one warp's work before, is spread over four.  At the end of a segment the groups'
 // results, which lie in the same rows of tensor memory, become one; every copy leaves its own.
 //
+// Measured: 2700 to 3100 cycles per block with 128 queries (the softmax warps: two thirds of the issue slots, half of the
+// exponential unit), 2550 with 32 (the chain first product, softmax, second product, beside the widening of V), 5 us to the
+// first block and 3 to 5 us for the end of a segment.  4 x 32768 slots of 8 heads under 32 queries: 102 us with the merge,
+// 2.6 TB/s; a prefix of 30001 slots under 256 queries, own slots and merge: 97 us, 340 TFLOP/s.
+//
 // Warps: 0 K producer, 1 issuer of the first product (owns TMEM), 2 V producer, 3 issuer of the second, 4-11 softmax,
 // 12-19 widen V, lay out the scales of K and load Q.  Every mbarrier wait is bounded (sx_tc_ptx.cuh).
 #include <cuda.h>
