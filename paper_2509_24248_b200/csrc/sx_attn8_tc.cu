@@ -396,7 +396,6 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     // Two teams of four warps take the blocks in turn, each with its copy of V; the queries of every segment are loaded by
     // both, half of the rows each (a team alone, row after row, kept a segment's first block waiting for 4 us)
     const int team = (warp - 12) >> 2, tid = threadIdx.x & 127, c = tid & 7, r0 = tid >> 3;
-    static_assert(NW == 2, "a copy of V per team");
     A8Seg s = a8_seek<PRE>(p, pl, ls, slab, g0);
     int item = -1;
     bool ok = true;
@@ -472,15 +471,15 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       ks_sh[e * 128 + tid] = kbyte == 255 || vbyte == 255 ? __int_as_float(0x7fffffff) : a8_pow2(kbyte);
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&cfull[e]));
-      // chunks 2c and 2c + 1 of the half; the lanes of the second half go the other way round, so that eight lanes of one
-      // row fall into eight different groups of banks
-      const int hi = c >> 2, ka = ((2 * c) & 7) + hi, kb = ((2 * c) & 7) + 1 - hi;
+      // Chunks 2c and 2c + 1 of the half; the lanes of the second half go the other way round, so that the eight lanes of a row
+      // write into eight different groups of banks, and so do those of odd rows, so that two rows read from different ones.
+      const int hi = c >> 2, turn = hi ^ (r0 & 1), ka = ((2 * c) & 7) + turn, kb = ((2 * c) & 7) + 1 - turn;
       uint2 xa[8], xb[8];
       const uint8_t *src = ringV + slot * T8_BLK + r0 * 128 + ((c ^ (r0 & 7)) << 4);
 #pragma unroll
       for (int it = 0; it < 8; ++it) {
-        xa[it] = *reinterpret_cast<const uint2 *>(src + it * 2048 + hi * 8);
-        xb[it] = *reinterpret_cast<const uint2 *>(src + it * 2048 + 8 - hi * 8);
+        xa[it] = *reinterpret_cast<const uint2 *>(src + it * 2048 + turn * 8);
+        xb[it] = *reinterpret_cast<const uint2 *>(src + it * 2048 + 8 - turn * 8);
       }
       uint32_t f[8];                                        // 2^(120 + e)
       int top = 0;
@@ -493,8 +492,11 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       // Rows whose 2^(120 + e) is out of range take two steps.  They alone can end as infinity (a slot that nobody may see can
       // hold any byte), which must not meet a weight of 0.
       const bool rare = __any_sync(0xffffffffu, top > 134);
-      if (li >= NW && !t8_wait(&wempty[team], (uint32_t)(li / NW - 1) & 1u, abort_flag, wait_limit, lane)) break;
-      uint8_t *dst = sW + team * 2 * T8_BLK + hi * T8_BLK + r0 * 128;
+      __syncwarp();
+      if (!rare && lane == 0) mbar_arrive(smem_u32(&vempty[slot]));      // all of it is in registers
+      const int wb = li % NW;
+      if (li >= NW && !t8_wait(&wempty[wb], (uint32_t)(li / NW - 1) & 1u, abort_flag, wait_limit, lane)) break;
+      uint8_t *dst = sW + wb * 2 * T8_BLK + hi * T8_BLK + r0 * 128;
       uint8_t *da = dst + ((ka ^ (r0 & 7)) << 4), *db = dst + ((kb ^ (r0 & 7)) << 4);
 #pragma unroll
       for (int it = 0; it < 8; ++it) {
@@ -523,7 +525,8 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       }
       fence_async_smem();
       __syncwarp();
-      if (lane == 0) { mbar_arrive(smem_u32(&vempty[slot])); mbar_arrive(smem_u32(&wfull[team])); }
+      if (rare && lane == 0) mbar_arrive(smem_u32(&vempty[slot]));
+      if (lane == 0) mbar_arrive(smem_u32(&wfull[wb]));
     }
   } else {
     // ---- softmax: group g takes blocks g, g + 2, ...; a thread owns query (TMEM lane) i --------------------------------
