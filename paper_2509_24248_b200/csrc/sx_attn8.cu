@@ -540,7 +540,7 @@ sx_status sx_launch_attn8(SxA8 p, int kernel, char *ws, int sm_count, cudaStream
   // queries and is bound by bytes up to there; the tensor-memory kernel's time per block of slots hardly depends on the queries.
   // Up to 16 queries the first is faster (one row of 4 heads over 32 x 4100 slots 57 against 107 us, two rows of 8 heads
   // over 8 x 16384 slots 63 against 93 us, one of 4096 slots 15 against 27 us), beyond 16 the second (32 queries, 4 x 32768
-  // slots: 105 against 146 us; a prefix of 16384 slots under 128 queries: 51 against 92 us; 4 prefixes under 128: 95
+  // slots: 98 against 146 us; a prefix of 16384 slots under 128 queries: 50 against 92 us; 4 prefixes under 128: 93
   // against 213 us).
   auto choose = [&](SxA8List &ls, int q, bool &tc) -> sx_status {
     const bool can = sx_attn8_tc_supported(p);

@@ -28,9 +28,9 @@
 // results, which lie in the same rows of tensor memory, become one; every copy leaves its own.
 //
 // Measured: 2700 to 3100 cycles per block with 128 queries (the softmax warps: two thirds of the issue slots, half of the
-// exponential unit), 2550 with 32 (the chain first product, softmax, second product, beside the widening of V), 5 us to the
-// first block and 3 to 5 us for the end of a segment.  4 x 32768 slots of 8 heads under 32 queries: 102 us with the merge,
-// 2.6 TB/s; a prefix of 30001 slots under 256 queries, own slots and merge: 97 us, 340 TFLOP/s.
+// exponential unit), 2450 with 32 (the chain first product, softmax, second product, beside the widening of V), 5 us to the
+// first block and 3 to 5 us for the end of a segment.  4 x 32768 slots of 8 heads under 32 queries: 98 us with the merge,
+// 2.8 TB/s; a prefix of 30001 slots under 256 queries, own slots and merge: 95 us, 350 TFLOP/s.
 //
 // Warps: 0 K producer, 1 issuer of the first product (owns TMEM), 2 V producer, 3 issuer of the second, 4-11 softmax,
 // 12-19 widen V, lay out the scales of K and load Q.  Every mbarrier wait is bounded (sx_tc_ptx.cuh).
@@ -481,7 +481,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         xa[it] = *reinterpret_cast<const uint2 *>(src + it * 2048 + turn * 8);
         xb[it] = *reinterpret_cast<const uint2 *>(src + it * 2048 + 8 - turn * 8);
       }
-      uint32_t f[8];                                        // 2^(120 + e)
+      uint32_t f[8];                                        // 2^(120 + e); one row per lane and a shuffle per row: 102 against 98 us
       int top = 0;
 #pragma unroll
       for (int it = 0; it < 8; ++it) {
