@@ -300,7 +300,8 @@ class KV8:
     ``v_scale`` (uint8 ``[num_pages, n_kv, page]``), ``page_table`` (int32 ``[B, max_pages]``), ``cache_len`` (int32
     ``[B]``) and, for sequences that share a prefix, ``group_start`` (int32 ``[n_groups + 1]``) with ``prefix_len``
     (int32 ``[n_groups]``).  The tensors are borrowed; what they hold may change between calls.  Work goes to the
-    current stream of their device.  The object owns the attention's workspace: use one per stream."""
+    current stream of their device.  The object owns the attention's workspace: use one per stream, and one per captured
+    graph that may run beside others."""
 
     def __init__(self, kv: Dict[str, torch.Tensor]):
         self.lib = load_library()
