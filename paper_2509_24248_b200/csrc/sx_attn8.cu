@@ -11,7 +11,11 @@
 //     O^T[d][q] += sum_slot vc[slot][d] P[slot][q]     fp16 x fp16, m16n8k16; e4m3 codes are exact in fp16
 // K's fragments are the codes as ldmatrix delivers them.  For V ldmatrix.trans delivers [slot][pair of d]; one byte permute
 // splits the pair into two rows of the product, whose order is undone where O is stored, and cvt.f16x2.e4m3x2
-// widens them.  The scale of K is a factor of the slot's scores, that of V is added to the score.
+// widens them.  The scale of K is a factor of the slot's scores, that of V is added to the score - but a row of V whose
+// codes are all zero has weight and gives nothing, so it must not lift the reference that the others' fp16 weights are
+// relative to (a sink whose value is zero, 10 nats above the rest, left 5 % of them).  Where such a row would, it is held
+// back by A8_ZERO, and what exceeds the range of a weight goes into the sum alone, which is fp32.  Rows are looked at only
+// where a reference would move, so the stream pays nothing for it.
 //
 // Bound by bytes: 12 warps per SM with 12 KB each on their way.  32 sequences of about 4100 slots, 8 heads of 128, one row
 // of four queries per head: 263 MB in 53 us of the kernel, 5.0 TB/s with its start and the spread of its ends, about 7 TB/s
@@ -25,6 +29,10 @@
 #include "sx_launch.cuh"
 
 #define A8S_WARPS 4
+// How far below its score (in powers of two) a row of zeros puts the reference: the others keep their bits unless they lie
+// further below it than this and A8_SLACK together, and its share of the sum, 2^(A8_ZERO + A8_SLACK) at most, leaves room for
+// 2^23 such rows in fp32.
+#define A8_ZERO 90.f
 
 __device__ __forceinline__ float a8_ex2(float x) {
   float y;
@@ -85,6 +93,23 @@ __device__ __forceinline__ void a8_ldm4(uint32_t addr, uint32_t (&r)[4]) {
 __device__ __forceinline__ void a8_ldm4t(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// Rows of a staged block of 16 that hold nothing but zeros of either sign, as bits; the first codes of a row nearly always
+// answer it
+template <int D>
+__device__ __forceinline__ uint32_t a8_zero_rows(const uint8_t *block, int lane) {
+  const uint32_t *row = reinterpret_cast<const uint32_t *>(block + (lane & 15) * D);
+  uint32_t zero = __ballot_sync(0xffffffffu, (row[0] & 0x7f7f7f7fu) == 0);
+  if (zero) {
+    uint32_t any = 0;
+#pragma unroll 1
+    for (int i = 0; i < D / 4; i += 4) {
+      const uint4 x = *reinterpret_cast<const uint4 *>(row + i);
+      any |= x.x | x.y | x.z | x.w;
+    }
+    zero = __ballot_sync(0xffffffffu, (any & 0x7f7f7f7fu) == 0);
+  }
+  return zero;
 }
 // 16-byte chunk position of a staged row (D bytes), so that eight rows of an ldmatrix phase fall into different banks
 template <int D>
@@ -286,11 +311,14 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, (A8S<D, NQT>::CTAS)) sx_attn8_
       for (int k = 0; k < 4; ++k) up |= S[i][k] > M[i][k & 1] + A8_SLACK;
     if (__any_sync(0xffffffffu, up)) {
       // a reference moves: it only has to keep the weights in range, so this is rare behind the first steps
+      const uint32_t zero = a8_zero_rows<D>(a8_smem + warp * C::WARP_BYTES + st * 2 * BLK + BLK, lane);
+      const bool z[2] = {((zero >> g) & 1u) != 0, ((zero >> (g + 8)) & 1u) != 0};
+      const float back[2] = {z[0] ? ev[0] + A8_ZERO : 0.f, z[1] ? ev[1] + A8_ZERO : 0.f};
 #pragma unroll
       for (int i = 0; i < NQT; ++i)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          float bm = fmaxf(S[i][k], S[i][k + 2]);
+          float bm = fmaxf(S[i][k] - back[0], S[i][k + 2] - back[1]);
 #pragma unroll
           for (int o = 4; o < 32; o <<= 1) bm = fmaxf(bm, __shfl_xor_sync(0xffffffffu, bm, o));
           if (bm > M[i][k] + A8_SLACK) {
@@ -301,6 +329,16 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, (A8S<D, NQT>::CTAS)) sx_attn8_
             for (int c = 0; c < CPR; ++c) { O[i][c][k] *= w; O[i][c][k + 2] *= w; }
           }
         }
+      if (zero) {
+#pragma unroll
+        for (int i = 0; i < NQT; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (z[k >> 1] && S[i][k] > M[i][k & 1] + A8_SLACK) {
+              L[i][k & 1] += a8_ex2(S[i][k] - ev[k >> 1] - M[i][k & 1]);
+              S[i][k] = -INFINITY;
+            }
+      }
     }
     // ---- weights (below 2^14), their sums without the value scale, P^T as fp16 -----------------------------------
     uint32_t pb[NQT][2];

@@ -279,9 +279,11 @@ __device__ __forceinline__ uint32_t a8_visible(const A8Seg &s, uint64_t mask, in
   return (uint32_t)v;
 }
 
-// running softmax in base 2 over s' = s + e, where 2^e is the scale of the slot's value row: the weight of a code row
-// is 2^(s' - ref) and the weight of the slot itself 2^(s' - ref - e).  So the value scales cost no multiplication
-// of V, and what is rounded (the weight) is the part that meets the codes, relative to the largest contribution.
+// The warp-level kernel's running softmax in base 2 is over s' = s + e, where 2^e is the scale of the slot's value row: the
+// weight of a code row is 2^(s' - ref) and the weight of the slot itself 2^(s' - ref - e).  So the value scales cost no
+// multiplication of V, and what is rounded (the weight) is the part that meets the codes, relative to the largest
+// contribution: the largest code of a row is above 224, unless its scale is the smallest there is or the row is all
+// zeros, which the kernel looks for.
 __device__ __forceinline__ float a8_pow2(int byte) { return __uint_as_float((uint32_t)byte << 23); }        // 2^(byte - 127)
 __device__ __forceinline__ float a8_pow2_inv(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
 __device__ __forceinline__ float a8_exponent(int byte) {       // 255 marks a row with a value that is not finite

@@ -1,0 +1,132 @@
+"""Rows and calls at the edges of the 8-bit cache: value rows of zeros, queries with an outlier channel, values at both ends
+of the format, pages that do not exist, members without slots of their own, calls from two threads."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2509_24248_b200 import binding as sx
+from tests import kv8_ref as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+KERNELS = [sx.ATTN_SPLIT, sx.ATTN_TC]
+WEIGHT = {sx.ATTN_SPLIT: 2.0 ** -11, sx.ATTN_TC: 2.0 ** -8, sx.ATTN_AUTO: 2.0 ** -8}    # half a step of a weight's type
+
+
+def to_dev(kv):
+    return {n: t.to(DEV) for n, t in kv.items()}
+
+
+def near(got, want, bound):
+    far = np.abs(got - want) / bound                              # NaN where either is
+    worst = np.nan_to_num(far, nan=np.inf)
+    assert worst.max() <= 1.0, f"{worst.max():.3g} x the bound at {np.unravel_index(worst.argmax(), far.shape)}: {got.flat[worst.argmax()]}, {want.flat[worst.argmax()]}"
+
+
+def one_sequence(k, v, page=64):
+    """A cache of one sequence (batch 1) that holds the rows ``k`` / ``v`` [n, n_kv, d], page behind page."""
+    n, n_kv, d = k.shape
+    M = -(-n // page)
+    kv = {"page_table": torch.arange(M, dtype=torch.int32).view(1, M), "cache_len": torch.tensor([n], dtype=torch.int32)}
+    for name, t in (("k", k), ("v", v)):
+        codes, byte = ref.quantise(t.to(torch.bfloat16))
+        full = torch.zeros(M * page, n_kv, d, dtype=torch.uint8)
+        full[:n] = codes
+        fb = torch.full((M * page, n_kv), 127, dtype=torch.uint8)
+        fb[:n] = byte
+        kv[name + "_pages"] = full.view(M, page, n_kv, d).permute(0, 2, 1, 3).contiguous()
+        kv[name + "_scale"] = fb.view(M, page, n_kv).permute(0, 2, 1).contiguous()
+    return kv
+
+
+def many(kv, B, group=None):
+    """The same sequence B times, in the same pages; ``group``: its first slots as a shared prefix of all of them."""
+    out = {n: t for n, t in kv.items() if n not in ("page_table", "cache_len")}
+    out["page_table"], out["cache_len"] = kv["page_table"].expand(B, -1).contiguous(), kv["cache_len"].expand(B).contiguous()
+    if group is not None:
+        out["group_start"], out["prefix_len"] = torch.tensor([0, B], dtype=torch.int32), torch.tensor([group], dtype=torch.int32)
+    return out
+
+
+def attend_like_one(kv, B, q, kernel, group=None, drafted=0, mask=None, scale=None):
+    """B equal sequences with equal queries ``q`` [1, rows, nq, d]: every one of them against the reference of one."""
+    scale = q.shape[-1] ** -0.5 if scale is None else scale
+    c = sx.KV8(to_dev(many(kv, B, group)))
+    got = c.sx_attention(q.expand(B, -1, -1, -1).contiguous().to(DEV), drafted,
+                         None if mask is None else mask.expand(B, -1).contiguous().to(DEV), scale, kernel=kernel)
+    c.check_status()
+    want, bound = ref.attention(kv, q, drafted, mask, scale, WEIGHT[kernel])
+    got = got.double().cpu().numpy()
+    for b in range(B):
+        near(got[b:b + 1], want, bound)
+    return got
+
+
+# ---- value rows of zeros ------------------------------------------------------------------------------------------
+def with_gap(n, n_kv, G, d, at, gap, size, seed, zero=True):
+    """Keys whose scores are small, but for slots ``at``, which lie ``gap`` nats higher and whose value rows are zeros (or
+    not); values of magnitude ``size``."""
+    g = torch.Generator().manual_seed(seed)
+    q = torch.ones(1, 1, n_kv * G, d) * torch.where(torch.rand(d, generator=g) < 0.5, -1.0, 1.0)
+    k = torch.randn(n, n_kv, d, generator=g) * 0.3
+    v = torch.randn(n, n_kv, d, generator=g) * size
+    for i, s in enumerate(at):
+        k[s] = q[0, 0, 0] * (gap - i) / d ** 0.5                    # scale q . k = gap - i
+        if zero:
+            v[s] = 0.0
+    return q.to(torch.bfloat16), k, v
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("n,B", [(256, 222), (4096, 40)])
+@pytest.mark.parametrize("size", [0.02, 2.0 ** -18])
+@pytest.mark.parametrize("gap", [0, 8, 10, 12, 30, 80])
+def test_a_value_row_of_zeros(kernel, n, B, size, gap):
+    """A sink whose value is zero takes weight and gives nothing; the others keep their precision (runs of hundreds of
+    slots: as many equal sequences as that takes)."""
+    q, k, v = with_gap(n, 8, 1, 128, [0], gap, size, n + gap)
+    attend_like_one(one_sequence(k, v), B, q, kernel)
+
+
+@pytest.mark.parametrize("kernel", [sx.ATTN_SPLIT])
+@pytest.mark.parametrize("d,G,n_kv", [(64, 1, 2), (64, 8, 2), (128, 2, 4), (128, 16, 1)])
+@pytest.mark.parametrize("at", [[0], [3, 19, 20, 70], [255], list(range(64)), list(range(16, 256))])
+@pytest.mark.parametrize("gap", [6, 13, 60])
+def test_several_value_rows_of_zeros(kernel, d, G, n_kv, at, gap):
+    q, k, v = with_gap(256, n_kv, G, d, at, gap, 1.0, gap + len(at))
+    v[:, :, ::2] *= -1.0                                            # zero rows hold both zeros
+    attend_like_one(one_sequence(k, v), 97, q, kernel)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("prefix", [100, 256])
+@pytest.mark.parametrize("gap", [11, 40])
+def test_a_value_row_of_zeros_in_a_shared_prefix(kernel, prefix, gap):
+    q, k, v = with_gap(300, 2, 4, 128, [0, 130, 299], gap, 0.02, 5)
+    attend_like_one(one_sequence(k, v), 40, q, kernel, group=prefix)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_drafted_value_rows_of_zeros(kernel):
+    """Some rows see the drafted slot whose value is zero and whose score is high, others do not."""
+    q, k, v = with_gap(70, 2, 2, 128, [66, 69], 14, 0.02, 6)
+    kv = one_sequence(k, v)
+    kv["cache_len"] -= 5                                            # slots 65 .. 69 are drafted
+    mask = torch.tensor([[0b00000, 0b00010, 0b10001, 0b11111]])
+    attend_like_one(kv, 33, q.expand(1, 4, -1, -1), kernel, drafted=5, mask=mask)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_nothing_but_value_rows_of_zeros(kernel):
+    q, k, v = with_gap(200, 2, 2, 128, list(range(200)), 100, 1.0, 7)
+    got = attend_like_one(one_sequence(k, v), 19, q, kernel)
+    assert (got == 0).all()
+
+
+@pytest.mark.parametrize("size", [2.0 ** 60, 2.0 ** 100])
+@pytest.mark.parametrize("gap", [0, 12, 40])
+def test_a_value_row_of_zeros_beside_huge_ones(size, gap):
+    q, k, v = with_gap(256, 2, 4, 128, [0, 200], gap, size, gap)
+    attend_like_one(one_sequence(k, v), 97, q, sx.ATTN_SPLIT)
