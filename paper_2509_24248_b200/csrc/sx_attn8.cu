@@ -7,7 +7,7 @@
 // The warp-level kernel: a warp streams its run of 16-slot steps (sx_attn8.cuh) through a ring of its own in shared
 // memory - cp.async, 512 contiguous bytes per instruction, XOR-swizzled - and needs no other warp.  Both products
 // run as mma.sync with the slots (then the head dimension) on the 16-row side and 8 queries on the 8-column side:
-//     S^T[slot][q] = sum_d kc[slot][d] Q[q][d]         e4m3 x e4m3, m16n8k32; Q as the exact sum of two e4m3 numbers
+//     S^T[slot][q] = sum_d kc[slot][d] Q[q][d]         8-bit, m16n8k32; Q as the sum of an e4m3 and an e5m2 number (a8_split)
 //     O^T[d][q] += sum_slot vc[slot][d] P[slot][q]     fp16 x fp16, m16n8k16; e4m3 codes are exact in fp16
 // K's fragments are the codes as ldmatrix delivers them.  For V ldmatrix.trans delivers [slot][pair of d]; one byte permute
 // splits the pair into two rows of the product, whose order is undone where O is stored, and cvt.f16x2.e4m3x2
@@ -52,10 +52,17 @@ __device__ __forceinline__ uint32_t a8_transpose(uint32_t x) {
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-// e4m3 x e4m3 -> fp32, 16 x 8 x 32
+// e4m3 x e4m3 -> fp32, 16 x 8 x 32; the same with B in e5m2
 __device__ __forceinline__ void a8_mma_f8(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void a8_mma_f8_low(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e5m2.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
       "{%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -204,7 +211,7 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, (A8S<D, NQT>::CTAS)) sx_attn8_
 #pragma unroll 1
   for (int x = xb; x < xe; ++x) {
     if (x == seg.x1) {
-      // ---- a new (unit, head, tile): its queries, scaled to fp16 --------------------------------------------
+      // ---- a new (unit, head, tile): its queries in two 8-bit parts --------------------------------------------
       seg = a8_seek<PRE>(p, pl, ls, A8_SPLIT_STEP, x);
 #pragma unroll
       for (int i = 0; i < NQT; ++i) {
@@ -221,8 +228,7 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, (A8S<D, NQT>::CTAS)) sx_attn8_
         top = max(top & 0xffffu, top >> 16);
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // 2^-e brings the largest magnitude into (224, 448]; two e4m3 numbers then hold a bf16 number, exactly down to
-        // 2^-10
+        // 2^-ex brings the largest magnitude into (224, 448]
         const int te = (int)(top >> 7);
         const int ex = te == 0 || te == 255 ? 0 : max(-126, te - 135 + ((top & 0x7f) > 96 ? 1 : 0));
         const float up = __uint_as_float((uint32_t)(127 - ex) << 23);
@@ -233,10 +239,8 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, (A8S<D, NQT>::CTAS)) sx_attn8_
           for (int k = 0; k < 2; ++k) {
             const uint32_t w = k ? raw[c].y : raw[c].x;
             const float2 f = make_float2(__uint_as_float(w << 16) * up, __uint_as_float(w & 0xffff0000u) * up);
-            const uint32_t h2 = te == 255 ? 0x7f7fu : (uint32_t)__nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
-            const __half2_raw wide = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h2, __NV_E4M3);
-            const float2 back = __half22float2(*reinterpret_cast<const __half2 *>(&wide));
-            const uint32_t l2 = te == 255 ? 0x7f7fu : (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f.x - back.x, f.y - back.y), __NV_SATFINITE, __NV_E4M3);
+            uint32_t h2, l2;
+            a8_split(f, te != 255, h2, l2);
             hi |= h2 << (16 * k);
             lo |= l2 << (16 * k);
           }
@@ -279,7 +283,7 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, (A8S<D, NQT>::CTAS)) sx_attn8_
 #pragma unroll
       for (int i = 0; i < NQT; ++i) {
         a8_mma_f8(S[i], r, qf[i][c][0], qf[i][c + 1][0]);
-        a8_mma_f8(S[i], r, qf[i][c][1], qf[i][c + 1][1]);
+        a8_mma_f8_low(S[i], r, qf[i][c][1], qf[i][c + 1][1]);
       }
     }
     float kscale[2], ev[2], inv[2];

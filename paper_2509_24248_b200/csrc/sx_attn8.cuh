@@ -12,6 +12,9 @@
 // tile * qt, where cols(unit) counts the queries of all units before it.  Going along the list either c grows by
 // one (qt rows further) or the tile does (exactly its rows further), so no two partials overlap.
 #pragma once
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
 #include "sx_common.cuh"
 #include "sx_launch.cuh"
 
@@ -288,6 +291,19 @@ __device__ __forceinline__ float a8_pow2(int byte) { return __uint_as_float((uin
 __device__ __forceinline__ float a8_pow2_inv(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
 __device__ __forceinline__ float a8_exponent(int byte) {       // 255 marks a row with a value that is not finite
   return byte == 255 ? __int_as_float(0x7fffffff) : (float)(byte - 127);
+}
+
+// A pair of query values, scaled so that their row's largest magnitude lies in (224, 448], as pairs of e4m3 (high part) and
+// e5m2 numbers (what is left).  A bf16 number has 8 significand bits; e4m3 keeps 4, and the rest is a multiple of the last
+// bit, at most 8 of them: three significand bits, which e5m2 has, over a wider range.  So the sum is exact for values
+// down to 2^-6, 2^-13 of the row's largest, and below that off by 2^-14 at most, 2^-21 of the largest (with e4m3 for both
+// parts the exact range ended at 2^-10 of the largest and a value of 2^-12 of it was off by 1 %).
+__device__ __forceinline__ void a8_split(float2 x, bool finite, uint32_t &hi, uint32_t &lo) {
+  hi = (uint32_t)__nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3);
+  const __half2_raw wide = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)hi, __NV_E4M3);
+  const float2 back = __half22float2(*reinterpret_cast<const __half2 *>(&wide));
+  lo = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x.x - back.x, x.y - back.y), __NV_SATFINITE, __NV_E5M2);
+  if (!finite) hi = lo = 0x7f7fu;                      // a number in neither
 }
 
 size_t sx_attn8_ws_bytes(int nq, int nkv, int d, int B, int rows, int groups, int sm_count);

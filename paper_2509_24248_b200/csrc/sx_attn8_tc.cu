@@ -6,10 +6,9 @@
 // queries on M:
 //     S[q][slot] = sum_d Q[q][d] kc[slot][d]         A = Q, B = K codes as they lie in the pages (both K-major)
 //     O[q][d]   += sum_slot P[q][slot] V[slot][d]    A = P from tensor memory, B = V as bf16 (N-major)
-// First product: e4m3 x e4m3.  A bf16 query is the exact sum of two e4m3 numbers (4 + 4 significand bits) once its
-// row is scaled by a power of two, down to 2^-10 / 224 of the row's largest value; so A is [high part] then [low part]
-// into the same accumulator - the cost of one bf16 product, and K is used as it was stored; its scale is a factor of the
-// slot's scores.  Second product: weights need 16 bits (in 8 a long flat tail of small weights would vanish), so V becomes
+// First product: a bf16 query, its row scaled by a power of two, is the sum of an e4m3 and an e5m2 number (a8_split); so A is
+// [high part] then [low part] into the same accumulator - the cost of one bf16 product, and K is used as it was
+// stored; its scale is a factor of the slot's scores.  Second product: weights need 16 bits (in 8 a long flat tail of small weights would vanish), so V becomes
 // bf16 in shared memory, exactly (4 significand bits, a power of two), by eight warps of their own, once per block
 // whatever the number of queries: a code's exponent and mantissa are moved to their places in a bf16 number and one packed
 // multiplication by 2^(120 + e) puts bias and scale right.
@@ -138,7 +137,7 @@ __device__ __forceinline__ f32x2 t8_fma2(f32x2 a, f32x2 b, f32x2 c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
-// D[tmem] (+)= A[smem] * B[smem], e4m3 x e4m3 -> fp32, M = 128, K = 32
+// D[tmem] (+)= A[smem] * B[smem], 8-bit x 8-bit -> fp32, M = 128, K = 32
 __device__ __forceinline__ void t8_mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -335,7 +334,8 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       int item = 0, seg_li = 0;                             // segment number, its first block in the run
       const uint32_t acc32 = (1u << 4) | (8u << 24);        // fp32 accumulate, M = 128 (M / 16 at bit 24)
       if (warp == 1) {
-        // ---- first product: e4m3 (format 0), both operands K-major, N = 64 (N / 8 at bit 17) -------------------------
+        // ---- first product: e4m3 (format 0; the low parts of A e5m2, format 1 at bit 7), both operands K-major, N = 64 (N / 8 at
+        // bit 17)
         const uint64_t qd = smem_desc(smem_u32(sQ));
         bool ok = true;
 #pragma unroll 1
@@ -356,7 +356,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 #pragma unroll
             for (int k = 0; k < 8; ++k)
               t8_mma_f8(tmem + (uint32_t)(g * 128 + b * 64), qd + (uint64_t)(((k >> 2) * T8_Q_BYTES + (k & 3) * 32) >> 4),
-                        kd + (uint64_t)((g * (T8_BLK / 2) + (k & 3) * 32) >> 4), acc32 | (8u << 17), k > 0 ? 1u : 0u);
+                        kd + (uint64_t)((g * (T8_BLK / 2) + (k & 3) * 32) >> 4), acc32 | (8u << 17) | (k < 4 ? 0u : 1u << 7), k > 0 ? 1u : 0u);
             tc_commit(smem_u32(&sfull[g * 2 + b]));
           }
           tc_commit(smem_u32(&kempty[slot]));
@@ -410,7 +410,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           s = a8_seek<PRE>(p, pl, ls, slab, s.x1);
         }
         ++item;
-        // two e4m3 parts (rows of 128 bytes, 128-byte swizzle) and factor; eight threads share a row
+        // the two parts (rows of 128 bytes, 128-byte swizzle) and factor; eight threads share a row
         const int buf = item % T8_NC;
         {
           const int q0 = team * 64 + r0;
@@ -444,10 +444,8 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               const float2 f = make_float2(__uint_as_float(in[k] << 16) * up, __uint_as_float(in[k] & 0xffff0000u) * up);
-              const uint32_t h2 = e == 255 ? 0x7f7fu : (uint32_t)__nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
-              const __half2_raw wide = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)h2, __NV_E4M3);
-              const float2 back = __half22float2(*reinterpret_cast<const __half2 *>(&wide));
-              const uint32_t l2 = e == 255 ? 0x7f7fu : (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f.x - back.x, f.y - back.y), __NV_SATFINITE, __NV_E4M3);
+              uint32_t h2, l2;
+              a8_split(f, e != 255, h2, l2);
               if (k & 1) { hi[k >> 1] |= h2 << 16; lo[k >> 1] |= l2 << 16; }
               else { hi[k >> 1] = h2; lo[k >> 1] = l2; }
             }

@@ -130,3 +130,20 @@ def test_nothing_but_value_rows_of_zeros(kernel):
 def test_a_value_row_of_zeros_beside_huge_ones(size, gap):
     q, k, v = with_gap(256, 2, 4, 128, [0, 200], gap, size, gap)
     attend_like_one(one_sequence(k, v), 97, q, sx.ATTN_SPLIT)
+
+
+# ---- queries with an outlier channel --------------------------------------------------------------------------------
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("power", [0, 9, 11, 13])
+def test_a_query_channel_far_above_the_rest(kernel, d, power):
+    """A channel 2^power times the others in which every key is zero: it decides nothing, and what decides keeps its bits.
+    (The others lie in [1, 2) and the outlier is 1.5 x 2^power, so that the smallest is 2^-14 of it or more.)"""
+    if kernel == sx.ATTN_TC and d != 128:
+        kernel = sx.ATTN_AUTO
+    g = torch.Generator().manual_seed(power)
+    q = (1 + torch.rand(1, 3, 8, d, generator=g)) * torch.where(torch.rand(1, 3, 8, d, generator=g) < 0.5, -1.0, 1.0)
+    k, v = torch.randn(500, 2, d, generator=g), torch.randn(500, 2, d, generator=g)
+    q[..., 5] = 1.5 * 2.0 ** power
+    k[..., 5] = 0.0
+    attend_like_one(one_sequence(k, v), 3, q.to(torch.bfloat16), kernel, scale=2.0 * d ** -0.5)
