@@ -340,8 +340,7 @@ sx_status sx_kv_read(const sx_kv_shape *shape, const sx_kv *kv, int32_t T, const
  * reported as SX_ERR_CAPACITY and the sequences concerned read their own tables.
  *
  * kernel: SX_ATTN_AUTO, or SX_ATTN_SPLIT / SX_ATTN_TC to force one (see sx_set_attention; SX_ATTN_TC needs head_dim 128, a
- * pool of less than 2^31 rows and a batch of at most about 500, and wants values below 2^96: its sums carry weights up to
- * 2^30).  Workspace (256-byte aligned, not shared by calls that may overlap): sx_attention_ws_bytes for the
+ * pool of less than 2^31 rows and a batch of at most about 500).  Workspace (256-byte aligned, not shared by calls that may overlap): sx_attention_ws_bytes for the
  * current device, or 0 for a shape that cannot be. */
 size_t sx_attention_ws_bytes(const sx_kv_shape *shape, int32_t batch, int32_t rows, int32_t n_groups);
 sx_status sx_attention(const sx_kv_shape *shape, const sx_kv *kv, int32_t rows, int32_t drafted, const void *q_d,

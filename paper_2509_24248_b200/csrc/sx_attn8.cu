@@ -432,6 +432,7 @@ __global__ void __launch_bounds__(A8_MERGE_THREADS) sx_attn8_merge_kernel(const 
     const SxA8List &ls = list ? p.pre : p.own;
     const int s = list ? p.group_start[grp] : b, u = list ? grp : b;
     const int nq = (list ? a8_members(p, grp) : 1) * p.rows * p.G, q = ((b - s) * p.rows + j) * p.G + gq;
+    const float unit = ls.unit;
     const int steps = ls.steps[u], cum = ls.cum[u];
     const uint32_t per = (uint32_t)a8_per(ls.total[0], ls);
     if (steps == 0) continue;
@@ -461,7 +462,7 @@ __global__ void __launch_bounds__(A8_MERGE_THREADS) sx_attn8_merge_kernel(const 
         M = m;
         L = L * a + ml[k].y * w;
 #pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] = acc[i] * a + v[k][i] * w;
+        for (int i = 0; i < V; ++i) acc[i] = acc[i] * a + v[k][i] * (w * unit);
       }
     }
   }
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(A8_MERGE_THREADS) sx_attn8_merge_kernel(const 
   if (!live) return;
   bf16 y[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) y[i] = __float2bfloat16_rn(L == 0.f ? 0.f : acc[i] / L);
+  for (int i = 0; i < V; ++i) y[i] = __float2bfloat16_rn(L == 0.f ? 0.f : acc[i] / L * p.unit);
   bf16 *o = p.o_out + ((int64_t)r * p.nq + hq) * D + lane * V;
   if (V == 4) *reinterpret_cast<uint2 *>(o) = *reinterpret_cast<uint2 *>(y);
   else *reinterpret_cast<uint32_t *>(o) = *reinterpret_cast<uint32_t *>(y);
@@ -603,8 +604,11 @@ sx_status sx_launch_attn8(SxA8 p, int kernel, char *ws, int sm_count, cudaStream
   };
   bool own_tc = false, pre_tc = false;
   SX_TRY(choose(p.own, own_q, own_tc));
+  if (p.n_groups > 0) SX_TRY(choose(p.pre, pre_q, pre_tc));
+  p.unit = own_tc || pre_tc ? ldexpf(1.f, A8_V_SHIFT) : 1.f;
+  p.own.unit = own_tc ? 1.f : 1.f / p.unit;
+  p.pre.unit = pre_tc ? 1.f : 1.f / p.unit;
   if (p.n_groups > 0) {
-    SX_TRY(choose(p.pre, pre_q, pre_tc));
     SX_TRY(pre_tc ? sx_launch_attn8_tc(p, true, sm_count, st) : split_list<true>(p, sm_count, st));
     p.after_prefix = 1;
   }

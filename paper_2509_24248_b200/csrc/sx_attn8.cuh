@@ -27,6 +27,8 @@
 // are held to 2^-25 of it or better.  With 2^8 the reference moved in most blocks of a prefix with 128 queries
 // whose scores spread over 2^4 (one query that exceeds is enough).
 #define A8_SLACK 14.f
+// The tensor-memory kernel's partial outputs are in units of 2^A8_V_SHIFT (sx_attn8_tc.cu)
+#define A8_V_SHIFT 50
 
 struct SxA8List {                  // one list: what the main kernel writes down for the merge
   int32_t *cum;                    // [units] first list position of the unit (the host has checked that lists fit)
@@ -37,6 +39,7 @@ struct SxA8List {                  // one list: what the main kernel writes down
   int qt, qt_shift, step, step_shift, runs, min_per, spread;
   int parts_shift;                 // log2 of the partial results per run and tile (the tensor-memory kernel's copies), `half`
   int64_t half;                    // rows apart
+  float unit;                      // factor that brings this list's partial outputs to the merge's unit
 };
 
 struct SxA8 {
@@ -51,6 +54,7 @@ struct SxA8 {
   int32_t *status;
   int32_t *seq_group;              // [B] for the merge: group of a sequence, -1 when it shares nothing
   SxA8List own, pre;
+  float unit;                      // the merge's unit: 2^A8_V_SHIFT where a list takes the tensor-memory kernel, else 1
   int early;                       // lengths and groups are inputs of the iteration: the plan may precede the wait
   int after_prefix;                // the own list's kernel: launched behind the prefix list's, see sx_attn8.cu
 };

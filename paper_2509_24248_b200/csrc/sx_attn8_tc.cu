@@ -11,7 +11,9 @@
 // stored; its scale is a factor of the slot's scores.  Second product: weights need 16 bits (in 8 a long flat tail of small weights would vanish), so V becomes
 // bf16 in shared memory, exactly (4 significand bits, a power of two), by eight warps of their own, once per block
 // whatever the number of queries: a code's exponent and mantissa are moved to their places in a bf16 number and one packed
-// multiplication by 2^(120 + e) puts bias and scale right.
+// multiplication by 2^(120 + e - A8_V_SHIFT) puts bias and scale right.  The shift leaves room for the sums: weights reach
+// 2^T8_SLACK and values 2^129, and without it 600 slots of 2^110 whose scores rise became infinity - infinity; with it 2^19
+// slots of any values are held, and the smallest codes of the smallest scale, 2^-123, are still normal numbers.
 // (Tried before: slots on M, so that a thread owned a slot and the softmax ran across threads - a barrier vote per block,
 // weights through shared memory, a reference per query to fetch for every score: 6500 cycles per block with 128 queries,
 // 3400 with 32.  V as fp16 codes with its scale in the score and a second factor in the sums: three broadcasts from
@@ -202,7 +204,7 @@ __device__ __forceinline__ void t8_ld(uint32_t taddr, float (&v)[64]) {
       : "r"(taddr) : "memory");
 }
 // four codes to bf16, times `f` (a packed pair of equal bf16 numbers): exponent and mantissa move to the low end of the
-// exponent's place and the high end of the mantissa's, which is the value times 2^-120; f = 2^(120 + e)
+// exponent's place and the high end of the mantissa's, which is the value times 2^-120; f = 2^(120 + e - A8_V_SHIFT)
 __device__ __forceinline__ void t8_widen4(uint32_t x, uint32_t f, uint32_t &lo2, uint32_t &hi2) {
   const uint32_t hi = ((x >> 4) & 0x07070707u) | (x & 0x80808080u), lo = (x << 4) & 0xf0f0f0f0u;
   uint32_t a = __byte_perm(lo, hi, 0x5140), b = __byte_perm(lo, hi, 0x7362);
@@ -215,13 +217,6 @@ __device__ __forceinline__ void t8_widen4(uint32_t x, uint32_t f, uint32_t &lo2,
 __device__ __forceinline__ uint32_t t8_pow2x2(int n) { return (uint32_t)(127 + n) * 0x00800080u; }
 __device__ __forceinline__ uint32_t t8_mulx2(uint32_t x, uint32_t f) {
   const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&f));
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
-// the largest finite number in place of infinity: what a slot holds that no query sees must not meet a weight of 0
-__device__ __forceinline__ uint32_t t8_finite(uint32_t x) {
-  const uint32_t top = 0x7f7f7f7fu, bottom = 0xff7fff7fu;
-  const __nv_bfloat162 v = __hmax2(__hmin2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&top)),
-                                   *reinterpret_cast<const __nv_bfloat162 *>(&bottom));
   return *reinterpret_cast<const uint32_t *>(&v);
 }
 
@@ -479,17 +474,18 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         xa[it] = *reinterpret_cast<const uint2 *>(src + it * 2048 + turn * 8);
         xb[it] = *reinterpret_cast<const uint2 *>(src + it * 2048 + 8 - turn * 8);
       }
-      uint32_t f[8];                                        // 2^(120 + e); one row per lane and a shuffle per row: 102 against 98 us
+      constexpr int TOP = 134 + A8_V_SHIFT;                 // byte of the largest factor
+      uint32_t f[8];                                        // 2^(120 + e - shift); one row per lane and a shuffle per row: 102 against 98 us
       int top = 0;
 #pragma unroll
       for (int it = 0; it < 8; ++it) {
         const int byte = vbytes[it * 16 + r0];
-        f[it] = byte == 255 ? 0u : t8_pow2x2(min(byte, 134) - 7);
+        f[it] = byte == 255 ? 0u : t8_pow2x2(min(byte, TOP) - TOP + 127);
         top = max(top, byte == 255 ? 0 : byte);
       }
-      // Rows whose 2^(120 + e) is out of range take two steps.  They alone can end as infinity (a slot that nobody may see can
-      // hold any byte), which must not meet a weight of 0.
-      const bool rare = __any_sync(0xffffffffu, top > 134);
+      // Rows whose factor is out of range take two steps.  Nothing ends as infinity, whatever the byte (a slot that nobody may
+      // see can hold any), which must not meet a weight of 0.
+      const bool rare = __any_sync(0xffffffffu, top > TOP);
       __syncwarp();
       if (!rare && lane == 0) mbar_arrive(smem_u32(&vempty[slot]));      // all of it is in registers
       const int wb = li % NW;
@@ -510,13 +506,13 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 #pragma unroll 1
         for (int it = 0; it < 8; ++it) {
           const int byte = vbytes[it * 16 + r0];
-          const uint32_t g2 = t8_pow2x2(byte > 134 && byte != 255 ? byte - 134 : 0);
+          const uint32_t g2 = t8_pow2x2(byte > TOP && byte != 255 ? byte - TOP : 0);
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             uint4 *at = reinterpret_cast<uint4 *>((k ? db : da) + it * 2048);
             uint4 v = *at;
-            v.x = t8_finite(t8_mulx2(v.x, g2)); v.y = t8_finite(t8_mulx2(v.y, g2));
-            v.z = t8_finite(t8_mulx2(v.z, g2)); v.w = t8_finite(t8_mulx2(v.w, g2));
+            v.x = t8_mulx2(v.x, g2); v.y = t8_mulx2(v.y, g2);
+            v.z = t8_mulx2(v.z, g2); v.w = t8_mulx2(v.w, g2);
             *at = v;
           }
         }

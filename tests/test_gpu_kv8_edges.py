@@ -147,3 +147,44 @@ def test_a_query_channel_far_above_the_rest(kernel, d, power):
     q[..., 5] = 1.5 * 2.0 ** power
     k[..., 5] = 0.0
     attend_like_one(one_sequence(k, v), 3, q.to(torch.bfloat16), kernel, scale=2.0 * d ** -0.5)
+
+
+# ---- values at both ends of the format --------------------------------------------------------------------------------
+def rising(n, n_kv, G, d, seed):
+    """Scores that rise by 18 nats behind the first 128 slots: weights of 2^26 relative to those of the first block."""
+    g = torch.Generator().manual_seed(seed)
+    q = torch.where(torch.rand(1, 1, n_kv * G, d, generator=g) < 0.5, -1.0, 1.0)
+    q[:] = q[:, :, :1]
+    k, v = torch.randn(n, n_kv, d, generator=g) * 0.3, torch.randn(n, n_kv, d, generator=g)
+    k[128:] += q[0, 0, 0] * 18.0 / d ** 0.5
+    return q, k, v
+
+
+@pytest.mark.parametrize("kernel", [sx.ATTN_AUTO, *KERNELS])
+@pytest.mark.parametrize("group", [None, 333])
+@pytest.mark.parametrize("power", [-62, -40, 96, 110, 122])
+@pytest.mark.parametrize("rows", [1, 8])
+def test_values_of_all_magnitudes_of_the_format(kernel, group, power, rows):
+    """The mean of finite values is finite, whatever weights they met on the way (enough equal sequences that a block whose
+    scores are low and one whose scores are high fall into one run)."""
+    q, k, v = rising(600, 1, 4, 128, 3)
+    v = v * 2.0 ** power
+    attend_like_one(one_sequence(k, v), 200, q.expand(1, rows, -1, -1).to(torch.bfloat16), kernel, group=group)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_many_values_at_the_top_of_the_format(kernel):
+    """20000 slots of +-1.5 x 2^126 with weights that rise: sums of what the format allows."""
+    q, k, v = rising(20000, 1, 4, 128, 4)
+    v = torch.where(v < -0.8, -1.5, 1.5) * 2.0 ** 126
+    attend_like_one(one_sequence(k, v), 1, q.expand(1, 8, -1, -1).to(torch.bfloat16), kernel)
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("low,high", [(-62, -55), (-30, 30), (70, 120)])
+def test_values_of_many_magnitudes_in_one_sequence(kernel, low, high):
+    g = torch.Generator().manual_seed(high)
+    k, v = torch.randn(700, 2, 128, generator=g), torch.randn(700, 2, 128, generator=g)
+    v *= torch.exp2(torch.randint(low, high + 1, (700, 2, 1), generator=g).float())
+    q = ref.make_q(1, 6, 8, 128, 7)
+    attend_like_one(one_sequence(k, v), 5, q, kernel)
