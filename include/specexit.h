@@ -327,7 +327,8 @@ sx_status sx_kv_read(const sx_kv_shape *shape, const sx_kv *kv, int32_t T, const
  * cache).  Sequence b has `rows` query rows (1..64), row r = b * rows + j, each with n_q_heads heads; a row sees the
  * slots [0, cache_len_d[b]) and, of the `drafted` (0..64) slots behind them, those whose bit is set in row_mask_d[r]
  * (NULL: all).  Softmax of scale * q.k; an output row that sees no slot is zero.  What a slot holds that a row
- * does not see never reaches that row, whatever it is.
+ * does not see never reaches that row, whatever it is.  A page that does not exist, or a cache_len that the table cannot
+ * hold, is reported as SX_ERR_CAPACITY; the slots of such a page count as rows of zeros, and the other sequences are served.
  *   q_d [batch * rows, n_q_heads, head_dim] bf16, q_stride elements from row to row (a multiple of 8)
  *   o_d [batch * rows, n_q_heads, head_dim] bf16
  * head_dim 64 or 128; n_q_heads a multiple of n_kv_heads; batch + n_groups <= 1024, batch * rows <= 65535.

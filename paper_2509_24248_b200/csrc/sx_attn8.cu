@@ -191,7 +191,10 @@ __global__ void __launch_bounds__(A8S_WARPS * 32, (A8S<D, NQT>::CTAS)) sx_attn8_
           a8_cp16_if(dst + BLK + at[i], on ? vp + i * 512 : p.v, on);
         }
       }
-      if (lane < 2) a8_cp16_if(scales + st * 32 + lane * 16, (lane ? p.vs : p.ks) + row0, ok);
+      if (lane < 2) {
+        if (ok) a8_cp16(scales + st * 32 + lane * 16, (lane ? p.vs : p.ks) + row0);
+        else *reinterpret_cast<uint4 *>(scale_sh + st * 32 + lane * 16) = make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
+      }
       ++lx;
       l_left -= 16;
       l_off += 16;

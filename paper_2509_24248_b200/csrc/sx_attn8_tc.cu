@@ -220,6 +220,11 @@ __device__ __forceinline__ uint32_t t8_mulx2(uint32_t x, uint32_t f) {
   return *reinterpret_cast<const uint32_t *>(&v);
 }
 
+// exponent bytes of rows of zeros, for boxes without slots or without a page (not what the ring held before)
+#define T8_16(b) b, b, b, b, b, b, b, b, b, b, b, b, b, b, b, b
+__device__ __align__(16) const uint8_t t8_zero_row_bytes[128] = {T8_16(127), T8_16(127), T8_16(127), T8_16(127),
+                                                                 T8_16(127), T8_16(127), T8_16(127), T8_16(127)};
+
 template <bool PRE, int COPIES>
 __global__ void __launch_bounds__(T8_THREADS, 1)
 sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -310,15 +315,14 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const int slot = li % depth;
         if (li >= depth && !t8_wait(&empty[slot], (uint32_t)(li / depth - 1) & 1u, abort_flag, wait_limit, lane)) break;
         const uint32_t fb = smem_u32(&full[slot]);
-        const uint32_t live = __ballot_sync(0xffffffffu, row >= 0);
-        if (lane == 0) mbar_expect_tx(fb, T8_BLK + (is_v ? 2u * (uint32_t)__popc(live) * (uint32_t)slab : 0u));
+        if (lane == 0) mbar_expect_tx(fb, T8_BLK + (is_v ? 256u : 0u));
         __syncwarp();
         if (lane < nbox) {
           // a box behind the last row of the pool reads zeros
           tma_load_2d(smem_u32(ring + slot * T8_BLK + lane * slab * 128), map, fb, 0, row >= 0 ? row : p.num_pages * p.nkv * p.page, pol);
-          if (is_v && row >= 0) {
-            bulk_load(smem_u32(sc + slot * 256 + lane * slab), p.ks + row, (uint32_t)slab, fb);
-            bulk_load(smem_u32(sc + slot * 256 + 128 + lane * slab), p.vs + row, (uint32_t)slab, fb);
+          if (is_v) {
+            bulk_load(smem_u32(sc + slot * 256 + lane * slab), row >= 0 ? p.ks + row : t8_zero_row_bytes, (uint32_t)slab, fb);
+            bulk_load(smem_u32(sc + slot * 256 + 128 + lane * slab), row >= 0 ? p.vs + row : t8_zero_row_bytes, (uint32_t)slab, fb);
           }
         }
         row = next;

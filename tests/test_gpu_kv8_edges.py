@@ -188,3 +188,58 @@ def test_values_of_many_magnitudes_in_one_sequence(kernel, low, high):
     v *= torch.exp2(torch.randint(low, high + 1, (700, 2, 1), generator=g).float())
     q = ref.make_q(1, 6, 8, 128, 7)
     attend_like_one(one_sequence(k, v), 5, q, kernel)
+
+
+# ---- pages that do not exist ------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("page", [-1, 1 << 20])
+@pytest.mark.parametrize("groups", [None, [0, 2, 4]])
+def test_a_page_that_does_not_exist_holds_zeros_and_is_reported(kernel, page, groups):
+    """Its slots count as rows of zeros; every other sequence, and every other group, is served as ever."""
+    lens, drafted = [300, 280, 260, 301], 2
+    kv = ref.make_cache(4, 2, 128, 64, lens, drafted, seed=41, groups=groups, prefix=[200, 140] if groups else None, share_pages=False, fill=0x7f)
+    q = ref.make_q(4, 2, 8, 128, 42)
+    bad = {n: t.clone() for n, t in kv.items()}
+    bad["page_table"][0, 1] = page
+    zero = {n: t.clone() for n, t in kv.items()}                   # the same with a page of zeros there
+    for b in range(2 if groups else 1):                             # the first member's table stands for both members
+        for n in ("k", "v"):
+            zero[n + "_pages"][int(kv["page_table"][b, 1])] = 0
+            zero[n + "_scale"][int(kv["page_table"][b, 1])] = 127
+    c = sx.KV8(to_dev(bad))
+    for _ in range(3):
+        got = c.sx_attention(q.to(DEV), drafted, kernel=kernel).double().cpu().numpy()
+        with pytest.raises(sx.SxError):
+            c.check_status()
+        near(got, *ref.attention(zero, q, drafted, None, 128 ** -0.5, WEIGHT[kernel]))
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_a_page_that_does_not_exist_takes_nothing_from_the_sequences_before(kernel):
+    """Sequences whose rows are not finite and sequences without a page in turn, several of them in a run: NaN and zero."""
+    B = 200
+    kv = ref.make_cache(1, 1, 128, 64, [384], 0, seed=43)
+    for n in ("k_scale", "v_scale"):
+        kv[n].fill_(255)
+    kv = many(kv, B)
+    kv["page_table"][1::2] = -1
+    c = sx.KV8(to_dev(kv))
+    got = c.sx_attention(ref.make_q(B, 2, 4, 128, 44).to(DEV), kernel=kernel)
+    with pytest.raises(sx.SxError):
+        c.check_status()
+    assert bool(got[::2].isnan().all()) and bool((got[1::2] == 0).all())
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("what", ["length", "negative"])
+def test_a_length_that_cannot_be_is_reported_and_the_others_are_served(kernel, what):
+    kv = ref.make_cache(3, 2, 128, 64, [200, 100, 70], 1, seed=6)
+    q = ref.make_q(3, 2, 8, 128, 12)
+    bad = {n: t.clone() for n, t in kv.items()}
+    bad["cache_len"][1] = 256 if what == "length" else -5
+    c = sx.KV8(to_dev(bad))
+    got = c.sx_attention(q.to(DEV), 1, kernel=kernel).double().cpu().numpy()
+    with pytest.raises(sx.SxError):
+        c.check_status()
+    want, bound = ref.attention(kv, q, 1, None, 128 ** -0.5, WEIGHT[kernel])
+    near(got[[0, 2]], want[[0, 2]], bound[[0, 2]])
