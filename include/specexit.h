@@ -334,11 +334,11 @@ sx_status sx_kv_read(const sx_kv_shape *shape, const sx_kv *kv, int32_t T, const
  * head_dim 64 or 128; n_q_heads a multiple of n_kv_heads; batch + n_groups <= 1024, batch * rows <= 65535.
  *
  * Shared prefix (kv->n_groups > 0): the members of a group hold the same keys and values in their first
- * prefix_len_d[g] slots - sampled answers to one question.  Those slots are read once, through the page table of
- * the group's first member, for the queries of all members together; every member's own slots follow from its own
- * table.  Whether the tables share the pages makes no difference to the result.  prefix_len_d[g] may end inside a page
- * and may be 0.  A prefix longer than a member's cache_len, or groups that do not cover the batch in order, are
- * reported as SX_ERR_CAPACITY and the sequences concerned read their own tables.
+ * prefix_len_d[g] slots - sampled answers to one question.  Those slots are read through the page table of the group's
+ * first member, for the queries of all members together; every member's own slots follow from its own table, which
+ * needs no pages for the rest.  Whether the tables share the pages makes no difference to the result.  prefix_len_d[g]
+ * may end inside a page and may be 0.  A prefix longer than a member's cache_len, or groups that do not cover the batch
+ * in order, are reported as SX_ERR_CAPACITY and the sequences concerned read their own tables.
  *
  * kernel: SX_ATTN_AUTO, or SX_ATTN_SPLIT / SX_ATTN_TC to force one (see sx_set_attention; SX_ATTN_TC needs head_dim 128, a
  * pool of less than 2^31 rows and a batch of at most about 500).  Workspace (256-byte aligned, not shared by calls that may overlap): sx_attention_ws_bytes for the

@@ -120,7 +120,8 @@ __device__ __forceinline__ int a8_steps(const SxA8 &p, const A8Plan &pl, const S
   }
   const int cap = p.max_pages * p.page;
   const int end = min(pl.len[u] + p.E, cap), a0 = a8_first_slot(pl, u, align);
-  return end > a0 ? (end - a0 + ls.step - 1) >> ls.step_shift : 0;
+  // (a sequence without a slot behind the prefix has no steps: its table may have no page there)
+  return end > pl.pre[u] ? (end - a0 + ls.step - 1) >> ls.step_shift : 0;
 }
 template <bool PRE>
 __device__ __forceinline__ int a8_unit_nq(const SxA8 &p, int u) {

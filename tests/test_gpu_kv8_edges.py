@@ -243,3 +243,22 @@ def test_a_length_that_cannot_be_is_reported_and_the_others_are_served(kernel, w
         c.check_status()
     want, bound = ref.attention(kv, q, 1, None, 128 ** -0.5, WEIGHT[kernel])
     near(got[[0, 2]], want[[0, 2]], bound[[0, 2]])
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("drafted", [0, 1])
+@pytest.mark.parametrize("prefix", [100, 128, 200])
+def test_members_need_no_pages_for_the_prefix(kernel, drafted, prefix):
+    """Only the first member's table is read for the prefix: the others' entries may be -1 there, also where a member has
+    no slot of its own behind a prefix that ends inside a page."""
+    lens = [prefix, prefix, prefix + 70, prefix]
+    kv = ref.make_cache(4, 2, 128, 64, lens, drafted, seed=43, groups=[0, 4], prefix=[prefix], share_pages=False)
+    q = ref.make_q(4, 2, 8, 128, 44)
+    want, bound = ref.attention(kv, q, drafted, None, 128 ** -0.5, WEIGHT[kernel])
+    for b in range(1, 4):
+        own = lens[b] + drafted > prefix
+        kv["page_table"][b, :prefix // 64 if own else None] = -1
+    c = sx.KV8(to_dev(kv))
+    got = c.sx_attention(q.to(DEV), drafted, kernel=kernel).double().cpu().numpy()
+    c.check_status()
+    near(got, want, bound)
