@@ -508,8 +508,10 @@ static sx_status launch_split(const SxA8 &p, int sm_count, cudaStream_t st) {
   using C = A8S<D, NQT>;
   const size_t smem = C::CODES + C::SCALES + a8_plan_bytes(p.B, p.n_groups);
   static_assert(C::CODES + C::SCALES + 48 * 1024 < 200 * 1024, "ring and the largest plan fit one SM");
-  // set on every call: the attribute belongs to the current device, and setting it costs less than remembering it
-  SX_TRY(sx_rc(cudaFuncSetAttribute(sx_attn8_split_kernel<PRE, D, NQT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)));
+  // Set on every call: the attribute belongs to the current device, and setting it costs less than remembering it.  Always to
+  // the same value, the largest plan's: another thread's call for a smaller batch may come between this and the launch.
+  const int most = C::CODES + C::SCALES + (int)a8_plan_bytes(A8_MAX_UNITS, A8_MAX_UNITS);
+  SX_TRY(sx_rc(cudaFuncSetAttribute(sx_attn8_split_kernel<PRE, D, NQT>, cudaFuncAttributeMaxDynamicSharedMemorySize, most)));
   SX_TRY(sx_rc(cudaFuncSetAttribute(sx_attn8_split_kernel<PRE, D, NQT>, cudaFuncAttributePreferredSharedMemoryCarveout, 100)));
   return sx_rc(sx_launch(sx_attn8_split_kernel<PRE, D, NQT>, dim3(sm_count * C::CTAS), dim3(A8S_WARPS * 32), smem, st, p));
 }

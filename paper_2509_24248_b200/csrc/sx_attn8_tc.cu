@@ -715,7 +715,8 @@ static sx_status launch_tc(const SxA8 &p, int sm_count, cudaStream_t st) {
   CUtensorMap mk, mv;
   if (!sx_tma_map_bytes(p.k, rows, 128, slab, &mk) || !sx_tma_map_bytes(p.v, rows, 128, slab, &mv)) return SX_ERR_CUDA;
   const size_t smem = t8_smem(p);
-  SX_TRY(sx_rc(cudaFuncSetAttribute(sx_attn8_tc_kernel<PRE, COPIES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)));
+  // the same value whatever the batch: another thread's call may come between this and the launch
+  SX_TRY(sx_rc(cudaFuncSetAttribute(sx_attn8_tc_kernel<PRE, COPIES>, cudaFuncAttributeMaxDynamicSharedMemorySize, T8_SMEM_MAX)));
   return sx_rc(sx_launch(sx_attn8_tc_kernel<PRE, COPIES>, dim3(sm_count), dim3(T8_THREADS), smem, st, mk, mv, p, slab, T8_WAIT_POLLS));
 }
 

@@ -2,6 +2,9 @@
 of the format, pages that do not exist, members without slots of their own, calls from two threads."""
 from __future__ import annotations
 
+import sys
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -262,3 +265,40 @@ def test_members_need_no_pages_for_the_prefix(kernel, drafted, prefix):
     got = c.sx_attention(q.to(DEV), drafted, kernel=kernel).double().cpu().numpy()
     c.check_status()
     near(got, want, bound)
+
+
+# ---- callers ---------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kernel", KERNELS)
+def test_threads_with_batches_of_different_sizes(kernel):
+    """Each thread has a cache and a stream of its own; nothing of one call is state of another's."""
+    jobs, wrong = [], []
+    for B in (440, 440, 1, 1):
+        kv = ref.make_cache(B, 1, 128, 16, [1] * B, 0, seed=B)
+        c, q = sx.KV8(to_dev(kv)), ref.make_q(B, 1, 2, 128, B).to(DEV)
+        jobs.append((c, q, c.sx_attention(q, kernel=kernel).clone()))
+    torch.cuda.synchronize()
+    gate, interval = threading.Barrier(len(jobs)), sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+
+    def work(c, q, want):
+        try:
+            s = torch.cuda.Stream()
+            with torch.cuda.stream(s):
+                got = torch.empty_like(want)
+                gate.wait()
+                for i in range(20000):
+                    c.sx_attention(q, kernel=kernel, out=got)
+                    if i % 20 == 19:                                # short queues: the calls themselves meet
+                        s.synchronize()
+                if not torch.equal(got, want):
+                    wrong.append("other bits")
+        except Exception as e:
+            wrong.append(repr(e))
+
+    threads = [threading.Thread(target=work, args=j) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    sys.setswitchinterval(interval)
+    assert not wrong, wrong
