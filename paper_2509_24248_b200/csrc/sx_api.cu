@@ -294,6 +294,17 @@ static sx_status check_kv(const sx_ctx *c, const sx_kv *kv) {
   return SX_OK;
 }
 
+// Rounds with nr rows per sequence: refused here, before anything is launched, where the forced attention kernel (or, on an
+// 8-bit cache, any) cannot run
+static sx_status check_attn(const sx_ctx *c, const sx_kv *kv, int nr) {
+  if (kv->dtype != SX_KV_E4M3)
+    return c->attn_kernel != SX_ATTN_TC || sx_attn_tc_supported(c->sh, nr, *kv) ? SX_OK : SX_ERR_UNSUPPORTED;
+  SxA8 p;
+  const sx_kv_shape sh = {c->sh.nq, c->sh.nkv, c->sh.d, c->sh.page};
+  SX_TRY(sx_attn8_params(sh, *kv, nr, 0, &p));
+  return sx_attn8_check(p, c->attn_kernel, c->sm_count);
+}
+
 static SxTree tree_view(const sx_ctx *c, char *ws) {
   SxTree t;
   char *b = ws + c->off_tree;
@@ -466,6 +477,7 @@ extern "C" sx_status sx_draft_step(sx_ctx *c, const sx_kv *kv, int32_t round, in
   if (R != expect) return SX_ERR_INVALID_ARG;
   if (tree && round > 1 && !row_mask_d) return SX_ERR_INVALID_ARG;
   if (tree && !logp_out_d) return SX_ERR_INVALID_ARG;
+  SX_TRY(check_attn(c, kv, R / kv->batch));
   const int T = tree ? c->dc.topk : 1;
   return draft_round(c, kv, round, R, (const bf16 *)feat_d, SxIndex{nullptr, 1, 0}, tok_d, SxIndex{nullptr, 1, 0},
                      (tree && round > 1) ? row_mask_d : nullptr, (bf16 *)hidden_out_d, SxIndex{nullptr, 1, 0},
@@ -575,6 +587,8 @@ extern "C" sx_status sx_spec_exit_iter(sx_ctx *c, const sx_kv *kv, const sx_exit
     return SX_ERR_INVALID_ARG;
   if (((uintptr_t)feat0_d & 15) || ((uintptr_t)o->hidden_d & 15) || ((uintptr_t)target_hidden_d & 15))
     return SX_ERR_INVALID_ARG;
+  SX_TRY(check_attn(c, kv, 1));
+  if (c->dc.mode == SX_MODE_TREE && c->dc.K > 1) SX_TRY(check_attn(c, kv, c->dc.topk));
   SxRange range("sx spec exit iteration");
   cudaStream_t st = (cudaStream_t)stream;
   char *ws = (char *)ws_d;

@@ -564,8 +564,49 @@ static sx_status merge(const SxA8 &p, int sm_count, cudaStream_t st) {
   return rows <= slots / 2 ? launch_merge<D, 8>(p, st) : rows <= 2 * slots ? launch_merge<D, 4>(p, st) : launch_merge<D, 1>(p, st);
 }
 
-sx_status sx_launch_attn8(SxA8 p, int kernel, char *ws, int sm_count, cudaStream_t st) {
+// Queries per KV head of a unit, in the own list and in the prefix list.
+static int own_queries(const SxA8 &p) { return p.rows * p.G; }
+// The host knows how many groups there are, not which; it takes them to be alike.  (A larger one becomes several tiles: a
+// group of 29 sequences among four of 32 takes 48 us instead of 43 us with the tile that it needs, but sixteen pairs take
+// 50 us instead of 87 us with the tile that one large group among them would need; prefixes of 4096 slots.)
+static int pre_queries(const SxA8 &p) { return p.n_groups > 0 ? (p.B + p.n_groups - 1) / p.n_groups * own_queries(p) : 0; }
+// Which kernel takes a list of `q` queries per KV head.  The warp-level kernel reads a unit's slots once for every 16
+// queries and is bound by bytes up to there; the tensor-memory kernel's time per block of slots hardly depends on the queries.
+// Up to 16 queries the first is faster (one row of 4 heads over 32 x 4100 slots 57 against 107 us, one row of 8 heads
+// over 8 x 16384 slots 63 against 93 us, one of 4096 slots 15 against 27 us), beyond 16 the second (32 queries, 4 x 32768
+// slots: 98 against 146 us; a prefix of 16384 slots under 128 queries: 50 against 92 us; 4 prefixes under 128: 93
+// against 213 us).
+static sx_status choose(const SxA8 &p, int kernel, int q, int sm_count, SxA8List &ls, bool &tc) {
+  auto log2i = [](int v) { int s = 0; while ((1 << s) < v) ++s; return s; };
+  const bool can = sx_attn8_tc_supported(p);
+  if (kernel == SX_ATTN_TC && !can) return SX_ERR_UNSUPPORTED;
+  tc = can && (kernel == SX_ATTN_TC || (kernel == SX_ATTN_AUTO && q > 16));
+  ls.step = tc ? A8_TC_STEP : A8_SPLIT_STEP;
+  ls.qt = tc ? tc_tile(q, (size_t)p.B * p.rows * p.nq) : q <= 8 ? 8 : 16;
+  ls.runs = tc ? sm_count : split_runs(sm_count);
+  ls.min_per = tc ? 1 : 4;
+  ls.spread = sm_count;
+  ls.qt_shift = log2i(ls.qt);
+  ls.step_shift = log2i(ls.step);
+  ls.parts_shift = tc ? log2i(128 / ls.qt) : 0;
+  ls.half = (int64_t)ls.qt * sm_count + (int64_t)p.B * p.rows * p.nq;
+  // list positions are 32-bit: steps of a sequence's whole capacity x KV heads x tiles of all units
+  const int64_t steps = (int64_t)p.max_pages * p.page / ls.step + 2, tiles = (int64_t)p.B * p.rows * p.G / ls.qt + p.B + p.n_groups;
+  return steps * p.nkv * tiles < (1ll << 31) - (1 << 20) ? SX_OK : SX_ERR_UNSUPPORTED;
+}
+static sx_status choose_both(SxA8 &p, int kernel, int sm_count, bool &own_tc, bool &pre_tc) {
   if ((p.d != 64 && p.d != 128) || p.page % A8_SPLIT_STEP || p.B + p.n_groups > A8_MAX_UNITS) return SX_ERR_UNSUPPORTED;
+  SX_TRY(choose(p, kernel, own_queries(p), sm_count, p.own, own_tc));
+  return p.n_groups > 0 ? choose(p, kernel, pre_queries(p), sm_count, p.pre, pre_tc) : SX_OK;
+}
+sx_status sx_attn8_check(SxA8 p, int kernel, int sm_count) {
+  bool own_tc = false, pre_tc = false;
+  return choose_both(p, kernel, sm_count, own_tc, pre_tc);
+}
+
+sx_status sx_launch_attn8(SxA8 p, int kernel, char *ws, int sm_count, cudaStream_t st) {
+  bool own_tc = false, pre_tc = false;
+  SX_TRY(choose_both(p, kernel, sm_count, own_tc, pre_tc));
   size_t o = 0;
   auto take = [&](size_t bytes) { char *at = ws + o; o += up256(bytes); return at; };
   p.seq_group = (int32_t *)take((size_t)p.B * 4);
@@ -576,40 +617,8 @@ sx_status sx_launch_attn8(SxA8 p, int kernel, char *ws, int sm_count, cudaStream
     ls.ml = (float2 *)take(list_rows(p.nq, p.B, p.rows, sm_count) * 8);
     ls.o = (float *)take(list_rows(p.nq, p.B, p.rows, sm_count) * p.d * 4);
   };
-  auto log2i = [](int v) { int s = 0; while ((1 << s) < v) ++s; return s; };
   place(p.own, p.B);
   if (p.n_groups > 0) place(p.pre, p.n_groups);
-  const int own_q = p.rows * p.G;
-  // The host knows how many groups there are, not which; it takes them to be alike.  (A larger one becomes several tiles: a
-  // group of 29 sequences among four of 32 takes 48 us instead of 43 us with the tile that it needs, but sixteen pairs take
-  // 50 us instead of 87 us with the tile that one large group among them would need; prefixes of 4096 slots.)
-  const int pre_q = p.n_groups > 0 ? (p.B + p.n_groups - 1) / p.n_groups * own_q : 0;
-  // Which kernel takes a list of `q` queries per KV head.  The warp-level kernel reads a unit's slots once for every 16
-  // queries and is bound by bytes up to there; the tensor-memory kernel's time per block of slots hardly depends on the queries.
-  // Up to 16 queries the first is faster (one row of 4 heads over 32 x 4100 slots 57 against 107 us, two rows of 8 heads
-  // over 8 x 16384 slots 63 against 93 us, one of 4096 slots 15 against 27 us), beyond 16 the second (32 queries, 4 x 32768
-  // slots: 98 against 146 us; a prefix of 16384 slots under 128 queries: 50 against 92 us; 4 prefixes under 128: 93
-  // against 213 us).
-  auto choose = [&](SxA8List &ls, int q, bool &tc) -> sx_status {
-    const bool can = sx_attn8_tc_supported(p);
-    if (kernel == SX_ATTN_TC && !can) return SX_ERR_UNSUPPORTED;
-    tc = can && (kernel == SX_ATTN_TC || (kernel == SX_ATTN_AUTO && q > 16));
-    ls.step = tc ? A8_TC_STEP : A8_SPLIT_STEP;
-    ls.qt = tc ? tc_tile(q, (size_t)p.B * p.rows * p.nq) : q <= 8 ? 8 : 16;
-    ls.runs = tc ? sm_count : split_runs(sm_count);
-    ls.min_per = tc ? 1 : 4;
-    ls.spread = sm_count;
-    ls.qt_shift = log2i(ls.qt);
-    ls.step_shift = log2i(ls.step);
-    ls.parts_shift = tc ? log2i(128 / ls.qt) : 0;
-    ls.half = (int64_t)ls.qt * sm_count + (int64_t)p.B * p.rows * p.nq;
-    // list positions are 32-bit: steps of a sequence's whole capacity x KV heads x tiles of all units
-    const int64_t steps = (int64_t)p.max_pages * p.page / ls.step + 2, tiles = (int64_t)p.B * p.rows * p.G / ls.qt + p.B + p.n_groups;
-    return steps * p.nkv * tiles < (1ll << 31) - (1 << 20) ? SX_OK : SX_ERR_UNSUPPORTED;
-  };
-  bool own_tc = false, pre_tc = false;
-  SX_TRY(choose(p.own, own_q, own_tc));
-  if (p.n_groups > 0) SX_TRY(choose(p.pre, pre_q, pre_tc));
   p.unit = own_tc || pre_tc ? ldexpf(1.f, A8_V_SHIFT) : 1.f;
   p.own.unit = own_tc ? 1.f : 1.f / p.unit;
   p.pre.unit = pre_tc ? 1.f : 1.f / p.unit;

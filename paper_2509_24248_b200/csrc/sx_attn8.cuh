@@ -315,4 +315,5 @@ size_t sx_attn8_ws_bytes(int nq, int nkv, int d, int B, int rows, int groups, in
 sx_status sx_launch_attn8_tc(const SxA8 &p, bool prefix, int sm_count, cudaStream_t st);
 bool sx_attn8_tc_supported(const SxA8 &p);
 sx_status sx_attn8_params(const sx_kv_shape &sh, const sx_kv &kv, int rows, int E, SxA8 *out);
+sx_status sx_attn8_check(SxA8 p, int kernel, int sm_count);      // what sx_launch_attn8 would refuse
 sx_status sx_launch_attn8(SxA8 p, int kernel, char *ws, int sm_count, cudaStream_t st);
