@@ -141,7 +141,7 @@ typedef struct {
   int32_t num_pages;            /* physical pages in k_pages_d / v_pages_d */
   void *k_pages_d;              /* [num_pages, n_kv, page_size, head_dim] bf16, or e4m3 codes (dtype) */
   void *v_pages_d;
-  int32_t dtype;                /* SX_KV_BF16 (0) or SX_KV_E4M3 */
+  int32_t dtype;                /* SX_KV_BF16 (0) or SX_KV_E4M3; with the first, the fields from here on mean nothing */
   int32_t n_groups;             /* SX_KV_E4M3: groups of sequences that share a prefix; 0: none (see sx_attention) */
   uint8_t *k_scale_d;           /* SX_KV_E4M3: [num_pages, n_kv, page_size] exponent bytes of the rows; 16-byte aligned */
   uint8_t *v_scale_d;
@@ -156,7 +156,9 @@ typedef struct {
  * significand bits is all that is lost (values below 2^-10 of a row's largest keep fewer).  A row with a value
  * that is not finite has the byte 255 and codes of zero, and reads as NaN.  Half the bytes of bf16 and one byte
  * per row.  Needs a page size that is a multiple of 16; attention (the draft step's too) needs head_dim 64 or 128.
- * A draft call takes the kind of cache that sx_set_cache named; fields behind v_pages_d are zero for bf16. */
+ * A draft call takes the kind of cache that sx_set_cache named.  With a bf16 one only the first seven fields of sx_kv mean
+ * anything (but dtype must not be SX_KV_E4M3); the struct is larger than it was without 8-bit caches, so code built against
+ * that header has to be built again. */
 enum { SX_KV_BF16 = 0, SX_KV_E4M3 = 1 };
 
 /* Shape of a cache for the calls that take no context. */

@@ -3,6 +3,7 @@
 #include <new>
 #include <vector>
 #include <math.h>
+#include <stddef.h>
 #include <stdio.h>
 #include <string.h>
 
@@ -282,12 +283,20 @@ static sx_status check_ws(const sx_ctx *c, const void *ws, size_t bytes) {
   return SX_OK;
 }
 
-static sx_status check_kv(const sx_ctx *c, const sx_kv *kv) {
+// Checks the caller's cache and copies what this context's kind of cache has: of a bf16 cache the fields up to v_pages_d, so
+// that a caller who sets no others (or garbage) is served; only a cache that says it is of the other kind is refused.
+static sx_status check_kv(const sx_ctx *c, const sx_kv *kv, sx_kv *own) {
   if (!kv || !kv->cache_len_d || !kv->page_table_d || !kv->k_pages_d || !kv->v_pages_d) return SX_ERR_INVALID_ARG;
   if (kv->batch < 1 || kv->batch > c->max_batch || kv->max_pages < 1 || kv->num_pages < 1) return SX_ERR_INVALID_ARG;
   if (((uintptr_t)kv->k_pages_d & 15) || ((uintptr_t)kv->v_pages_d & 15)) return SX_ERR_INVALID_ARG;
+  if (c->kv_dtype == SX_KV_BF16) {
+    if (kv->dtype == SX_KV_E4M3) return SX_ERR_INVALID_ARG;
+    memset(own, 0, sizeof(*own));
+    memcpy(own, kv, offsetof(sx_kv, dtype));
+    return SX_OK;
+  }
   if (kv->dtype != c->kv_dtype) return SX_ERR_INVALID_ARG;
-  if (kv->dtype == SX_KV_BF16) return kv->n_groups == 0 ? SX_OK : SX_ERR_UNSUPPORTED;
+  *own = *kv;
   SxA8 p;                                           // the checks of the 8-bit attention, before anything is launched
   const sx_kv_shape sh = {c->sh.nq, c->sh.nkv, c->sh.d, c->sh.page};
   SX_TRY(sx_attn8_params(sh, *kv, c->dc.mode == SX_MODE_TREE ? c->dc.topk : 1, 0, &p));
@@ -468,7 +477,9 @@ extern "C" sx_status sx_draft_step(sx_ctx *c, const sx_kv *kv, int32_t round, in
                                    int32_t *tok_out_d, float *logp_out_d, float *signals_out_d, void *ws_d,
                                    size_t ws_bytes, int32_t *status_d, void *stream) {
   if (!c || !feat_d || !tok_d || !hidden_out_d || !tok_out_d || !signals_out_d || !status_d) return SX_ERR_INVALID_ARG;
-  SX_TRY(check_kv(c, kv));
+  sx_kv own;
+  SX_TRY(check_kv(c, kv, &own));
+  kv = &own;
   SX_TRY(check_ws(c, ws_d, ws_bytes));
   if (((uintptr_t)feat_d & 15) || ((uintptr_t)hidden_out_d & 15)) return SX_ERR_INVALID_ARG;
   const bool tree = c->dc.mode == SX_MODE_TREE;
@@ -580,7 +591,9 @@ extern "C" sx_status sx_spec_exit_iter(sx_ctx *c, const sx_kv *kv, const sx_exit
                                        const sx_iter_out *o, void *ws_d, size_t ws_bytes, int32_t *status_d,
                                        void *stream) {
   if (!c || !cfg || !state || !feat0_d || !tok0_d || !target_hidden_d || !o || !status_d) return SX_ERR_INVALID_ARG;
-  SX_TRY(check_kv(c, kv));
+  sx_kv own;
+  SX_TRY(check_kv(c, kv, &own));
+  kv = &own;
   SX_TRY(check_ws(c, ws_d, ws_bytes));
   if (!o->cand_tok_d || !o->hidden_d || !o->slot_signal_d || !o->target_tok_d || !o->accept_len_d || !o->path_d ||
       !o->recover_tok_d || !o->exit_flag_d || !o->accept_len_out_d || !o->recover_tok_out_d || !o->smoothed_d)
@@ -730,7 +743,9 @@ extern "C" sx_status sx_commit(sx_ctx *c, const sx_kv *kv, int32_t P, const void
   if (!c || !target_hidden_d || !cand_tok_d || !path_d || !accept_len_out_d || !recover_tok_out_d || !feat0_next_d ||
       !tok0_next_d || !status_d)
     return SX_ERR_INVALID_ARG;
-  SX_TRY(check_kv(c, kv));
+  sx_kv own;
+  SX_TRY(check_kv(c, kv, &own));
+  kv = &own;
   SX_TRY(check_ws(c, ws_d, ws_bytes));
   if (P < 1 || path_stride < 1 || path_stride - 1 > c->dc.K) return SX_ERR_INVALID_ARG;
   if (((uintptr_t)target_hidden_d & 15) || ((uintptr_t)feat0_next_d & 15)) return SX_ERR_INVALID_ARG;

@@ -30,3 +30,26 @@ def test_a_forced_kernel_that_cannot_run_is_refused_before_anything_is_written(k
     sx.sx_set_attention(binding.ATTN_AUTO)
     sx.sx_draft_step(1, case.f0.to(sx.dev), case.t0.to(sx.dev))
     sx.check_status()
+
+
+def test_a_bf16_cache_is_seven_fields():
+    """What lies behind v_pages_d is not looked at in a context whose cache is bf16: a caller that knows only the first seven
+    fields, or sets no others, is served as before."""
+    wl = synth.Workload(shape=SHAPE, B=2, **CHAIN)
+    case = harness.build_case(wl, poison_tail=False)
+    got = []
+    for junk in (False, True):
+        sx = binding.SpecExit(SHAPE, case.weights, 2, wl.mode, wl.K)
+        sx.set_kv(case.kv)
+        if junk:
+            k = sx._kv_struct
+            k.dtype, k.n_groups, k.k_scale_d, k.v_scale_d, k.group_start_d, k.prefix_len_d = 0x5a5a5a5a, 77, 3, 5, 7, 9
+        one = sx.sx_draft_step(1, case.f0.to(sx.dev), case.t0.to(sx.dev))
+        out, st = sx.new_outputs(2), sx.new_state(2)
+        th = torch.randn(2, wl.K + 1, SHAPE.H, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).to(sx.dev)
+        sx.sx_spec_exit_iter(binding.ExitParams(), st, case.f0.to(sx.dev), case.t0.to(sx.dev), th, out)
+        nxt = sx.sx_commit(th, out["cand_tok_d"], out["path_d"], out["accept_len_out_d"], out["recover_tok_out_d"])
+        sx.check_status()
+        got.append([*(t for t in one if t is not None), *(out[n] for n in sorted(out)), *nxt, *sx.kv.values()])
+    for a, b in zip(*got):
+        assert torch.equal(torch.nan_to_num(a.float(), nan=9.0), torch.nan_to_num(b.float(), nan=9.0))
