@@ -245,6 +245,8 @@ def _kv_struct(kv: Dict[str, torch.Tensor], n_kv: int, page: int, d: int) -> KV:
     """Argument block of a paged cache; an 8-bit one (codes in one byte per value) carries its exponent bytes and, if
     it has them, its groups.  Checks what the C side cannot see: types, shapes, contiguity, one device."""
     dev = kv["k_pages"].device
+    if (kv.get("group_start") is None) != (kv.get("prefix_len") is None):
+        raise SxError("group_start and prefix_len belong together")
     for name in _CACHE_NAMES:
         t = kv.get(name)
         if t is not None and (not t.is_cuda or t.device != dev or not t.is_contiguous()):
@@ -277,7 +279,7 @@ def _kv_struct(kv: Dict[str, torch.Tensor], n_kv: int, page: int, d: int) -> KV:
     st.k_scale_d, st.v_scale_d = kv["k_scale"].data_ptr(), kv["v_scale"].data_ptr()
     if kv.get("group_start") is not None:
         n = int(kv["group_start"].numel()) - 1
-        if n < 1 or kv.get("prefix_len") is None or int(kv["prefix_len"].numel()) != n:
+        if n < 1 or int(kv["prefix_len"].numel()) != n:
             raise SxError("group_start must be [n_groups + 1] and prefix_len [n_groups]")
         st.n_groups = n
         st.group_start_d, st.prefix_len_d = kv["group_start"].data_ptr(), kv["prefix_len"].data_ptr()
