@@ -465,7 +465,8 @@ sx_status sx_profile_end(sx_ctx *ctx, float *ms_out, int32_t *count_out);
  * at their next poll, SX_ERR_TIMEOUT goes to the status word, copies in flight are given time to land,
  * the CTA frees its tensor memory and returns - the context stays usable.  This call runs that path on
  * its own: `ctas` CTAs (1..1024) with the GEMM kernel's thread layout allocate tensor memory and wait, with
- * `limit` polls (1..2^20), on barriers nothing arrives at; no copy is issued.  Afterwards *status_d is
+ * `limit` polls (1..2^20; every second CTA with polls that sleep, as in the attention over an 8-bit cache, 4096 of them at
+ * most), on barriers nothing arrives at; no copy is issued.  Afterwards *status_d is
  * SX_ERR_TIMEOUT, reached_d[0] == 0 (no wait reported success) and reached_d[1] == ctas (every CTA
  * returned through the tear-down).  reached_d: two int32 on the device, zeroed by the caller. */
 sx_status sx_selftest_bounded_wait(uint32_t limit, int32_t ctas, int32_t *status_d, int32_t *reached_d,

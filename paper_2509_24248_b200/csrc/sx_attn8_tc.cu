@@ -75,31 +75,7 @@ __device__ __forceinline__ float t8_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// Bounded wait of one thread.  The poll carries a time for which the hardware may keep the thread asleep: a dozen warps
-// polling without one kept the shared-memory pipe so busy that every access of the others took hundreds of cycles.
-#define T8_NAP_NS 20000u
-#define T8_WAIT_POLLS (1u << 17)          // x T8_NAP_NS: about 2.6 s
-__device__ __forceinline__ bool t8_poll(uint64_t *bar, uint32_t parity, volatile int *abort_flag, uint32_t limit) {
-  const uint32_t at = smem_u32(bar);
-  for (uint32_t i = 0; i < limit; ++i) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(at), "r"(parity), "r"(T8_NAP_NS) : "memory");
-    if (ok) return true;
-    if (*abort_flag) return false;
-  }
-  *abort_flag = 1;
-  return false;
-}
-// of a warp: one lane polls for all of it
-__device__ __forceinline__ bool t8_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag, uint32_t limit, int lane) {
-  bool ok = true;
-  if (lane == 0) ok = t8_poll(bar, parity, abort_flag, limit);
-  return __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
-}
+#define T8_WAIT_POLLS (1u << 17)          // x SX_NAP_NS: 2.6 s at most
 // true in one thread of the warp; unlike a test of the lane, the compiler knows that of it, and issues the tensor-core
 // instructions (whose operands live in uniform registers) without a loop over the threads that might be there
 __device__ __forceinline__ bool t8_elect() {
@@ -313,7 +289,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           next = row_of(g0 + li + 1);
         }
         const int slot = li % depth;
-        if (li >= depth && !t8_wait(&empty[slot], (uint32_t)(li / depth - 1) & 1u, abort_flag, wait_limit, lane)) break;
+        if (li >= depth && !mbar_wait_warp(&empty[slot], (uint32_t)(li / depth - 1) & 1u, abort_flag, wait_limit, lane)) break;
         const uint32_t fb = smem_u32(&full[slot]);
         if (lane == 0) mbar_expect_tx(fb, T8_BLK + (is_v ? 256u : 0u));
         __syncwarp();
@@ -340,16 +316,16 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 #pragma unroll 1
         for (int li = 0; li < nblk && ok; ++li) {
           if (li > 0 && g0 + li == s.x1) { s = a8_seek<PRE>(p, pl, ls, slab, g0 + li); ++item; seg_li = li; }
-          if (li == seg_li && !t8_poll(qfull, (uint32_t)item & 1u, abort_flag, wait_limit)) break;
+          if (li == seg_li && !mbar_wait_nap(qfull, (uint32_t)item & 1u, abort_flag, wait_limit)) break;
           const int slot = li % NK, b = li & 1;
-          if (!t8_poll(&kfull[slot], (uint32_t)(li / NK) & 1u, abort_flag, wait_limit)) break;
+          if (!mbar_wait_nap(&kfull[slot], (uint32_t)(li / NK) & 1u, abort_flag, wait_limit)) break;
           // the scales too: whoever sees the scores may read them
-          if (!t8_poll(&cfull[li % T8_NC], (uint32_t)(li / T8_NC) & 1u, abort_flag, wait_limit)) break;
+          if (!mbar_wait_nap(&cfull[li % T8_NC], (uint32_t)(li / T8_NC) & 1u, abort_flag, wait_limit)) break;
           const uint64_t kd = smem_desc(smem_u32(ringK + slot * T8_BLK));
 #pragma unroll 1
           for (int g = 0; g < 2 && ok; ++g) {
             // the weights of the group's block before last, which lie in place of its scores, have met V
-            if (li >= 2) ok = t8_poll(&pvdone[g * 2 + b], (uint32_t)((li >> 1) - 1) & 1u, abort_flag, wait_limit);
+            if (li >= 2) ok = mbar_wait_nap(&pvdone[g * 2 + b], (uint32_t)((li >> 1) - 1) & 1u, abort_flag, wait_limit);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
@@ -369,13 +345,13 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           if (li > 0 && g0 + li == s.x1) { s = a8_seek<PRE>(p, pl, ls, slab, g0 + li); ++item; seg_li = li; }
           const int wb = li % NW, b = li & 1;
           const bool first = li == seg_li;
-          if (!t8_poll(&wfull[wb], (uint32_t)(li / NW) & 1u, abort_flag, wait_limit)) break;
+          if (!mbar_wait_nap(&wfull[wb], (uint32_t)(li / NW) & 1u, abort_flag, wait_limit)) break;
           const uint64_t wd = smem_desc_mn(smem_u32(sW + wb * 2 * T8_BLK), T8_BLK, 1024u);
 #pragma unroll 1
           for (int g = 0; g < 2 && ok; ++g) {
-            ok = t8_poll(&pfull[g * 2 + b], (uint32_t)(li >> 1) & 1u, abort_flag, wait_limit);
+            ok = mbar_wait_nap(&pfull[g * 2 + b], (uint32_t)(li >> 1) & 1u, abort_flag, wait_limit);
             // the group has read out its output of the segment before
-            if (ok && first && item > 0) ok = t8_poll(&ofree[g], (uint32_t)(item - 1) & 1u, abort_flag, wait_limit);
+            if (ok && first && item > 0) ok = mbar_wait_nap(&ofree[g], (uint32_t)(item - 1) & 1u, abort_flag, wait_limit);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
@@ -405,7 +381,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       while (ok && (item < 0 || at_x >= s.x1)) {
         // both teams wait for the end of every segment's first products, so that neither can be a phase behind
         if (item >= 0) {
-          ok = t8_wait(qempty, (uint32_t)item & 1u, abort_flag, wait_limit, lane);
+          ok = mbar_wait_warp(qempty, (uint32_t)item & 1u, abort_flag, wait_limit, lane);
           s = a8_seek<PRE>(p, pl, ls, slab, s.x1);
         }
         ++item;
@@ -460,7 +436,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       }
       if (!ok || li >= nblk) break;
       const int slot = li % NV, e = li % T8_NC;
-      if (!t8_wait(&vfull[slot], (uint32_t)(li / NV) & 1u, abort_flag, wait_limit, lane)) break;
+      if (!mbar_wait_warp(&vfull[slot], (uint32_t)(li / NV) & 1u, abort_flag, wait_limit, lane)) break;
       const uint8_t *kbytes = sc + slot * 256, *vbytes = kbytes + 128;
       // a row of K or V that is not finite makes the slot's scores so (whoever sees the slot gets it, whoever does not is
       // spared); such a V is zero here
@@ -493,7 +469,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       __syncwarp();
       if (!rare && lane == 0) mbar_arrive(smem_u32(&vempty[slot]));      // all of it is in registers
       const int wb = li % NW;
-      if (li >= NW && !t8_wait(&wempty[wb], (uint32_t)(li / NW - 1) & 1u, abort_flag, wait_limit, lane)) break;
+      if (li >= NW && !mbar_wait_warp(&wempty[wb], (uint32_t)(li / NW - 1) & 1u, abort_flag, wait_limit, lane)) break;
       uint8_t *dst = sW + wb * 2 * T8_BLK + hi * T8_BLK + r0 * 128;
       uint8_t *da = dst + ((ka ^ (r0 & 7)) << 4), *db = dst + ((kb ^ (r0 & 7)) << 4);
 #pragma unroll
@@ -547,7 +523,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       const bool work = (w * 32) % QT < s.cols;              // some thread of this warp has a query
       const int e = li % T8_NC, b = li & 1;
       const uint32_t s_col = lane_base + (uint32_t)(g * 128 + b * 64);
-      ok = t8_wait(&sfull[g * 2 + b], (uint32_t)(li >> 1) & 1u, abort_flag, wait_limit, lane);
+      ok = mbar_wait_warp(&sfull[g * 2 + b], (uint32_t)(li >> 1) & 1u, abort_flag, wait_limit, lane);
       if (!ok) break;
       if (work) {
         tc_fence_after();
@@ -597,7 +573,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
           l2 = t8_mul2(l2, t8_pack(corr, corr));
           if (!first) {
             // O is at rest once the group's product before has completed
-            ok = t8_wait(&pvdone[g * 2 + (b ^ 1)], (uint32_t)((li - 1) >> 1) & 1u, abort_flag, wait_limit, lane);
+            ok = mbar_wait_warp(&pvdone[g * 2 + (b ^ 1)], (uint32_t)((li - 1) >> 1) & 1u, abort_flag, wait_limit, lane);
             if (!ok) break;
             tc_fence_after();
 #pragma unroll 1
@@ -644,14 +620,14 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       if (lane == 0) mbar_arrive(smem_u32(&pfull[g * 2 + b]));
       if (last) {
         // ---- leave the segment: both groups' results become this copy's partial result, half of the columns each ------------
-        ok = t8_wait(&pvdone[g * 2 + b], (uint32_t)(li >> 1) & 1u, abort_flag, wait_limit, lane);
+        ok = mbar_wait_warp(&pvdone[g * 2 + b], (uint32_t)(li >> 1) & 1u, abort_flag, wait_limit, lane);
         if (!ok) break;
         float la, lb;
         t8_unpack(l2, la, lb);
         ml_sh[g * 128 + i] = make_float2(m, la + lb);
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(xfull));
-        ok = t8_wait(xfull, (uint32_t)item & 1u, abort_flag, wait_limit, lane);
+        ok = mbar_wait_warp(xfull, (uint32_t)item & 1u, abort_flag, wait_limit, lane);
         if (!ok) break;
         if (work) {
           const int64_t row = s.base + (int64_t)QT * blockIdx.x + (int64_t)copy * ls.half + query;

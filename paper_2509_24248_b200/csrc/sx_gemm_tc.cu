@@ -449,7 +449,9 @@ sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
 // TMEM, then every role waits on a barrier that nothing ever arrives at (no copy is in flight).  The
 // first wait to run out raises the abort flag, the others see it at their next poll, and the CTA leaves
 // through the same tear-down as the GEMM kernel: SX_ERR_TIMEOUT in the status word, TMEM freed, a
-// normal return.  Used by the tests; `limit` is small there.
+// normal return.  Odd CTAs wait with polls that sleep, as the attention over an 8-bit cache does (at most SX_NAP_POLLS x 4 x
+// SX_NAP_NS, a third of a second).  Used by the tests; `limit` is small there.
+#define SX_NAP_POLLS 4096u
 __global__ void __launch_bounds__(192, 1) sx_wait_selftest_kernel(uint32_t limit, int32_t *status, int32_t *reached) {
   __shared__ __align__(8) uint64_t bars[3];
   __shared__ uint32_t tmem_slot;
@@ -470,7 +472,14 @@ __global__ void __launch_bounds__(192, 1) sx_wait_selftest_kernel(uint32_t limit
   tc_fence_after();
   const uint32_t tmem_base = tmem_slot;
   bool ok = false;
-  if (warp == 0) {
+  const uint32_t naps = min(limit, SX_NAP_POLLS);
+  if (blockIdx.x & 1) {
+    if (warp == 0) {
+      if (lane == 0) ok = mbar_wait_nap(&bars[0], 0u, abort_flag, naps);
+    } else {
+      ok = mbar_wait_warp(&bars[warp == 1 ? 1 : 2], 0u, abort_flag, naps * 4u, lane);
+    }
+  } else if (warp == 0) {
     if (lane == 0) ok = mbar_wait(smem_u32(&bars[0]), 0u, abort_flag, limit);                 // producer's wait
   } else if (warp == 1) {
     if (lane == 0) ok = mbar_wait(smem_u32(&bars[1]), 0u, abort_flag, limit * 4u);            // MMA issuer's wait

@@ -41,6 +41,31 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   return false;
 }
 
+// The same, polls with a time for which the hardware may keep the thread asleep (a poll can return earlier): a dozen warps
+// polling without one kept the shared-memory pipe so busy that every access of the others took hundreds of cycles.
+#define SX_NAP_NS 20000u
+__device__ __forceinline__ bool mbar_wait_nap(uint64_t *bar, uint32_t parity, volatile int *abort_flag, uint32_t limit) {
+  const uint32_t at = smem_u32(bar);
+  for (uint32_t i = 0; i < limit; ++i) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(at), "r"(parity), "r"(SX_NAP_NS) : "memory");
+    if (ok) return true;
+    if (*abort_flag) return false;
+  }
+  *abort_flag = 1;
+  return false;
+}
+// of a warp: one lane polls for all of it
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag, uint32_t limit, int lane) {
+  bool ok = true;
+  if (lane == 0) ok = mbar_wait_nap(bar, parity, abort_flag, limit);
+  return __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+}
+
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y,
                                             uint64_t policy) {
   asm volatile(

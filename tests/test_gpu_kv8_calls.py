@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2509_24248_b200 import binding, synth
-from tests import harness
+from tests import harness, kv8_ref as ref
 from tests.test_gpu_kv8_draft import CHAIN, SHAPE, as_codes
 
 pytestmark = pytest.mark.gpu
@@ -53,3 +53,21 @@ def test_a_bf16_cache_is_seven_fields():
         got.append([*(t for t in one if t is not None), *(out[n] for n in sorted(out)), *nxt, *sx.kv.values()])
     for a, b in zip(*got):
         assert torch.equal(torch.nan_to_num(a.float(), nan=9.0), torch.nan_to_num(b.float(), nan=9.0))
+
+
+@pytest.mark.parametrize("ctas", [2, 301])
+def test_waits_that_sleep_give_up_too(ctas):
+    """Odd CTAs of the self-test wait as the attention's kernels do: none may report success, all must return, and the
+    attention must go on working."""
+    lib = binding.load_library()
+    status, reached = (torch.zeros(n, dtype=torch.int32, device="cuda:0") for n in (1, 2))
+    assert lib.sx_selftest_bounded_wait(50, ctas, status.data_ptr(), reached.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    assert int(status.item()) == -6 and reached.tolist() == [0, ctas]
+    kv = ref.make_cache(2, 2, 128, 64, [300, 200], 0, seed=1)
+    q = ref.make_q(2, 3, 8, 128, 2)
+    c = binding.KV8({n: t.to("cuda:0") for n, t in kv.items()})
+    got = c.sx_attention(q.to("cuda:0"), kernel=binding.ATTN_TC).double().cpu().numpy()
+    c.check_status()
+    want, bound = ref.attention(kv, q, 0, None, 128 ** -0.5)
+    assert (abs(got - want) <= bound).all()
