@@ -303,7 +303,7 @@ class KV8:
     ``[B]``) and, for sequences that share a prefix, ``group_start`` (int32 ``[n_groups + 1]``) with ``prefix_len``
     (int32 ``[n_groups]``).  The tensors are borrowed; what they hold may change between calls.  Work goes to the
     current stream of their device.  The object owns the attention's workspace: use one per stream, and one per captured
-    graph that may run beside others."""
+    graph that may run beside others, and keep it as long as graphs captured through it."""
 
     def __init__(self, kv: Dict[str, torch.Tensor]):
         self.lib = load_library()
@@ -330,7 +330,7 @@ class KV8:
     def _rows(self, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, pos_start: Optional[torch.Tensor]) -> int:
         for name, t in (("k", k), ("v", v)):
             shape, stride = t.shape, t.stride()
-            if (len(shape) != 3 or shape[1] != self.n_kv or shape[2] != self.d or stride[2] != 1 or stride[1] != self.d
+            if (len(shape) != 3 or shape[1] != self.n_kv or shape[2] != self.d or stride[2] != 1 or (stride[1] != self.d and self.n_kv > 1)
                     or t.dtype is not torch.bfloat16 or t.device != self.dev):
                 raise SxError(f"{name} must be bf16 [T, {self.n_kv}, {self.d}] on {self.dev}, rows of heads contiguous")
         if k.shape[0] != v.shape[0]:
@@ -384,7 +384,7 @@ class KV8:
             raise SxError(f"q must be bf16 [{self.B}, rows, n_q, {self.d}] on {self.dev}")
         _, rows, nq, d = shape
         stride = step[1] if rows > 1 else (step[0] if self.B > 1 else nq * d)
-        if step[3] != 1 or step[2] != d or (self.B > 1 and step[0] != rows * stride):
+        if step[3] != 1 or (step[2] != d and nq > 1) or (self.B > 1 and step[0] != rows * stride):
             raise SxError("the heads of a row of q must be contiguous and its rows evenly spaced")
         if row_mask is not None and (row_mask.dtype is not torch.int64 or row_mask.device != self.dev
                                      or row_mask.numel() != self.B * rows or not row_mask.is_contiguous()):

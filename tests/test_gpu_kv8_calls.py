@@ -71,3 +71,23 @@ def test_waits_that_sleep_give_up_too(ctas):
     c.check_status()
     want, bound = ref.attention(kv, q, 0, None, 128 ** -0.5)
     assert (abs(got - want) <= bound).all()
+
+
+def test_strides_of_single_heads_do_not_matter():
+    """With one KV head (or one query head) the distance between heads is never used, whatever the view says."""
+    kv = ref.make_cache(3, 1, 64, 16, [20, 7, 33], 1, seed=3)
+    g = torch.Generator().manual_seed(4)
+    rows = torch.randn(1, 3, 64, generator=g).to(torch.bfloat16).to("cuda:0").transpose(0, 1)      # strides 64, 192, 1
+    q = torch.randn(1, 3, 2, 64, generator=g).to(torch.bfloat16).to("cuda:0").permute(1, 2, 0, 3)  # strides 128, 64, 384, 1
+    assert rows.stride(1) != 64 and q.stride(2) != 64
+    start = torch.arange(4, dtype=torch.int32, device="cuda:0")
+    got = []
+    for k, x in ((rows, q), (rows.clone(memory_format=torch.contiguous_format), q.clone(memory_format=torch.contiguous_format))):
+        c = binding.KV8({n: t.to("cuda:0") for n, t in kv.items()})
+        c.sx_kv_append(k, k, start)
+        back = torch.empty_strided(k.shape, k.stride(), dtype=torch.bfloat16, device="cuda:0")
+        c.sx_kv_read(back, back.clone(), start, c.kv["cache_len"].clone())
+        got.append((c.sx_attention(x, 1), back, *c.kv.values()))
+        c.check_status()
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
