@@ -548,8 +548,9 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 #pragma unroll
         for (int j = 0; j < CH; j += 4) {
           const ulonglong2 k = kb[j >> 2];
-          t8_unpack(t8_fma2(t8_mul2(t8_pack(t[j], t[j + 1]), k.x), f2, r2), t[j], t[j + 1]);
-          t8_unpack(t8_fma2(t8_mul2(t8_pack(t[j + 2], t[j + 3]), k.y), f2, r2), t[j + 2], t[j + 3]);
+          // (both factors first: the product of huge keys with tiny queries stays in range)
+          t8_unpack(t8_fma2(t8_pack(t[j], t[j + 1]), t8_mul2(k.x, f2), r2), t[j], t[j + 1]);
+          t8_unpack(t8_fma2(t8_pack(t[j + 2], t[j + 3]), t8_mul2(k.y, f2), r2), t[j + 2], t[j + 3]);
         }
         if (!whole) {
 #pragma unroll

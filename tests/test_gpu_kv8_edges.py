@@ -302,3 +302,13 @@ def test_threads_with_batches_of_different_sizes(kernel):
         t.join()
     sys.setswitchinterval(interval)
     assert not wrong, wrong
+
+
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("power", [-50, 60, 110, 120])
+def test_keys_of_all_magnitudes_of_the_format(kernel, power):
+    """Huge keys under tiny queries, and the other way round: ordinary scores."""
+    g = torch.Generator().manual_seed(9)
+    k, v = torch.randn(400, 2, 128, generator=g), torch.randn(400, 2, 128, generator=g)
+    q = ref.make_q(1, 3, 8, 128, 10) * 2.0 ** -power
+    attend_like_one(one_sequence(k * 2.0 ** power, v), 4, q, kernel)
