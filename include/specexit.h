@@ -153,9 +153,11 @@ typedef struct {
 /* Element type of the cache.  SX_KV_E4M3 keeps a row (one token of one KV head) as e4m3 codes with one power-of-two
  * scale 2^e, e = ceil(log2(max |x| / 448)) held to [-64, 120] (0 for a row of zeros), stored as the byte e + 127;
  * code = e4m3(x * 2^-e), round to nearest even.  x * 2^-e and code * 2^e are exact, so the rounding to 4
- * significand bits is all that is lost (values below 2^-10 of a row's largest keep fewer).  A row with a value
- * that is not finite has the byte 255 and codes of zero, and reads as NaN.  Half the bytes of bf16 and one byte
- * per row.  Needs a page size that is a multiple of 16; attention (the draft step's too) needs head_dim 64 or 128.
+ * significand bits is all that is lost (values below 2^-10 of a row's largest keep fewer; a value from 248 * 2^120 up
+ * rounds to 2^128 and reads as infinity).  A row with a value that is not finite has the byte 255 and codes of zero, and
+ * reads as NaN.  A cache that something else has written must not hold 0x7f or 0xff in a row that is seen.  Half the
+ * bytes of bf16 and one byte per row.  Needs a page size that is a multiple of 16; attention (the draft step's too) needs
+ * head_dim 64 or 128.
  * A draft call takes the kind of cache that sx_set_cache named.  With a bf16 one only the first seven fields of sx_kv mean
  * anything (but dtype must not be SX_KV_E4M3); the struct is larger than it was without 8-bit caches, so code built against
  * that header has to be built again. */
@@ -328,23 +330,26 @@ sx_status sx_kv_read(const sx_kv_shape *shape, const sx_kv *kv, int32_t T, const
 /* Decode attention over an 8-bit cache (no context needed; the draft step runs the same kernels when it is given such a
  * cache).  Sequence b has `rows` query rows (1..64), row r = b * rows + j, each with n_q_heads heads; a row sees the
  * slots [0, cache_len_d[b]) and, of the `drafted` (0..64) slots behind them, those whose bit is set in row_mask_d[r]
- * (NULL: all).  Softmax of scale * q.k; an output row that sees no slot is zero.  What a slot holds that a row
- * does not see never reaches that row, whatever it is.  A page that does not exist, or a cache_len that the table cannot
- * hold, is reported as SX_ERR_CAPACITY; the slots of such a page count as rows of zeros, and the other sequences are served.
+ * (NULL: all).  Softmax of scale * q.k, with q exact down to 2^-13 of its row's largest value and to 2^-21 of that
+ * value below; an output row that sees no slot is zero.  The scales of the value rows that a query row sees have to lie
+ * within 2^100 of one another: SX_ATTN_SPLIT loses the weight of smaller ones.  What a slot holds that a row does not see
+ * never reaches that row, whatever it is.  A page that does not exist, or a cache_len that the table cannot hold, is
+ * reported as SX_ERR_CAPACITY; the slots of such a page count as rows of zeros, and the other sequences are served.
  *   q_d [batch * rows, n_q_heads, head_dim] bf16, q_stride elements from row to row (a multiple of 8)
  *   o_d [batch * rows, n_q_heads, head_dim] bf16
  * head_dim 64 or 128; n_q_heads a multiple of n_kv_heads; batch + n_groups <= 1024, batch * rows <= 65535.
  *
  * Shared prefix (kv->n_groups > 0): the members of a group hold the same keys and values in their first
  * prefix_len_d[g] slots - sampled answers to one question.  Those slots are read through the page table of the group's
- * first member, for the queries of all members together; every member's own slots follow from its own table, which
- * needs no pages for the rest.  Whether the tables share the pages makes no difference to the result.  prefix_len_d[g]
- * may end inside a page and may be 0.  A prefix longer than a member's cache_len, or groups that do not cover the batch
- * in order, are reported as SX_ERR_CAPACITY and the sequences concerned read their own tables.
+ * first member, for the queries of all members together: once for every 128 of them per KV head where SX_ATTN_TC runs
+ * (chosen by the average group), else once for every 16.  Every member's own slots follow from its own table, which needs
+ * no pages for the rest.  Whether the tables share the pages makes no difference to the result.  prefix_len_d[g] may end
+ * inside a page and may be 0.  A prefix longer than a member's cache_len, or groups that do not cover the batch in order,
+ * are reported as SX_ERR_CAPACITY and the sequences concerned read their own tables.
  *
  * kernel: SX_ATTN_AUTO, or SX_ATTN_SPLIT / SX_ATTN_TC to force one (see sx_set_attention; SX_ATTN_TC needs head_dim 128, a
- * pool of less than 2^31 rows and a batch of at most about 500).  Workspace (256-byte aligned, not shared by calls that may overlap): sx_attention_ws_bytes for the
- * current device, or 0 for a shape that cannot be. */
+ * pool of less than 2^31 rows and a batch of at most about 500).  Workspace (256-byte aligned, not shared by calls that
+ * may overlap): sx_attention_ws_bytes for the current device, or 0 for a shape that cannot be. */
 size_t sx_attention_ws_bytes(const sx_kv_shape *shape, int32_t batch, int32_t rows, int32_t n_groups);
 sx_status sx_attention(const sx_kv_shape *shape, const sx_kv *kv, int32_t rows, int32_t drafted, const void *q_d,
                        int64_t q_stride, const uint64_t *row_mask_d, float scale, int32_t kernel, void *o_d, void *ws_d,

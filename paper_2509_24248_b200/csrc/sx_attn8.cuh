@@ -24,8 +24,7 @@
 #define A8_MERGE_THREADS 256
 // How far (in powers of two) a score may exceed its reference before the reference moves.  A weight then stays below
 // 2^14 in fp16, whose subnormals reach down to 2^-24: whatever a row's largest weight is between 1 and 2^14, weights
-// are held to 2^-25 of it or better.  With 2^8 the reference moved in most blocks of a prefix with 128 queries
-// whose scores spread over 2^4 (one query that exceeds is enough).
+// are held to 2^-25 of it or better.  One query that exceeds is enough to make a warp look at all of them.
 #define A8_SLACK 14.f
 // The tensor-memory kernel's partial outputs are in units of 2^A8_V_SHIFT (sx_attn8_tc.cu)
 #define A8_V_SHIFT 50

@@ -30,8 +30,9 @@
 //
 // Measured: 2700 to 3100 cycles per block with 128 queries (the softmax warps: two thirds of the issue slots, half of the
 // exponential unit), 2450 with 32 (the chain first product, softmax, second product, beside the widening of V), 5 us to the
-// first block and 3 to 5 us for the end of a segment.  4 x 32768 slots of 8 heads under 32 queries: 98 us with the merge,
-// 2.8 TB/s; a prefix of 30001 slots under 256 queries, own slots and merge: 95 us, 350 TFLOP/s.
+// first block and 3 to 5 us for the end of a segment.  4 x 32768 slots of 8 heads under 32 queries: 98 us with the merge in a
+// graph of calls, 2.8 TB/s (108 us as a call of its own); a prefix of 30001 slots under 256 queries, own slots and merge: 97 us,
+// 340 TFLOP/s.
 //
 // Warps: 0 K producer, 1 issuer of the first product (owns TMEM), 2 V producer, 3 issuer of the second, 4-11 softmax,
 // 12-19 widen V, lay out the scales of K and load Q.  Every mbarrier wait is bounded (sx_tc_ptx.cuh).
@@ -503,7 +504,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       if (lane == 0) mbar_arrive(smem_u32(&wfull[wb]));
     }
   } else {
-    // ---- softmax: group g takes blocks g, g + 2, ...; a thread owns query (TMEM lane) i --------------------------------
+    // ---- softmax: group g takes half g of every block; a thread owns query (TMEM lane) i --------------------------------
     t8_setreg_inc<128>();       // 56 + 2 x 128 + 2 x 80 <= 5 x 96, what the block was launched with
     const int g = (warp - 4) >> 2, w = warp & 3, i = w * 32 + lane;
     const int copy = i / QT, query = i % QT;

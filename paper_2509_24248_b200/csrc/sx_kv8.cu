@@ -4,7 +4,7 @@
 //     e = ceil(log2(max |x| / 448)), held to [-64, 120]; 0 for a row of zeros,   stored as the byte e + 127,
 // and its codes are e4m3(x * 2^-e), round to nearest even.  448 = 1.75 * 2^8 is the largest e4m3 value, so e follows from
 // the exponent and the top of the mantissa of max |x| alone, x * 2^-e is exact, and a code times its scale is exact in
-// bf16 again: nothing but the rounding to 4 significand bits happens, the same on every path that writes a row.  A row
+// bf16 again (but for values from 248 * 2^120 up, which round to 2^128): nothing but the rounding to 4 significand bits happens, the same on every path that writes a row.  A row
 // with a value that is not finite gets the byte 255 and codes of zero; readers turn the byte into NaN.
 //
 // Both kernels are bound by bytes: 4 d + 2 d + 2 per token and head.  A CTA takes a few consecutive rows of the
