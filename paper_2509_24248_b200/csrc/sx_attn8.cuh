@@ -27,7 +27,7 @@
 // are held to 2^-25 of it or better.  One query that exceeds is enough to make a warp look at all of them.
 #define A8_SLACK 14.f
 // The tensor-memory kernel's partial outputs are in units of 2^A8_V_SHIFT (sx_attn8_tc.cu)
-#define A8_V_SHIFT 50
+#define A8_V_SHIFT 44
 
 struct SxA8List {                  // one list: what the main kernel writes down for the merge
   int32_t *cum;                    // [units] first list position of the unit (the host has checked that lists fit)

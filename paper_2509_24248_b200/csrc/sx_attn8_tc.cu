@@ -7,13 +7,14 @@
 //     S[q][slot] = sum_d Q[q][d] kc[slot][d]         A = Q, B = K codes as they lie in the pages (both K-major)
 //     O[q][d]   += sum_slot P[q][slot] V[slot][d]    A = P from tensor memory, B = V as bf16 (N-major)
 // First product: a bf16 query, its row scaled by a power of two, is the sum of an e4m3 and an e5m2 number (a8_split); so A is
-// [high part] then [low part] into the same accumulator - the cost of one bf16 product, and K is used as it was
-// stored; its scale is a factor of the slot's scores.  Second product: weights need 16 bits (in 8 a long flat tail of small weights would vanish), so V becomes
-// bf16 in shared memory, exactly (4 significand bits, a power of two), by eight warps of their own, once per block
-// whatever the number of queries: a code's exponent and mantissa are moved to their places in a bf16 number and one packed
-// multiplication by 2^(120 + e - A8_V_SHIFT) puts bias and scale right.  The shift leaves room for the sums: weights reach
-// 2^T8_SLACK and values 2^129, and without it 600 slots of 2^110 whose scores rise became infinity - infinity; with it 2^19
-// slots of any values are held, and the smallest codes of the smallest scale, 2^-123, are still normal numbers.
+// [high part] then [low part] into the same accumulator - the cost of one bf16 product, and K is used as it was stored;
+// its scale is a factor of the slot's scores.  Second product: weights need 16 bits (in 8 a long flat tail of small weights
+// would vanish), so V becomes bf16 in shared memory, exactly (4 significand bits, a power of two), by eight warps of
+// their own, once per block whatever the number of queries: a code's exponent and mantissa are moved to their places in a
+// bf16 number and one packed multiplication by 2^(120 + e - A8_V_SHIFT) puts bias and scale right.  The shift leaves room
+// for the sums: weights reach 2^T8_SLACK and values 2^129, and without it 600 slots of 2^110 whose scores rise became
+// infinity - infinity; with it 2^19 slots of any values are held, and the smallest codes of the smallest scale, 2^-117, are
+// still normal numbers.
 // (Tried before: slots on M, so that a thread owned a slot and the softmax ran across threads - a barrier vote per block,
 // weights through shared memory, a reference per query to fetch for every score: 6500 cycles per block with 128 queries,
 // 3400 with 32.  V as fp16 codes with its scale in the score and a second factor in the sums: three broadcasts from
@@ -31,14 +32,15 @@
 // Measured: 2700 to 3100 cycles per block with 128 queries (the softmax warps: two thirds of the issue slots, half of the
 // exponential unit), 2450 with 32 (the chain first product, softmax, second product, beside the widening of V), 5 us to the
 // first block and 3 to 5 us for the end of a segment.  4 x 32768 slots of 8 heads under 32 queries: 98 us with the merge in a
-// graph of calls, 2.8 TB/s (108 us as a call of its own); a prefix of 30001 slots under 256 queries, own slots and merge: 97 us,
-// 340 TFLOP/s.
+// graph of calls, 2.8 TB/s (108 us as a call of its own); a prefix of 30001 slots under 256 queries, own slots and merge: 96 us,
+// 345 TFLOP/s.
 //
 // Warps: 0 K producer, 1 issuer of the first product (owns TMEM), 2 V producer, 3 issuer of the second, 4-11 softmax,
 // 12-19 widen V, lay out the scales of K and load Q.  Every mbarrier wait is bounded (sx_tc_ptx.cuh).
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
+#include <float.h>
 #include <math.h>
 
 #include "sx_attn8.cuh"
@@ -50,8 +52,9 @@
 #define T8_BLK (128 * 128)               // bytes of the codes of a block
 #define T8_NONE (-3e38f)                 // reference before the first visible score
 // Weights are bf16, sums fp32: their precision does not depend on where the reference lies, so it moves only where the
-// range of numbers asks for it.
-#define T8_SLACK 30.f
+// range of numbers asks for it: 2^T8_SLACK below, 2^129 for a value, 2^19 slots and A8_V_SHIFT off fill fp32 to the top, and
+// what falls off its bottom is below 2^-105 (values of 1 behind a sink of zeros 72 nats above).
+#define T8_SLACK 24.f
 #define T8_NK 4                          // ring slots of 16 KB for the codes of K,
 #define T8_NV 3                          // of V
 #define T8_NW 2                          // bf16 copies (32 KB) of V blocks
@@ -222,6 +225,11 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(xfull + 1);
   static_assert(COPIES == 1 || COPIES == 2 || COPIES == 4, "rows of a product hold whole copies");
   constexpr int QT = 128 / COPIES, CH = 64 / COPIES;       // queries of a copy; its slots of a group's half
+  // A product of codes reaches 2^25 and a scale of K 2^120, which fp32 does not hold.  With 128 queries part of the scale is
+  // left to the query's factor; with fewer both factors are multiplied first, which needs no shift and is done before the
+  // product arrives (tree 98 against 101 us; but a prefix under 256 queries 98 against 96 us).
+  constexpr bool FACTORS_FIRST = COPIES > 1;
+  constexpr float K_SHIFT = FACTORS_FIRST ? 1.f : 131072.f;
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -428,7 +436,11 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             uint8_t *at = sQ + q * 128 + ((c ^ (q & 7)) << 4);
             *reinterpret_cast<uint4 *>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
             *reinterpret_cast<uint4 *>(at + T8_Q_BYTES) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-            if (c == 0) qf[buf * 128 + q] = __uint_as_float((uint32_t)(127 + ex) << 23) * p.scale_log2;
+            // (held to finite numbers: under a query that large every score is beyond telling apart)
+            if (c == 0) {
+              const float f = __uint_as_float((uint32_t)(127 + ex) << 23) * p.scale_log2 * K_SHIFT;
+              qf[buf * 128 + q] = fminf(fmaxf(f, -FLT_MAX), FLT_MAX);
+            }
           }
         }
         fence_async_smem();
@@ -442,7 +454,7 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       // a row of K or V that is not finite makes the slot's scores so (whoever sees the slot gets it, whoever does not is
       // spared); such a V is zero here
       const int kbyte = kbytes[tid], vbyte = vbytes[tid];
-      ks_sh[e * 128 + tid] = kbyte == 255 || vbyte == 255 ? __int_as_float(0x7fffffff) : a8_pow2(kbyte);
+      ks_sh[e * 128 + tid] = kbyte == 255 || vbyte == 255 ? __int_as_float(0x7fffffff) : a8_pow2(kbyte) * (1.f / K_SHIFT);
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&cfull[e]));
       // Chunks 2c and 2c + 1 of the half; the lanes of the second half go the other way round, so that the eight lanes of a row
@@ -549,9 +561,9 @@ sx_attn8_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 #pragma unroll
         for (int j = 0; j < CH; j += 4) {
           const ulonglong2 k = kb[j >> 2];
-          // (both factors first: the product of huge keys with tiny queries stays in range)
-          t8_unpack(t8_fma2(t8_pack(t[j], t[j + 1]), t8_mul2(k.x, f2), r2), t[j], t[j + 1]);
-          t8_unpack(t8_fma2(t8_pack(t[j + 2], t[j + 3]), t8_mul2(k.y, f2), r2), t[j + 2], t[j + 3]);
+          const f32x2 ta = t8_pack(t[j], t[j + 1]), tb = t8_pack(t[j + 2], t[j + 3]);
+          t8_unpack(FACTORS_FIRST ? t8_fma2(ta, t8_mul2(k.x, f2), r2) : t8_fma2(t8_mul2(ta, k.x), f2, r2), t[j], t[j + 1]);
+          t8_unpack(FACTORS_FIRST ? t8_fma2(tb, t8_mul2(k.y, f2), r2) : t8_fma2(t8_mul2(tb, k.y), f2, r2), t[j + 2], t[j + 3]);
         }
         if (!whole) {
 #pragma unroll

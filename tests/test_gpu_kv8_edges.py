@@ -128,6 +128,16 @@ def test_nothing_but_value_rows_of_zeros(kernel):
     assert (got == 0).all()
 
 
+@pytest.mark.parametrize("kernel", KERNELS)
+@pytest.mark.parametrize("n", [5, 256])
+@pytest.mark.parametrize("size,gap", [(1.0, 64), (1.0, 68), (16.0, 70), (2.0 ** 40, 84)])
+def test_a_value_row_of_zeros_far_above_the_rest(kernel, n, size, gap):
+    """Outputs down to 2^-98: every one of the other slots still counts.  (Its weight is a number of 32 bits, so the gap ends
+    at 2^-126 = e^-87.)"""
+    q, k, v = with_gap(n, 2, 4, 128, [0], gap, size, 11)
+    attend_like_one(one_sequence(k, v), 33, q, kernel)
+
+
 @pytest.mark.parametrize("size", [2.0 ** 60, 2.0 ** 100])
 @pytest.mark.parametrize("gap", [0, 12, 40])
 def test_a_value_row_of_zeros_beside_huge_ones(size, gap):
