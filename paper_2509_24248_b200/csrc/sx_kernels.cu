@@ -273,7 +273,7 @@ __global__ void sx_finish_qkv_rope_kernel(int nq, int nkv, int d, double theta, 
   const int slot = ri.n + ri.rel;
   const int lp = slot / page, off = slot % page;
   int pp = -1;
-  if (lp < kv.max_pages) pp = kv.page_table_d[(size_t)ri.b * kv.max_pages + lp];
+  if (slot >= 0 && lp < kv.max_pages) pp = kv.page_table_d[(size_t)ri.b * kv.max_pages + lp];
   if (pp < 0 || pp >= kv.num_pages) {
     if (i == 0) sx_set_status(status, SX_ERR_CAPACITY);
     return;

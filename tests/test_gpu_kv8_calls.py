@@ -91,3 +91,26 @@ def test_strides_of_single_heads_do_not_matter():
         c.check_status()
     for a, b in zip(*got):
         assert torch.equal(a, b)
+
+
+def test_a_draft_step_behind_a_negative_length_writes_nothing():
+    """Such a sequence's new row has no place: reported, its pages and everyone else's as they were."""
+    wl = synth.Workload(shape=SHAPE, B=2, **CHAIN)
+    case = harness.build_case(wl, poison_tail=False)
+    sx = binding.SpecExit(SHAPE, case.weights, 2, wl.mode, wl.K, kv_dtype=binding.KV_E4M3)
+    sx.set_kv(as_codes(case.kv))
+    sx.kv["cache_len"][1] = -5
+    before = {n: t.clone() for n, t in sx.kv.items()}
+    hid, *_ = sx.sx_draft_step(1, case.f0.to(sx.dev), case.t0.to(sx.dev))
+    with pytest.raises(binding.SxError):
+        sx.check_status()
+    n, page = int(before["cache_len"][0]), SHAPE.page
+    pp, off = int(before["page_table"][0, n // page]), n % page
+    for name in ("k_pages", "v_pages", "k_scale", "v_scale"):
+        before[name][pp, :, off] = sx.kv[name][pp, :, off]          # the first sequence's new row
+        assert torch.equal(before[name], sx.kv[name]), name
+    ok = binding.SpecExit(SHAPE, case.weights, 2, wl.mode, wl.K, kv_dtype=binding.KV_E4M3)
+    ok.set_kv(as_codes(case.kv))
+    want, *_ = ok.sx_draft_step(1, case.f0.to(sx.dev), case.t0.to(sx.dev))
+    ok.check_status()
+    assert torch.equal(hid[0], want[0])
