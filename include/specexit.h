@@ -321,6 +321,60 @@ sx_status sx_kv_append(const sx_kv_shape *shape, const sx_kv *kv, int32_t T, con
                        const int32_t *pos_start_d, const void *k_d, int64_t k_stride, const void *v_d, int64_t v_stride,
                        int32_t *status_d, void *stream);
 
+/* Rotary positions.  A head's rotated part, rot_dim elements from rot_start on, is rot_dim / 2 pairs: (x[i], x[i + rot_dim / 2])
+ * in SX_ROPE_HALF, (x[2 i], x[2 i + 1]) in SX_ROPE_INTERLEAVED; the other elements of the head stay as they are.  At position
+ * pos pair i = (u, v) becomes magnitude * (u cos a - v sin a, v cos a + u sin a), a = pos * f_i, modulo one turn exact to
+ * pos * 2^-64 turns; cos, sin and products are fp32, the result is rounded once.  f_i = theta^(-2 i / rot_dim), and with a
+ * scaling for contexts longer than the trained one (F = factor, n_i = original_len * f_i / 2 pi turns over the trained length):
+ *   SX_ROPE_LINEAR  f_i / F
+ *   SX_ROPE_BASE    theta becomes theta * F^(rot_dim / (rot_dim - 2))
+ *   SX_ROPE_BANDS   f_i where n_i >= high, f_i / F where n_i <= low, between them w f_i + (1 - w) f_i / F with
+ *                   w = (n_i - low) / (high - low)
+ *   SX_ROPE_RAMP    (1 - w_i) f_i + w_i f_i / F; w_i rises from 0 to 1 between i = max(floor(at(high)), 0) and
+ *                   i = min(ceil(at(low)), rot_dim - 1), at(n) = rot_dim ln(original_len / (2 pi n)) / (2 ln theta).  The
+ *                   factor on the attention's logits that goes with it is magnitude's square
+ *   SX_ROPE_LIST    f_i / divisors[i]
+ * sx_rope_plan (host only) makes a plan of it, which the caller keeps and which calls copy.  head_dim: a multiple of 8 up to
+ * SX_ROPE_MAX_HEAD; rot_dim and rot_start even. */
+enum { SX_ROPE_HALF = 0, SX_ROPE_INTERLEAVED = 1 };
+enum { SX_ROPE_NONE = 0, SX_ROPE_LINEAR = 1, SX_ROPE_BASE = 2, SX_ROPE_BANDS = 3, SX_ROPE_RAMP = 4, SX_ROPE_LIST = 5 };
+enum { SX_BF16 = 0, SX_F16 = 1, SX_F32 = 2 };       /* element types of the calls that take several */
+#define SX_ROPE_MAX_HEAD 256
+#define SX_ROPE_MAX_PAIRS (SX_ROPE_MAX_HEAD / 2)
+#define SX_ROPE_MAX_ROWS 4096                       /* heads of a token in one call */
+#define SX_ROPE_READY 0x526f5065
+typedef struct {
+  int32_t head_dim, rot_start, rot_dim, layout, scaling, original_len;
+  double theta, factor, low, high, magnitude;       /* magnitude: 1 for a plain rotation */
+  const double *divisors;                           /* SX_ROPE_LIST: host, rot_dim / 2 of them, read by sx_rope_plan alone */
+} sx_rope_cfg;
+typedef struct {
+  int32_t ready, head_dim, rot_start, rot_dim, layout;
+  float magnitude;
+  uint64_t step[SX_ROPE_MAX_PAIRS];                 /* f_i / 2 pi in 2^-64 turns */
+} sx_rotation;
+sx_status sx_rope_plan(const sx_rope_cfg *cfg, sx_rotation *out);
+
+/* Turns queries and keys: row t of both is a token at position pos_d[t] (any int32, negative ones too).
+ *   q_d      [T, n_q, head_dim] of `dtype`, q_stride elements from row to row (rows on 16-byte boundaries); out to q_out_d, which
+ *            may be q_d itself (with the same stride) but not overlap it otherwise.  n_q = 0: no queries.  k likewise
+ *   transpose  1: by the transposed matrix, magnitude included - the gradient of the rotation, and with magnitude 1 its
+ *            inverse, which takes a row back to position 0 */
+sx_status sx_rope(const sx_rotation *plan, int32_t dtype, int32_t transpose, int32_t T, const int32_t *pos_d, int32_t n_q,
+                  const void *q_d, int64_t q_stride, void *q_out_d, int64_t q_out_stride, int32_t n_k, const void *k_d,
+                  int64_t k_stride, void *k_out_d, int64_t k_out_stride, void *stream);
+
+/* sx_kv_append for a cache of either kind (kv->dtype), with the rotation on the way: the keys of every row are turned to the
+ * row's position - rot_pos_d[t], or its slot where rot_pos_d is NULL - rounded to bf16 and written to their pages, as codes in
+ * an 8-bit cache; values go as they are.  With q_d the rows' queries (shape->n_q_heads heads, strides as in sx_rope) are turned
+ * in the same launch to q_out_d, which may be q_d.  plan NULL: nothing is turned, the keys are as the attention wants them.
+ * Rows, slots, refusals and reports as in sx_kv_append; rows behind the last sequence stay as they are in q_out_d too, and
+ * of a row that is reported the queries may or may not be written.  head_dim 16, 32, 64 or 128. */
+sx_status sx_kv_append_rope(const sx_rotation *plan, const sx_kv_shape *shape, const sx_kv *kv, int32_t T,
+                            const int32_t *row_start_d, const int32_t *pos_start_d, const int32_t *rot_pos_d, const void *k_d,
+                            int64_t k_stride, const void *v_d, int64_t v_stride, const void *q_d, int64_t q_stride,
+                            void *q_out_d, int64_t q_out_stride, int32_t *status_d, void *stream);
+
 /* The way back: slots pos_start_d[b] .. of every sequence to bf16 rows (exact), arguments as above with the buffers
  * written; pos_start_d is needed.  Rows behind the last sequence, and rows that are reported, stay as they are. */
 sx_status sx_kv_read(const sx_kv_shape *shape, const sx_kv *kv, int32_t T, const int32_t *row_start_d,

@@ -26,6 +26,9 @@ DIR_GT, DIR_LT = 0, 1
 EMA_VERIFIED_CONTEXT, EMA_FIRST_ONLY = 0, 1
 ATTN_AUTO, ATTN_SPLIT, ATTN_TC = 0, 1, 2
 KV_BF16, KV_E4M3 = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_NONE, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS, ROPE_RAMP, ROPE_LIST = 0, 1, 2, 3, 4, 5
+SX_ROPE_MAX_PAIRS = 128
 SMOOTH_EWMA, SMOOTH_NONE, SMOOTH_WINDOW, SMOOTH_MOMENTUM, SMOOTH_PARAGRAPH = 0, 1, 2, 3, 4
 HIST = 16
 
@@ -33,7 +36,8 @@ EXPORTS = ["sx_create", "sx_destroy", "sx_workspace_bytes", "sx_strerror", "sx_l
            "sx_draft_step", "sx_verify", "sx_exit_update", "sx_spec_exit_iter",
            "sx_spec_exit_iter_host", "sx_profile_begin", "sx_profile_end", "sx_verify_noalloc", "sx_commit",
            "sx_set_sampling", "sx_tiled_weight_bytes", "sx_tile_weight", "sx_selftest_bounded_wait", "sx_set_attention",
-           "sx_set_cache", "sx_kv_append", "sx_kv_read", "sx_attention", "sx_attention_ws_bytes"]
+           "sx_set_cache", "sx_kv_append", "sx_kv_read", "sx_attention", "sx_attention_ws_bytes",
+           "sx_rope_plan", "sx_rope", "sx_kv_append_rope"]
 PROF_CLASSES = ["head_draft", "head_verify", "gemm_fc", "gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down",
                 "attention"]
 
@@ -66,6 +70,17 @@ class KV(C.Structure):
 
 class KVShape(C.Structure):
     _fields_ = [("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32)]
+
+
+class RopeCfg(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rot_start", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32),
+                ("scaling", C.c_int32), ("original_len", C.c_int32), ("theta", C.c_double), ("factor", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_double), ("divisors", C.POINTER(C.c_double))]
+
+
+class Rotation(C.Structure):
+    _fields_ = [("ready", C.c_int32), ("head_dim", C.c_int32), ("rot_start", C.c_int32), ("rot_dim", C.c_int32),
+                ("layout", C.c_int32), ("magnitude", C.c_float), ("step", C.c_uint64 * SX_ROPE_MAX_PAIRS)]
 
 
 class DraftCfg(C.Structure):
@@ -157,6 +172,13 @@ def load_library() -> C.CDLL:
     lib.sx_attention.restype = i32
     lib.sx_attention.argtypes = [C.POINTER(KVShape), C.POINTER(KV), i32, i32, vp, i64, vp, C.c_float, i32, vp, vp, sz,
                                  vp, vp]
+    lib.sx_rope_plan.restype = i32
+    lib.sx_rope_plan.argtypes = [C.POINTER(RopeCfg), C.POINTER(Rotation)]
+    lib.sx_rope.restype = i32
+    lib.sx_rope.argtypes = [C.POINTER(Rotation), i32, i32, i32, vp, i32, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp]
+    lib.sx_kv_append_rope.restype = i32
+    lib.sx_kv_append_rope.argtypes = [C.POINTER(Rotation), C.POINTER(KVShape), C.POINTER(KV), i32, vp, vp, vp, vp, i64, vp, i64,
+                                      vp, i64, vp, i64, vp, vp]
     lib.sx_set_cache.restype = i32
     lib.sx_set_cache.argtypes = [vp, i32]
     lib.sx_verify_noalloc.restype = i32
@@ -295,21 +317,96 @@ def _raw_stream(dev: torch.device) -> int:
     return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
-class KV8:
-    """An 8-bit paged cache and the operators over it (no draft model needed).
+_FLOATS = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}       # SX_BF16, SX_F16, SX_F32
 
-    ``kv`` holds ``k_pages`` / ``v_pages`` (uint8 or float8_e4m3fn ``[num_pages, n_kv, page, d]``), ``k_scale`` /
-    ``v_scale`` (uint8 ``[num_pages, n_kv, page]``), ``page_table`` (int32 ``[B, max_pages]``), ``cache_len`` (int32
-    ``[B]``) and, for sequences that share a prefix, ``group_start`` (int32 ``[n_groups + 1]``) with ``prefix_len``
-    (int32 ``[n_groups]``).  The tensors are borrowed; what they hold may change between calls.  Work goes to the
-    current stream of their device.  The object owns the attention's workspace: use one per stream, and one per captured
-    graph that may run beside others, and keep it as long as graphs captured through it."""
+
+def _guard_of(dev: torch.device):
+    """`dev` becomes the current device for a launch (entering a device costs more than the launch does, so only where
+    another one is current)."""
+    return _NO_GUARD if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+
+
+def _heads_stride(name: str, t: torch.Tensor, dtype: torch.dtype, heads: int, d: int, dev: torch.device, rows: int = -1) -> int:
+    """Row stride of ``t [T, heads, d]`` whose heads lie side by side."""
+    shape, stride = t.shape, t.stride()
+    if (len(shape) != 3 or shape[1] != heads or shape[2] != d or (rows >= 0 and shape[0] != rows) or (stride[2] != 1 and d > 1)
+            or (stride[1] != d and heads > 1) or t.dtype is not dtype or t.device != dev):
+        raise SxError(f"{name} must be {dtype} [{'T' if rows < 0 else rows}, {heads}, {d}] on {dev}, rows of heads contiguous")
+    return stride[0] if shape[0] > 1 else heads * d
+
+
+class Rope:
+    """Rotary positions: a plan made once on the host (``sx_rope_plan``), and the rotation of queries and keys by it.
+
+    ``rot_dim`` elements of a head from ``rot_start`` on turn (default: all of it), as pairs ``(i, i + rot_dim / 2)``
+    (``ROPE_HALF``) or ``(2i, 2i + 1)`` (``ROPE_INTERLEAVED``).  ``scaling`` stretches the frequencies for contexts longer than
+    ``original_len``: ``ROPE_LINEAR``, ``ROPE_BASE``, ``ROPE_BANDS`` and ``ROPE_RAMP`` by ``factor`` (the last two with the bounds
+    ``low`` and ``high``, in turns over the trained length), ``ROPE_LIST`` by ``divisors``, one per pair.  ``magnitude``
+    multiplies the rotated part.  The plan lives on the host and fits every device and stream."""
+
+    def __init__(self, head_dim: int, theta: float, rot_dim: Optional[int] = None, rot_start: int = 0, layout: int = ROPE_HALF,
+                 scaling: int = ROPE_NONE, factor: float = 1.0, low: float = 1.0, high: float = 32.0, original_len: int = 0,
+                 magnitude: float = 1.0, divisors=None):
+        self.lib = load_library()
+        rot_dim = head_dim if rot_dim is None else rot_dim
+        table = None
+        if divisors is not None:
+            if scaling != ROPE_LIST or len(divisors) != rot_dim // 2:
+                raise SxError(f"divisors belong to ROPE_LIST, {rot_dim // 2} of them")
+            table = (C.c_double * len(divisors))(*[float(v) for v in divisors])
+        cfg = RopeCfg(head_dim, rot_start, rot_dim, layout, scaling, original_len, theta, factor, low, high, magnitude, table)
+        self.plan = Rotation()
+        self.plan_ref = C.byref(self.plan)
+        _check(self.lib.sx_rope_plan(C.byref(cfg), self.plan_ref), "sx_rope_plan")
+        self.d = head_dim
+
+    def sx_rope(self, pos: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                k_out: Optional[torch.Tensor] = None, transpose: bool = False):
+        """Turns ``q [T, n_q, d]`` and, in the same launch, ``k [T, n_k, d]`` (bf16, fp16 or fp32, slices of a projection's
+        output will do) to the positions ``pos`` (int32 ``[T]``) and returns both.  An output may be its input itself;
+        ``transpose`` turns by the transposed matrix (the gradient, and with magnitude 1 the way back to position 0)."""
+        dev, T = q.device, q.shape[0]
+        if not q.is_cuda or q.dtype not in _FLOATS or q.dim() != 3:
+            raise SxError("q must be bf16, fp16 or fp32 [T, n_q, d] on a device")
+        if pos.dtype is not torch.int32 or pos.device != dev or pos.shape != (T,) or (T > 1 and pos.stride(0) != 1):
+            raise SxError(f"pos must be int32 [{T}] on {dev}, contiguous")
+        if k is None and k_out is not None:
+            raise SxError("k_out without k")
+        args = []
+        for name, x, y in (("q", q, q_out), ("k", k, k_out)):
+            if x is None:
+                args += [0, None, 0, None, 0]
+                continue
+            y = torch.empty(x.shape, dtype=x.dtype, device=dev) if y is None else y
+            n = x.shape[1] if x.dim() == 3 else -1
+            args += [n, x.data_ptr(), _heads_stride(name, x, q.dtype, n, self.d, dev, T), y.data_ptr(),
+                     _heads_stride(name + "_out", y, q.dtype, n, self.d, dev, T)]
+            if name == "q":
+                q_out = y
+            else:
+                k_out = y
+        if T == 0:
+            return q_out, k_out
+        with _guard_of(dev):
+            _check(self.lib.sx_rope(self.plan_ref, _FLOATS[q.dtype], 1 if transpose else 0, T, pos.data_ptr(), *args,
+                                    _raw_stream(dev)), "sx_rope")
+        return q_out, k_out
+
+
+class KVPages:
+    """A paged cache of either kind and the writing of rows into it (no draft model needed).
+
+    ``kv`` holds ``k_pages`` / ``v_pages`` (bf16, or uint8 / float8_e4m3fn codes, ``[num_pages, n_kv, page, d]``),
+    ``page_table`` (int32 ``[B, max_pages]``), ``cache_len`` (int32 ``[B]``) and for codes ``k_scale`` / ``v_scale`` (uint8
+    ``[num_pages, n_kv, page]``): the tensors of :class:`KV8` or of :meth:`SpecExit.set_kv` (``KVPages(spec.kv)`` writes a prompt
+    into a draft layer's cache).  The tensors are borrowed; what they hold may change between calls.  Work goes to the
+    current stream of their device."""
 
     def __init__(self, kv: Dict[str, torch.Tensor]):
         self.lib = load_library()
         self.kv = {n: kv[n] for n in _CACHE_NAMES if kv.get(n) is not None}
-        if kv["k_pages"].dim() != 4 or kv["k_pages"].element_size() != 1:
-            raise SxError("k_pages must be 8-bit codes [num_pages, n_kv, page, d]")
+        if kv["k_pages"].dim() != 4:
+            raise SxError("k_pages must be [num_pages, n_kv, page, d]")
         self.n_kv, self.page, self.d = (int(v) for v in kv["k_pages"].shape[1:])
         self.dev = kv["k_pages"].device
         self._kv = _kv_struct(self.kv, self.n_kv, self.page, self.d)
@@ -318,8 +415,6 @@ class KV8:
         self.status = torch.zeros(1, dtype=torch.int32, device=self.dev)
         self._shape = KVShape(self.n_kv, self.n_kv, self.d, self.page)
         self._shape_ref = C.byref(self._shape)
-        # a captured graph goes on using the workspace it was captured with, so one that became too small is kept
-        self._ws, self._ws_at, self._ws_bytes, self._ws_for = [], 0, 0, None
 
     def check_status(self, what: str = "device") -> None:
         code = int(self.status.item())
@@ -344,9 +439,56 @@ class KV8:
         return t.stride(0) if t.shape[0] > 1 else self.n_kv * self.d
 
     def _guard(self):
-        """The cache's device becomes the current one for a launch (entering a device costs more than the launch does, so
-        only where another one is current)."""
-        return _NO_GUARD if torch.cuda.current_device() == self.dev.index else torch.cuda.device(self.dev)
+        return _guard_of(self.dev)
+
+    def sx_kv_append_rope(self, rope: Optional[Rope], k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor,
+                          pos_start: Optional[torch.Tensor] = None, rot_pos: Optional[torch.Tensor] = None,
+                          q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """Rows ``row_start[b] .. row_start[b + 1] - 1`` of ``k`` / ``v`` (bf16 ``[T, n_kv, d]``) become slots ``pos_start[b] ..``
+        of sequence ``b`` (default: behind ``cache_len``, which is not advanced), the keys turned by ``rope`` to their slots or to
+        ``rot_pos`` (int32 ``[T]``); ``rope=None`` turns nothing.  The rows' queries ``q [T, n_q, d]`` are turned in the same
+        launch and returned (in ``q_out``, which may be ``q``; rows behind the last sequence stay as they are there)."""
+        T = self._rows(k, v, row_start, pos_start)
+        if rope is not None and rope.d != self.d:
+            raise SxError(f"rope is planned for heads of {rope.d}, the cache has {self.d}")
+        if rot_pos is not None and (rot_pos.dtype is not torch.int32 or rot_pos.device != self.dev or rot_pos.shape != (T,)
+                                    or not rot_pos.is_contiguous()):
+            raise SxError(f"rot_pos must be int32 [{T}] on {self.dev}")
+        if q is None and q_out is not None:
+            raise SxError("q_out without q")
+        nq, args = 0, (None, 0, None, 0)
+        if q is not None:
+            nq = q.shape[1] if q.dim() == 3 else -1
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=self.dev) if q_out is None else q_out
+            args = (q.data_ptr(), _heads_stride("q", q, torch.bfloat16, nq, self.d, self.dev, T), q_out.data_ptr(),
+                    _heads_stride("q_out", q_out, torch.bfloat16, nq, self.d, self.dev, T))
+        if T == 0:
+            return q_out
+        with self._guard():
+            self._shape.n_q_heads = nq
+            _check(self.lib.sx_kv_append_rope(None if rope is None else rope.plan_ref, self._shape_ref, self._kv_ref, T,
+                                              row_start.data_ptr(), _p(pos_start), _p(rot_pos), k.data_ptr(), self._stride(k),
+                                              v.data_ptr(), self._stride(v), *args, self.status.data_ptr(),
+                                              _raw_stream(self.dev)), "sx_kv_append_rope")
+        return q_out
+
+
+class KV8(KVPages):
+    """An 8-bit paged cache and the operators over it (no draft model needed).
+
+    ``kv`` holds ``k_pages`` / ``v_pages`` (uint8 or float8_e4m3fn ``[num_pages, n_kv, page, d]``), ``k_scale`` /
+    ``v_scale`` (uint8 ``[num_pages, n_kv, page]``), ``page_table`` (int32 ``[B, max_pages]``), ``cache_len`` (int32
+    ``[B]``) and, for sequences that share a prefix, ``group_start`` (int32 ``[n_groups + 1]``) with ``prefix_len``
+    (int32 ``[n_groups]``).  The tensors are borrowed; what they hold may change between calls.  Work goes to the
+    current stream of their device.  The object owns the attention's workspace: use one per stream, and one per captured
+    graph that may run beside others, and keep it as long as graphs captured through it."""
+
+    def __init__(self, kv: Dict[str, torch.Tensor]):
+        if kv["k_pages"].dim() != 4 or kv["k_pages"].element_size() != 1:
+            raise SxError("k_pages must be 8-bit codes [num_pages, n_kv, page, d]")
+        super().__init__(kv)
+        # a captured graph goes on using the workspace it was captured with, so one that became too small is kept
+        self._ws, self._ws_at, self._ws_bytes, self._ws_for = [], 0, 0, None
 
     def sx_kv_append(self, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor,
                      pos_start: Optional[torch.Tensor] = None) -> None:

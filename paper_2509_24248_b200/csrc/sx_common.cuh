@@ -1,6 +1,7 @@
 // Shared device-side helpers and host/device structs of the speculative-exit kernels.
 #pragma once
 #include <cuda_bf16.h>
+#include <cuda_fp8.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -77,7 +78,7 @@ __device__ __forceinline__ uint32_t sx_pack_index(unsigned long long p) {
 }
 
 // 8-bit cache: exponent byte of a row whose largest magnitude has the bf16 bits `top` (448 = 1.75 * 2^8 is the largest
-// e4m3 value, so the exponent and the top of the mantissa decide), and two codes
+// e4m3 value, so the exponent and the top of the mantissa decide), its inverse scale, and the codes of four bf16 values
 __device__ __forceinline__ int sx_kv8_scale_byte(uint32_t top) {
   if (top == 0) return 127;
   const int e = (int)(top >> 7);
@@ -85,6 +86,12 @@ __device__ __forceinline__ int sx_kv8_scale_byte(uint32_t top) {
   return max(63, e - 8 + ((top & 0x7f) > 96 ? 1 : 0));
 }
 __device__ __forceinline__ float sx_kv8_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }   // 2^(127 - byte)
+__device__ __forceinline__ uint32_t sx_kv8_codes4(uint32_t ab, uint32_t cd, float up) {
+  const float2 x = make_float2(__uint_as_float(ab << 16) * up, __uint_as_float(ab & 0xffff0000u) * up);
+  const float2 y = make_float2(__uint_as_float(cd << 16) * up, __uint_as_float(cd & 0xffff0000u) * up);
+  return (uint32_t)__nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3) |
+         (uint32_t)__nv_cvt_float2_to_fp8x2(y, __NV_SATFINITE, __NV_E4M3) << 16;
+}
 
 __device__ __forceinline__ float sx_warp_sum(float v) {
 #pragma unroll

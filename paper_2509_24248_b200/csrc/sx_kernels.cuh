@@ -13,6 +13,7 @@ struct SxIndex {
 #define SX_TRY(e) do { sx_status _s = (e); if (_s != SX_OK) return _s; } while (0)
 static inline sx_status sx_rc(cudaError_t e) { return e == cudaSuccess ? SX_OK : SX_ERR_CUDA; }
 sx_status sx_kernels_init(int device);
+sx_status sx_kv_check_cache(const sx_kv_shape *sh, const sx_kv *kv);       // a cache of either kind (sx_kv8.cu)
 
 struct SxShape {
   int H, nq, nkv, d, F, V, S, page;

@@ -62,13 +62,6 @@ __device__ __forceinline__ void kv8_places(const SxKv8Rows &p, int t0, int nt, i
   __syncthreads();
 }
 
-__device__ __forceinline__ uint32_t kv8_codes4(uint32_t ab, uint32_t cd, float up) {
-  const float2 x = make_float2(__uint_as_float(ab << 16) * up, __uint_as_float(ab & 0xffff0000u) * up);
-  const float2 y = make_float2(__uint_as_float(cd << 16) * up, __uint_as_float(cd & 0xffff0000u) * up);
-  return (uint32_t)__nv_cvt_float2_to_fp8x2(x, __NV_SATFINITE, __NV_E4M3) |
-         (uint32_t)__nv_cvt_float2_to_fp8x2(y, __NV_SATFINITE, __NV_E4M3) << 16;
-}
-
 template <int D>
 __global__ void __launch_bounds__(KV8_THREADS) sx_kv8_append_kernel(SxKv8Rows p, const bf16 *__restrict__ k, const bf16 *__restrict__ v) {
   constexpr int LPR = D / 8;
@@ -110,7 +103,7 @@ __global__ void __launch_bounds__(KV8_THREADS) sx_kv8_append_kernel(SxKv8Rows p,
       const int byte = sx_kv8_scale_byte(top);
       const float up = sx_kv8_inverse(byte);
       uint2 c = make_uint2(0, 0);
-      if (byte != 255) c = make_uint2(kv8_codes4(x[i].x, x[i].y, up), kv8_codes4(x[i].z, x[i].w, up));
+      if (byte != 255) c = make_uint2(sx_kv8_codes4(x[i].x, x[i].y, up), sx_kv8_codes4(x[i].z, x[i].w, up));
       if (at[i] >= 0) {
         *reinterpret_cast<uint2 *>((is_v[i] ? p.v : p.k) + at[i] * D + lane * 8) = c;
         if (lane == 0) (is_v[i] ? p.vs : p.ks)[at[i]] = (uint8_t)byte;
@@ -174,15 +167,21 @@ __global__ void __launch_bounds__(KV8_THREADS) sx_kv8_read_kernel(SxKv8Rows p, b
 // ---- entry points ------------------------------------------------------------------------------------------------
 static bool aligned16(const void *p) { return p && ((uintptr_t)p & 15) == 0; }
 
-static sx_status check_cache(const sx_kv_shape *sh, const sx_kv *kv) {
+// a cache of either kind
+sx_status sx_kv_check_cache(const sx_kv_shape *sh, const sx_kv *kv) {
   if (!sh || !kv || !kv->cache_len_d || !kv->page_table_d || !aligned16(kv->k_pages_d) || !aligned16(kv->v_pages_d))
     return SX_ERR_INVALID_ARG;
-  if (kv->dtype != SX_KV_E4M3) return SX_ERR_UNSUPPORTED;
-  if (!aligned16(kv->k_scale_d) || !aligned16(kv->v_scale_d)) return SX_ERR_INVALID_ARG;
+  if (kv->dtype != SX_KV_BF16 && kv->dtype != SX_KV_E4M3) return SX_ERR_UNSUPPORTED;
+  if (kv->dtype == SX_KV_E4M3 && (!aligned16(kv->k_scale_d) || !aligned16(kv->v_scale_d))) return SX_ERR_INVALID_ARG;
   if (kv->batch < 1 || kv->max_pages < 1 || kv->num_pages < 1 || sh->n_kv_heads < 1 || sh->page_size < 1) return SX_ERR_INVALID_ARG;
-  if (sh->page_size % 16) return SX_ERR_UNSUPPORTED;
+  if (kv->dtype == SX_KV_E4M3 && sh->page_size % 16) return SX_ERR_UNSUPPORTED;
   if ((int64_t)kv->max_pages * sh->page_size > 0x7fffff00ll) return SX_ERR_UNSUPPORTED;     // slots are 32-bit
   return SX_OK;
+}
+
+static sx_status check_cache(const sx_kv_shape *sh, const sx_kv *kv) {
+  SX_TRY(sx_kv_check_cache(sh, kv));
+  return kv->dtype == SX_KV_E4M3 ? SX_OK : SX_ERR_UNSUPPORTED;
 }
 
 static int sms_of_current_device() {
