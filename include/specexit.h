@@ -451,6 +451,30 @@ sx_status sx_attention(const sx_kv_shape *shape, const sx_kv *kv, int32_t rows, 
  * every drafted row and verify slot are written to the workspace (fp32, batch * (rows + P) * vocab values). */
 sx_status sx_set_sampling(sx_ctx *ctx, float temperature, uint64_t seed, uint32_t offset);
 
+/* Log-probabilities of given tokens, entropy and best alternatives of rows of logits: what a server returns beside the tokens,
+ * and what sx_verify's argmax leaves out.  log p = log softmax(logits / temperature), natural logarithms.
+ *   logits_d   [T, V] of `dtype`, `stride` elements from row to row (any, at least V)
+ *   tok_d      [T, n_given] token ids, n_given 0..SX_MAX_GIVEN; -1: none, its log p is written as 0; another id outside
+ *              [0, V) is reported as SX_ERR_CAPACITY and its log p is NaN
+ *   top        0..SX_MAX_ALTERNATIVES: the largest logits, best first, the lower id first among equals (-0 equals 0); an
+ *              alternative without probability (a logit of -inf, or more asked for than there are) has the id -1 and log p -inf
+ *   out        logp_d [T, n_given], entropy_d [T] (sum of -p log p) or NULL, top_tok_d [T, top], top_logp_d [T, top], either
+ *              of them or both; fp32
+ * Logits of -inf (masked tokens) have no probability; a row of nothing else gives log p -inf and entropy 0.  A row with a NaN
+ * or +inf among its logits gives NaN and ids of -1.  Sums are fp32: results are off by about 1e-6 absolute, and a log p by
+ * 2^-22 of itself.  temperature > 0, and its inverse below 1e30. */
+#define SX_MAX_GIVEN 64
+#define SX_MAX_ALTERNATIVES 32
+#define SX_MAX_SCORE_VOCAB (1 << 24)
+typedef struct {
+  float *logp_d, *entropy_d;
+  int32_t *top_tok_d;
+  float *top_logp_d;
+} sx_logprob_out;
+sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void *logits_d, int64_t stride, int32_t n_given,
+                      const int32_t *tok_d, float temperature, int32_t top, const sx_logprob_out *out, int32_t *status_d,
+                      void *stream);
+
 /* Exit decision (Section 3.3; Appendix A.1).  Walks path slots 0..accept_len; each slot that
  * carries a signal updates the EWMA (all of them, or only the first, per ema_positions); the
  * first slot whose token is a step-split token while the smoothed signals pass ends the

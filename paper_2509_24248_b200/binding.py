@@ -37,7 +37,7 @@ EXPORTS = ["sx_create", "sx_destroy", "sx_workspace_bytes", "sx_strerror", "sx_l
            "sx_spec_exit_iter_host", "sx_profile_begin", "sx_profile_end", "sx_verify_noalloc", "sx_commit",
            "sx_set_sampling", "sx_tiled_weight_bytes", "sx_tile_weight", "sx_selftest_bounded_wait", "sx_set_attention",
            "sx_set_cache", "sx_kv_append", "sx_kv_read", "sx_attention", "sx_attention_ws_bytes",
-           "sx_rope_plan", "sx_rope", "sx_kv_append_rope"]
+           "sx_rope_plan", "sx_rope", "sx_kv_append_rope", "sx_logprobs"]
 PROF_CLASSES = ["head_draft", "head_verify", "gemm_fc", "gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down",
                 "attention"]
 
@@ -81,6 +81,10 @@ class RopeCfg(C.Structure):
 class Rotation(C.Structure):
     _fields_ = [("ready", C.c_int32), ("head_dim", C.c_int32), ("rot_start", C.c_int32), ("rot_dim", C.c_int32),
                 ("layout", C.c_int32), ("magnitude", C.c_float), ("step", C.c_uint64 * SX_ROPE_MAX_PAIRS)]
+
+
+class LogProbOut(C.Structure):
+    _fields_ = [("logp_d", C.c_void_p), ("entropy_d", C.c_void_p), ("top_tok_d", C.c_void_p), ("top_logp_d", C.c_void_p)]
 
 
 class DraftCfg(C.Structure):
@@ -179,6 +183,8 @@ def load_library() -> C.CDLL:
     lib.sx_kv_append_rope.restype = i32
     lib.sx_kv_append_rope.argtypes = [C.POINTER(Rotation), C.POINTER(KVShape), C.POINTER(KV), i32, vp, vp, vp, vp, i64, vp, i64,
                                       vp, i64, vp, i64, vp, vp]
+    lib.sx_logprobs.restype = i32
+    lib.sx_logprobs.argtypes = [i32, i32, i32, vp, i64, i32, vp, C.c_float, i32, C.POINTER(LogProbOut), vp, vp]
     lib.sx_set_cache.restype = i32
     lib.sx_set_cache.argtypes = [vp, i32]
     lib.sx_verify_noalloc.restype = i32
@@ -548,6 +554,72 @@ class KV8(KVPages):
                                          d ** -0.5 if scale is None else scale, kernel, out.data_ptr(), self._ws_at,
                                          self._ws_bytes, self.status.data_ptr(), _raw_stream(self.dev)),
                    "sx_attention")
+        return out
+
+
+class LogProbs:
+    """Log-probabilities of given tokens with the entropy and the best alternatives of every row: from logits, or
+    from hidden states through ``head`` (bf16 ``[rows, H]``, of which the first ``vocab`` are the vocabulary; rows behind it, such as
+    signal rows, are not looked at).  Without a head the object needs nothing but a device, the current one by default.
+
+    Calls return ``{"logp": [T, n_given], "entropy": [T], "top_tok": [T, top], "top_logp": [T, top]}`` (fp32, ids int32; the last
+    two only with ``top > 0``), or fill the tensors of an ``out`` that an earlier call returned.  ``tokens`` is int32 ``[T, n_given]`` or
+    ``[T]``; -1 stands for no token.  Work goes to the current stream of the device."""
+
+    def __init__(self, head: Optional[torch.Tensor] = None, vocab: Optional[int] = None, device=None):
+        self.lib = load_library()
+        self.dev = head.device if head is not None else torch.device(device or f"cuda:{torch.cuda.current_device()}")
+        if self.dev.type != "cuda":
+            raise SxError("a CUDA device is required (there is no CPU fallback)")
+        self.head, self.vocab = head, vocab
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.dev)
+        self._out = LogProbOut()
+        self._out_ref = C.byref(self._out)
+
+    def check_status(self, what: str = "device") -> None:
+        code = int(self.status.item())
+        if code != 0:
+            self.status.zero_()
+            _check(code, what)
+
+    def _results(self, T: int, tokens: Optional[torch.Tensor], top: int, out: Optional[Dict[str, torch.Tensor]]):
+        """(number of given tokens, results), the argument block filled."""
+        n = 0
+        if tokens is not None:
+            n = tokens.shape[1] if tokens.dim() == 2 else 1
+            if (tokens.dtype is not torch.int32 or tokens.device != self.dev or not 1 <= tokens.dim() <= 2 or tokens.shape[0] != T
+                    or not tokens.is_contiguous()):
+                raise SxError(f"tokens must be contiguous int32 [{T}, n_given] or [{T}] on {self.dev}")
+        want = {"logp": (T, n), "entropy": (T,), "top_tok": (T, top), "top_logp": (T, top)}
+        if top == 0:
+            del want["top_tok"], want["top_logp"]
+        if out is None:
+            out = {name: torch.empty(shape, dtype=torch.int32 if name == "top_tok" else torch.float32, device=self.dev)
+                   for name, shape in want.items()}
+        else:
+            for name, shape in want.items():
+                t = out.get(name)
+                if (t is None or tuple(t.shape) != shape or t.dtype != (torch.int32 if name == "top_tok" else torch.float32)
+                        or t.device != self.dev or not t.is_contiguous()):
+                    raise SxError(f"out[{name!r}] must be contiguous {list(shape)} on {self.dev}")
+        o = self._out
+        o.logp_d, o.entropy_d = out["logp"].data_ptr(), out["entropy"].data_ptr()
+        o.top_tok_d, o.top_logp_d = (out["top_tok"].data_ptr(), out["top_logp"].data_ptr()) if top else (None, None)
+        return n, out
+
+    def sx_logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0,
+                    out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+        """Of rows of logits (bf16, fp16 or fp32 ``[T, V]``, any row stride)."""
+        if logits.dim() != 2 or logits.device != self.dev or logits.dtype not in _FLOATS or (logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise SxError(f"logits must be bf16, fp16 or fp32 [T, V] on {self.dev}, rows contiguous")
+        T, V = logits.shape
+        n, out = self._results(T, tokens, top, out)
+        if T == 0:
+            return out
+        with _guard_of(self.dev):
+            _check(self.lib.sx_logprobs(_FLOATS[logits.dtype], T, V, logits.data_ptr(), logits.stride(0) if T > 1 else V, n,
+                                        _p(tokens), temperature, top, self._out_ref, self.status.data_ptr(),
+                                        _raw_stream(self.dev)), "sx_logprobs")
         return out
 
 
