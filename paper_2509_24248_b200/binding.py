@@ -37,7 +37,8 @@ EXPORTS = ["sx_create", "sx_destroy", "sx_workspace_bytes", "sx_strerror", "sx_l
            "sx_spec_exit_iter_host", "sx_profile_begin", "sx_profile_end", "sx_verify_noalloc", "sx_commit",
            "sx_set_sampling", "sx_tiled_weight_bytes", "sx_tile_weight", "sx_selftest_bounded_wait", "sx_set_attention",
            "sx_set_cache", "sx_kv_append", "sx_kv_read", "sx_attention", "sx_attention_ws_bytes",
-           "sx_rope_plan", "sx_rope", "sx_kv_append_rope", "sx_logprobs"]
+           "sx_rope_plan", "sx_rope", "sx_kv_append_rope", "sx_logprobs",
+           "sx_head_logprobs", "sx_head_logprobs_ws_bytes"]
 PROF_CLASSES = ["head_draft", "head_verify", "gemm_fc", "gemm_qkv", "gemm_o", "gemm_gate_up", "gemm_down",
                 "attention"]
 
@@ -185,6 +186,10 @@ def load_library() -> C.CDLL:
                                       vp, i64, vp, i64, vp, vp]
     lib.sx_logprobs.restype = i32
     lib.sx_logprobs.argtypes = [i32, i32, i32, vp, i64, i32, vp, C.c_float, i32, C.POINTER(LogProbOut), vp, vp]
+    lib.sx_head_logprobs_ws_bytes.restype = sz
+    lib.sx_head_logprobs_ws_bytes.argtypes = [i32, i32]
+    lib.sx_head_logprobs.restype = i32
+    lib.sx_head_logprobs.argtypes = [vp, i32, i32, i32, i32, vp, i32, vp, C.c_float, i32, C.POINTER(LogProbOut), vp, sz, vp, vp]
     lib.sx_set_cache.restype = i32
     lib.sx_set_cache.argtypes = [vp, i32]
     lib.sx_verify_noalloc.restype = i32
@@ -559,22 +564,42 @@ class KV8(KVPages):
 
 class LogProbs:
     """Log-probabilities of given tokens with the entropy and the best alternatives of every row: from logits, or
-    from hidden states through ``head`` (bf16 ``[rows, H]``, of which the first ``vocab`` are the vocabulary; rows behind it, such as
-    signal rows, are not looked at).  Without a head the object needs nothing but a device, the current one by default.
+    from hidden states through a head.
+
+    ``head`` is bf16 ``[rows, H]``, of which the first ``vocab`` (default: all) are the vocabulary - rows behind it, such as signal rows,
+    are not looked at - or the flat result of :func:`sx_tile_weight` on it, with ``vocab`` and ``hidden`` (H) given.  Without a head
+    the object needs nothing but a device, the current one by default.
 
     Calls return ``{"logp": [T, n_given], "entropy": [T], "top_tok": [T, top], "top_logp": [T, top]}`` (fp32, ids int32; the last
     two only with ``top > 0``), or fill the tensors of an ``out`` that an earlier call returned.  ``tokens`` is int32 ``[T, n_given]`` or
-    ``[T]``; -1 stands for no token.  Work goes to the current stream of the device."""
+    ``[T]``; -1 stands for no token.  Work goes to the current stream of the device.  The object owns the workspace of
+    ``sx_head_logprobs``: use one per stream, and one per captured graph that may run beside others, and keep it as long as
+    graphs captured through it."""
 
-    def __init__(self, head: Optional[torch.Tensor] = None, vocab: Optional[int] = None, device=None):
+    def __init__(self, head: Optional[torch.Tensor] = None, vocab: Optional[int] = None, hidden: Optional[int] = None, device=None):
         self.lib = load_library()
         self.dev = head.device if head is not None else torch.device(device or f"cuda:{torch.cuda.current_device()}")
         if self.dev.type != "cuda":
             raise SxError("a CUDA device is required (there is no CPU fallback)")
-        self.head, self.vocab = head, vocab
+        if self.dev.index is None:
+            self.dev = torch.device("cuda", torch.cuda.current_device())
+        self.head, self.tiled, self.H, self.V = head, False, 0, 0
+        if head is not None:
+            self.tiled = head.dim() == 1
+            if head.dtype is not torch.bfloat16 or head.dim() not in (1, 2) or not head.is_contiguous():
+                raise SxError("head must be contiguous bf16 [rows, H], or flat from sx_tile_weight")
+            if self.tiled and (vocab is None or hidden is None):
+                raise SxError("a repacked head needs vocab and hidden")
+            self.H = int(hidden) if self.tiled else int(head.shape[1])
+            self.V = int(vocab) if vocab is not None else int(head.shape[0])
+            rows = head.numel() * 2 // max(1, int(self.lib.sx_tiled_weight_bytes(128, self.H))) * 128 if self.tiled else int(head.shape[0])
+            if not 0 < self.V <= rows or (hidden is not None and hidden != self.H):
+                raise SxError(f"head holds {rows} rows of {self.H}: it cannot have a vocabulary of {self.V} and a hidden size of {hidden or self.H}")
         self.status = torch.zeros(1, dtype=torch.int32, device=self.dev)
         self._out = LogProbOut()
         self._out_ref = C.byref(self._out)
+        # a captured graph goes on using the workspace it was captured with, so one that became too small is kept
+        self._ws, self._ws_at, self._ws_bytes, self._ws_for = [], 0, 0, None
 
     def check_status(self, what: str = "device") -> None:
         code = int(self.status.item())
@@ -620,6 +645,30 @@ class LogProbs:
             _check(self.lib.sx_logprobs(_FLOATS[logits.dtype], T, V, logits.data_ptr(), logits.stride(0) if T > 1 else V, n,
                                         _p(tokens), temperature, top, self._out_ref, self.status.data_ptr(),
                                         _raw_stream(self.dev)), "sx_logprobs")
+        return out
+
+    def sx_head_logprobs(self, hidden: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0,
+                         out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+        """Of hidden states (bf16 ``[T, H]``, contiguous) through the head, without a matrix of logits in the caller's hands."""
+        if self.head is None:
+            raise SxError("this object was made without a head")
+        if hidden.dtype is not torch.bfloat16 or hidden.device != self.dev or hidden.dim() != 2 or hidden.shape[1] != self.H or not hidden.is_contiguous():
+            raise SxError(f"hidden must be contiguous bf16 [T, {self.H}] on {self.dev}")
+        T = hidden.shape[0]
+        n, out = self._results(T, tokens, top, out)
+        if T == 0:
+            return out
+        with _guard_of(self.dev):
+            if self._ws_for != T:
+                need = int(self.lib.sx_head_logprobs_ws_bytes(T, self.V))
+                if need > self._ws_bytes:
+                    self._ws.append(torch.empty(need + 256, dtype=torch.uint8, device=self.dev))
+                    self._ws_at = self._ws[-1].data_ptr() + (-self._ws[-1].data_ptr()) % 256
+                    self._ws_bytes = need
+                self._ws_for = T
+            _check(self.lib.sx_head_logprobs(self.head.data_ptr(), 1 if self.tiled else 0, self.V, self.H, T, hidden.data_ptr(), n,
+                                             _p(tokens), temperature, top, self._out_ref, self._ws_at, self._ws_bytes,
+                                             self.status.data_ptr(), _raw_stream(self.dev)), "sx_head_logprobs")
         return out
 
 

@@ -24,6 +24,7 @@
 
 #include "sx_kernels.cuh"
 #include "sx_launch.cuh"
+#include "sx_score.cuh"
 #include "sx_tc_ptx.cuh"
 
 #define SX_BK 64                 // K elements per stage (128 bytes: one swizzle row)
@@ -45,13 +46,17 @@ struct SxTcParams {
   SxLogitsOut lo;                // argmax epilogue: also leave the logits in global memory
   int w_tiled;                   // weights stored tile by tile: [row tile][k-block][128 rows][64 columns]
   uint32_t wait_limit;           // polls of an mbarrier before a wait gives up
+  SxScoreOut sc;                 // KIND_SCORE
 };
 
 __device__ __forceinline__ int sx_lo_row(const SxLogitsOut &lo, int r) { return lo.ri.idx ? lo.ri.idx[r] : r * lo.ri.mul + lo.ri.add; }
 
-template <bool HEAD>
+enum { KIND_GEMM = 0, KIND_HEAD = 1, KIND_SCORE = 2 };      // what the epilogue makes of a tile
+
+template <int KIND>
 __global__ void __launch_bounds__(192, 1)
 sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, SxTcParams p) {
+  constexpr bool HEAD = KIND != KIND_GEMM;
   extern __shared__ uint8_t sx_tc_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>(((uintptr_t)sx_tc_raw + 1023) & ~(uintptr_t)1023);
   const uint32_t stage_bytes = SX_A_BYTES + (uint32_t)p.nmma * 128u;
@@ -162,7 +167,85 @@ sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     int acc = 0;
     uint32_t acc_phase = 0;
     sx_pdl_wait();
-    if (HEAD && p.T == 1 && !p.lse) {
+    if constexpr (KIND == KIND_SCORE) {
+      // Log-probabilities.  The same data flow as the argmax below: a thread owns one token row and a quarter of the vocabulary
+      // rows of each tile, here 32 neighbouring logits at a time, and keeps the running sums of every row it owns in
+      // registers.  The logits and the maximum of each 32 go to memory, for the alternatives and the given tokens alone.
+      float *tb = reinterpret_cast<float *>(epi_smem);          // [128 rows][33]
+      const int tid = threadIdx.x - 64, col = tid & 31, part = tid >> 5;
+      ScoreSum sum[SX_ARGMAX_CHUNKS];
+#pragma unroll
+      for (int ch = 0; ch < SX_ARGMAX_CHUNKS; ++ch) sum[ch].clear();
+      for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        if (!epi_all(mbar_wait(smem_u32(&tfull[acc]), acc_phase, abort_flag, p.wait_limit))) break;
+        tc_fence_after();
+        const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * p.acc_cols);
+        const bool in_vocab = item * SX_TILE_M + et < p.V;
+#pragma unroll
+        for (int ch = 0; ch < SX_ARGMAX_CHUNKS; ++ch) {
+          if (ch * 32 < p.R) {
+            {
+              float v[32];
+              tc_ld16(taddr + ch * 32, v);
+              if (ch * 32 + 16 < p.nmma) tc_ld16(taddr + ch * 32 + 16, v + 16);
+              else {
+#pragma unroll
+                for (int j = 16; j < 32; ++j) v[j] = 0.f;
+              }
+              if ((ch + 1) * 32 >= p.R) {                         // last chunk: the accumulator is free again
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&tempty[acc]));
+              }
+#pragma unroll
+              for (int j = 0; j < 32; ++j) tb[et * 33 + j] = in_vocab ? v[j] : -INFINITY;
+            }
+            epi_bar();
+            if (ch * 32 + col < p.R) {
+              const float *src = tb + (part * 32) * 33 + col;
+              const int row = ch * 32 + col;
+              float x[32];
+#pragma unroll
+              for (int rr = 0; rr < 32; ++rr) x[rr] = src[rr * 33];
+              float4 *dst = reinterpret_cast<float4 *>(p.sc.logits + ((size_t)row * p.num_tiles + item) * SX_TILE_M + part * 32);
+#pragma unroll
+              for (int rr = 0; rr < 32; rr += 4) dst[rr / 4] = make_float4(x[rr], x[rr + 1], x[rr + 2], x[rr + 3]);
+              float mx = x[0];
+#pragma unroll
+              for (int rr = 1; rr < 32; ++rr) mx = fmaxf(mx, x[rr]);
+              p.sc.maxima[((size_t)row * p.num_tiles + item) * 4 + part] = mx;
+              if (mx > sum[ch].m) sum[ch].raise(mx, p.sc.scale);
+              const float ref = sum[ch].m > -INFINITY ? sum[ch].m : 0.f;
+              float2 s2 = make_float2(sum[ch].s, 0.f), t2 = make_float2(sum[ch].t, 0.f);
+#pragma unroll
+              for (int rr = 0; rr < 32; rr += 2) score_pair(make_float2(x[rr], x[rr + 1]), p.sc.scale, ref, s2, t2);
+              sum[ch].s = s2.x + s2.y;
+              sum[ch].t = t2.x + t2.y;
+            }
+            epi_bar();
+          }
+        }
+        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+      }
+      epi_bar();
+#pragma unroll
+      for (int ch = 0; ch < SX_ARGMAX_CHUNKS; ++ch)
+        if (ch * 32 + col < p.R) {
+          float *at = tb + (part * 256 + ch * 32 + col) * 3;
+          at[0] = sum[ch].m; at[1] = sum[ch].s; at[2] = sum[ch].t;
+        }
+      epi_bar();
+      for (int r = tid; r < p.R; r += 128) {
+        ScoreSum all;
+        all.clear();
+        for (int w = 0; w < 4; ++w) {
+          const float *at = tb + (w * 256 + r) * 3;
+          all.join(at[0], at[1], at[2], p.sc.scale);
+        }
+        float *out = p.sc.sums + ((size_t)blockIdx.x * SX_SCORE_ROWS + r) * 3;
+        out[0] = all.m; out[1] = all.s; out[2] = all.t;
+      }
+    } else if (HEAD && p.T == 1 && !p.lse) {
       // Plain argmax (chain drafting, verification).  The logits of a tile go through a small
       // shared-memory buffer, 32 token rows at a time, so that afterwards a thread owns one token
       // row (column of the tile) and a quarter of the vocabulary rows: it scans them in index
@@ -571,8 +654,9 @@ static size_t smem_bytes(const SxTcParams &p, size_t epi_bytes) {
 
 sx_status sx_gemm_init(int device) {
   (void)device;
-  if (cudaFuncSetAttribute(sx_tc_gemm_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SX_SMEM_MAX) != cudaSuccess ||
-      cudaFuncSetAttribute(sx_tc_gemm_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SX_SMEM_MAX) != cudaSuccess)
+  if (cudaFuncSetAttribute(sx_tc_gemm_kernel<KIND_GEMM>, cudaFuncAttributeMaxDynamicSharedMemorySize, SX_SMEM_MAX) != cudaSuccess ||
+      cudaFuncSetAttribute(sx_tc_gemm_kernel<KIND_HEAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, SX_SMEM_MAX) != cudaSuccess ||
+      cudaFuncSetAttribute(sx_tc_gemm_kernel<KIND_SCORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SX_SMEM_MAX) != cudaSuccess)
     return SX_ERR_CUDA;
   return SX_OK;
 }
@@ -627,7 +711,7 @@ sx_status sx_launch_gemm_partial(const bf16 *W, int N, int K, const bf16 *X, int
     const int items = p.num_tiles * p.splits;
     const int per_cta = (items + sm_count - 1) / sm_count;          // the same number of items for every CTA
     const int grid = (items + per_cta - 1) / per_cta;
-    if (sx_launch(sx_tc_gemm_kernel<false>, dim3(grid), dim3(192), smem_bytes(p, 0), st, mw, mx, p) != cudaSuccess)
+    if (sx_launch(sx_tc_gemm_kernel<KIND_GEMM>, dim3(grid), dim3(192), smem_bytes(p, 0), st, mw, mx, p) != cudaSuccess)
       return SX_ERR_CUDA;
   }
   return SX_OK;
@@ -657,10 +741,28 @@ sx_status sx_launch_head(const bf16 *W, int Ntot, int V, int K, const bf16 *X, i
   // with w = ceil(tiles / SMs) tiles per CTA, ceil(tiles / w) CTAs cover the matrix
   const int per_cta = (p.num_tiles + sm_count - 1) / sm_count;
   const int grid = (p.num_tiles + per_cta - 1) / per_cta;
-  if (sx_launch(sx_tc_gemm_kernel<true>, dim3(grid), dim3(192), smem_bytes(p, epi), st, mw, mx, p) != cudaSuccess)
+  if (sx_launch(sx_tc_gemm_kernel<KIND_HEAD>, dim3(grid), dim3(192), smem_bytes(p, epi), st, mw, mx, p) != cudaSuccess)
     return SX_ERR_CUDA;
   *G = grid;
   return SX_OK;
+}
+
+sx_status sx_launch_score_head(const bf16 *W, bool tiled, int V, int K, const bf16 *X, int R, const SxScoreOut &out, int *ctas,
+                               int sm_count, int32_t *status, cudaStream_t st) {
+  if ((K % 8) != 0 || R < 1 || R > SX_SCORE_ROWS) return SX_ERR_UNSUPPORTED;
+  SxTcParams p;
+  memset(&p, 0, sizeof(p));
+  if (!fill_common(p, V, K, R, SX_ARGMAX_SMEM)) return SX_ERR_UNSUPPORTED;
+  p.splits = 1;
+  p.kb_per_split = p.num_kb;
+  p.V = V; p.status = status; p.sc = out;
+  CUtensorMap mw, mx;
+  p.w_tiled = tiled ? 1 : 0;
+  if (!weight_map(W, V, K, tiled, &mw) || !sx_tma_map_2d(X, R, K, p.nmma, &mx)) return SX_ERR_CUDA;
+  const int per_cta = (p.num_tiles + sm_count - 1) / sm_count;      // as in sx_launch_head
+  const int grid = (p.num_tiles + per_cta - 1) / per_cta;
+  *ctas = grid;
+  return sx_rc(sx_launch(sx_tc_gemm_kernel<KIND_SCORE>, dim3(grid), dim3(192), smem_bytes(p, SX_ARGMAX_SMEM), st, mw, mx, p));
 }
 
 // ---- weight tiling ------------------------------------------------------------------------

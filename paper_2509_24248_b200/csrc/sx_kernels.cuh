@@ -151,6 +151,16 @@ sx_status sx_launch_head(const bf16 *W, int Ntot, int V, int K, const bf16 *X, i
                          int32_t *status, cudaStream_t st, const SxSample *smp = nullptr,
                          SxLogitsOut lo = SxLogitsOut{nullptr, 0, SxIndex{nullptr, 1, 0}}, bool tiled = false);
 
+// Head product for log-probabilities: R <= SX_SCORE_ROWS rows; logits [R][tiles * 128] (-inf behind the vocabulary), the maxima of
+// every 32 of them [R][tiles * 4], and per CTA and row the running sums (m, s, t) [ctas][SX_SCORE_ROWS][3] (see sx_score.cuh).
+#define SX_SCORE_ROWS SX_SCORE_MAX_PART
+struct SxScoreOut {
+  float scale;                   // log2(e) / temperature
+  float *logits, *maxima, *sums;
+};
+sx_status sx_launch_score_head(const bf16 *W, bool tiled, int V, int K, const bf16 *X, int R, const SxScoreOut &out, int *ctas,
+                               int sm_count, int32_t *status, cudaStream_t st);
+
 // Speculative sampling with sampled drafts: writes the kept draft token or the residual draw of every
 // verify slot to target_tok [B, P].  target_logits [B * P, V], draft_logits [B, K, V] (K = P - 1), both
 // fp32.  Three small launches (partition sums per slice, accept test + best residual score per slice,

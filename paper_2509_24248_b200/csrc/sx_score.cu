@@ -19,6 +19,7 @@
 
 #include "sx_kernels.cuh"
 #include "sx_launch.cuh"
+#include "sx_score.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -34,47 +35,6 @@ struct SxScoreArgs {
   const int32_t *tok;
   float *logp, *entropy, *top_logp;
   int32_t *top_tok, *status;
-};
-
-__device__ __forceinline__ float score_exp2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-// the larger of two, NaN if either is
-__device__ __forceinline__ float score_max_nan(float a, float b) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-  return y;
-}
-
-struct ScoreSum {
-  float m, s, t;
-  __device__ __forceinline__ void clear() { m = -INFINITY; s = t = 0.f; }
-  // a new reference; sums of nothing have none
-  __device__ __forceinline__ void raise(float to, float scale) {
-    if (m > -INFINITY) {
-      const float d = fmaxf((m - to) * scale, -200.f), f = score_exp2(d);
-      t = f * fmaf(s, d, t);
-      s *= f;
-    }
-    m = to;
-  }
-  __device__ __forceinline__ void join(float om, float os, float ot, float scale) {
-    if (os == 0.f) return;
-    if (om > m) raise(om, scale);
-    if (om == m || !(om > -INFINITY)) { s += os; t += ot; return; }         // equal references, or a NaN without one
-    const float d = fmaxf((om - m) * scale, -200.f), f = score_exp2(d);
-    t += f * fmaf(os, d, ot);
-    s = fmaf(os, f, s);
-  }
-  __device__ __forceinline__ void warp_join(float scale) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, s, o), ot = __shfl_xor_sync(0xffffffffu, t, o);
-      join(om, os, ot, scale);
-    }
-  }
 };
 
 // The 32 best (value, id) that a warp has met, best first, lane by lane.  Entries come with ascending ids, so an equal value goes
@@ -234,33 +194,6 @@ __device__ __forceinline__ void score_load32(const void *p, uint32_t *w) {
       : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
 }
 
-// Two more elements.  Nothing below 2^-126 of the reference counts; holding d to -200 keeps 0 * -inf out of t.
-__device__ __forceinline__ float2 score_add2(float2 a, float2 b) {
-  float2 y;
-  asm("{.reg .b64 p, q, r;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tadd.rn.f32x2 r, p, q;\n\tmov.b64 {%0, %1}, r;}"
-      : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return y;
-}
-__device__ __forceinline__ float2 score_mul2(float2 a, float2 b) {
-  float2 y;
-  asm("{.reg .b64 p, q, r;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tmul.rn.f32x2 r, p, q;\n\tmov.b64 {%0, %1}, r;}"
-      : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return y;
-}
-__device__ __forceinline__ float2 score_fma2(float2 a, float2 b, float2 c) {
-  float2 y;
-  asm("{.reg .b64 p, q, r;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tmov.b64 r, {%6, %7};\n\tfma.rn.f32x2 r, p, q, r;\n\tmov.b64 {%0, %1}, r;}"
-      : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return y;
-}
-__device__ __forceinline__ void score_pair(float2 x, float scale, float ref, float2 &s, float2 &t) {
-  float2 d = score_mul2(score_add2(x, make_float2(-ref, -ref)), make_float2(scale, scale));
-  d = make_float2(score_max_nan(d.x, -200.f), score_max_nan(d.y, -200.f));
-  const float2 e = make_float2(score_exp2(d.x), score_exp2(d.y));
-  s = score_add2(s, e);
-  t = score_fma2(e, d, t);
-}
-
 template <typename E>
 __device__ __forceinline__ float score_group(const uint32_t *w, float scale, ScoreSum &a) {
   float gm;
@@ -387,6 +320,44 @@ __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScor
   score_write(sh, p, row, best, [&](int i) { return ScoreElem<E>::one(x[i]); });
 }
 
+// ---- from hidden states: what the product left ---------------------------------------------------------------------------
+// One CTA per row: sums [ctas][SX_SCORE_ROWS] of the product's CTAs, maxima of groups of 32 logits, the logits themselves (both
+// with `tiles` tiles of 128 to a row, -inf behind the vocabulary).
+__global__ void __launch_bounds__(SCORE_THREADS) sx_score_head_kernel(const SxScoreArgs p, const SxScoreOut o, int row0, int ctas, int tiles) {
+  __shared__ ScoreShared sh;
+  sx_pdl_launch_dependents();
+  sx_pdl_wait();
+  const int row = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, groups = tiles * 4;
+  const float *x = o.logits + (size_t)row * tiles * SX_TILE_M, *gm = o.maxima + (size_t)row * groups;
+  ScoreSum a;
+  a.clear();
+  for (int i = threadIdx.x; i < ctas; i += SCORE_THREADS) {
+    const float *from = o.sums + ((size_t)i * SX_SCORE_ROWS + row) * 3;
+    a.join(from[0], from[1], from[2], p.scale);
+  }
+  score_block_sum(sh, a, p.scale);
+  if (p.top) {
+    ScoreList l;
+    l.clear();
+#pragma unroll 2
+    for (int g = threadIdx.x; g - lane < groups; g += SCORE_THREADS) {
+      const float v = g < groups ? gm[g] : -INFINITY;
+      l.offer(v, g, v > -INFINITY, p.top, lane);
+    }
+    score_best_groups(sh, l, p.top);
+    const float kth = sh.group[p.top - 1] ? sx_pack_value(sh.group[p.top - 1]) : -INFINITY;
+    for (int i = warp; i < p.top; i += SCORE_WARPS) {
+      if (!sh.group[i]) break;
+      const int at = (int)sx_pack_index(sh.group[i]) * 32 + lane;
+      score_candidate(sh, x[at], at, kth);
+    }
+    __syncthreads();
+    score_rank(sh.cand, sh.n_cand, p.top, sh.best);
+    __syncthreads();
+  }
+  score_write(sh, p, row0 + row, sh.best, [&](int i) { return x[i]; });
+}
+
 // ---- entry point -----------------------------------------------------------------------------------------------------------
 static bool aligned16(const void *p) { return p && ((uintptr_t)p & 15) == 0; }
 static bool aligned4(const void *p) { return ((uintptr_t)p & 3) == 0; }
@@ -438,4 +409,58 @@ extern "C" sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void
     case SX_F16: return sx_rc(sx_launch_cluster(sx_score_kernel<__half>, grid, block, 0, (unsigned)cluster, st, p, (const __half *)logits_d, stride, cluster));
     default: return sx_rc(sx_launch_cluster(sx_score_kernel<float>, grid, block, 0, (unsigned)cluster, st, p, (const float *)logits_d, stride, cluster));
   }
+}
+
+// Rows are taken SX_SCORE_ROWS at a time at most, in as few equal parts as that allows: every part reads the whole head.
+static int score_part(int T) {
+  const int parts = (T + SX_SCORE_ROWS - 1) / SX_SCORE_ROWS;
+  return (T + parts - 1) / parts;
+}
+
+struct ScoreWs { size_t logits, maxima, sums, total; };
+static ScoreWs score_ws(int rows, int V, int sm) {
+  const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+  const size_t tiles = (V + SX_TILE_M - 1) / SX_TILE_M;
+  ScoreWs w;
+  w.logits = 0;
+  w.maxima = up(rows * tiles * SX_TILE_M * sizeof(float));
+  w.sums = w.maxima + up(rows * tiles * 4 * sizeof(float));
+  w.total = w.sums + up((size_t)sm * SX_SCORE_ROWS * 3 * sizeof(float));
+  return w;
+}
+
+extern "C" size_t sx_head_logprobs_ws_bytes(int32_t T, int32_t V) {
+  const int sm = sms_of_current_device();
+  if (T < 1 || V < 1 || V > SX_MAX_SCORE_VOCAB || !sm) return 0;
+  return score_ws(score_part(T), V, sm).total;
+}
+
+extern "C" sx_status sx_head_logprobs(const void *head_d, int32_t tiled, int32_t V, int32_t H, int32_t T, const void *hidden_d,
+                                      int32_t n_given, const int32_t *tok_d, float temperature, int32_t top,
+                                      const sx_logprob_out *out, void *ws_d, size_t ws_bytes, int32_t *status_d, void *stream) {
+  SxScoreArgs p;
+  SX_TRY(score_args(T, V, n_given, tok_d, temperature, top, out, status_d, &p));
+  if (!aligned16(head_d) || !aligned16(hidden_d) || (tiled != 0 && tiled != 1)) return SX_ERR_INVALID_ARG;
+  if (H < 8 || H % 8) return SX_ERR_UNSUPPORTED;
+  if (T == 0) return SX_OK;
+  int dev = 0, sm = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || !(sm = sms_of_current_device())) return SX_ERR_CUDA;
+  const int part = score_part(T);
+  const ScoreWs w = score_ws(part, V, sm);
+  if (!ws_d || ((uintptr_t)ws_d & 255) || ws_bytes < w.total) return SX_ERR_WORKSPACE;
+  SX_TRY(sx_gemm_init(dev));
+  SxScoreOut o;
+  o.scale = p.scale;
+  o.logits = (float *)((char *)ws_d + w.logits);
+  o.maxima = (float *)((char *)ws_d + w.maxima);
+  o.sums = (float *)((char *)ws_d + w.sums);
+  const int tiles = (V + SX_TILE_M - 1) / SX_TILE_M;
+  cudaStream_t st = (cudaStream_t)stream;
+  for (int r0 = 0; r0 < T; r0 += part) {
+    const int R = T - r0 < part ? T - r0 : part;
+    int ctas = 0;
+    SX_TRY(sx_launch_score_head((const bf16 *)head_d, tiled != 0, V, H, (const bf16 *)hidden_d + (size_t)r0 * H, R, o, &ctas, sm, status_d, st));
+    SX_TRY(sx_rc(sx_launch(sx_score_head_kernel, dim3(R), dim3(SCORE_THREADS), 0, st, p, o, r0, ctas, tiles)));
+  }
+  return SX_OK;
 }
