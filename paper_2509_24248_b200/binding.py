@@ -331,19 +331,19 @@ def _raw_stream(dev: torch.device) -> int:
 _FLOATS = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}       # SX_BF16, SX_F16, SX_F32
 
 
-def _guard_of(dev: torch.device):
-    """`dev` becomes the current device for a launch (entering a device costs more than the launch does, so only where
+def _guard_of(index: int):
+    """Device `index` becomes the current one for a launch (entering a device costs more than the launch does, so only where
     another one is current)."""
-    return _NO_GUARD if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
+    return _NO_GUARD if torch._C._cuda_getDevice() == index else torch.cuda.device(index)
 
 
-def _heads_stride(name: str, t: torch.Tensor, dtype: torch.dtype, heads: int, d: int, dev: torch.device, rows: int = -1) -> int:
-    """Row stride of ``t [T, heads, d]`` whose heads lie side by side."""
+def _heads_stride(name: str, t: torch.Tensor, dtype: torch.dtype, T: int, heads: int, d: int, index: int) -> int:
+    """Row stride of ``t [T, heads, d]`` on device `index` whose heads lie side by side."""
     shape, stride = t.shape, t.stride()
-    if (len(shape) != 3 or shape[1] != heads or shape[2] != d or (rows >= 0 and shape[0] != rows) or (stride[2] != 1 and d > 1)
-            or (stride[1] != d and heads > 1) or t.dtype is not dtype or t.device != dev):
-        raise SxError(f"{name} must be {dtype} [{'T' if rows < 0 else rows}, {heads}, {d}] on {dev}, rows of heads contiguous")
-    return stride[0] if shape[0] > 1 else heads * d
+    if (t.dtype is not dtype or t.get_device() != index or shape != (T, heads, d) or (stride[2] != 1 and d > 1)
+            or (stride[1] != d and heads > 1)):
+        raise SxError(f"{name} must be {dtype} [{T}, {heads}, {d}] on cuda:{index}, rows of heads contiguous")
+    return stride[0] if T > 1 else heads * d
 
 
 class Rope:
@@ -369,38 +369,40 @@ class Rope:
         self.plan = Rotation()
         self.plan_ref = C.byref(self.plan)
         _check(self.lib.sx_rope_plan(C.byref(cfg), self.plan_ref), "sx_rope_plan")
-        self.d = head_dim
+        self.d, self._call = head_dim, self.lib.sx_rope
 
     def sx_rope(self, pos: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
                 k_out: Optional[torch.Tensor] = None, transpose: bool = False):
         """Turns ``q [T, n_q, d]`` and, in the same launch, ``k [T, n_k, d]`` (bf16, fp16 or fp32, slices of a projection's
         output will do) to the positions ``pos`` (int32 ``[T]``) and returns both.  An output may be its input itself;
         ``transpose`` turns by the transposed matrix (the gradient, and with magnitude 1 the way back to position 0)."""
-        dev, T = q.device, q.shape[0]
-        if not q.is_cuda or q.dtype not in _FLOATS or q.dim() != 3:
+        dtype, index, d = q.dtype, q.get_device(), self.d
+        if index < 0 or dtype not in _FLOATS or q.dim() != 3:
             raise SxError("q must be bf16, fp16 or fp32 [T, n_q, d] on a device")
-        if pos.dtype is not torch.int32 or pos.device != dev or pos.shape != (T,) or (T > 1 and pos.stride(0) != 1):
-            raise SxError(f"pos must be int32 [{T}] on {dev}, contiguous")
-        if k is None and k_out is not None:
+        T, nq, _ = q.shape
+        if pos.dtype is not torch.int32 or pos.get_device() != index or pos.shape != (T,) or (T > 1 and pos.stride(0) != 1):
+            raise SxError(f"pos must be int32 [{T}] on cuda:{index}, contiguous")
+        qs = _heads_stride("q", q, dtype, T, nq, d, index)
+        if q_out is None:
+            q_out = q.new_empty((T, nq, d))
+        qos = qs if q_out is q else _heads_stride("q_out", q_out, dtype, T, nq, d, index)
+        nk, ks, kos, k_at, k_out_at = 0, 0, 0, None, None
+        if k is not None:
+            nk = k.shape[1] if k.dim() == 3 else -1
+            ks = _heads_stride("k", k, dtype, T, nk, d, index)
+            if k_out is None:
+                k_out = k.new_empty((T, nk, d))
+            kos = ks if k_out is k else _heads_stride("k_out", k_out, dtype, T, nk, d, index)
+            k_at, k_out_at = k.data_ptr(), k_out.data_ptr()
+        elif k_out is not None:
             raise SxError("k_out without k")
-        args = []
-        for name, x, y in (("q", q, q_out), ("k", k, k_out)):
-            if x is None:
-                args += [0, None, 0, None, 0]
-                continue
-            y = torch.empty(x.shape, dtype=x.dtype, device=dev) if y is None else y
-            n = x.shape[1] if x.dim() == 3 else -1
-            args += [n, x.data_ptr(), _heads_stride(name, x, q.dtype, n, self.d, dev, T), y.data_ptr(),
-                     _heads_stride(name + "_out", y, q.dtype, n, self.d, dev, T)]
-            if name == "q":
-                q_out = y
-            else:
-                k_out = y
         if T == 0:
             return q_out, k_out
-        with _guard_of(dev):
-            _check(self.lib.sx_rope(self.plan_ref, _FLOATS[q.dtype], 1 if transpose else 0, T, pos.data_ptr(), *args,
-                                    _raw_stream(dev)), "sx_rope")
+        with _guard_of(index):
+            code = self._call(self.plan_ref, _FLOATS[dtype], 1 if transpose else 0, T, pos.data_ptr(), nq, q.data_ptr(), qs,
+                              q_out.data_ptr(), qos, nk, k_at, ks, k_out_at, kos, torch._C._cuda_getCurrentRawStream(index))
+        if code:
+            _check(code, "sx_rope")
         return q_out, k_out
 
 
@@ -420,12 +422,14 @@ class KVPages:
             raise SxError("k_pages must be [num_pages, n_kv, page, d]")
         self.n_kv, self.page, self.d = (int(v) for v in kv["k_pages"].shape[1:])
         self.dev = kv["k_pages"].device
+        self._index = self.dev.index
         self._kv = _kv_struct(self.kv, self.n_kv, self.page, self.d)
         self._kv_ref = C.byref(self._kv)
         self.B = int(self._kv.batch)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.dev)
         self._shape = KVShape(self.n_kv, self.n_kv, self.d, self.page)
         self._shape_ref = C.byref(self._shape)
+        self._append_rope, self._status_at = self.lib.sx_kv_append_rope, self.status.data_ptr()
 
     def check_status(self, what: str = "device") -> None:
         code = int(self.status.item())
@@ -450,7 +454,7 @@ class KVPages:
         return t.stride(0) if t.shape[0] > 1 else self.n_kv * self.d
 
     def _guard(self):
-        return _guard_of(self.dev)
+        return _guard_of(self._index)
 
     def sx_kv_append_rope(self, rope: Optional[Rope], k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor,
                           pos_start: Optional[torch.Tensor] = None, rot_pos: Optional[torch.Tensor] = None,
@@ -459,28 +463,38 @@ class KVPages:
         of sequence ``b`` (default: behind ``cache_len``, which is not advanced), the keys turned by ``rope`` to their slots or to
         ``rot_pos`` (int32 ``[T]``); ``rope=None`` turns nothing.  The rows' queries ``q [T, n_q, d]`` are turned in the same
         launch and returned (in ``q_out``, which may be ``q``; rows behind the last sequence stay as they are there)."""
-        T = self._rows(k, v, row_start, pos_start)
-        if rope is not None and rope.d != self.d:
-            raise SxError(f"rope is planned for heads of {rope.d}, the cache has {self.d}")
-        if rot_pos is not None and (rot_pos.dtype is not torch.int32 or rot_pos.device != self.dev or rot_pos.shape != (T,)
-                                    or not rot_pos.is_contiguous()):
-            raise SxError(f"rot_pos must be int32 [{T}] on {self.dev}")
-        if q is None and q_out is not None:
-            raise SxError("q_out without q")
-        nq, args = 0, (None, 0, None, 0)
+        index, n_kv, d = self._index, self.n_kv, self.d
+        T = k.shape[0]
+        ks = _heads_stride("k", k, torch.bfloat16, T, n_kv, d, index)
+        vs = _heads_stride("v", v, torch.bfloat16, T, n_kv, d, index)
+        for name, t, n in (("row_start", row_start, self.B + 1), ("pos_start", pos_start, self.B), ("rot_pos", rot_pos, T)):
+            if t is not None and (t.dtype is not torch.int32 or t.numel() != n or t.get_device() != index or not t.is_contiguous()):
+                raise SxError(f"{name} must be contiguous int32 [{n}] on {self.dev}")
+        plan = None
+        if rope is not None:
+            if rope.d != d:
+                raise SxError(f"rope is planned for heads of {rope.d}, the cache has {d}")
+            plan = rope.plan_ref
+        nq, q_at, q_out_at, qs, qos = 0, None, None, 0, 0
         if q is not None:
             nq = q.shape[1] if q.dim() == 3 else -1
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=self.dev) if q_out is None else q_out
-            args = (q.data_ptr(), _heads_stride("q", q, torch.bfloat16, nq, self.d, self.dev, T), q_out.data_ptr(),
-                    _heads_stride("q_out", q_out, torch.bfloat16, nq, self.d, self.dev, T))
+            qs = _heads_stride("q", q, torch.bfloat16, T, nq, d, index)
+            if q_out is None:
+                q_out = q.new_empty((T, nq, d))
+            qos = qs if q_out is q else _heads_stride("q_out", q_out, torch.bfloat16, T, nq, d, index)
+            q_at, q_out_at = q.data_ptr(), q_out.data_ptr()
+        elif q_out is not None:
+            raise SxError("q_out without q")
         if T == 0:
             return q_out
-        with self._guard():
-            self._shape.n_q_heads = nq
-            _check(self.lib.sx_kv_append_rope(None if rope is None else rope.plan_ref, self._shape_ref, self._kv_ref, T,
-                                              row_start.data_ptr(), _p(pos_start), _p(rot_pos), k.data_ptr(), self._stride(k),
-                                              v.data_ptr(), self._stride(v), *args, self.status.data_ptr(),
-                                              _raw_stream(self.dev)), "sx_kv_append_rope")
+        self._shape.n_q_heads = nq
+        with _guard_of(index):
+            code = self._append_rope(plan, self._shape_ref, self._kv_ref, T, row_start.data_ptr(),
+                                     None if pos_start is None else pos_start.data_ptr(),
+                                     None if rot_pos is None else rot_pos.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs,
+                                     q_out_at, qos, self._status_at, torch._C._cuda_getCurrentRawStream(index))
+        if code:
+            _check(code, "sx_kv_append_rope")
         return q_out
 
 
@@ -598,6 +612,8 @@ class LogProbs:
         self.status = torch.zeros(1, dtype=torch.int32, device=self.dev)
         self._out = LogProbOut()
         self._out_ref = C.byref(self._out)
+        self._index, self._f32, self._status_at = self.dev.index, torch.empty(0, dtype=torch.float32, device=self.dev), self.status.data_ptr()
+        self._logprobs, self._head_logprobs = self.lib.sx_logprobs, self.lib.sx_head_logprobs
         # a captured graph goes on using the workspace it was captured with, so one that became too small is kept
         self._ws, self._ws_at, self._ws_bytes, self._ws_for = [], 0, 0, None
 
@@ -609,42 +625,50 @@ class LogProbs:
 
     def _results(self, T: int, tokens: Optional[torch.Tensor], top: int, out: Optional[Dict[str, torch.Tensor]]):
         """(number of given tokens, results), the argument block filled."""
+        index = self._index
         n = 0
         if tokens is not None:
-            n = tokens.shape[1] if tokens.dim() == 2 else 1
-            if (tokens.dtype is not torch.int32 or tokens.device != self.dev or not 1 <= tokens.dim() <= 2 or tokens.shape[0] != T
+            shape = tokens.shape
+            n = shape[1] if len(shape) == 2 else 1
+            if (tokens.dtype is not torch.int32 or tokens.get_device() != index or not 1 <= len(shape) <= 2 or shape[0] != T
                     or not tokens.is_contiguous()):
                 raise SxError(f"tokens must be contiguous int32 [{T}, n_given] or [{T}] on {self.dev}")
-        want = {"logp": (T, n), "entropy": (T,), "top_tok": (T, top), "top_logp": (T, top)}
-        if top == 0:
-            del want["top_tok"], want["top_logp"]
-        if out is None:
-            out = {name: torch.empty(shape, dtype=torch.int32 if name == "top_tok" else torch.float32, device=self.dev)
-                   for name, shape in want.items()}
-        else:
-            for name, shape in want.items():
-                t = out.get(name)
-                if (t is None or tuple(t.shape) != shape or t.dtype != (torch.int32 if name == "top_tok" else torch.float32)
-                        or t.device != self.dev or not t.is_contiguous()):
-                    raise SxError(f"out[{name!r}] must be contiguous {list(shape)} on {self.dev}")
         o = self._out
-        o.logp_d, o.entropy_d = out["logp"].data_ptr(), out["entropy"].data_ptr()
+        if out is None:
+            if top < 0:
+                raise SxError("top must not be negative")
+            f, i = self._f32, self.status
+            logp, entropy = f.new_empty((T, n)), f.new_empty((T,))
+            out = {"logp": logp, "entropy": entropy}
+            if top:
+                out["top_tok"], out["top_logp"] = i.new_empty((T, top)), f.new_empty((T, top))
+        else:
+            want = {"logp": (T, n), "entropy": (T,), "top_tok": (T, top), "top_logp": (T, top)}
+            for name in ("logp", "entropy", "top_tok", "top_logp")[:4 if top else 2]:
+                t = out.get(name)
+                if (t is None or t.shape != want[name] or t.dtype is not (torch.int32 if name == "top_tok" else torch.float32)
+                        or t.get_device() != index or not t.is_contiguous()):
+                    raise SxError(f"out[{name!r}] must be contiguous {list(want[name])} on {self.dev}")
+            logp, entropy = out["logp"], out["entropy"]
+        o.logp_d, o.entropy_d = logp.data_ptr(), entropy.data_ptr()
         o.top_tok_d, o.top_logp_d = (out["top_tok"].data_ptr(), out["top_logp"].data_ptr()) if top else (None, None)
         return n, out
 
     def sx_logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0,
                     out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
         """Of rows of logits (bf16, fp16 or fp32 ``[T, V]``, any row stride)."""
-        if logits.dim() != 2 or logits.device != self.dev or logits.dtype not in _FLOATS or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        shape, stride, dtype = logits.shape, logits.stride(), _FLOATS.get(logits.dtype)
+        if len(shape) != 2 or logits.get_device() != self._index or dtype is None or (shape[1] > 1 and stride[1] != 1):
             raise SxError(f"logits must be bf16, fp16 or fp32 [T, V] on {self.dev}, rows contiguous")
-        T, V = logits.shape
+        T, V = shape
         n, out = self._results(T, tokens, top, out)
         if T == 0:
             return out
-        with _guard_of(self.dev):
-            _check(self.lib.sx_logprobs(_FLOATS[logits.dtype], T, V, logits.data_ptr(), logits.stride(0) if T > 1 else V, n,
-                                        _p(tokens), temperature, top, self._out_ref, self.status.data_ptr(),
-                                        _raw_stream(self.dev)), "sx_logprobs")
+        with _guard_of(self._index):
+            code = self._logprobs(dtype, T, V, logits.data_ptr(), stride[0] if T > 1 else V, n, tokens.data_ptr() if n else None,
+                                  temperature, top, self._out_ref, self._status_at, torch._C._cuda_getCurrentRawStream(self._index))
+        if code:
+            _check(code, "sx_logprobs")
         return out
 
     def sx_head_logprobs(self, hidden: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0,
@@ -652,13 +676,15 @@ class LogProbs:
         """Of hidden states (bf16 ``[T, H]``, contiguous) through the head, without a matrix of logits in the caller's hands."""
         if self.head is None:
             raise SxError("this object was made without a head")
-        if hidden.dtype is not torch.bfloat16 or hidden.device != self.dev or hidden.dim() != 2 or hidden.shape[1] != self.H or not hidden.is_contiguous():
+        shape = hidden.shape
+        if (hidden.dtype is not torch.bfloat16 or hidden.get_device() != self._index or len(shape) != 2 or shape[1] != self.H
+                or not hidden.is_contiguous()):
             raise SxError(f"hidden must be contiguous bf16 [T, {self.H}] on {self.dev}")
-        T = hidden.shape[0]
+        T = shape[0]
         n, out = self._results(T, tokens, top, out)
         if T == 0:
             return out
-        with _guard_of(self.dev):
+        with _guard_of(self._index):
             if self._ws_for != T:
                 need = int(self.lib.sx_head_logprobs_ws_bytes(T, self.V))
                 if need > self._ws_bytes:
@@ -666,9 +692,11 @@ class LogProbs:
                     self._ws_at = self._ws[-1].data_ptr() + (-self._ws[-1].data_ptr()) % 256
                     self._ws_bytes = need
                 self._ws_for = T
-            _check(self.lib.sx_head_logprobs(self.head.data_ptr(), 1 if self.tiled else 0, self.V, self.H, T, hidden.data_ptr(), n,
-                                             _p(tokens), temperature, top, self._out_ref, self._ws_at, self._ws_bytes,
-                                             self.status.data_ptr(), _raw_stream(self.dev)), "sx_head_logprobs")
+            code = self._head_logprobs(self.head.data_ptr(), 1 if self.tiled else 0, self.V, self.H, T, hidden.data_ptr(), n,
+                                       tokens.data_ptr() if n else None, temperature, top, self._out_ref, self._ws_at, self._ws_bytes,
+                                       self._status_at, torch._C._cuda_getCurrentRawStream(self._index))
+        if code:
+            _check(code, "sx_head_logprobs")
         return out
 
 

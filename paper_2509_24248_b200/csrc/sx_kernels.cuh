@@ -14,6 +14,7 @@ struct SxIndex {
 static inline sx_status sx_rc(cudaError_t e) { return e == cudaSuccess ? SX_OK : SX_ERR_CUDA; }
 sx_status sx_kernels_init(int device);
 sx_status sx_kv_check_cache(const sx_kv_shape *sh, const sx_kv *kv);       // a cache of either kind (sx_kv8.cu)
+int sx_sm_count();                                                         // of the current device; 0 on an error
 
 struct SxShape {
   int H, nq, nkv, d, F, V, S, page;

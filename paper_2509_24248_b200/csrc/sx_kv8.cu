@@ -18,6 +18,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <atomic>
+
 #include "sx_attn8.cuh"
 #include "sx_kernels.cuh"
 #include "sx_launch.cuh"
@@ -184,10 +186,14 @@ static sx_status check_cache(const sx_kv_shape *sh, const sx_kv *kv) {
   return kv->dtype == SX_KV_E4M3 ? SX_OK : SX_ERR_UNSUPPORTED;
 }
 
-static int sms_of_current_device() {
+// SMs of the current device (asked for once per device), 0 on an error
+int sx_sm_count() {
+  static std::atomic<int> known[64];
   int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return 0;
+  if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
   return n;
 }
 
@@ -210,7 +216,7 @@ static sx_status rows_call(const sx_kv_shape *sh, const sx_kv *kv, int32_t T, co
   p.status = status_d;
   // as many tokens per CTA as make one wave of about six CTAs per SM: finding the places is a chain of three dependent
   // reads, which a CTA of few tokens spends half its time on
-  const int wave = 6 * sms_of_current_device();
+  const int wave = 6 * sx_sm_count();
   p.tokens = wave ? (T + wave - 1) / wave : 1;
   if (p.tokens > KV8_MAX_TOKENS) p.tokens = KV8_MAX_TOKENS;
   if (p.tokens < 1) p.tokens = 1;
@@ -261,7 +267,7 @@ extern "C" sx_status sx_kv_read(const sx_kv_shape *sh, const sx_kv *kv, int32_t 
 
 extern "C" size_t sx_attention_ws_bytes(const sx_kv_shape *sh, int32_t batch, int32_t rows, int32_t n_groups) {
   if (!sh || batch < 1 || rows < 1 || sh->n_q_heads < 1 || sh->head_dim < 1 || n_groups < 0) return 0;
-  const int sm = sms_of_current_device();
+  const int sm = sx_sm_count();
   return sm ? sx_attn8_ws_bytes(sh->n_q_heads, sh->n_kv_heads, sh->head_dim, batch, rows, n_groups, sm) : 0;
 }
 
@@ -294,7 +300,7 @@ extern "C" sx_status sx_attention(const sx_kv_shape *sh, const sx_kv *kv, int32_
   if (!aligned16(q_d) || !aligned16(o_d) || !status_d || !(scale > -INFINITY && scale < INFINITY)) return SX_ERR_INVALID_ARG;
   if (kernel < SX_ATTN_AUTO || kernel > SX_ATTN_TC) return SX_ERR_INVALID_ARG;
   if (q_stride < (int64_t)p.nq * p.d || q_stride % 8) return SX_ERR_INVALID_ARG;
-  const int sm = sms_of_current_device();
+  const int sm = sx_sm_count();
   if (!sm) return SX_ERR_CUDA;
   if (!ws_d || ((uintptr_t)ws_d & 255) || ws_bytes < sx_attn8_ws_bytes(p.nq, p.nkv, p.d, p.B, rows, p.n_groups, sm))
     return SX_ERR_WORKSPACE;

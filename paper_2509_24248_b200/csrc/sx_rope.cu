@@ -5,8 +5,8 @@
 // with u, v = x[i], x[i + r/2] (half order) or x[2i], x[2i + 1] (interleaved).  What has to be exact is the angle modulo one
 // turn: in fp32 a position of 10^5 alone costs it 0.01 rad.  The plan keeps f_i / 2 pi as a 64-bit fraction of a turn, so
 // that pos * f_i modulo one turn is one 64-bit integer product, whatever the position (off by pos * 2^-64 turns); its
-// quadrant is taken off as an integer too, and what is left, at most an eighth of a turn, goes through sincospif.  cos, sin and
-// the products are fp32, the result is rounded once.
+// quadrant is taken off as an integer too, and what is left, at most an eighth of a turn, is small enough for a short series.  cos,
+// sin and the products are fp32, the result is rounded once.
 //
 // Bound by bytes: every element is read and written once, three flops on the way.  A row (a head of a token) belongs to
 // d / 8 neighbouring lanes with 8 elements each, 16-byte accesses; the partner half comes from another lane by shuffle,
@@ -21,7 +21,6 @@
 #include "sx_launch.cuh"
 
 #define ROPE_THREADS 128
-#define ROPE_U 4                 // rows of a lane that are on the way together
 
 enum { PARTNER_LANE = 0, PARTNER_SHUFFLE = 1, PARTNER_LOAD = 2 };
 
@@ -46,16 +45,25 @@ struct SxRopeArgs {
 
 struct SxRopeSteps { uint64_t step[SX_ROPE_MAX_PAIRS]; };
 
-// magnitude * (cos, sin) of pos * step, step in 2^-64 turns
+// magnitude * (cos, sin) of pos * step, step in 2^-64 turns.  After the quadrant is taken off, |x| <= pi / 4 and the Taylor
+// series to x^9 and x^10 are off by 2e-9 and 1e-10 at most, below the roundings of their evaluation.
 __device__ __forceinline__ void rope_angle(uint64_t step, int pos, float magnitude, float *c, float *s) {
   const uint64_t ph = step * (uint64_t)(int64_t)pos;
-  const uint32_t quad = (uint32_t)((ph + (1ull << 61)) >> 62);
-  const int32_t rest = (int32_t)(uint32_t)((ph - ((uint64_t)quad << 62)) >> 32);     // [-2^29, 2^29) of 2^32 to a turn
-  float sn, cs;
-  sincospif((float)rest * 4.656612873077392578125e-10f, &sn, &cs);                   // 2^-31: half turns
-  const float x = (quad & 1) ? -sn : cs, y = (quad & 1) ? cs : sn;
-  *c = magnitude * ((quad & 2) ? -x : x);
-  *s = magnitude * ((quad & 2) ? -y : y);
+  const uint32_t hi = (uint32_t)(ph >> 32), quad = (hi + (1u << 29)) >> 30;
+  const float x = (float)(int32_t)(hi - (quad << 30)) * 1.4629180792671596e-9f;      // 2 pi / 2^32
+  const float z = x * x;
+  float sn = fmaf(z, 2.7557319223985893e-6f, -1.9841269841269841e-4f);
+  sn = fmaf(z, sn, 8.3333333333333333e-3f);
+  sn = fmaf(z, sn, -1.6666666666666667e-1f);
+  sn = fmaf(z * x, sn, x);
+  float cs = fmaf(z, -2.7557319223985891e-7f, 2.4801587301587302e-5f);
+  cs = fmaf(z, cs, -1.3888888888888889e-3f);
+  cs = fmaf(z, cs, 4.1666666666666667e-2f);
+  cs = fmaf(z, cs, -0.5f);
+  cs = fmaf(z, cs, 1.0f);
+  const float u = (quad & 1) ? -sn : cs, v = (quad & 1) ? cs : sn;
+  *c = magnitude * ((quad & 2) ? -u : u);
+  *s = magnitude * ((quad & 2) ? -v : v);
 }
 
 template <typename E> struct Rope8;                     // eight elements as words, and one element from memory
@@ -104,6 +112,7 @@ struct RopeLane {
   int src;                       // PARTNER_SHUFFLE: lane of the partner's elements
 };
 
+template <int PARTNER>
 __device__ __forceinline__ void rope_lane_set(const SxRopeArgs &p, int e0, int lane, RopeLane *r) {
   r->in = 0;
   r->src = lane;
@@ -112,42 +121,62 @@ __device__ __forceinline__ void rope_lane_set(const SxRopeArgs &p, int e0, int l
 #pragma unroll
   for (int e = 0; e < 8; ++e)
     if ((unsigned)(e0 + e - p.rot_start) < (unsigned)p.rot_dim) r->in |= 1u << e;
-  if (p.partner == PARTNER_SHUFFLE && r->in) r->src = e0 - p.rot_start < p.half ? lane + p.half / 8 : lane - p.half / 8;
+  if (PARTNER == PARTNER_SHUFFLE && r->in) r->src = e0 - p.rot_start < p.half ? lane + p.half / 8 : lane - p.half / 8;
 }
 
+// Every lane of the warp calls it (shuffles).
+template <int PARTNER>
 __device__ __forceinline__ void rope_lane_angles(const SxRopeArgs &p, const SxRopeSteps &st, int e0, int pos, RopeLane *r) {
-  if (p.half == 0) {
+  const int i0 = e0 - p.rot_start;
+  if (PARTNER == PARTNER_LANE) {
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
-      float c = 1.f, s = 0.f;
-      if (r->in >> e & 1) rope_angle(st.step[(e0 + e - p.rot_start) >> 1], pos, p.magnitude, &c, &s);
+      float c = 0.f, s = 0.f;
+      if (r->in >> e & 1) rope_angle(st.step[(i0 + e) >> 1], pos, p.magnitude, &c, &s);
       if (p.transpose) s = -s;
       r->c[e] = r->c[e + 1] = c;
       r->s[e] = -s;
       r->s[e + 1] = s;
     }
-    return;
-  }
+  } else if (PARTNER == PARTNER_SHUFFLE) {
+    // both halves of the eight pairs turn by the same angles: the lane of the first half computes four, its partner the others
+    const bool first = i0 < p.half;
+    const uint64_t *step = st.step + (r->in ? (first ? i0 : i0 - p.half + 4) : 0);
+    float c[4], s[4];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float c = 1.f, s = 0.f;
-    const int i = e0 + e - p.rot_start;
-    if (r->in >> e & 1) rope_angle(st.step[i < p.half ? i : i - p.half], pos, p.magnitude, &c, &s);
-    r->c[e] = c;
-    r->s[e] = ((i < p.half) != (p.transpose != 0)) ? -s : s;
+    for (int e = 0; e < 4; ++e) rope_angle(step[e], pos, p.magnitude, &c[e], &s[e]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float oc = __shfl_sync(0xffffffffu, c[e], r->src), os = __shfl_sync(0xffffffffu, s[e], r->src);
+      r->c[e] = first ? c[e] : oc;
+      r->c[e + 4] = first ? oc : c[e];
+      const bool minus = first != (p.transpose != 0);
+      const float lo = first ? s[e] : os, hi = first ? os : s[e];
+      r->s[e] = minus ? -lo : lo;
+      r->s[e + 4] = minus ? -hi : hi;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float c = 0.f, s = 0.f;
+      const int i = i0 + e;
+      if (r->in >> e & 1) rope_angle(st.step[i < p.half ? i : i - p.half], pos, p.magnitude, &c, &s);
+      r->c[e] = c;
+      r->s[e] = ((i < p.half) != (p.transpose != 0)) ? -s : s;
+    }
   }
 }
 
-// One row's words turned in place.  Every lane of the warp calls it (shuffles).
-template <typename E>
+// One row's words turned in place.  Every lane of the warp calls it (shuffles); row: nullptr where the lane has none.
+template <typename E, int PARTNER>
 __device__ __forceinline__ void rope_turn(const SxRopeArgs &p, const RopeLane &r, const E *row, int e0, uint32_t *w) {
   constexpr int W = Rope8<E>::W;
   float x[8], o[8];
   Rope8<E>::unpack(w, x);
-  if (p.partner == PARTNER_LANE) {
+  if (PARTNER == PARTNER_LANE) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = x[e ^ 1];
-  } else if (p.partner == PARTNER_SHUFFLE) {
+  } else if (PARTNER == PARTNER_SHUFFLE) {
     uint32_t ow[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) ow[i] = __shfl_sync(0xffffffffu, w[i], r.src);
@@ -164,8 +193,10 @@ __device__ __forceinline__ void rope_turn(const SxRopeArgs &p, const RopeLane &r
   for (int e = 0; e < 8; ++e) y[e] = fmaf(x[e], r.c[e], o[e] * r.s[e]);
   // a word outside the rotated part keeps its bits (the part begins and ends between 32-bit words)
 #pragma unroll
-  for (int i = 0; i < W; ++i)
-    if (r.in >> (i * (8 / W)) & 1) w[i] = Rope8<E>::pack(y, i);
+  for (int i = 0; i < W; ++i) {
+    const uint32_t m = 0u - (r.in >> (PARTNER == PARTNER_SHUFFLE ? 0 : i * (8 / W)) & 1u);
+    w[i] = (w[i] & ~m) | (Rope8<E>::pack(y, i) & m);
+  }
 }
 
 template <int W>
@@ -182,45 +213,53 @@ __device__ __forceinline__ void rope_store(void *dst, const uint32_t *w) {
   for (int i = 0; i < W; i += 4) reinterpret_cast<uint4 *>(dst)[i / 4] = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
 }
 
-// LPR lanes per row: the power of two from d / 8 up
-template <typename E, int LPR>
-__global__ void __launch_bounds__(ROPE_THREADS) sx_rope_kernel(const SxRopeArgs p, const __grid_constant__ SxRopeSteps st) {
-  constexpr int W = Rope8<E>::W, G = 32 / LPR;
+// Rows [h0, h1) of a token's queries or keys, G at a time, U times that on the way together.  angles() is called once the
+// first rows have been asked for.
+template <typename E, int LPR, int PARTNER, typename A>
+__device__ __forceinline__ void rope_rows(const SxRopeArgs &p, RopeLane &rl, int h0, int h1, const E *src, E *dst, int lane, A angles) {
+  constexpr int W = Rope8<E>::W, G = 32 / LPR, U = PARTNER == PARTNER_LOAD ? 2 : 16 / W;
+  const int e0 = (lane % LPR) * 8;
+#pragma unroll 1
+  for (int r = h0; r < h1; r += G * U) {
+    uint32_t w[U][W];
+    const int h = r + lane / LPR;
+    const E *from = src + (int64_t)h * p.D + e0;
+    E *to = dst + (int64_t)h * p.D + e0;
+    const int n = e0 < p.D ? (h1 - h + G - 1) / G : 0;           // rows that this lane has
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) w[i][j] = 0;
+      if (i < n) rope_load<W>(from + i * G * p.D, w[i]);
+    }
+    angles();
+#pragma unroll
+    for (int i = 0; i < U; ++i) rope_turn<E, PARTNER>(p, rl, i < n ? from + i * G * p.D - e0 : nullptr, e0, w[i]);
+    __syncwarp();                                   // in place: all of a row is read before any of it is written
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (i < n) rope_store<W>(to + i * G * p.D, w[i]);
+  }
+}
+
+// LPR lanes per row: the power of two from d / 8 up, at least 4
+template <typename E, int LPR, int PARTNER>
+__global__ void __launch_bounds__(ROPE_THREADS, PARTNER == PARTNER_LOAD ? 4 : 8) sx_rope_kernel(const SxRopeArgs p, const __grid_constant__ SxRopeSteps st) {
   sx_pdl_wait();
   const int lane = threadIdx.x & 31, unit = blockIdx.x * (ROPE_THREADS / 32) + (threadIdx.x >> 5);
   const int t = unit / p.slices;
   if (t >= p.T) return;
   const int r0 = (unit - t * p.slices) * p.rows_per_warp, r1 = min(p.nq + p.nk, r0 + p.rows_per_warp);
-  const int e0 = (lane % LPR) * 8;
-  const bool mine = e0 < p.D;
-  const E *q = reinterpret_cast<const E *>(p.q) + t * p.qs, *k = reinterpret_cast<const E *>(p.k) + t * p.ks;
-  E *qo = reinterpret_cast<E *>(p.qo) + t * p.qos, *ko = reinterpret_cast<E *>(p.ko) + t * p.kos;
+  const int e0 = (lane % LPR) * 8, pos = p.pos[t];
   RopeLane rl;
-  rope_lane_set(p, e0, lane, &rl);
-  const int pos = p.pos[t];
+  rope_lane_set<PARTNER>(p, e0, lane, &rl);
   bool set = false;
-#pragma unroll 1
-  for (int r = r0 + lane / LPR; r - lane / LPR < r1; r += G * ROPE_U) {
-    uint32_t w[ROPE_U][W];
-    const E *src[ROPE_U];
-#pragma unroll
-    for (int i = 0; i < ROPE_U; ++i) {
-      const int h = r + i * G;
-      src[i] = (mine && h < r1) ? (h < p.nq ? q + (int64_t)h * p.D : k + (int64_t)(h - p.nq) * p.D) : nullptr;
-#pragma unroll
-      for (int j = 0; j < W; ++j) w[i][j] = 0;
-      if (src[i]) rope_load<W>(src[i] + e0, w[i]);
-    }
-    if (!set) { rope_lane_angles(p, st, e0, pos, &rl); set = true; }      // while the first rows are on their way
-#pragma unroll
-    for (int i = 0; i < ROPE_U; ++i) rope_turn<E>(p, rl, src[i], e0, w[i]);
-    __syncwarp();                                   // in place: all of a row is read before any of it is written
-#pragma unroll
-    for (int i = 0; i < ROPE_U; ++i) {
-      const int h = r + i * G;
-      if (src[i]) rope_store<W>((h < p.nq ? qo + (int64_t)h * p.D : ko + (int64_t)(h - p.nq) * p.D) + e0, w[i]);
-    }
-  }
+  const auto angles = [&]() {
+    if (!set) rope_lane_angles<PARTNER>(p, st, e0, pos, &rl);
+    set = true;
+  };
+  rope_rows<E, LPR, PARTNER>(p, rl, r0, min(r1, p.nq), reinterpret_cast<const E *>(p.q) + t * p.qs, reinterpret_cast<E *>(p.qo) + t * p.qos, lane, angles);
+  rope_rows<E, LPR, PARTNER>(p, rl, max(r0 - p.nq, 0), r1 - p.nq, reinterpret_cast<const E *>(p.k) + t * p.ks, reinterpret_cast<E *>(p.ko) + t * p.kos, lane, angles);
 }
 
 // The sequence of row t (the last one that starts at or before it), found by the whole warp 32 at a time; -1: none.
@@ -240,11 +279,57 @@ __device__ __forceinline__ int rope_sequence(const SxRopeArgs &p, int t, int lan
   return t < p.row_start[lo + 1] ? lo : -1;
 }
 
-// Rows of new tokens: queries and keys turned, keys and values to their pages.  Q8: as e4m3 codes with one power-of-two scale
+// Rows [h0, h1) of a token's keys (TURN) or values to their places in the pool; Q8: as e4m3 codes with one power-of-two scale
 // per row, exactly as the unrotated append writes the bf16 row that the rotation leaves.
-template <int LPR, bool Q8>
-__global__ void __launch_bounds__(ROPE_THREADS) sx_rope_append_kernel(const SxRopeArgs p, const __grid_constant__ SxRopeSteps st) {
-  constexpr int G = 32 / LPR;
+template <int LPR, int PARTNER, bool Q8, bool TURN, typename A>
+__device__ __forceinline__ void rope_place(const SxRopeArgs &p, RopeLane &rl, int h0, int h1, const bf16 *src, void *pool, uint8_t *scales,
+                                           const int64_t &place, int lane, A angles) {
+  constexpr int G = 32 / LPR, U = PARTNER == PARTNER_LOAD ? 2 : 4;
+  const int e0 = (lane % LPR) * 8;
+#pragma unroll 1
+  for (int r = h0; r < h1; r += G * U) {
+    uint32_t w[U][4];
+    const int h = r + lane / LPR;
+    const bf16 *from = src + (int64_t)h * p.D + e0;
+    int n = e0 < p.D ? (h1 - h + G - 1) / G : 0;                 // rows that this lane has
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      w[i][0] = w[i][1] = w[i][2] = w[i][3] = 0;
+      if (i < n) rope_load<4>(from + i * G * p.D, w[i]);
+    }
+    angles();
+    if (TURN) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) rope_turn<bf16, PARTNER>(p, rl, i < n ? from + i * G * p.D - e0 : nullptr, e0, w[i]);
+    }
+    if (place < 0) n = 0;
+    int64_t at = place + (int64_t)h * p.page;
+#pragma unroll
+    for (int i = 0; i < U; ++i, at += G * p.page) {
+      if (Q8) {
+        const uint32_t m = 0x7fff7fffu;
+        uint32_t top = __vmaxu2(__vmaxu2(w[i][0] & m, w[i][1] & m), __vmaxu2(w[i][2] & m, w[i][3] & m));
+        top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+        for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (i < n) {
+          const int byte = sx_kv8_scale_byte(top);
+          const float up = sx_kv8_inverse(byte);
+          uint2 c = make_uint2(0, 0);
+          if (byte != 255) c = make_uint2(sx_kv8_codes4(w[i][0], w[i][1], up), sx_kv8_codes4(w[i][2], w[i][3], up));
+          *reinterpret_cast<uint2 *>(reinterpret_cast<uint8_t *>(pool) + at * p.D + e0) = c;
+          if (e0 == 0) scales[at] = (uint8_t)byte;
+        }
+      } else if (i < n) {
+        rope_store<4>(reinterpret_cast<bf16 *>(pool) + at * p.D + e0, w[i]);
+      }
+    }
+  }
+}
+
+// Rows of new tokens: queries and keys turned, keys and values to their pages.
+template <int LPR, int PARTNER, bool Q8>
+__global__ void __launch_bounds__(ROPE_THREADS, PARTNER == PARTNER_LOAD ? 4 : 8) sx_rope_append_kernel(const SxRopeArgs p, const __grid_constant__ SxRopeSteps st) {
   sx_pdl_wait();                              // dependents start when this kernel has completed: they may read the pages
   if (blockIdx.x == 0)
     for (int b = threadIdx.x; b < p.B; b += ROPE_THREADS) {
@@ -254,76 +339,29 @@ __global__ void __launch_bounds__(ROPE_THREADS) sx_rope_append_kernel(const SxRo
   const int lane = threadIdx.x & 31, unit = blockIdx.x * (ROPE_THREADS / 32) + (threadIdx.x >> 5);
   const int t = unit / p.slices;
   if (t >= p.T) return;
-  const int all = p.nq + p.nk + p.nv, turned = p.nq + p.nk;
-  const int r0 = (unit - t * p.slices) * p.rows_per_warp, r1 = min(all, r0 + p.rows_per_warp);
+  const int r0 = (unit - t * p.slices) * p.rows_per_warp, r1 = min(p.nq + p.nk + p.nv, r0 + p.rows_per_warp);
   const int e0 = (lane % LPR) * 8;
-  const bool mine = e0 < p.D;
-  const bf16 *q = reinterpret_cast<const bf16 *>(p.q) + t * p.qs, *k = reinterpret_cast<const bf16 *>(p.k) + t * p.ks,
-             *v = reinterpret_cast<const bf16 *>(p.v) + t * p.vs;
-  bf16 *qo = reinterpret_cast<bf16 *>(p.qo) + t * p.qos;
+  int first = 0;
+  const int b = rope_sequence(p, t, lane, &first);
+  if (b < 0) return;                          // a row behind the last sequence
   RopeLane rl;
-  rope_lane_set(p, e0, lane, &rl);
+  rope_lane_set<PARTNER>(p, e0, lane, &rl);
   int64_t place = -1;                         // first row of the pool for this token
-  bool set = false, exists = true;
-#pragma unroll 1
-  for (int r = r0 + lane / LPR; r - lane / LPR < r1; r += G * ROPE_U) {
-    uint32_t w[ROPE_U][4];
-    const bf16 *src[ROPE_U];
-#pragma unroll
-    for (int i = 0; i < ROPE_U; ++i) {
-      const int h = r + i * G;
-      src[i] = (mine && h < r1) ? (h < p.nq ? q + (int64_t)h * p.D : h < turned ? k + (int64_t)(h - p.nq) * p.D : v + (int64_t)(h - turned) * p.D) : nullptr;
-      w[i][0] = w[i][1] = w[i][2] = w[i][3] = 0;
-      if (src[i]) rope_load<4>(src[i] + e0, w[i]);
-    }
-    if (!set) {                               // while the first rows are on their way
-      set = true;
-      int first = 0;
-      const int b = rope_sequence(p, t, lane, &first);
-      exists = b >= 0;
-      if (exists) {
-        const int64_t slot = (int64_t)p.pos_start[b] + (t - first), lp = slot < 0 ? -1 : slot / p.page;
-        int pp = -1;
-        if (lp >= 0 && lp < p.max_pages) pp = p.page_table[(int64_t)b * p.max_pages + lp];
-        if (pp < 0 || pp >= p.num_pages) sx_set_status(p.status, SX_ERR_CAPACITY);
-        else place = (int64_t)pp * p.nk * p.page + slot % p.page;
-        if (rl.in) rope_lane_angles(p, st, e0, p.pos ? p.pos[t] : (int)slot, &rl);
-      }
-    }
-    if (!exists) return;                      // a row behind the last sequence (the same for the whole warp)
-#pragma unroll
-    for (int i = 0; i < ROPE_U; ++i) {
-      const int h = r + i * G;
-      uint32_t x[4] = {w[i][0], w[i][1], w[i][2], w[i][3]};
-      rope_turn<bf16>(p, rl, src[i], e0, x);
-      if (h < turned) { w[i][0] = x[0]; w[i][1] = x[1]; w[i][2] = x[2]; w[i][3] = x[3]; }
-    }
-    __syncwarp();                             // queries in place: all of a row is read before any of it is written
-#pragma unroll
-    for (int i = 0; i < ROPE_U; ++i) {
-      const int h = r + i * G;
-      const bool is_v = h >= turned;
-      const int64_t at = place + (int64_t)(is_v ? h - turned : h - p.nq) * p.page;
-      if (Q8) {
-        const uint32_t m = 0x7fff7fffu;
-        uint32_t top = __vmaxu2(__vmaxu2(w[i][0] & m, w[i][1] & m), __vmaxu2(w[i][2] & m, w[i][3] & m));
-        top = max(top & 0xffffu, top >> 16);
-#pragma unroll
-        for (int o = 1; o < LPR; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (src[i] && h >= p.nq && place >= 0) {
-          const int byte = sx_kv8_scale_byte(top);
-          const float up = sx_kv8_inverse(byte);
-          uint2 c = make_uint2(0, 0);
-          if (byte != 255) c = make_uint2(sx_kv8_codes4(w[i][0], w[i][1], up), sx_kv8_codes4(w[i][2], w[i][3], up));
-          *reinterpret_cast<uint2 *>(reinterpret_cast<uint8_t *>(is_v ? p.vp : p.kp) + at * p.D + e0) = c;
-          if (e0 == 0) (is_v ? p.vsc : p.ksc)[at] = (uint8_t)byte;
-        }
-      } else if (src[i] && h >= p.nq && place >= 0) {
-        rope_store<4>(reinterpret_cast<bf16 *>(is_v ? p.vp : p.kp) + at * p.D + e0, w[i]);
-      }
-      if (src[i] && h < p.nq) rope_store<4>(qo + (int64_t)h * p.D + e0, w[i]);
-    }
-  }
+  bool set = false;
+  const auto angles = [&]() {                 // while the first rows are on their way: the token's place and angles
+    if (set) return;
+    set = true;
+    const int64_t slot = (int64_t)p.pos_start[b] + (t - first), lp = slot < 0 ? -1 : slot / p.page;
+    int pp = -1;
+    if (lp >= 0 && lp < p.max_pages) pp = p.page_table[(int64_t)b * p.max_pages + lp];
+    if (r0 < p.nq + p.nk) rope_lane_angles<PARTNER>(p, st, e0, p.pos ? p.pos[t] : (int)slot, &rl);
+    if (pp < 0 || pp >= p.num_pages) sx_set_status(p.status, SX_ERR_CAPACITY);
+    else place = (int64_t)pp * p.nk * p.page + slot % p.page;
+  };
+  const int k0 = p.nq, v0 = p.nq + p.nk;
+  rope_rows<bf16, LPR, PARTNER>(p, rl, r0, min(r1, k0), reinterpret_cast<const bf16 *>(p.q) + t * p.qs, reinterpret_cast<bf16 *>(p.qo) + t * p.qos, lane, angles);
+  rope_place<LPR, PARTNER, Q8, true>(p, rl, max(r0 - k0, 0), min(r1, v0) - k0, reinterpret_cast<const bf16 *>(p.k) + t * p.ks, p.kp, p.ksc, place, lane, angles);
+  rope_place<LPR, PARTNER, Q8, false>(p, rl, max(r0 - v0, 0), r1 - v0, reinterpret_cast<const bf16 *>(p.v) + t * p.vs, p.vp, p.vsc, place, lane, angles);
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
@@ -408,20 +446,13 @@ static sx_status rope_args(const sx_rotation *plan, int head_dim, SxRopeArgs *p,
   return SX_OK;
 }
 
-static int sms_of_current_device() {
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return 0;
-  return n;
-}
-
-static int lanes_per_row(int d) { int l = 2; while (l * 8 < d) l <<= 1; return l; }
+static int lanes_per_row(int d) { int l = 4; while (l * 8 < d) l <<= 1; return l; }
 
 // A warp takes all rows of a token where that makes 16 warps per SM; below that the rows are cut into as many slices as make
 // them, down to one row per lane.
 static sx_status rope_grid(SxRopeArgs *p, unsigned *grid) {
   const int all = p->nq + p->nk + p->nv, G = 32 / lanes_per_row(p->D);
-  const int sm = sms_of_current_device();
+  const int sm = sx_sm_count();
   if (!sm) return SX_ERR_CUDA;
   int slices = (16 * sm + p->T - 1) / p->T, most = (all + G - 1) / G;
   if (slices > most) slices = most;
@@ -433,15 +464,20 @@ static sx_status rope_grid(SxRopeArgs *p, unsigned *grid) {
   return SX_OK;
 }
 
+template <typename E, int PARTNER>
+static sx_status launch_rope_of(const SxRopeArgs &p, const SxRopeSteps &s, unsigned grid, cudaStream_t st) {
+  switch (lanes_per_row(p.D)) {
+    case 4: return sx_rc(sx_launch(sx_rope_kernel<E, 4, PARTNER>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
+    case 8: return sx_rc(sx_launch(sx_rope_kernel<E, 8, PARTNER>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
+    case 16: return sx_rc(sx_launch(sx_rope_kernel<E, 16, PARTNER>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
+    default: return sx_rc(sx_launch(sx_rope_kernel<E, 32, PARTNER>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
+  }
+}
 template <typename E>
 static sx_status launch_rope(const SxRopeArgs &p, const SxRopeSteps &s, unsigned grid, cudaStream_t st) {
-  switch (lanes_per_row(p.D)) {
-    case 2: return sx_rc(sx_launch(sx_rope_kernel<E, 2>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
-    case 4: return sx_rc(sx_launch(sx_rope_kernel<E, 4>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
-    case 8: return sx_rc(sx_launch(sx_rope_kernel<E, 8>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
-    case 16: return sx_rc(sx_launch(sx_rope_kernel<E, 16>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
-    default: return sx_rc(sx_launch(sx_rope_kernel<E, 32>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
-  }
+  if (p.partner == PARTNER_LANE) return launch_rope_of<E, PARTNER_LANE>(p, s, grid, st);
+  if (p.partner == PARTNER_SHUFFLE) return launch_rope_of<E, PARTNER_SHUFFLE>(p, s, grid, st);
+  return launch_rope_of<E, PARTNER_LOAD>(p, s, grid, st);
 }
 
 extern "C" sx_status sx_rope(const sx_rotation *plan, int32_t dtype, int32_t transpose, int32_t T, const int32_t *pos_d,
@@ -472,14 +508,19 @@ extern "C" sx_status sx_rope(const sx_rotation *plan, int32_t dtype, int32_t tra
   return launch_rope<float>(p, s, grid, st);
 }
 
+template <bool Q8, int PARTNER>
+static sx_status launch_append_of(const SxRopeArgs &p, const SxRopeSteps &s, unsigned grid, cudaStream_t st) {
+  switch (lanes_per_row(p.D)) {
+    case 4: return sx_rc(sx_launch(sx_rope_append_kernel<4, PARTNER, Q8>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
+    case 8: return sx_rc(sx_launch(sx_rope_append_kernel<8, PARTNER, Q8>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
+    default: return sx_rc(sx_launch(sx_rope_append_kernel<16, PARTNER, Q8>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
+  }
+}
 template <bool Q8>
 static sx_status launch_append(const SxRopeArgs &p, const SxRopeSteps &s, unsigned grid, cudaStream_t st) {
-  switch (p.D) {
-    case 16: return sx_rc(sx_launch(sx_rope_append_kernel<2, Q8>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
-    case 32: return sx_rc(sx_launch(sx_rope_append_kernel<4, Q8>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
-    case 64: return sx_rc(sx_launch(sx_rope_append_kernel<8, Q8>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
-    default: return sx_rc(sx_launch(sx_rope_append_kernel<16, Q8>, dim3(grid), dim3(ROPE_THREADS), 0, st, p, s));
-  }
+  if (p.partner == PARTNER_LANE) return launch_append_of<Q8, PARTNER_LANE>(p, s, grid, st);
+  if (p.partner == PARTNER_SHUFFLE) return launch_append_of<Q8, PARTNER_SHUFFLE>(p, s, grid, st);
+  return launch_append_of<Q8, PARTNER_LOAD>(p, s, grid, st);
 }
 
 extern "C" sx_status sx_kv_append_rope(const sx_rotation *plan, const sx_kv_shape *sh, const sx_kv *kv, int32_t T,

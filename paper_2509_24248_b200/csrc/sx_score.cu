@@ -381,13 +381,6 @@ static sx_status score_args(int32_t T, int32_t V, int32_t n_given, const int32_t
   return SX_OK;
 }
 
-static int sms_of_current_device() {
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-    return 0;
-  return n;
-}
-
 extern "C" sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void *logits_d, int64_t stride, int32_t n_given,
                                  const int32_t *tok_d, float temperature, int32_t top, const sx_logprob_out *out, int32_t *status_d,
                                  void *stream) {
@@ -395,7 +388,7 @@ extern "C" sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void
   SX_TRY(score_args(T, V, n_given, tok_d, temperature, top, out, status_d, &p));
   if (dtype < SX_BF16 || dtype > SX_F32 || !aligned16(logits_d) || stride < V) return SX_ERR_INVALID_ARG;
   if (T == 0) return SX_OK;
-  const int sm = sms_of_current_device();
+  const int sm = sx_sm_count();
   if (!sm) return SX_ERR_CUDA;
   // CTAs per row: until there are four per SM, as long as each has two groups per lane
   const int64_t groups = (int64_t)V * (dtype == SX_F32 ? 4 : 2) / SCORE_GROUP_BYTES;
@@ -430,7 +423,7 @@ static ScoreWs score_ws(int rows, int V, int sm) {
 }
 
 extern "C" size_t sx_head_logprobs_ws_bytes(int32_t T, int32_t V) {
-  const int sm = sms_of_current_device();
+  const int sm = sx_sm_count();
   if (T < 1 || V < 1 || V > SX_MAX_SCORE_VOCAB || !sm) return 0;
   return score_ws(score_part(T), V, sm).total;
 }
@@ -444,7 +437,7 @@ extern "C" sx_status sx_head_logprobs(const void *head_d, int32_t tiled, int32_t
   if (H < 8 || H % 8) return SX_ERR_UNSUPPORTED;
   if (T == 0) return SX_OK;
   int dev = 0, sm = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || !(sm = sms_of_current_device())) return SX_ERR_CUDA;
+  if (cudaGetDevice(&dev) != cudaSuccess || !(sm = sx_sm_count())) return SX_ERR_CUDA;
   const int part = score_part(T);
   const ScoreWs w = score_ws(part, V, sm);
   if (!ws_d || ((uintptr_t)ws_d & 255) || ws_bytes < w.total) return SX_ERR_WORKSPACE;
