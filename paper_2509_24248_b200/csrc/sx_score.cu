@@ -37,30 +37,44 @@ struct SxScoreArgs {
   int32_t *top_tok, *status;
 };
 
-// The 32 best (value, id) that a warp has met, best first, lane by lane.  Entries come with ascending ids, so an equal value goes
-// behind.
+// The 32 best (value, id) that a warp has met as packed keys, best first, lane by lane; 0 = none.  Entries come with ascending ids,
+// so one that only equals the `top`-th value is not among the first `top`.
 struct ScoreList {
-  float v;
-  int id;
-  __device__ __forceinline__ void clear() { v = -INFINITY; id = -1; }
-  __device__ __forceinline__ void insert(float nv, int nid, int lane) {
-    // an entry stays in front if it is not smaller; empty ones (id -1) are behind everything
-    const int at = __popc(__ballot_sync(0xffffffffu, id >= 0 && v >= nv));
-    const float uv = __shfl_up_sync(0xffffffffu, v, 1);
-    const int ui = __shfl_up_sync(0xffffffffu, id, 1);
-    if (lane > at) { v = uv; id = ui; }
-    if (lane == at) { v = nv; id = nid; }
+  unsigned long long key;
+  float floor;                         // value of the top-th entry, -inf while there is none
+  __device__ __forceinline__ void clear() { key = 0ull; floor = -INFINITY; }
+  static __device__ __forceinline__ unsigned long long step(unsigned long long k, int stride, bool larger) {
+    const unsigned long long o = __shfl_xor_sync(0xffffffffu, k, stride);
+    return (o > k) == larger ? o : k;
   }
-  // a candidate of every lane, ids ascending with the lanes; those that cannot be among the first `top` are left out
-  __device__ __forceinline__ void offer(float nv, int nid, bool on, int top, int lane) {
-    const float kth = __shfl_sync(0xffffffffu, v, top - 1);
-    const int kid = __shfl_sync(0xffffffffu, id, top - 1);
-    uint32_t m = __ballot_sync(0xffffffffu, on && (kid < 0 || nv > kth));
-    while (m) {
-      const int l = __ffs(m) - 1;
-      m &= m - 1;
-      insert(__shfl_sync(0xffffffffu, nv, l), __shfl_sync(0xffffffffu, nid, l), lane);
+  __device__ __forceinline__ void offer(float v, int id, int top, int lane) {
+    uint32_t m = __ballot_sync(0xffffffffu, v > floor);
+    if (m == 0) return;
+    const unsigned long long k = v > floor ? sx_pack(v, (uint32_t)id) : 0ull;
+    if (__popc(m) > 8) {
+      // sort the new ones (a bitonic network over the lanes), then the better half of both lists, which is bitonic, again
+      unsigned long long n = k;
+#pragma unroll
+      for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+        for (int stride = size / 2; stride > 0; stride /= 2) n = step(n, stride, ((lane & size) == 0) == ((lane & stride) == 0));
+      // size 32: (lane & 32) == 0 always, so the whole descends
+      n = __shfl_sync(0xffffffffu, n, 31 - lane);
+      key = n > key ? n : key;
+#pragma unroll
+      for (int stride = 16; stride > 0; stride /= 2) key = step(key, stride, (lane & stride) == 0);
+    } else {
+      while (m) {
+        const unsigned long long n = __shfl_sync(0xffffffffu, k, __ffs(m) - 1);
+        m &= m - 1;
+        const int at = __popc(__ballot_sync(0xffffffffu, key > n));
+        const unsigned long long up = __shfl_up_sync(0xffffffffu, key, 1);
+        if (lane > at) key = up;
+        if (lane == at) key = n;
+      }
     }
+    const unsigned long long kth = __shfl_sync(0xffffffffu, key, top - 1);
+    floor = kth ? sx_pack_value(kth) : -INFINITY;
   }
 };
 
@@ -68,7 +82,7 @@ struct ScoreShared {
   unsigned long long list[SCORE_WARPS * 32];                          // the warps' lists of groups, packed (value, id)
   unsigned long long group[32];                                       // the best groups
   unsigned long long cand[32 * SCORE_MAX_GROUP];                      // their elements that can be among the best
-  unsigned long long best[SCORE_MAX_CLUSTER * 32];                    // the best elements (of every CTA of a row, in the first)
+  unsigned long long best[32];                                        // the best elements
   float sum[SCORE_WARPS][3], row[3];
   int n_cand;
 };
@@ -93,13 +107,14 @@ __device__ __forceinline__ void score_block_sum(ScoreShared &sh, ScoreSum a, flo
 // the warps' lists -> the `top` best groups in sh.group (0: none)
 __device__ __forceinline__ void score_best_groups(ScoreShared &sh, const ScoreList &l, int top) {
   const int lane = threadIdx.x & 31;
-  const unsigned long long mine = l.id >= 0 ? sx_pack(l.v, (uint32_t)l.id) : 0ull;
+  const unsigned long long mine = l.key;
   sh.list[threadIdx.x] = mine;
   if (threadIdx.x < 32) sh.group[threadIdx.x] = 0ull;
   if (threadIdx.x == 0) sh.n_cand = 0;
   __syncthreads();
   if (mine && lane < top) {
     int rank = 0;
+#pragma unroll
     for (int w = 0; w < SCORE_WARPS; ++w) {
       // lists descend: the number of entries before mine, by halving
       const unsigned long long *p = sh.list + w * 32;
@@ -119,15 +134,16 @@ __device__ __forceinline__ void score_candidate(ScoreShared &sh, float v, int in
   if (v >= kth && v > -INFINITY) sh.cand[atomicAdd(&sh.n_cand, 1)] = sx_pack(v + 0.f, (uint32_t)index);    // -0 counts as 0
 }
 
-// The `top` best of n different keys in src, best first, to dst (0 behind the last).  The order in which src was filled does not
-// matter.
+// The `top` best of n keys in src (different but for zeros, which are none), best first, to dst (0 behind the last).  The order
+// in which src was filled does not matter.
 __device__ __forceinline__ void score_rank(const unsigned long long *src, int n, int top, unsigned long long *dst) {
-  for (int i = threadIdx.x; i < top; i += SCORE_THREADS)
-    if (i >= n) dst[i] = 0ull;
+  if (threadIdx.x < 32) dst[threadIdx.x] = 0ull;
+  __syncthreads();
   for (int i = threadIdx.x; i < n; i += SCORE_THREADS) {
     const unsigned long long mine = src[i];
-    int rank = mine ? 0 : top;
-    for (int j = 0; j < n && rank < top; ++j) rank += src[j] > mine ? 1 : 0;
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) rank += src[j] > mine ? 1 : 0;
     if (mine && rank < top) dst[rank] = mine;
   }
 }
@@ -258,7 +274,7 @@ __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScor
     a.s = s2.x;
     a.t = t2.x;
     const float gm = sx_warp_max(v);
-    if (p.top) l.offer(gm, id, lane == 0 && gm > -INFINITY, p.top, lane);
+    if (p.top) l.offer(lane == 0 ? gm : -INFINITY, id, p.top, lane);
   };
   if (at == 0 && lead) edge(x, lead, 0);
   uint32_t w[16];
@@ -271,14 +287,37 @@ __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScor
     if (next < whole) { score_load32(body + (int64_t)next * GE, n); score_load32(body + (int64_t)next * GE + GE / 2, n + 8); }
     float gm = -INFINITY;
     if (g < whole) gm = score_group<E>(w, p.scale, a);
-    if (p.top) l.offer(gm, g + 1, g < whole && gm > -INFINITY, p.top, lane);
+    if (p.top) l.offer(gm, g + 1, p.top, lane);
 #pragma unroll
     for (int i = 0; i < 16; ++i) w[i] = n[i];
   }
   if (at == 0 && rest) edge(body + (int64_t)whole * GE, rest, whole + 1);
   score_block_sum(sh, a, p.scale);
+  if (p.top) score_best_groups(sh, l, p.top);
+  if (cluster > 1) {
+    // the first CTA joins the sums and the lists of groups of all
+    cg::cluster_group cl = cg::this_cluster();
+    cl.sync();
+    if (rank == 0) {
+      if (warp == 0) {
+        ScoreSum b;
+        b.clear();
+        if (lane < cluster) {
+          const ScoreShared *o = cl.map_shared_rank(&sh, lane);
+          b.m = o->row[0]; b.s = o->row[1]; b.t = o->row[2];
+        }
+        b.warp_join(p.scale);
+        if (lane == 0) { sh.row[0] = b.m; sh.row[1] = b.s; sh.row[2] = b.t; }
+      }
+      for (int i = threadIdx.x; i < cluster * p.top; i += SCORE_THREADS)
+        sh.list[i] = cl.map_shared_rank(&sh, i / p.top)->group[i % p.top];
+    }
+    cl.sync();                                   // no CTA leaves while its shared memory is read
+    if (rank != 0) return;
+    if (p.top) score_rank(sh.list, cluster * p.top, p.top, sh.group);
+    __syncthreads();
+  }
   if (p.top) {
-    score_best_groups(sh, l, p.top);
     const float kth = sh.group[p.top - 1] ? sx_pack_value(sh.group[p.top - 1]) : -INFINITY;
     for (int i = warp; i < p.top; i += SCORE_WARPS) {
       if (!sh.group[i]) break;
@@ -290,34 +329,7 @@ __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScor
     score_rank(sh.cand, sh.n_cand, p.top, sh.best);
     __syncthreads();
   }
-  const unsigned long long *best = sh.best;
-  if (cluster > 1) {
-    cg::cluster_group cl = cg::this_cluster();
-    cl.sync();
-    if (rank == 0) {
-      // the other CTAs' sums and lists; the lists side by side, then ranked together
-      if (warp == 0) {
-        ScoreSum b;
-        b.clear();
-        if (lane < cluster) {
-          const ScoreShared *o = cl.map_shared_rank(&sh, lane);
-          b.m = o->row[0]; b.s = o->row[1]; b.t = o->row[2];
-        }
-        b.warp_join(p.scale);
-        __syncwarp();
-        if (lane == 0) { sh.row[0] = b.m; sh.row[1] = b.s; sh.row[2] = b.t; }
-      }
-      for (int i = threadIdx.x; i < cluster * p.top; i += SCORE_THREADS)
-        sh.cand[i] = cl.map_shared_rank(&sh, i / p.top)->best[i % p.top];
-      __syncthreads();
-      if (p.top) score_rank(sh.cand, cluster * p.top, p.top, sh.list);
-      __syncthreads();
-      best = sh.list;
-    }
-    cl.sync();                                   // no CTA leaves while its shared memory is read
-    if (rank != 0) return;
-  }
-  score_write(sh, p, row, best, [&](int i) { return ScoreElem<E>::one(x[i]); });
+  score_write(sh, p, row, sh.best, [&](int i) { return ScoreElem<E>::one(x[i]); });
 }
 
 // ---- from hidden states: what the product left ---------------------------------------------------------------------------
@@ -342,7 +354,7 @@ __global__ void __launch_bounds__(SCORE_THREADS) sx_score_head_kernel(const SxSc
 #pragma unroll 2
     for (int g = threadIdx.x; g - lane < groups; g += SCORE_THREADS) {
       const float v = g < groups ? gm[g] : -INFINITY;
-      l.offer(v, g, v > -INFINITY, p.top, lane);
+      l.offer(v, g, p.top, lane);
     }
     score_best_groups(sh, l, p.top);
     const float kth = sh.group[p.top - 1] ? sx_pack_value(sh.group[p.top - 1]) : -INFINITY;
