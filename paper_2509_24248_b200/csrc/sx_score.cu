@@ -27,6 +27,7 @@ namespace cg = cooperative_groups;
 #define SCORE_WARPS (SCORE_THREADS / 32)
 #define SCORE_GROUP_BYTES 64
 #define SCORE_MAX_GROUP 32             // elements of a group
+static_assert(SX_MAX_GIVEN <= SCORE_THREADS && SX_MAX_ALTERNATIVES <= 32, "a thread per given token, a lane per alternative");
 #define SCORE_MAX_CLUSTER 8
 
 struct SxScoreArgs {
@@ -47,10 +48,13 @@ struct ScoreList {
     const unsigned long long o = __shfl_xor_sync(0xffffffffu, k, stride);
     return (o > k) == larger ? o : k;
   }
-  __device__ __forceinline__ void offer(float v, int id, int top, int lane) {
-    uint32_t m = __ballot_sync(0xffffffffu, v > floor);
+  // shared: the floor of some warp of the CTA, the largest but for races.  A group below any warp's floor is not among the best of
+  // the row, so whatever is read here lets enough through and the result does not depend on it.
+  __device__ __forceinline__ void offer(float v, int id, int top, int lane, volatile float *shared) {
+    const bool on = v > floor && v >= *shared;
+    uint32_t m = __ballot_sync(0xffffffffu, on);
     if (m == 0) return;
-    const unsigned long long k = v > floor ? sx_pack(v, (uint32_t)id) : 0ull;
+    const unsigned long long k = on ? sx_pack(v, (uint32_t)id) : 0ull;
     if (__popc(m) > 8) {
       // sort the new ones (a bitonic network over the lanes), then the better half of both lists, which is bitonic, again
       unsigned long long n = k;
@@ -75,6 +79,7 @@ struct ScoreList {
     }
     const unsigned long long kth = __shfl_sync(0xffffffffu, key, top - 1);
     floor = kth ? sx_pack_value(kth) : -INFINITY;
+    if (lane == 0 && floor > *shared) *shared = floor;
   }
 };
 
@@ -85,6 +90,7 @@ struct ScoreShared {
   unsigned long long best[32];                                        // the best elements
   float sum[SCORE_WARPS][3], row[3];
   int n_cand;
+  float floor;
 };
 
 // ---- steps shared by both forms; every thread of the CTA calls them ------------------------------------------------
@@ -106,13 +112,12 @@ __device__ __forceinline__ void score_block_sum(ScoreShared &sh, ScoreSum a, flo
 
 // the warps' lists -> the `top` best groups in sh.group (0: none)
 __device__ __forceinline__ void score_best_groups(ScoreShared &sh, const ScoreList &l, int top) {
-  const int lane = threadIdx.x & 31;
-  const unsigned long long mine = l.key;
-  sh.list[threadIdx.x] = mine;
+  sh.list[threadIdx.x] = l.key;
   if (threadIdx.x < 32) sh.group[threadIdx.x] = 0ull;
   if (threadIdx.x == 0) sh.n_cand = 0;
   __syncthreads();
-  if (mine && lane < top) {
+  if ((int)threadIdx.x < SCORE_WARPS * top) {
+    const unsigned long long mine = sh.list[threadIdx.x / top * 32 + threadIdx.x % top];
     int rank = 0;
 #pragma unroll
     for (int w = 0; w < SCORE_WARPS; ++w) {
@@ -124,7 +129,7 @@ __device__ __forceinline__ void score_best_groups(ScoreShared &sh, const ScoreLi
         if (p[lo + step - 1] > mine) lo += step;
       rank += lo + (p[lo] > mine ? 1 : 0);
     }
-    if (rank < top) sh.group[rank] = mine;
+    if (mine && rank < top) sh.group[rank] = mine;
   }
   __syncthreads();
 }
@@ -148,31 +153,27 @@ __device__ __forceinline__ void score_rank(const unsigned long long *src, int n,
   }
 }
 
-// Results of a row.  logit(i): the raw logit of token i.  A row with a NaN or an infinite logit has no probabilities: NaN, and no
+// Results of a row.  Thread i holds the i-th given token and, if that is one of the vocabulary, its logit.  A row with a NaN or an infinite logit has no probabilities: NaN, and no
 // alternatives; where every logit is -inf no token has any.
-template <typename F>
-__device__ __forceinline__ void score_write(const ScoreShared &sh, const SxScoreArgs &p, int row, const unsigned long long *best, F logit) {
+__device__ __forceinline__ void score_write(const ScoreShared &sh, const SxScoreArgs &p, int row, const unsigned long long *best, int tok, float given) {
   const float m = sh.row[0], s = sh.row[1], t = sh.row[2], LN2 = 0.6931471805599453f, NaN = __int_as_float(0x7fffffff);
   const bool bad = !(s >= 0.f) || m == INFINITY, none = !bad && m == -INFINITY;
   const float ln = none ? 0.f : logf(s);
   const auto log_p = [&](float x) { return fmaf(x - m, p.inverse, -ln); };
-  for (int i = threadIdx.x; i < p.n_given; i += SCORE_THREADS) {
-    const int64_t at = (int64_t)row * p.n_given + i;
-    const int tok = p.tok[at];
+  if ((int)threadIdx.x < p.n_given) {
     float y = 0.f;
     if (tok >= 0 && tok < p.V) {
-      const float x = logit(tok);
-      y = bad ? NaN : x == -INFINITY ? -INFINITY : log_p(x);
+      y = bad ? NaN : given == -INFINITY ? -INFINITY : log_p(given);
     } else if (tok != -1) {
       y = NaN;
       sx_set_status(p.status, SX_ERR_CAPACITY);
     }
-    p.logp[at] = y;
+    p.logp[(int64_t)row * p.n_given + threadIdx.x] = y;
   }
   if (p.entropy && threadIdx.x == 0) p.entropy[row] = bad ? NaN : none ? 0.f : ln - LN2 * (t / s);
-  for (int i = threadIdx.x; i < p.top; i += SCORE_THREADS) {
-    const unsigned long long key = best[i];
-    const int64_t at = (int64_t)row * p.top + i;
+  if ((int)threadIdx.x < p.top) {
+    const unsigned long long key = best[threadIdx.x];
+    const int64_t at = (int64_t)row * p.top + threadIdx.x;
     const bool on = key != 0ull && !bad;
     if (p.top_tok) p.top_tok[at] = on ? (int)sx_pack_index(key) : -1;
     if (p.top_logp) p.top_logp[at] = bad ? NaN : on ? log_p(sx_pack_value(key)) : -INFINITY;
@@ -211,12 +212,12 @@ __device__ __forceinline__ void score_load32(const void *p, uint32_t *w) {
 }
 
 template <typename E>
-__device__ __forceinline__ float score_group(const uint32_t *w, float scale, ScoreSum &a) {
-  float gm;
+__device__ __forceinline__ float score_group_max(const uint32_t *w) {
   if constexpr (sizeof(E) == 4) {
-    gm = __uint_as_float(w[0]);
+    float gm = __uint_as_float(w[0]);
 #pragma unroll
     for (int i = 1; i < 16; ++i) gm = fmaxf(gm, __uint_as_float(w[i]));
+    return gm;
   } else {
     uint32_t x[8];
 #pragma unroll
@@ -227,11 +228,12 @@ __device__ __forceinline__ float score_group(const uint32_t *w, float scale, Sco
       for (int i = 0; i < o; ++i) x[i] = ScoreElem<E>::max(x[i], x[i + o]);
     float u, v;
     ScoreElem<E>::pair(x[0], &u, &v);
-    gm = fmaxf(u, v);
+    return fmaxf(u, v);
   }
-  if (gm > a.m) a.raise(gm, scale);
-  const float ref = a.m > -INFINITY ? a.m : 0.f;
-  float2 s2 = make_float2(a.s, 0.f), t2 = make_float2(a.t, 0.f);
+}
+// f(pair of neighbouring elements) for all of a group
+template <typename E, typename F>
+__device__ __forceinline__ void score_pairs(const uint32_t *w, F f) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     float2 x;
@@ -241,12 +243,57 @@ __device__ __forceinline__ float score_group(const uint32_t *w, float scale, Sco
     } else {
       ScoreElem<E>::pair(w[i], &x.x, &x.y);
     }
-    score_pair(x, scale, ref, s2, t2);
+    f(x);
   }
-  a.s = s2.x + s2.y;
-  a.t = t2.x + t2.y;
-  return gm;
 }
+
+// The sums of a lane over its groups.  Issue slots bound this pass, so the plain way takes as few as it can: d = fma(x, c, -r),
+// r = fl(c m), with sums relative to 2^r, and a new reference only where a group is more than 2^SCORE_SLACK above the old one.
+// It has no place for -inf (0 * -inf) and none for logits so large that the rounding of r counts: the first such group
+// turns the warp over to the careful way for the rest of the row (score_pair: two more instructions an element), whose sums are
+// relative to 2^(c m).  r is off by fma(m, c, -r), exactly; the two differ by that power of two.
+#define SCORE_SLACK 4.f
+struct ScorePlain {
+  ScoreSum a;
+  float r, limit;                  // limit: a group maximum above it asks for a new reference
+  __device__ __forceinline__ void clear() { a.clear(); r = 0.f; limit = -INFINITY; }
+  // false: not added, the careful way has to
+  template <typename E>
+  __device__ __forceinline__ bool add(const uint32_t *w, float gm, bool on, float scale, float slack) {
+    if (on && gm > limit) {
+      const float to = gm * scale;
+      if (a.m > -INFINITY) {
+        const float d = fmaxf(r - to, -200.f), f = score_exp2(d);
+        a.t = f * fmaf(a.s, d, a.t);
+        a.s *= f;
+      }
+      a.m = gm;
+      r = to;
+      limit = gm + slack;
+    }
+    float s0 = a.s, s1 = 0.f, t0 = a.t, t1 = 0.f;
+    score_pairs<E>(w, [&](float2 x) {
+      const float d0 = fmaf(x.x, scale, -r), d1 = fmaf(x.y, scale, -r), e0 = score_exp2(d0), e1 = score_exp2(d1);
+      s0 += e0;
+      s1 += e1;
+      t0 = fmaf(e0, d0, t0);
+      t1 = fmaf(e1, d1, t1);
+    });
+    t0 += t1;
+    if (!__all_sync(0xffffffffu, !on || (t0 == t0 && fabsf(r) < 1048576.f))) return false;
+    if (on) { a.s = s0 + s1; a.t = t0; }
+    return true;
+  }
+  // relative to 2^(c m) from here on
+  __device__ __forceinline__ ScoreSum exact(float scale) {
+    if (a.s != 0.f) {
+      const float off = fmaf(a.m, scale, -r), f = score_exp2(-off);
+      a.t = f * fmaf(-off, a.s, a.t);
+      a.s *= f;
+    }
+    return a;
+  }
+};
 
 // A cluster of CTAs per row.  Groups of 64 bytes on 32-byte boundaries, a lane each; what a row has before its first boundary is
 // group 0, what is behind the last whole group the last one (their elements one per lane, by the first warp of the row).
@@ -254,6 +301,8 @@ template <typename E>
 __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScoreArgs p, const E *__restrict__ logits, int64_t stride, int cluster) {
   constexpr int GE = SCORE_GROUP_BYTES / (int)sizeof(E);
   __shared__ ScoreShared sh;
+  if (threadIdx.x == 0) sh.floor = -INFINITY;
+  __syncthreads();
   sx_pdl_wait();
   const int row = blockIdx.x / cluster, rank = blockIdx.x - row * cluster;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -261,37 +310,80 @@ __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScor
   const int lead = min(p.V, (int)((32u - ((uint32_t)(uintptr_t)x & 31u)) & 31u) / (int)sizeof(E));
   const int whole = (p.V - lead) / GE, rest = p.V - lead - whole * GE;
   const E *body = x + lead;
-  ScoreSum a;
-  ScoreList l;
-  a.clear();
-  l.clear();
-  const int at = rank * SCORE_WARPS + warp, all = cluster * SCORE_WARPS;
-  const auto edge = [&](const E *from, int n, int id) {
-    const float v = lane < n ? ScoreElem<E>::one(from[lane]) : -INFINITY;
-    if (v > a.m) a.raise(v, p.scale);
-    float2 s2 = make_float2(a.s, 0.f), t2 = make_float2(a.t, 0.f);
-    score_pair(make_float2(v, -INFINITY), p.scale, a.m > -INFINITY ? a.m : 0.f, s2, t2);
-    a.s = s2.x;
-    a.t = t2.x;
-    const float gm = sx_warp_max(v);
-    if (p.top) l.offer(lane == 0 ? gm : -INFINITY, id, p.top, lane);
-  };
-  if (at == 0 && lead) edge(x, lead, 0);
-  uint32_t w[16];
-  int g = at * 32 + lane;
-  if (g < whole) { score_load32(body + (int64_t)g * GE, w); score_load32(body + (int64_t)g * GE + GE / 2, w + 8); }
-#pragma unroll 1
-  for (; g - lane < whole; g += all * 32) {
-    uint32_t n[16];
-    const int next = g + all * 32;
-    if (next < whole) { score_load32(body + (int64_t)next * GE, n); score_load32(body + (int64_t)next * GE + GE / 2, n + 8); }
-    float gm = -INFINITY;
-    if (g < whole) gm = score_group<E>(w, p.scale, a);
-    if (p.top) l.offer(gm, g + 1, p.top, lane);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) w[i] = n[i];
+  // what the results need of the given tokens is on its way during the pass
+  int tok = -1;
+  float given = 0.f;
+  if (rank == 0 && (int)threadIdx.x < p.n_given) {
+    tok = p.tok[(int64_t)row * p.n_given + threadIdx.x];
+    if (tok >= 0 && tok < p.V) given = ScoreElem<E>::one(x[tok]);
   }
-  if (at == 0 && rest) edge(body + (int64_t)whole * GE, rest, whole + 1);
+  ScoreList l;
+  l.clear();
+  const int at = rank * SCORE_WARPS + warp, stride_g = cluster * SCORE_THREADS;
+  // the elements before and behind the groups, one per lane; their sums are added last
+  const float e0 = at == 0 && lane < lead ? ScoreElem<E>::one(x[lane]) : -INFINITY;
+  const float e1 = at == 0 && lane < rest ? ScoreElem<E>::one(body[(int64_t)whole * GE + lane]) : -INFINITY;
+  if (p.top && at == 0 && lead) {
+    const float gm = sx_warp_max(e0);
+    l.offer(lane == 0 ? gm : -INFINITY, 0, p.top, lane, &sh.floor);
+  }
+  // a lane without a group reads the last one again (a load under a condition costs a move for every word)
+  const auto load = [&](int g, uint32_t *w) {
+    const E *from = body + (int64_t)min(g, whole - 1) * GE;
+    score_load32(from, w);
+    score_load32(from + GE / 2, w + 8);
+  };
+  int g = at * 32 + lane;
+  ScoreSum a;
+  {
+    ScorePlain f;
+    f.clear();
+    const float slack = SCORE_SLACK / p.scale;
+    uint32_t w0[16], w1[16];
+    const auto take = [&](const uint32_t *w) {
+      const bool on = g < whole;
+      const float gm = on ? score_group_max<E>(w) : -INFINITY;
+      if (!f.add<E>(w, gm, on, p.scale, slack)) return false;
+      if (p.top) l.offer(gm, g + 1, p.top, lane, &sh.floor);
+      g += stride_g;
+      return true;
+    };
+    if (g - lane < whole) load(g, w0);
+#pragma unroll 1
+    while (g - lane < whole) {
+      load(g + stride_g, w1);
+      if (!take(w0)) break;
+      if (g - lane >= whole) break;
+      load(g + stride_g, w0);
+      if (!take(w1)) break;
+    }
+    a = f.exact(p.scale);
+  }
+#pragma unroll 1
+  for (; g - lane < whole; g += stride_g) {     // the careful way
+    uint32_t w[16];
+    load(g, w);
+    const float gm = g < whole ? score_group_max<E>(w) : -INFINITY;
+    if (g < whole) {
+      if (gm > a.m) a.raise(gm, p.scale);
+      const float ref = a.m > -INFINITY ? a.m : 0.f;
+      float2 s2 = make_float2(a.s, 0.f), t2 = make_float2(a.t, 0.f);
+      score_pairs<E>(w, [&](float2 v) { score_pair(v, p.scale, ref, s2, t2); });
+      a.s = s2.x + s2.y;
+      a.t = t2.x + t2.y;
+    }
+    if (p.top) l.offer(gm, g + 1, p.top, lane, &sh.floor);
+  }
+  if (at == 0 && lead + rest) {
+    const float gm = sx_warp_max(e1);
+    if (p.top && rest) l.offer(lane == 0 ? gm : -INFINITY, whole + 1, p.top, lane, &sh.floor);
+    const float top = fmaxf(e0, e1);
+    if (top > a.m) a.raise(top, p.scale);
+    float2 s2 = make_float2(a.s, 0.f), t2 = make_float2(a.t, 0.f);
+    score_pair(make_float2(e0, e1), p.scale, a.m > -INFINITY ? a.m : 0.f, s2, t2);
+    a.s = s2.x + s2.y;
+    a.t = t2.x + t2.y;
+  }
   score_block_sum(sh, a, p.scale);
   if (p.top) score_best_groups(sh, l, p.top);
   if (cluster > 1) {
@@ -329,7 +421,7 @@ __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScor
     score_rank(sh.cand, sh.n_cand, p.top, sh.best);
     __syncthreads();
   }
-  score_write(sh, p, row, sh.best, [&](int i) { return ScoreElem<E>::one(x[i]); });
+  score_write(sh, p, row, sh.best, tok, given);
 }
 
 // ---- from hidden states: what the product left ---------------------------------------------------------------------------
@@ -337,10 +429,18 @@ __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScor
 // with `tiles` tiles of 128 to a row, -inf behind the vocabulary).
 __global__ void __launch_bounds__(SCORE_THREADS) sx_score_head_kernel(const SxScoreArgs p, const SxScoreOut o, int row0, int ctas, int tiles) {
   __shared__ ScoreShared sh;
+  if (threadIdx.x == 0) sh.floor = -INFINITY;
+  __syncthreads();
   sx_pdl_launch_dependents();
   sx_pdl_wait();
   const int row = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, groups = tiles * 4;
   const float *x = o.logits + (size_t)row * tiles * SX_TILE_M, *gm = o.maxima + (size_t)row * groups;
+  int tok = -1;
+  float given = 0.f;
+  if ((int)threadIdx.x < p.n_given) {
+    tok = p.tok[(int64_t)(row0 + row) * p.n_given + threadIdx.x];
+    if (tok >= 0 && tok < p.V) given = x[tok];
+  }
   ScoreSum a;
   a.clear();
   for (int i = threadIdx.x; i < ctas; i += SCORE_THREADS) {
@@ -354,7 +454,7 @@ __global__ void __launch_bounds__(SCORE_THREADS) sx_score_head_kernel(const SxSc
 #pragma unroll 2
     for (int g = threadIdx.x; g - lane < groups; g += SCORE_THREADS) {
       const float v = g < groups ? gm[g] : -INFINITY;
-      l.offer(v, g, p.top, lane);
+      l.offer(v, g, p.top, lane, &sh.floor);
     }
     score_best_groups(sh, l, p.top);
     const float kth = sh.group[p.top - 1] ? sx_pack_value(sh.group[p.top - 1]) : -INFINITY;
@@ -367,7 +467,7 @@ __global__ void __launch_bounds__(SCORE_THREADS) sx_score_head_kernel(const SxSc
     score_rank(sh.cand, sh.n_cand, p.top, sh.best);
     __syncthreads();
   }
-  score_write(sh, p, row0 + row, sh.best, [&](int i) { return x[i]; });
+  score_write(sh, p, row0 + row, sh.best, tok, given);
 }
 
 // ---- entry point -----------------------------------------------------------------------------------------------------------
@@ -402,10 +502,10 @@ extern "C" sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void
   if (T == 0) return SX_OK;
   const int sm = sx_sm_count();
   if (!sm) return SX_ERR_CUDA;
-  // CTAs per row: until there are four per SM, as long as each has two groups per lane
+  // CTAs per row: as many as there is room for at a time (four per SM), as long as each has two groups per lane
   const int64_t groups = (int64_t)V * (dtype == SX_F32 ? 4 : 2) / SCORE_GROUP_BYTES;
   int cluster = 1;
-  while (cluster < SCORE_MAX_CLUSTER && (int64_t)T * cluster < 4 * sm && groups >= (int64_t)cluster * 2 * SCORE_THREADS) cluster *= 2;
+  while (cluster < SCORE_MAX_CLUSTER && (int64_t)T * cluster * 2 <= 4 * sm && groups >= (int64_t)cluster * 2 * SCORE_THREADS) cluster *= 2;
   if ((int64_t)T * cluster > 0x7fffffffll) return SX_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)(T * cluster)), block(SCORE_THREADS);
   cudaStream_t st = (cudaStream_t)stream;

@@ -44,29 +44,13 @@ struct ScoreSum {
   }
 };
 
-// Two more elements.  Nothing below 2^-126 of the reference counts; holding d to -200 keeps 0 * -inf out of t.
-__device__ __forceinline__ float2 score_add2(float2 a, float2 b) {
-  float2 y;
-  asm("{.reg .b64 p, q, r;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tadd.rn.f32x2 r, p, q;\n\tmov.b64 {%0, %1}, r;}"
-      : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return y;
-}
-__device__ __forceinline__ float2 score_mul2(float2 a, float2 b) {
-  float2 y;
-  asm("{.reg .b64 p, q, r;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tmul.rn.f32x2 r, p, q;\n\tmov.b64 {%0, %1}, r;}"
-      : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return y;
-}
-__device__ __forceinline__ float2 score_fma2(float2 a, float2 b, float2 c) {
-  float2 y;
-  asm("{.reg .b64 p, q, r;\n\tmov.b64 p, {%2, %3};\n\tmov.b64 q, {%4, %5};\n\tmov.b64 r, {%6, %7};\n\tfma.rn.f32x2 r, p, q, r;\n\tmov.b64 {%0, %1}, r;}"
-      : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return y;
-}
+// Two more elements.  Nothing below 2^-126 of the reference counts; holding d to -200 keeps 0 * -inf out of t.  (Packed fp32
+// pairs were tried: the moves that bring the pairs together cost more than the instructions saved.)
 __device__ __forceinline__ void score_pair(float2 x, float scale, float ref, float2 &s, float2 &t) {
-  float2 d = score_mul2(score_add2(x, make_float2(-ref, -ref)), make_float2(scale, scale));
-  d = make_float2(score_max_nan(d.x, -200.f), score_max_nan(d.y, -200.f));
-  const float2 e = make_float2(score_exp2(d.x), score_exp2(d.y));
-  s = score_add2(s, e);
-  t = score_fma2(e, d, t);
+  const float d0 = score_max_nan((x.x - ref) * scale, -200.f), d1 = score_max_nan((x.y - ref) * scale, -200.f);
+  const float e0 = score_exp2(d0), e1 = score_exp2(d1);
+  s.x += e0;
+  s.y += e1;
+  t.x = fmaf(e0, d0, t.x);
+  t.y = fmaf(e1, d1, t.y);
 }
