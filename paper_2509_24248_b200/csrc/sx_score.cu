@@ -10,8 +10,8 @@
 // Alternatives without a sort: the row is cut into groups of neighbouring elements whose maxima fall out of the pass.  The k
 // best elements (larger first, then the lower index) lie in the k best groups (larger maximum first, then the lower group), so
 // every warp keeps a sorted list of its 32 best groups, one per lane; the lists are joined by counting, for each entry, how many
-// others are before it, and the elements of the k best groups that are not below the k-th of these maxima are ranked the
-// same way.  The cost does not depend on the values but for the number of insertions.
+// others are before it, and the elements of the k best groups go through lists of the same kind.  The cost does not depend on
+// the values but for the number of insertions.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -23,12 +23,10 @@
 
 namespace cg = cooperative_groups;
 
-#define SCORE_THREADS 256
-#define SCORE_WARPS (SCORE_THREADS / 32)
 #define SCORE_GROUP_BYTES 64
-#define SCORE_MAX_GROUP 32             // elements of a group
-static_assert(SX_MAX_GIVEN <= SCORE_THREADS && SX_MAX_ALTERNATIVES <= 32, "a thread per given token, a lane per alternative");
-#define SCORE_MAX_CLUSTER 8
+#define SCORE_MAX_WARPS 8              // warps of a CTA, which has one row
+#define SCORE_MAX_CLUSTER 8            // CTAs of a row
+static_assert(SX_MAX_GIVEN <= 64 && SX_MAX_ALTERNATIVES <= 32, "two given tokens per lane of the smallest CTA, a lane per alternative");
 
 struct SxScoreArgs {
   int T, V, n_given, top;
@@ -38,8 +36,7 @@ struct SxScoreArgs {
   int32_t *top_tok, *status;
 };
 
-// The 32 best (value, id) that a warp has met as packed keys, best first, lane by lane; 0 = none.  Entries come with ascending ids,
-// so one that only equals the `top`-th value is not among the first `top`.
+// The 32 best entries that a warp has met, as packed (value, id) keys: best first, lane by lane; 0 = none.
 struct ScoreList {
   unsigned long long key;
   float floor;                         // value of the top-th entry, -inf while there is none
@@ -48,21 +45,15 @@ struct ScoreList {
     const unsigned long long o = __shfl_xor_sync(0xffffffffu, k, stride);
     return (o > k) == larger ? o : k;
   }
-  // shared: the floor of some warp of the CTA, the largest but for races.  A group below any warp's floor is not among the best of
-  // the row, so whatever is read here lets enough through and the result does not depend on it.
-  __device__ __forceinline__ void offer(float v, int id, int top, int lane, volatile float *shared) {
-    const bool on = v > floor && v >= *shared;
-    uint32_t m = __ballot_sync(0xffffffffu, on);
-    if (m == 0) return;
-    const unsigned long long k = on ? sx_pack(v, (uint32_t)id) : 0ull;
+  // the keys k of the lanes in m
+  __device__ __forceinline__ void take(unsigned long long k, uint32_t m, int top, int lane) {
     if (__popc(m) > 8) {
-      // sort the new ones (a bitonic network over the lanes), then the better half of both lists, which is bitonic, again
-      unsigned long long n = k;
+      // sort the new ones (a bitonic network over the lanes, descending), then the better half of both lists, which is bitonic
+      unsigned long long n = m >> lane & 1 ? k : 0ull;
 #pragma unroll
       for (int size = 2; size <= 32; size *= 2)
 #pragma unroll
         for (int stride = size / 2; stride > 0; stride /= 2) n = step(n, stride, ((lane & size) == 0) == ((lane & stride) == 0));
-      // size 32: (lane & 32) == 0 always, so the whole descends
       n = __shfl_sync(0xffffffffu, n, 31 - lane);
       key = n > key ? n : key;
 #pragma unroll
@@ -79,100 +70,159 @@ struct ScoreList {
     }
     const unsigned long long kth = __shfl_sync(0xffffffffu, key, top - 1);
     floor = kth ? sx_pack_value(kth) : -INFINITY;
+  }
+  // Groups: ids ascend with the lanes and from call to call, so one that only equals the floor is not among the first `top`.
+  // shared: the floor of some warp of the CTA, the largest but for races.  A group below any warp's floor is not among the best of
+  // the row, so whatever is read here lets enough through and the result does not depend on it.
+  __device__ __forceinline__ void offer_group(float v, int id, int top, int lane, volatile float *shared) {
+    const bool on = v > floor && v >= *shared;
+    const uint32_t m = __ballot_sync(0xffffffffu, on);
+    if (m == 0) return;
+    take(sx_pack(v + 0.f, (uint32_t)id), m, top, lane);                  // -0 counts as 0
     if (lane == 0 && floor > *shared) *shared = floor;
+  }
+  // Elements of groups in any order
+  __device__ __forceinline__ void offer(float v, int id, bool on, int top, int lane) {
+    const unsigned long long k = on && v > -INFINITY ? sx_pack(v + 0.f, (uint32_t)id) : 0ull;      // a NaN is not above -inf
+    const unsigned long long kth = __shfl_sync(0xffffffffu, key, top - 1);
+    const uint32_t m = __ballot_sync(0xffffffffu, k > kth);
+    if (m) take(k, m, top, lane);
   }
 };
 
 struct ScoreShared {
-  unsigned long long list[SCORE_WARPS * 32];                          // the warps' lists of groups, packed (value, id)
-  unsigned long long group[32];                                       // the best groups
-  unsigned long long cand[32 * SCORE_MAX_GROUP];                      // their elements that can be among the best
-  unsigned long long best[32];                                        // the best elements
-  float sum[SCORE_WARPS][3], row[3];
-  int n_cand;
+  unsigned long long list[SCORE_MAX_WARPS * 32];                      // the lists of the warps, or of the CTAs of a cluster
+  unsigned long long group[32], best[32];                             // the best groups, the best elements
+  float sum[SCORE_MAX_WARPS][3], row[3];
   float floor;
 };
+static_assert(SCORE_MAX_CLUSTER <= SCORE_MAX_WARPS, "the lists of a cluster lie where those of the warps did");
 
-// ---- steps shared by both forms; every thread of the CTA calls them ------------------------------------------------
+// ---- steps shared by both forms; all W warps of the CTA call them ---------------------------------------------------
+template <int W> __device__ __forceinline__ void score_sync() { if (W == 1) __syncwarp(); else __syncthreads(); }
+
 // sums of the warps -> sh.row
-__device__ __forceinline__ void score_block_sum(ScoreShared &sh, ScoreSum a, float scale) {
+template <int W>
+__device__ __forceinline__ void score_join_sums(ScoreShared &sh, ScoreSum a, float scale) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   a.warp_join(scale);
-  if (lane == 0) { sh.sum[warp][0] = a.m; sh.sum[warp][1] = a.s; sh.sum[warp][2] = a.t; }
-  __syncthreads();
-  if (warp == 0) {
-    ScoreSum b;
-    b.clear();
-    if (lane < SCORE_WARPS) { b.m = sh.sum[lane][0]; b.s = sh.sum[lane][1]; b.t = sh.sum[lane][2]; }
-    b.warp_join(scale);
-    if (lane == 0) { sh.row[0] = b.m; sh.row[1] = b.s; sh.row[2] = b.t; }
+  if (W > 1) {
+    if (lane == 0) { sh.sum[warp][0] = a.m; sh.sum[warp][1] = a.s; sh.sum[warp][2] = a.t; }
+    __syncthreads();
+    if (warp == 0) {
+      a.clear();
+      if (lane < W) { a.m = sh.sum[lane][0]; a.s = sh.sum[lane][1]; a.t = sh.sum[lane][2]; }
+      a.warp_join(scale);
+    }
   }
-  __syncthreads();
+  if (threadIdx.x == 0) { sh.row[0] = a.m; sh.row[1] = a.s; sh.row[2] = a.t; }
+  score_sync<W>();
 }
 
-// the warps' lists -> the `top` best groups in sh.group (0: none)
-__device__ __forceinline__ void score_best_groups(ScoreShared &sh, const ScoreList &l, int top) {
-  sh.list[threadIdx.x] = l.key;
-  if (threadIdx.x < 32) sh.group[threadIdx.x] = 0ull;
-  if (threadIdx.x == 0) sh.n_cand = 0;
-  __syncthreads();
-  if ((int)threadIdx.x < SCORE_WARPS * top) {
-    const unsigned long long mine = sh.list[threadIdx.x / top * 32 + threadIdx.x % top];
+// The `top` best of n descending lists of 32 in sh.list -> dst, best first, 0 behind the last: an entry's place is the number of
+// entries before it, found in every list by halving.
+template <int W>
+__device__ __forceinline__ void score_join_lists(ScoreShared &sh, int n, int top, unsigned long long *dst) {
+  if (threadIdx.x < 32) dst[threadIdx.x] = 0ull;
+  score_sync<W>();
+  for (int e = threadIdx.x; e < n * top; e += W * 32) {
+    const unsigned long long mine = sh.list[e / top * 32 + e % top];
     int rank = 0;
-#pragma unroll
-    for (int w = 0; w < SCORE_WARPS; ++w) {
-      // lists descend: the number of entries before mine, by halving
-      const unsigned long long *p = sh.list + w * 32;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const unsigned long long *p = sh.list + i * 32;
       int lo = 0;
 #pragma unroll
       for (int step = 16; step > 0; step >>= 1)
         if (p[lo + step - 1] > mine) lo += step;
       rank += lo + (p[lo] > mine ? 1 : 0);
     }
-    if (mine && rank < top) sh.group[rank] = mine;
-  }
-  __syncthreads();
-}
-
-// one element of one of the best groups
-__device__ __forceinline__ void score_candidate(ScoreShared &sh, float v, int index, float kth) {
-  if (v >= kth && v > -INFINITY) sh.cand[atomicAdd(&sh.n_cand, 1)] = sx_pack(v + 0.f, (uint32_t)index);    // -0 counts as 0
-}
-
-// The `top` best of n keys in src (different but for zeros, which are none), best first, to dst (0 behind the last).  The order
-// in which src was filled does not matter.
-__device__ __forceinline__ void score_rank(const unsigned long long *src, int n, int top, unsigned long long *dst) {
-  if (threadIdx.x < 32) dst[threadIdx.x] = 0ull;
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += SCORE_THREADS) {
-    const unsigned long long mine = src[i];
-    int rank = 0;
-#pragma unroll 8
-    for (int j = 0; j < n; ++j) rank += src[j] > mine ? 1 : 0;
     if (mine && rank < top) dst[rank] = mine;
   }
+  score_sync<W>();
+}
+template <int W>
+__device__ __forceinline__ void score_join_warps(ScoreShared &sh, const ScoreList &l, int top, unsigned long long *dst) {
+  if (W == 1) {
+    dst[threadIdx.x] = (int)threadIdx.x < top ? l.key : 0ull;
+    __syncwarp();
+  } else {
+    sh.list[threadIdx.x] = l.key;
+    score_join_lists<W>(sh, W, top, dst);
+  }
 }
 
-// Results of a row.  Thread i holds the i-th given token and, if that is one of the vocabulary, its logit.  A row with a NaN or an infinite logit has no probabilities: NaN, and no
-// alternatives; where every logit is -inf no token has any.
-__device__ __forceinline__ void score_write(const ScoreShared &sh, const SxScoreArgs &p, int row, const unsigned long long *best, int tok, float given) {
+// The best elements of the best groups -> sh.best.  element(group id, lane, &index): the lane's element, on: whether it has one.
+template <int W, typename F>
+__device__ __forceinline__ void score_best_elements(ScoreShared &sh, int top, F element) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  ScoreList l;
+  l.clear();
+  // four groups' elements on the way at a time
+#pragma unroll 1
+  for (int i = warp; i < top; i += 4 * W) {
+    float v[4];
+    int index[4];
+    bool on[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const unsigned long long g = i + j * W < top ? sh.group[i + j * W] : 0ull;
+      on[j] = g != 0ull;
+      v[j] = -INFINITY;
+      index[j] = 0;
+      if (on[j]) v[j] = element((int)sx_pack_index(g), lane, &index[j], &on[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) l.offer(v[j], index[j], on[j], top, lane);
+  }
+  score_join_warps<W>(sh, l, top, sh.best);
+}
+
+// The given tokens of a row and their logits, which are on their way during the pass.
+template <int W> struct ScoreGiven {
+  enum { N = W == 1 ? 2 : 1 };
+  int tok[N];
+  float x[N];
+  template <typename F>
+  __device__ __forceinline__ void fetch(const SxScoreArgs &p, int row, F logit) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int i = threadIdx.x + j * W * 32;
+      tok[j] = -1;
+      x[j] = 0.f;
+      if (i < p.n_given) {
+        tok[j] = p.tok[(int64_t)row * p.n_given + i];
+        if (tok[j] >= 0 && tok[j] < p.V) x[j] = logit(tok[j]);
+      }
+    }
+  }
+};
+
+// Results of a row.  A row with a NaN or an infinite logit has no probabilities: NaN, and no alternatives; where every logit is -inf
+// no token has any.
+template <int W>
+__device__ __forceinline__ void score_write(const ScoreShared &sh, const SxScoreArgs &p, int row, const ScoreGiven<W> &given) {
   const float m = sh.row[0], s = sh.row[1], t = sh.row[2], LN2 = 0.6931471805599453f, NaN = __int_as_float(0x7fffffff);
   const bool bad = !(s >= 0.f) || m == INFINITY, none = !bad && m == -INFINITY;
   const float ln = none ? 0.f : logf(s);
   const auto log_p = [&](float x) { return fmaf(x - m, p.inverse, -ln); };
-  if ((int)threadIdx.x < p.n_given) {
-    float y = 0.f;
-    if (tok >= 0 && tok < p.V) {
-      y = bad ? NaN : given == -INFINITY ? -INFINITY : log_p(given);
-    } else if (tok != -1) {
-      y = NaN;
-      sx_set_status(p.status, SX_ERR_CAPACITY);
+#pragma unroll
+  for (int j = 0; j < ScoreGiven<W>::N; ++j) {
+    const int i = threadIdx.x + j * W * 32;
+    if (i < p.n_given) {
+      float y = 0.f;
+      if (given.tok[j] >= 0 && given.tok[j] < p.V) {
+        y = bad ? NaN : given.x[j] == -INFINITY ? -INFINITY : log_p(given.x[j]);
+      } else if (given.tok[j] != -1) {
+        y = NaN;
+        sx_set_status(p.status, SX_ERR_CAPACITY);
+      }
+      p.logp[(int64_t)row * p.n_given + i] = y;
     }
-    p.logp[(int64_t)row * p.n_given + threadIdx.x] = y;
   }
   if (p.entropy && threadIdx.x == 0) p.entropy[row] = bad ? NaN : none ? 0.f : ln - LN2 * (t / s);
   if ((int)threadIdx.x < p.top) {
-    const unsigned long long key = best[threadIdx.x];
+    const unsigned long long key = sh.best[threadIdx.x];
     const int64_t at = (int64_t)row * p.top + threadIdx.x;
     const bool on = key != 0ull && !bad;
     if (p.top_tok) p.top_tok[at] = on ? (int)sx_pack_index(key) : -1;
@@ -295,14 +345,15 @@ struct ScorePlain {
   }
 };
 
-// A cluster of CTAs per row.  Groups of 64 bytes on 32-byte boundaries, a lane each; what a row has before its first boundary is
-// group 0, what is behind the last whole group the last one (their elements one per lane, by the first warp of the row).
-template <typename E>
-__global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScoreArgs p, const E *__restrict__ logits, int64_t stride, int cluster) {
+// W warps per CTA, a cluster of CTAs per row.  Groups of 64 bytes on 32-byte boundaries, a lane each; what a row has before its
+// first boundary is group 0, what is behind the last whole group the last one (their elements one per lane, by the first
+// warp of the row).
+template <typename E, int W>
+__global__ void __launch_bounds__(W * 32, 32 / W) sx_score_kernel(const SxScoreArgs p, const E *__restrict__ logits, int64_t stride, int cluster) {
   constexpr int GE = SCORE_GROUP_BYTES / (int)sizeof(E);
   __shared__ ScoreShared sh;
   if (threadIdx.x == 0) sh.floor = -INFINITY;
-  __syncthreads();
+  score_sync<W>();
   sx_pdl_wait();
   const int row = blockIdx.x / cluster, rank = blockIdx.x - row * cluster;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -310,22 +361,17 @@ __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScor
   const int lead = min(p.V, (int)((32u - ((uint32_t)(uintptr_t)x & 31u)) & 31u) / (int)sizeof(E));
   const int whole = (p.V - lead) / GE, rest = p.V - lead - whole * GE;
   const E *body = x + lead;
-  // what the results need of the given tokens is on its way during the pass
-  int tok = -1;
-  float given = 0.f;
-  if (rank == 0 && (int)threadIdx.x < p.n_given) {
-    tok = p.tok[(int64_t)row * p.n_given + threadIdx.x];
-    if (tok >= 0 && tok < p.V) given = ScoreElem<E>::one(x[tok]);
-  }
+  ScoreGiven<W> given;
+  if (rank == 0) given.fetch(p, row, [&](int i) { return ScoreElem<E>::one(x[i]); });
   ScoreList l;
   l.clear();
-  const int at = rank * SCORE_WARPS + warp, stride_g = cluster * SCORE_THREADS;
+  const int at = rank * W + warp, stride_g = cluster * W * 32;
   // the elements before and behind the groups, one per lane; their sums are added last
   const float e0 = at == 0 && lane < lead ? ScoreElem<E>::one(x[lane]) : -INFINITY;
   const float e1 = at == 0 && lane < rest ? ScoreElem<E>::one(body[(int64_t)whole * GE + lane]) : -INFINITY;
   if (p.top && at == 0 && lead) {
     const float gm = sx_warp_max(e0);
-    l.offer(lane == 0 ? gm : -INFINITY, 0, p.top, lane, &sh.floor);
+    l.offer_group(lane == 0 ? gm : -INFINITY, 0, p.top, lane, &sh.floor);
   }
   // a lane without a group reads the last one again (a load under a condition costs a move for every word)
   const auto load = [&](int g, uint32_t *w) {
@@ -344,7 +390,7 @@ __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScor
       const bool on = g < whole;
       const float gm = on ? score_group_max<E>(w) : -INFINITY;
       if (!f.add<E>(w, gm, on, p.scale, slack)) return false;
-      if (p.top) l.offer(gm, g + 1, p.top, lane, &sh.floor);
+      if (p.top) l.offer_group(gm, g + 1, p.top, lane, &sh.floor);
       g += stride_g;
       return true;
     };
@@ -372,11 +418,11 @@ __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScor
       a.s = s2.x + s2.y;
       a.t = t2.x + t2.y;
     }
-    if (p.top) l.offer(gm, g + 1, p.top, lane, &sh.floor);
+    if (p.top) l.offer_group(gm, g + 1, p.top, lane, &sh.floor);
   }
   if (at == 0 && lead + rest) {
     const float gm = sx_warp_max(e1);
-    if (p.top && rest) l.offer(lane == 0 ? gm : -INFINITY, whole + 1, p.top, lane, &sh.floor);
+    if (p.top && rest) l.offer_group(lane == 0 ? gm : -INFINITY, whole + 1, p.top, lane, &sh.floor);
     const float top = fmaxf(e0, e1);
     if (top > a.m) a.raise(top, p.scale);
     float2 s2 = make_float2(a.s, 0.f), t2 = make_float2(a.t, 0.f);
@@ -384,8 +430,8 @@ __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScor
     a.s = s2.x + s2.y;
     a.t = t2.x + t2.y;
   }
-  score_block_sum(sh, a, p.scale);
-  if (p.top) score_best_groups(sh, l, p.top);
+  score_join_sums<W>(sh, a, p.scale);
+  if (p.top) score_join_warps<W>(sh, l, p.top, sh.group);
   if (cluster > 1) {
     // the first CTA joins the sums and the lists of groups of all
     cg::cluster_group cl = cg::this_cluster();
@@ -401,73 +447,57 @@ __global__ void __launch_bounds__(SCORE_THREADS, 4) sx_score_kernel(const SxScor
         b.warp_join(p.scale);
         if (lane == 0) { sh.row[0] = b.m; sh.row[1] = b.s; sh.row[2] = b.t; }
       }
-      for (int i = threadIdx.x; i < cluster * p.top; i += SCORE_THREADS)
-        sh.list[i] = cl.map_shared_rank(&sh, i / p.top)->group[i % p.top];
+      for (int i = threadIdx.x; i < cluster * 32; i += W * 32)
+        sh.list[i] = cl.map_shared_rank(&sh, i / 32)->group[i % 32];
     }
     cl.sync();                                   // no CTA leaves while its shared memory is read
     if (rank != 0) return;
-    if (p.top) score_rank(sh.list, cluster * p.top, p.top, sh.group);
-    __syncthreads();
+    if (p.top) score_join_lists<W>(sh, cluster, p.top, sh.group);
   }
-  if (p.top) {
-    const float kth = sh.group[p.top - 1] ? sx_pack_value(sh.group[p.top - 1]) : -INFINITY;
-    for (int i = warp; i < p.top; i += SCORE_WARPS) {
-      if (!sh.group[i]) break;
-      const int id = (int)sx_pack_index(sh.group[i]);
+  if (p.top)
+    score_best_elements<W>(sh, p.top, [&](int id, int i, int *index, bool *on) {
       const int from = id == 0 ? 0 : lead + (id - 1) * GE, n = id == 0 ? lead : id == whole + 1 ? rest : GE;
-      if (lane < n) score_candidate(sh, ScoreElem<E>::one(x[from + lane]), from + lane, kth);
-    }
-    __syncthreads();
-    score_rank(sh.cand, sh.n_cand, p.top, sh.best);
-    __syncthreads();
-  }
-  score_write(sh, p, row, sh.best, tok, given);
+      *on = i < n;
+      *index = from + i;
+      return i < n ? ScoreElem<E>::one(x[from + i]) : -INFINITY;
+    });
+  score_write<W>(sh, p, row, given);
 }
 
 // ---- from hidden states: what the product left ---------------------------------------------------------------------------
 // One CTA per row: sums [ctas][SX_SCORE_ROWS] of the product's CTAs, maxima of groups of 32 logits, the logits themselves (both
 // with `tiles` tiles of 128 to a row, -inf behind the vocabulary).
-__global__ void __launch_bounds__(SCORE_THREADS) sx_score_head_kernel(const SxScoreArgs p, const SxScoreOut o, int row0, int ctas, int tiles) {
+__global__ void __launch_bounds__(SCORE_MAX_WARPS * 32) sx_score_head_kernel(const SxScoreArgs p, const SxScoreOut o, int row0, int ctas, int tiles) {
+  constexpr int W = SCORE_MAX_WARPS;
   __shared__ ScoreShared sh;
   if (threadIdx.x == 0) sh.floor = -INFINITY;
   __syncthreads();
   sx_pdl_launch_dependents();
   sx_pdl_wait();
-  const int row = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, groups = tiles * 4;
+  const int row = blockIdx.x, lane = threadIdx.x & 31, groups = tiles * 4;
   const float *x = o.logits + (size_t)row * tiles * SX_TILE_M, *gm = o.maxima + (size_t)row * groups;
-  int tok = -1;
-  float given = 0.f;
-  if ((int)threadIdx.x < p.n_given) {
-    tok = p.tok[(int64_t)(row0 + row) * p.n_given + threadIdx.x];
-    if (tok >= 0 && tok < p.V) given = x[tok];
-  }
+  ScoreGiven<W> given;
+  given.fetch(p, row0 + row, [&](int i) { return x[i]; });
   ScoreSum a;
   a.clear();
-  for (int i = threadIdx.x; i < ctas; i += SCORE_THREADS) {
+  for (int i = threadIdx.x; i < ctas; i += W * 32) {
     const float *from = o.sums + ((size_t)i * SX_SCORE_ROWS + row) * 3;
     a.join(from[0], from[1], from[2], p.scale);
   }
-  score_block_sum(sh, a, p.scale);
+  score_join_sums<W>(sh, a, p.scale);
   if (p.top) {
     ScoreList l;
     l.clear();
-#pragma unroll 2
-    for (int g = threadIdx.x; g - lane < groups; g += SCORE_THREADS) {
-      const float v = g < groups ? gm[g] : -INFINITY;
-      l.offer(v, g, p.top, lane, &sh.floor);
-    }
-    score_best_groups(sh, l, p.top);
-    const float kth = sh.group[p.top - 1] ? sx_pack_value(sh.group[p.top - 1]) : -INFINITY;
-    for (int i = warp; i < p.top; i += SCORE_WARPS) {
-      if (!sh.group[i]) break;
-      const int at = (int)sx_pack_index(sh.group[i]) * 32 + lane;
-      score_candidate(sh, x[at], at, kth);
-    }
-    __syncthreads();
-    score_rank(sh.cand, sh.n_cand, p.top, sh.best);
-    __syncthreads();
+#pragma unroll 4
+    for (int g = threadIdx.x; g - lane < groups; g += W * 32)
+      l.offer_group(g < groups ? gm[g] : -INFINITY, g, p.top, lane, &sh.floor);
+    score_join_warps<W>(sh, l, p.top, sh.group);
+    score_best_elements<W>(sh, p.top, [&](int id, int i, int *index, bool *on) {
+      *index = id * 32 + i;
+      return x[id * 32 + i];
+    });
   }
-  score_write(sh, p, row0 + row, sh.best, tok, given);
+  score_write<W>(sh, p, row0 + row, given);
 }
 
 // ---- entry point -----------------------------------------------------------------------------------------------------------
@@ -493,6 +523,34 @@ static sx_status score_args(int32_t T, int32_t V, int32_t n_given, const int32_t
   return SX_OK;
 }
 
+// Warps and CTAs per row.  An SM has room for 32 warps of this kernel.  Where there are rows enough to fill the card four warps
+// share one: the ends of a row (first loads, joining, alternatives: some 5 us in which it reads nothing, at the same time
+// for all rows that began together) weigh less the longer it takes, but more rows at a time mean more places in
+// memory that are read at once (4096 rows of 151936 in bf16 with 8, 4, 2, 1 warps: 237, 220, 297, 424 us).  Below that, as many
+// warps and then CTAs as there is room for at once.  Every warp gets two rounds of groups, where the row has as many.
+struct ScoreSplit { int warps, cluster; };
+static ScoreSplit score_split(int64_t T, int64_t groups, int sm) {
+  const int64_t room = 32ll * sm, most = groups / (2 * 32);
+  ScoreSplit n = {1, 1};
+  while (n.warps < 4 && n.warps * 2 <= most) n.warps *= 2;
+  while (n.warps < SCORE_MAX_WARPS && n.warps * 2 <= most && T * n.warps * 2 <= room) n.warps *= 2;
+  while (n.cluster < SCORE_MAX_CLUSTER && n.warps * n.cluster * 2 <= most && T * n.warps * n.cluster * 2 <= room) n.cluster *= 2;
+  return n;
+}
+
+template <typename E>
+static sx_status launch_score(const SxScoreArgs &p, const void *logits, int64_t stride, ScoreSplit n, cudaStream_t st) {
+  const dim3 grid((unsigned)(p.T * n.cluster)), block(n.warps * 32);
+  const E *x = (const E *)logits;
+  const unsigned c = (unsigned)n.cluster;
+  switch (n.warps) {
+    case 1: return sx_rc(sx_launch_cluster(sx_score_kernel<E, 1>, grid, block, 0, c, st, p, x, stride, n.cluster));
+    case 2: return sx_rc(sx_launch_cluster(sx_score_kernel<E, 2>, grid, block, 0, c, st, p, x, stride, n.cluster));
+    case 4: return sx_rc(sx_launch_cluster(sx_score_kernel<E, 4>, grid, block, 0, c, st, p, x, stride, n.cluster));
+    default: return sx_rc(sx_launch_cluster(sx_score_kernel<E, 8>, grid, block, 0, c, st, p, x, stride, n.cluster));
+  }
+}
+
 extern "C" sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void *logits_d, int64_t stride, int32_t n_given,
                                  const int32_t *tok_d, float temperature, int32_t top, const sx_logprob_out *out, int32_t *status_d,
                                  void *stream) {
@@ -502,18 +560,13 @@ extern "C" sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void
   if (T == 0) return SX_OK;
   const int sm = sx_sm_count();
   if (!sm) return SX_ERR_CUDA;
-  // CTAs per row: as many as there is room for at a time (four per SM), as long as each has two groups per lane
   const int64_t groups = (int64_t)V * (dtype == SX_F32 ? 4 : 2) / SCORE_GROUP_BYTES;
-  int cluster = 1;
-  while (cluster < SCORE_MAX_CLUSTER && (int64_t)T * cluster * 2 <= 4 * sm && groups >= (int64_t)cluster * 2 * SCORE_THREADS) cluster *= 2;
-  if ((int64_t)T * cluster > 0x7fffffffll) return SX_ERR_UNSUPPORTED;
-  const dim3 grid((unsigned)(T * cluster)), block(SCORE_THREADS);
+  const ScoreSplit n = score_split(T, groups, sm);
+  if ((int64_t)T * n.cluster > 0x7fffffffll) return SX_ERR_UNSUPPORTED;
   cudaStream_t st = (cudaStream_t)stream;
-  switch (dtype) {
-    case SX_BF16: return sx_rc(sx_launch_cluster(sx_score_kernel<bf16>, grid, block, 0, (unsigned)cluster, st, p, (const bf16 *)logits_d, stride, cluster));
-    case SX_F16: return sx_rc(sx_launch_cluster(sx_score_kernel<__half>, grid, block, 0, (unsigned)cluster, st, p, (const __half *)logits_d, stride, cluster));
-    default: return sx_rc(sx_launch_cluster(sx_score_kernel<float>, grid, block, 0, (unsigned)cluster, st, p, (const float *)logits_d, stride, cluster));
-  }
+  if (dtype == SX_BF16) return launch_score<bf16>(p, logits_d, stride, n, st);
+  if (dtype == SX_F16) return launch_score<__half>(p, logits_d, stride, n, st);
+  return launch_score<float>(p, logits_d, stride, n, st);
 }
 
 // Rows are taken SX_SCORE_ROWS at a time at most, in as few equal parts as that allows: every part reads the whole head.
@@ -565,7 +618,7 @@ extern "C" sx_status sx_head_logprobs(const void *head_d, int32_t tiled, int32_t
     const int R = T - r0 < part ? T - r0 : part;
     int ctas = 0;
     SX_TRY(sx_launch_score_head((const bf16 *)head_d, tiled != 0, V, H, (const bf16 *)hidden_d + (size_t)r0 * H, R, o, &ctas, sm, status_d, st));
-    SX_TRY(sx_rc(sx_launch(sx_score_head_kernel, dim3(R), dim3(SCORE_THREADS), 0, st, p, o, r0, ctas, tiles)));
+    SX_TRY(sx_rc(sx_launch(sx_score_head_kernel, dim3(R), dim3(SCORE_MAX_WARPS * 32), 0, st, p, o, r0, ctas, tiles)));
   }
   return SX_OK;
 }
