@@ -475,15 +475,15 @@ sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void *logits_d,
                       const int32_t *tok_d, float temperature, int32_t top, const sx_logprob_out *out, int32_t *status_d,
                       void *stream);
 
-/* The same from hidden states: logits = hidden . head^T are formed tile by tile on the tensor cores (fp32 accumulators), their
- * sums taken on the way.  Beside sx_verify, which gives the argmax of the same product alone.
+/* The same from hidden states: logits = hidden . head^T are formed tile by tile on the tensor cores (fp32, in chains of
+ * 512 products whose sums are added with rounding to nearest), their softmax sums taken on the way.  Beside sx_verify, which gives the argmax of the same product alone.
  *   head_d    [V, H] bf16 row-major, or repacked by sx_tile_weight (tiled = 1; rows behind the first V, such as signal rows,
  *             may follow and are not looked at); complete and visible before the call (see the conventions)
  *   hidden_d  [T, H] bf16, contiguous; H a multiple of 8
  * Workspace (256-byte aligned, not shared by calls that may overlap): sx_head_logprobs_ws_bytes for the current device, or 0
  * for a shape that cannot be: about 4.2 bytes per row and token id for up to SX_SCORE_MAX_PART rows (more are taken
  * in parts).  Of it the logits are written once, and read where an alternative or a given token needs them. */
-#define SX_SCORE_MAX_PART 256
+#define SX_SCORE_MAX_PART 1024
 size_t sx_head_logprobs_ws_bytes(int32_t T, int32_t V);
 sx_status sx_head_logprobs(const void *head_d, int32_t tiled, int32_t V, int32_t H, int32_t T, const void *hidden_d,
                            int32_t n_given, const int32_t *tok_d, float temperature, int32_t top, const sx_logprob_out *out,

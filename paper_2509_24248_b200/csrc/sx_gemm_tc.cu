@@ -144,15 +144,25 @@ sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
         const int kb1 = min(p.num_kb, kb0 + p.kb_per_split);
         if (!mbar_wait(smem_u32(&tempty[acc]), acc_phase ^ 1u, abort_flag, p.wait_limit)) break;
         tc_fence_after();
-        const uint32_t d_tmem = tmem_base + (uint32_t)(acc * p.acc_cols);
+        uint32_t d_tmem = tmem_base + (uint32_t)(acc * p.acc_cols);
+        int first = kb0;                                // k-block that begins the accumulator's chain
         for (int kb = kb0; kb < kb1; ++kb) {
+          if (KIND == KIND_SCORE && kb == first + SX_SCORE_CHUNK) {
+            // the chain is long enough (the accumulator truncates): hand it over and go on in the other one
+            tc_commit(smem_u32(&tfull[acc]));
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            if (!mbar_wait(smem_u32(&tempty[acc]), acc_phase ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
+            tc_fence_after();
+            d_tmem = tmem_base + (uint32_t)(acc * p.acc_cols);
+            first = kb;
+          }
           if (!mbar_wait(smem_u32(&full[stage]), phase, abort_flag, p.wait_limit)) { ok = false; break; }
           tc_fence_after();
           const uint32_t a = smem_u32(smem + (size_t)stage * stage_bytes);
           const uint32_t b = a + SX_A_BYTES;
 #pragma unroll
           for (int k = 0; k < SX_BK / 16; ++k)
-            tc_mma(d_tmem, smem_desc(a + k * 32), smem_desc(b + k * 32), idesc, (kb > kb0 || k > 0) ? 1u : 0u);
+            tc_mma(d_tmem, smem_desc(a + k * 32), smem_desc(b + k * 32), idesc, (kb > first || k > 0) ? 1u : 0u);
           tc_commit(smem_u32(&empty[stage]));          // frees the stage once these MMAs have read it
           if (++stage == p.stages) { stage = 0; phase ^= 1u; }
         }
@@ -168,38 +178,46 @@ sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     uint32_t acc_phase = 0;
     sx_pdl_wait();
     if constexpr (KIND == KIND_SCORE) {
-      // Log-probabilities.  The same data flow as the argmax below: a thread owns one token row and a quarter of the vocabulary
-      // rows of each tile, here 32 neighbouring logits at a time, and keeps the running sums of every row it owns in
-      // registers.  The logits and the maximum of each 32 go to memory, for the alternatives and the given tokens alone.
+      // Log-probabilities.  The sums of the accumulator's chains are added in registers, rounding to nearest; then the same data
+      // flow as the argmax below: a thread owns one token row and a quarter of the vocabulary rows of each tile, here 32
+      // neighbouring logits at a time, and keeps the running sums of every row it owns in registers.  The logits and the maximum
+      // of each 32 go to memory, for the alternatives and the given tokens alone.
+      constexpr int CHUNKS = SX_SCORE_FEW / 32;
       float *tb = reinterpret_cast<float *>(epi_smem);          // [128 rows][33]
       const int tid = threadIdx.x - 64, col = tid & 31, part = tid >> 5;
-      ScoreSum sum[SX_ARGMAX_CHUNKS];
+      ScoreSum sum[CHUNKS];
 #pragma unroll
-      for (int ch = 0; ch < SX_ARGMAX_CHUNKS; ++ch) sum[ch].clear();
-      for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        if (!epi_all(mbar_wait(smem_u32(&tfull[acc]), acc_phase, abort_flag, p.wait_limit))) break;
-        tc_fence_after();
-        const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * p.acc_cols);
+      for (int ch = 0; ch < CHUNKS; ++ch) sum[ch].clear();
+      bool ok = true;
+      for (int item = blockIdx.x; item < items && ok; item += gridDim.x) {
+        float v[SX_SCORE_FEW];
+#pragma unroll
+        for (int j = 0; j < SX_SCORE_FEW; ++j) v[j] = 0.f;
+        for (int kb = 0; kb < p.num_kb; kb += SX_SCORE_CHUNK) {
+          ok = epi_all(mbar_wait(smem_u32(&tfull[acc]), acc_phase, abort_flag, p.wait_limit));
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * p.acc_cols);
+#pragma unroll
+          for (int c = 0; c < SX_SCORE_FEW; c += 16)
+            if (c < p.nmma) {
+              float x[16];
+              tc_ld16(taddr + c, x);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) v[c + j] += x[j];
+            }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&tempty[acc]));
+          if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        }
+        if (!ok) break;
         const bool in_vocab = item * SX_TILE_M + et < p.V;
 #pragma unroll
-        for (int ch = 0; ch < SX_ARGMAX_CHUNKS; ++ch) {
+        for (int ch = 0; ch < CHUNKS; ++ch) {
           if (ch * 32 < p.R) {
-            {
-              float v[32];
-              tc_ld16(taddr + ch * 32, v);
-              if (ch * 32 + 16 < p.nmma) tc_ld16(taddr + ch * 32 + 16, v + 16);
-              else {
 #pragma unroll
-                for (int j = 16; j < 32; ++j) v[j] = 0.f;
-              }
-              if ((ch + 1) * 32 >= p.R) {                         // last chunk: the accumulator is free again
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&tempty[acc]));
-              }
-#pragma unroll
-              for (int j = 0; j < 32; ++j) tb[et * 33 + j] = in_vocab ? v[j] : -INFINITY;
-            }
+            for (int j = 0; j < 32; ++j) tb[et * 33 + j] = in_vocab ? v[ch * 32 + j] : -INFINITY;
             epi_bar();
             if (ch * 32 + col < p.R) {
               const float *src = tb + (part * 32) * 33 + col;
@@ -225,24 +243,23 @@ sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
             epi_bar();
           }
         }
-        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
       }
       epi_bar();
 #pragma unroll
-      for (int ch = 0; ch < SX_ARGMAX_CHUNKS; ++ch)
+      for (int ch = 0; ch < CHUNKS; ++ch)
         if (ch * 32 + col < p.R) {
-          float *at = tb + (part * 256 + ch * 32 + col) * 3;
+          float *at = tb + (part * SX_SCORE_FEW + ch * 32 + col) * 3;
           at[0] = sum[ch].m; at[1] = sum[ch].s; at[2] = sum[ch].t;
         }
       epi_bar();
-      for (int r = tid; r < p.R; r += 128) {
+      if (tid < p.R) {
         ScoreSum all;
         all.clear();
         for (int w = 0; w < 4; ++w) {
-          const float *at = tb + (w * 256 + r) * 3;
+          const float *at = tb + (w * SX_SCORE_FEW + tid) * 3;
           all.join(at[0], at[1], at[2], p.sc.scale);
         }
-        float *out = p.sc.sums + ((size_t)blockIdx.x * SX_SCORE_ROWS + r) * 3;
+        float *out = p.sc.sums + ((size_t)blockIdx.x * p.sc.rows + tid) * 3;
         out[0] = all.m; out[1] = all.s; out[2] = all.t;
       }
     } else if (HEAD && p.T == 1 && !p.lse) {
@@ -685,7 +702,7 @@ int sx_gemm_pick_splits(int N, int K, int sm_count) {
 // Tensor map of a weight matrix.  Row-major [N, K]: a box is 128 rows x 64 columns, i.e. 128 pieces of
 // 128 bytes that lie K * 2 bytes apart.  Tiled ([row tile][k-block][128][64], zero padded): the same box
 // is one contiguous 16 KB block, which keeps the DRAM pages it touches open for the whole transfer.
-static bool weight_map(const bf16 *W, int N, int K, bool tiled, CUtensorMap *out) {
+bool sx_weight_map(const bf16 *W, int N, int K, bool tiled, CUtensorMap *out) {
   if (!tiled) return sx_tma_map_2d(W, N, K, SX_TILE_M, out);
   const int tiles = (N + SX_TILE_M - 1) / SX_TILE_M, kbs = (K + SX_BK - 1) / SX_BK;
   return sx_tma_map_2d(W, tiles * kbs * SX_TILE_M, SX_BK, SX_TILE_M, out);
@@ -707,7 +724,7 @@ sx_status sx_launch_gemm_partial(const bf16 *W, int N, int K, const bf16 *X, int
     p.status = status;
     CUtensorMap mw, mx;
     p.w_tiled = tiled ? 1 : 0;
-    if (!weight_map(W, N, K, tiled, &mw) || !sx_tma_map_2d(X + (size_t)r0 * K, rc, K, p.nmma, &mx)) return SX_ERR_CUDA;
+    if (!sx_weight_map(W, N, K, tiled, &mw) || !sx_tma_map_2d(X + (size_t)r0 * K, rc, K, p.nmma, &mx)) return SX_ERR_CUDA;
     const int items = p.num_tiles * p.splits;
     const int per_cta = (items + sm_count - 1) / sm_count;          // the same number of items for every CTA
     const int grid = (items + per_cta - 1) / per_cta;
@@ -736,7 +753,7 @@ sx_status sx_launch_head(const bf16 *W, int Ntot, int V, int K, const bf16 *X, i
   p.lo = lo;
   CUtensorMap mw, mx;
   p.w_tiled = tiled ? 1 : 0;
-  if (!weight_map(W, Ntot, K, tiled, &mw) || !sx_tma_map_2d(X, R, K, p.nmma, &mx)) return SX_ERR_CUDA;
+  if (!sx_weight_map(W, Ntot, K, tiled, &mw) || !sx_tma_map_2d(X, R, K, p.nmma, &mx)) return SX_ERR_CUDA;
   // every CTA gets the same number of tiles (no CTA is left alone with one more 1 MB tile at the end):
   // with w = ceil(tiles / SMs) tiles per CTA, ceil(tiles / w) CTAs cover the matrix
   const int per_cta = (p.num_tiles + sm_count - 1) / sm_count;
@@ -747,9 +764,9 @@ sx_status sx_launch_head(const bf16 *W, int Ntot, int V, int K, const bf16 *X, i
   return SX_OK;
 }
 
-sx_status sx_launch_score_head(const bf16 *W, bool tiled, int V, int K, const bf16 *X, int R, const SxScoreOut &out, int *ctas,
+sx_status sx_launch_score_head(const bf16 *W, bool tiled, int V, int K, const bf16 *X, int R, const SxScoreOut &out, int *parts,
                                int sm_count, int32_t *status, cudaStream_t st) {
-  if ((K % 8) != 0 || R < 1 || R > SX_SCORE_ROWS) return SX_ERR_UNSUPPORTED;
+  if ((K % 8) != 0 || R < 1 || R > SX_SCORE_FEW || R > out.rows) return SX_ERR_UNSUPPORTED;
   SxTcParams p;
   memset(&p, 0, sizeof(p));
   if (!fill_common(p, V, K, R, SX_ARGMAX_SMEM)) return SX_ERR_UNSUPPORTED;
@@ -758,10 +775,10 @@ sx_status sx_launch_score_head(const bf16 *W, bool tiled, int V, int K, const bf
   p.V = V; p.status = status; p.sc = out;
   CUtensorMap mw, mx;
   p.w_tiled = tiled ? 1 : 0;
-  if (!weight_map(W, V, K, tiled, &mw) || !sx_tma_map_2d(X, R, K, p.nmma, &mx)) return SX_ERR_CUDA;
+  if (!sx_weight_map(W, V, K, tiled, &mw) || !sx_tma_map_2d(X, R, K, p.nmma, &mx)) return SX_ERR_CUDA;
   const int per_cta = (p.num_tiles + sm_count - 1) / sm_count;      // as in sx_launch_head
   const int grid = (p.num_tiles + per_cta - 1) / per_cta;
-  *ctas = grid;
+  *parts = grid;
   return sx_rc(sx_launch(sx_tc_gemm_kernel<KIND_SCORE>, dim3(grid), dim3(192), smem_bytes(p, SX_ARGMAX_SMEM), st, mw, mx, p));
 }
 

@@ -125,6 +125,7 @@ sx_status sx_launch_tile_weight(const bf16 *src, int N, int K, bf16 *dst, cudaSt
 sx_status sx_gemm_init(int device);
 // cached 2-D tensor map of a bf16 matrix [rows, cols], box = box_rows x 64 columns, 128-byte swizzle
 struct CUtensorMap_st;
+bool sx_weight_map(const bf16 *W, int N, int K, bool tiled, CUtensorMap_st *out);      // of a GEMM weight, either layout
 bool sx_tma_map_2d(const void *ptr, long long rows, int cols, int box_rows, CUtensorMap_st *out);
 // the same for a matrix of bytes, box = box_rows x 128 columns
 bool sx_tma_map_bytes(const void *ptr, long long rows, int cols, int box_rows, CUtensorMap_st *out);
@@ -152,15 +153,21 @@ sx_status sx_launch_head(const bf16 *W, int Ntot, int V, int K, const bf16 *X, i
                          int32_t *status, cudaStream_t st, const SxSample *smp = nullptr,
                          SxLogitsOut lo = SxLogitsOut{nullptr, 0, SxIndex{nullptr, 1, 0}}, bool tiled = false);
 
-// Head product for log-probabilities: R <= SX_SCORE_ROWS rows; logits [R][tiles * 128] (-inf behind the vocabulary), the maxima of
-// every 32 of them [R][tiles * 4], and per CTA and row the running sums (m, s, t) [ctas][SX_SCORE_ROWS][3] (see sx_score.cuh).
-#define SX_SCORE_ROWS SX_SCORE_MAX_PART
+// Head product for log-probabilities: logits [R][tiles * 128] (-inf behind the vocabulary), the maxima of every 32 of them
+// [R][tiles * 4], and running sums (m, s, t) of the row, [parts][rows][3], one per part of the vocabulary (see sx_score.cuh).  Two kernels:
+// weights on the rows of the product, for up to SX_SCORE_FEW rows (sx_gemm_tc.cu, a part per CTA), and pairs of CTAs with the
+// token rows there, for more (sx_score_tc.cu, a part per tile).
+#define SX_SCORE_FEW 128
+#define SX_SCORE_CHUNK 8         // k-blocks of 64 that one chain of the tensor core's accumulator is long
 struct SxScoreOut {
   float scale;                   // log2(e) / temperature
   float *logits, *maxima, *sums;
+  int rows;                      // of sums
 };
-sx_status sx_launch_score_head(const bf16 *W, bool tiled, int V, int K, const bf16 *X, int R, const SxScoreOut &out, int *ctas,
+sx_status sx_launch_score_head(const bf16 *W, bool tiled, int V, int K, const bf16 *X, int R, const SxScoreOut &out, int *parts,
                                int sm_count, int32_t *status, cudaStream_t st);
+sx_status sx_launch_score_pairs(const bf16 *W, bool tiled, int V, int K, const bf16 *X, int R, const SxScoreOut &out, int *parts,
+                                int32_t *status, cudaStream_t st);
 
 // Speculative sampling with sampled drafts: writes the kept draft token or the residual draw of every
 // verify slot to target_tok [B, P].  target_logits [B * P, V], draft_logits [B, K, V] (K = P - 1), both

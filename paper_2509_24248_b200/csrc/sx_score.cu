@@ -465,9 +465,9 @@ __global__ void __launch_bounds__(W * 32, 32 / W) sx_score_kernel(const SxScoreA
 }
 
 // ---- from hidden states: what the product left ---------------------------------------------------------------------------
-// One CTA per row: sums [ctas][SX_SCORE_ROWS] of the product's CTAs, maxima of groups of 32 logits, the logits themselves (both
+// One CTA per row: sums of the parts of the vocabulary, maxima of groups of 32 logits, the logits themselves (both
 // with `tiles` tiles of 128 to a row, -inf behind the vocabulary).
-__global__ void __launch_bounds__(SCORE_MAX_WARPS * 32) sx_score_head_kernel(const SxScoreArgs p, const SxScoreOut o, int row0, int ctas, int tiles) {
+__global__ void __launch_bounds__(SCORE_MAX_WARPS * 32) sx_score_head_kernel(const SxScoreArgs p, const SxScoreOut o, int row0, int parts, int tiles) {
   constexpr int W = SCORE_MAX_WARPS;
   __shared__ ScoreShared sh;
   if (threadIdx.x == 0) sh.floor = -INFINITY;
@@ -480,8 +480,9 @@ __global__ void __launch_bounds__(SCORE_MAX_WARPS * 32) sx_score_head_kernel(con
   given.fetch(p, row0 + row, [&](int i) { return x[i]; });
   ScoreSum a;
   a.clear();
-  for (int i = threadIdx.x; i < ctas; i += W * 32) {
-    const float *from = o.sums + ((size_t)i * SX_SCORE_ROWS + row) * 3;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < parts; i += W * 32) {
+    const float *from = o.sums + ((size_t)i * o.rows + row) * 3;
     a.join(from[0], from[1], from[2], p.scale);
   }
   score_join_sums<W>(sh, a, p.scale);
@@ -569,21 +570,21 @@ extern "C" sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void
   return launch_score<float>(p, logits_d, stride, n, st);
 }
 
-// Rows are taken SX_SCORE_ROWS at a time at most, in as few equal parts as that allows: every part reads the whole head.
+// Rows are taken SX_SCORE_MAX_PART at a time at most, in as few equal parts as that allows: every part reads the whole head.
 static int score_part(int T) {
-  const int parts = (T + SX_SCORE_ROWS - 1) / SX_SCORE_ROWS;
+  const int parts = (T + SX_SCORE_MAX_PART - 1) / SX_SCORE_MAX_PART;
   return (T + parts - 1) / parts;
 }
 
 struct ScoreWs { size_t logits, maxima, sums, total; };
 static ScoreWs score_ws(int rows, int V, int sm) {
   const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-  const size_t tiles = (V + SX_TILE_M - 1) / SX_TILE_M;
+  const size_t tiles = (V + SX_TILE_M - 1) / SX_TILE_M, parts = rows > SX_SCORE_FEW || tiles < (size_t)sm ? tiles : (size_t)sm;
   ScoreWs w;
   w.logits = 0;
   w.maxima = up(rows * tiles * SX_TILE_M * sizeof(float));
   w.sums = w.maxima + up(rows * tiles * 4 * sizeof(float));
-  w.total = w.sums + up((size_t)sm * SX_SCORE_ROWS * 3 * sizeof(float));
+  w.total = w.sums + up(parts * rows * 3 * sizeof(float));
   return w;
 }
 
@@ -599,26 +600,29 @@ extern "C" sx_status sx_head_logprobs(const void *head_d, int32_t tiled, int32_t
   SxScoreArgs p;
   SX_TRY(score_args(T, V, n_given, tok_d, temperature, top, out, status_d, &p));
   if (!aligned16(head_d) || !aligned16(hidden_d) || (tiled != 0 && tiled != 1)) return SX_ERR_INVALID_ARG;
-  if (H < 8 || H % 8) return SX_ERR_UNSUPPORTED;
+  if (H < 8 || H % 8 || ((int64_t)V + 255) * (H + 63) / 64 > 0x7fffffff) return SX_ERR_UNSUPPORTED;     // boxes of a repacked head
   if (T == 0) return SX_OK;
   int dev = 0, sm = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || !(sm = sx_sm_count())) return SX_ERR_CUDA;
   const int part = score_part(T);
   const ScoreWs w = score_ws(part, V, sm);
   if (!ws_d || ((uintptr_t)ws_d & 255) || ws_bytes < w.total) return SX_ERR_WORKSPACE;
-  SX_TRY(sx_gemm_init(dev));
+  if (part <= SX_SCORE_FEW) SX_TRY(sx_gemm_init(dev));
   SxScoreOut o;
   o.scale = p.scale;
   o.logits = (float *)((char *)ws_d + w.logits);
   o.maxima = (float *)((char *)ws_d + w.maxima);
   o.sums = (float *)((char *)ws_d + w.sums);
+  o.rows = part;
+  const bf16 *head = (const bf16 *)head_d, *rows = (const bf16 *)hidden_d;
   const int tiles = (V + SX_TILE_M - 1) / SX_TILE_M;
   cudaStream_t st = (cudaStream_t)stream;
   for (int r0 = 0; r0 < T; r0 += part) {
     const int R = T - r0 < part ? T - r0 : part;
-    int ctas = 0;
-    SX_TRY(sx_launch_score_head((const bf16 *)head_d, tiled != 0, V, H, (const bf16 *)hidden_d + (size_t)r0 * H, R, o, &ctas, sm, status_d, st));
-    SX_TRY(sx_rc(sx_launch(sx_score_head_kernel, dim3(R), dim3(SCORE_MAX_WARPS * 32), 0, st, p, o, r0, ctas, tiles)));
+    int parts = 0;
+    if (part <= SX_SCORE_FEW) SX_TRY(sx_launch_score_head(head, tiled != 0, V, H, rows + (size_t)r0 * H, R, o, &parts, sm, status_d, st));
+    else SX_TRY(sx_launch_score_pairs(head, tiled != 0, V, H, rows + (size_t)r0 * H, R, o, &parts, status_d, st));
+    SX_TRY(sx_rc(sx_launch(sx_score_head_kernel, dim3(R), dim3(SCORE_MAX_WARPS * 32), 0, st, p, o, r0, parts, tiles)));
   }
   return SX_OK;
 }
