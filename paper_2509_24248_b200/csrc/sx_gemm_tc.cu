@@ -225,13 +225,12 @@ sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
               float x[32];
 #pragma unroll
               for (int rr = 0; rr < 32; ++rr) x[rr] = src[rr * 33];
-              float4 *dst = reinterpret_cast<float4 *>(p.sc.logits + ((size_t)row * p.num_tiles + item) * SX_TILE_M + part * 32);
 #pragma unroll
-              for (int rr = 0; rr < 32; rr += 4) dst[rr / 4] = make_float4(x[rr], x[rr + 1], x[rr + 2], x[rr + 3]);
+              for (int rr = 0; rr < 32; rr += 8) sx_store8(p.sc.logits + sx_score_at(p.sc, row, item * SX_TILE_M + part * 32 + rr), x + rr);
               float mx = x[0];
 #pragma unroll
               for (int rr = 1; rr < 32; ++rr) mx = fmaxf(mx, x[rr]);
-              p.sc.maxima[((size_t)row * p.num_tiles + item) * 4 + part] = mx;
+              p.sc.maxima[((size_t)item * p.sc.rows + row) * 4 + part] = mx;
               if (mx > sum[ch].m) sum[ch].raise(mx, p.sc.scale);
               const float ref = sum[ch].m > -INFINITY ? sum[ch].m : 0.f;
               float2 s2 = make_float2(sum[ch].s, 0.f), t2 = make_float2(sum[ch].t, 0.f);

@@ -153,17 +153,21 @@ sx_status sx_launch_head(const bf16 *W, int Ntot, int V, int K, const bf16 *X, i
                          int32_t *status, cudaStream_t st, const SxSample *smp = nullptr,
                          SxLogitsOut lo = SxLogitsOut{nullptr, 0, SxIndex{nullptr, 1, 0}}, bool tiled = false);
 
-// Head product for log-probabilities: logits [R][tiles * 128] (-inf behind the vocabulary), the maxima of every 32 of them
-// [R][tiles * 4], and running sums (m, s, t) of the row, [parts][rows][3], one per part of the vocabulary (see sx_score.cuh).  Two kernels:
-// weights on the rows of the product, for up to SX_SCORE_FEW rows (sx_gemm_tc.cu, a part per CTA), and pairs of CTAs with the
-// token rows there, for more (sx_score_tc.cu, a part per tile).
+// Head product for log-probabilities.  It leaves the logits (-inf behind the vocabulary), the maxima of every 32 of them and running
+// sums (m, s, t) of each row per part of the vocabulary (see sx_score.cuh), all with the rows side by side, as the threads that
+// write them are: logits [tiles][16][rows][8] (sx_score_at), maxima [tiles][rows][4], sums [parts][rows][3].  Two kernels: weights on
+// the rows of the product, for up to SX_SCORE_FEW token rows (sx_gemm_tc.cu, a part per CTA), and pairs of CTAs with the token
+// rows there, for more (sx_score_tc.cu, a part per tile).
 #define SX_SCORE_FEW 128
 #define SX_SCORE_CHUNK 8         // k-blocks of 64 that one chain of the tensor core's accumulator is long
 struct SxScoreOut {
   float scale;                   // log2(e) / temperature
   float *logits, *maxima, *sums;
-  int rows;                      // of sums
+  int rows;                      // that there is room for
 };
+__host__ __device__ __forceinline__ size_t sx_score_at(const SxScoreOut &o, int row, int n) {
+  return ((size_t)(n >> 3) * o.rows + row) * 8 + (n & 7);
+}
 sx_status sx_launch_score_head(const bf16 *W, bool tiled, int V, int K, const bf16 *X, int R, const SxScoreOut &out, int *parts,
                                int sm_count, int32_t *status, cudaStream_t st);
 sx_status sx_launch_score_pairs(const bf16 *W, bool tiled, int V, int K, const bf16 *X, int R, const SxScoreOut &out, int *parts,

@@ -152,6 +152,32 @@ __device__ __forceinline__ void score_join_warps(ScoreShared &sh, const ScoreLis
   }
 }
 
+// The sums and the lists of groups of a row's CTAs -> sh.row, sh.group of the first of them; false in the others, which are done.
+template <int W>
+__device__ __forceinline__ bool score_join_cluster(ScoreShared &sh, int cluster, int rank, int top, float scale) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  cg::cluster_group cl = cg::this_cluster();
+  cl.sync();
+  if (rank == 0) {
+    if (warp == 0) {
+      ScoreSum b;
+      b.clear();
+      if (lane < cluster) {
+        const ScoreShared *o = cl.map_shared_rank(&sh, lane);
+        b.m = o->row[0]; b.s = o->row[1]; b.t = o->row[2];
+      }
+      b.warp_join(scale);
+      if (lane == 0) { sh.row[0] = b.m; sh.row[1] = b.s; sh.row[2] = b.t; }
+    }
+    if (top)
+      for (int i = threadIdx.x; i < cluster * 32; i += W * 32) sh.list[i] = cl.map_shared_rank(&sh, i / 32)->group[i % 32];
+  }
+  cl.sync();                                   // no CTA leaves while its shared memory is read
+  if (rank != 0) return false;
+  if (top) score_join_lists<W>(sh, cluster, top, sh.group);
+  return true;
+}
+
 // The best elements of the best groups -> sh.best.  element(group id, lane, &index): the lane's element, on: whether it has one.
 template <int W, typename F>
 __device__ __forceinline__ void score_best_elements(ScoreShared &sh, int top, F element) {
@@ -432,28 +458,7 @@ __global__ void __launch_bounds__(W * 32, 32 / W) sx_score_kernel(const SxScoreA
   }
   score_join_sums<W>(sh, a, p.scale);
   if (p.top) score_join_warps<W>(sh, l, p.top, sh.group);
-  if (cluster > 1) {
-    // the first CTA joins the sums and the lists of groups of all
-    cg::cluster_group cl = cg::this_cluster();
-    cl.sync();
-    if (rank == 0) {
-      if (warp == 0) {
-        ScoreSum b;
-        b.clear();
-        if (lane < cluster) {
-          const ScoreShared *o = cl.map_shared_rank(&sh, lane);
-          b.m = o->row[0]; b.s = o->row[1]; b.t = o->row[2];
-        }
-        b.warp_join(p.scale);
-        if (lane == 0) { sh.row[0] = b.m; sh.row[1] = b.s; sh.row[2] = b.t; }
-      }
-      for (int i = threadIdx.x; i < cluster * 32; i += W * 32)
-        sh.list[i] = cl.map_shared_rank(&sh, i / 32)->group[i % 32];
-    }
-    cl.sync();                                   // no CTA leaves while its shared memory is read
-    if (rank != 0) return;
-    if (p.top) score_join_lists<W>(sh, cluster, p.top, sh.group);
-  }
+  if (cluster > 1 && !score_join_cluster<W>(sh, cluster, rank, p.top, p.scale)) return;
   if (p.top)
     score_best_elements<W>(sh, p.top, [&](int id, int i, int *index, bool *on) {
       const int from = id == 0 ? 0 : lead + (id - 1) * GE, n = id == 0 ? lead : id == whole + 1 ? rest : GE;
@@ -465,23 +470,23 @@ __global__ void __launch_bounds__(W * 32, 32 / W) sx_score_kernel(const SxScoreA
 }
 
 // ---- from hidden states: what the product left ---------------------------------------------------------------------------
-// One CTA per row: sums of the parts of the vocabulary, maxima of groups of 32 logits, the logits themselves (both
-// with `tiles` tiles of 128 to a row, -inf behind the vocabulary).
-__global__ void __launch_bounds__(SCORE_MAX_WARPS * 32) sx_score_head_kernel(const SxScoreArgs p, const SxScoreOut o, int row0, int parts, int tiles) {
+// A cluster of CTAs per row: sums of the parts of the vocabulary, maxima of groups of 32 logits, and the logits (all laid out for the
+// threads that write them, see SxScoreOut; -inf behind the vocabulary).
+__global__ void __launch_bounds__(SCORE_MAX_WARPS * 32) sx_score_head_kernel(const SxScoreArgs p, const SxScoreOut o, int row0, int parts, int tiles, int cluster) {
   constexpr int W = SCORE_MAX_WARPS;
   __shared__ ScoreShared sh;
   if (threadIdx.x == 0) sh.floor = -INFINITY;
   __syncthreads();
   sx_pdl_launch_dependents();
   sx_pdl_wait();
-  const int row = blockIdx.x, lane = threadIdx.x & 31, groups = tiles * 4;
-  const float *x = o.logits + (size_t)row * tiles * SX_TILE_M, *gm = o.maxima + (size_t)row * groups;
+  const int row = blockIdx.x / cluster, rank = blockIdx.x - row * cluster, lane = threadIdx.x & 31, groups = tiles * 4;
+  const int first = rank * W * 32 + threadIdx.x, step = cluster * W * 32;
   ScoreGiven<W> given;
-  given.fetch(p, row0 + row, [&](int i) { return x[i]; });
+  if (rank == 0) given.fetch(p, row0 + row, [&](int i) { return o.logits[sx_score_at(o, row, i)]; });
   ScoreSum a;
   a.clear();
 #pragma unroll 4
-  for (int i = threadIdx.x; i < parts; i += W * 32) {
+  for (int i = first; i < parts; i += step) {
     const float *from = o.sums + ((size_t)i * o.rows + row) * 3;
     a.join(from[0], from[1], from[2], p.scale);
   }
@@ -490,14 +495,16 @@ __global__ void __launch_bounds__(SCORE_MAX_WARPS * 32) sx_score_head_kernel(con
     ScoreList l;
     l.clear();
 #pragma unroll 4
-    for (int g = threadIdx.x; g - lane < groups; g += W * 32)
-      l.offer_group(g < groups ? gm[g] : -INFINITY, g, p.top, lane, &sh.floor);
+    for (int g = first; g - lane < groups; g += step)
+      l.offer_group(g < groups ? o.maxima[((size_t)(g >> 2) * o.rows + row) * 4 + (g & 3)] : -INFINITY, g, p.top, lane, &sh.floor);
     score_join_warps<W>(sh, l, p.top, sh.group);
+  }
+  if (cluster > 1 && !score_join_cluster<W>(sh, cluster, rank, p.top, p.scale)) return;
+  if (p.top)
     score_best_elements<W>(sh, p.top, [&](int id, int i, int *index, bool *on) {
       *index = id * 32 + i;
-      return x[id * 32 + i];
+      return o.logits[sx_score_at(o, row, id * 32 + i)];
     });
-  }
   score_write<W>(sh, p, row0 + row, given);
 }
 
@@ -622,7 +629,11 @@ extern "C" sx_status sx_head_logprobs(const void *head_d, int32_t tiled, int32_t
     int parts = 0;
     if (part <= SX_SCORE_FEW) SX_TRY(sx_launch_score_head(head, tiled != 0, V, H, rows + (size_t)r0 * H, R, o, &parts, sm, status_d, st));
     else SX_TRY(sx_launch_score_pairs(head, tiled != 0, V, H, rows + (size_t)r0 * H, R, o, &parts, status_d, st));
-    SX_TRY(sx_rc(sx_launch(sx_score_head_kernel, dim3(R), dim3(SCORE_MAX_WARPS * 32), 0, st, p, o, r0, parts, tiles)));
+    // CTAs per row: as many as there is room for at a time, four rounds of groups for each
+    int cluster = 1;
+    while (cluster < SCORE_MAX_CLUSTER && R * cluster * 2 <= 4 * sm && tiles * 4 >= cluster * 2 * 4 * SCORE_MAX_WARPS * 32) cluster *= 2;
+    SX_TRY(sx_rc(sx_launch_cluster(sx_score_head_kernel, dim3(R * cluster), dim3(SCORE_MAX_WARPS * 32), 0, (unsigned)cluster, st, p, o, r0,
+                                   parts, tiles, cluster)));
   }
   return SX_OK;
 }

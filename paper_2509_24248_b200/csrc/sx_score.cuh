@@ -54,3 +54,9 @@ __device__ __forceinline__ void score_pair(float2 x, float scale, float ref, flo
   t.x = fmaf(e0, d0, t.x);
   t.y = fmaf(e1, d1, t.y);
 }
+
+// eight floats to a 32-byte boundary, a whole sector
+__device__ __forceinline__ void sx_store8(float *dst, const float *v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(dst), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]) : "memory");
+}

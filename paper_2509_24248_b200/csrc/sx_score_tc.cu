@@ -214,13 +214,9 @@ sx_score_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
         mx = fmaxf(mx, gm[g]);
       }
       if (tile < p.tiles && row < p.R) {
-        float *dst = p.sc.logits + ((size_t)row * p.tiles + tile) * SX_TILE_M;
 #pragma unroll
-        for (int j = 0; j < 128; j += 8)                        // a whole 32-byte sector at a time
-          asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                       ::"l"(dst + j), "f"(v[j]), "f"(v[j + 1]), "f"(v[j + 2]), "f"(v[j + 3]), "f"(v[j + 4]), "f"(v[j + 5]), "f"(v[j + 6]),
-                       "f"(v[j + 7]) : "memory");
-        *reinterpret_cast<float4 *>(p.sc.maxima + ((size_t)row * p.tiles + tile) * 4) = make_float4(gm[0], gm[1], gm[2], gm[3]);
+        for (int j = 0; j < 128; j += 8) sx_store8(p.sc.logits + sx_score_at(p.sc, row, n0 + j), v + j);
+        *reinterpret_cast<float4 *>(p.sc.maxima + ((size_t)tile * p.sc.rows + row) * 4) = make_float4(gm[0], gm[1], gm[2], gm[3]);
         const float ref = mx > -INFINITY ? mx : 0.f;
         float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
 #pragma unroll
