@@ -476,7 +476,7 @@ sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void *logits_d,
                       void *stream);
 
 /* The same from hidden states: logits = hidden . head^T are formed tile by tile on the tensor cores (fp32, in chains of
- * 512 products whose sums are added with rounding to nearest), their softmax sums taken on the way.  Beside sx_verify, which gives the argmax of the same product alone.
+ * at most 512 products whose sums are added with rounding to nearest), their softmax sums taken on the way.  Beside sx_verify, which gives the argmax of the same product alone.
  *   head_d    [V, H] bf16 row-major, or repacked by sx_tile_weight (tiled = 1; rows behind the first V, such as signal rows,
  *             may follow and are not looked at); complete and visible before the call (see the conventions)
  *   hidden_d  [T, H] bf16, contiguous; H a multiple of 8

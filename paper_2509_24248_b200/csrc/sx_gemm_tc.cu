@@ -47,6 +47,7 @@ struct SxTcParams {
   int w_tiled;                   // weights stored tile by tile: [row tile][k-block][128 rows][64 columns]
   uint32_t wait_limit;           // polls of an mbarrier before a wait gives up
   SxScoreOut sc;                 // KIND_SCORE
+  int chains;                    // KIND_SCORE: accumulators side by side in a buffer
 };
 
 __device__ __forceinline__ int sx_lo_row(const SxLogitsOut &lo, int r) { return lo.ri.idx ? lo.ri.idx[r] : r * lo.ri.mul + lo.ri.add; }
@@ -145,16 +146,22 @@ sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
         if (!mbar_wait(smem_u32(&tempty[acc]), acc_phase ^ 1u, abort_flag, p.wait_limit)) break;
         tc_fence_after();
         uint32_t d_tmem = tmem_base + (uint32_t)(acc * p.acc_cols);
-        int first = kb0;                                // k-block that begins the accumulator's chain
+        int first = kb0;                                // KIND_SCORE: k-block that begins a chain, and chains before it in this buffer
+        int chain = 0;
         for (int kb = kb0; kb < kb1; ++kb) {
           if (KIND == KIND_SCORE && kb == first + SX_SCORE_CHUNK) {
-            // the chain is long enough (the accumulator truncates): hand it over and go on in the other one
-            tc_commit(smem_u32(&tfull[acc]));
-            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
-            if (!mbar_wait(smem_u32(&tempty[acc]), acc_phase ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
-            tc_fence_after();
-            d_tmem = tmem_base + (uint32_t)(acc * p.acc_cols);
+            // the chain is long enough (the accumulator truncates): go on in the columns beside it, and behind the last of
+            // them in the other buffer
             first = kb;
+            d_tmem += (uint32_t)p.nmma;
+            if (++chain == p.chains) {
+              chain = 0;
+              tc_commit(smem_u32(&tfull[acc]));
+              if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+              if (!mbar_wait(smem_u32(&tempty[acc]), acc_phase ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
+              tc_fence_after();
+              d_tmem = tmem_base + (uint32_t)(acc * p.acc_cols);
+            }
           }
           if (!mbar_wait(smem_u32(&full[stage]), phase, abort_flag, p.wait_limit)) { ok = false; break; }
           tc_fence_after();
@@ -193,19 +200,22 @@ sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
         float v[SX_SCORE_FEW];
 #pragma unroll
         for (int j = 0; j < SX_SCORE_FEW; ++j) v[j] = 0.f;
-        for (int kb = 0; kb < p.num_kb; kb += SX_SCORE_CHUNK) {
+        for (int kb = 0; kb < p.num_kb;) {
           ok = epi_all(mbar_wait(smem_u32(&tfull[acc]), acc_phase, abort_flag, p.wait_limit));
           if (!ok) break;
           tc_fence_after();
           const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * p.acc_cols);
+#pragma unroll 1
+          for (int u = 0; u < p.chains && kb < p.num_kb; ++u, kb += SX_SCORE_CHUNK) {
 #pragma unroll
-          for (int c = 0; c < SX_SCORE_FEW; c += 16)
-            if (c < p.nmma) {
-              float x[16];
-              tc_ld16(taddr + c, x);
+            for (int c = 0; c < SX_SCORE_FEW; c += 16)
+              if (c < p.nmma) {
+                float x[16];
+                tc_ld16(taddr + u * p.nmma + c, x);
 #pragma unroll
-              for (int j = 0; j < 16; ++j) v[c + j] += x[j];
-            }
+                for (int j = 0; j < 16; ++j) v[c + j] += x[j];
+              }
+          }
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(smem_u32(&tempty[acc]));
@@ -226,7 +236,7 @@ sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
 #pragma unroll
               for (int rr = 0; rr < 32; ++rr) x[rr] = src[rr * 33];
 #pragma unroll
-              for (int rr = 0; rr < 32; rr += 8) sx_store8(p.sc.logits + sx_score_at(p.sc, row, item * SX_TILE_M + part * 32 + rr), x + rr);
+              for (int rr = 0; rr < 32; rr += 8) sx_store8<false>(p.sc.logits + sx_score_at(p.sc, row, item * SX_TILE_M + part * 32 + rr), x + rr);
               float mx = x[0];
 #pragma unroll
               for (int rr = 1; rr < 32; ++rr) mx = fmaxf(mx, x[rr]);
@@ -772,6 +782,9 @@ sx_status sx_launch_score_head(const bf16 *W, bool tiled, int V, int K, const bf
   p.splits = 1;
   p.kb_per_split = p.num_kb;
   p.V = V; p.status = status; p.sc = out;
+  p.acc_cols = 256;
+  p.tmem_cols = 512;
+  p.chains = 256 / p.nmma;
   CUtensorMap mw, mx;
   p.w_tiled = tiled ? 1 : 0;
   if (!sx_weight_map(W, V, K, tiled, &mw) || !sx_tma_map_2d(X, R, K, p.nmma, &mx)) return SX_ERR_CUDA;

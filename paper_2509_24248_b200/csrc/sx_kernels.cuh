@@ -159,7 +159,8 @@ sx_status sx_launch_head(const bf16 *W, int Ntot, int V, int K, const bf16 *X, i
 // the rows of the product, for up to SX_SCORE_FEW token rows (sx_gemm_tc.cu, a part per CTA), and pairs of CTAs with the token
 // rows there, for more (sx_score_tc.cu, a part per tile).
 #define SX_SCORE_FEW 128
-#define SX_SCORE_CHUNK 8         // k-blocks of 64 that one chain of the tensor core's accumulator is long
+#define SX_SCORE_CHUNK 4         // k-blocks of 64 that one chain of the tensor core's accumulator is long, with few rows
+#define SX_SCORE_CHUNK_PAIR 8    // and in the pairs of CTAs (see there)
 struct SxScoreOut {
   float scale;                   // log2(e) / temperature
   float *logits, *maxima, *sums;

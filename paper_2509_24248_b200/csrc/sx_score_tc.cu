@@ -6,7 +6,7 @@
 // for every 64 elements of K, two thirds of what a CTA of its own would need for the same tile.
 //
 // The tensor core's fp32 accumulator cuts off where a CPU rounds: every step of 16 elements of K loses up to an ulp of the
-// running sum, always towards zero (measured: 6e-6 of a logit at K = 4096).  So no chain is longer than SX_SCORE_CHUNK k-blocks: the
+// running sum, always towards zero (measured: 6e-6 of a logit at K = 4096).  So no chain is longer than SX_SCORE_CHUNK_PAIR k-blocks: the
 // epilogue adds the chunks' sums in registers, rounding to nearest, two TMEM accumulators in turn.  A thread of the epilogue owns a
 // token row and half of the tile's columns; softmax sums and maxima of groups of 32 need no exchange between threads.
 //
@@ -113,7 +113,11 @@ sx_score_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
     if (lane == 0) {
       // As in sx_gemm_tc.cu: the weights of the first stages are requested before the wait on the preceding kernel (pass 0), the
       // rows of those stages behind it (pass 1), then both together (pass 2).
-      const uint64_t pol_w = policy_evict_first(), pol_x = policy_evict_last();
+      // (The weights are not marked evict-first as they are there: the row tiles read them at about the same time, one of
+      // them from memory.)
+      uint64_t pol_w;
+      asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol_w));
+      const uint64_t pol_x = policy_evict_last();
       bool ok = true;
       for (int pass = 0; pass < 3 && ok; ++pass) {
         if (pass == 1) sx_pdl_wait();
@@ -147,8 +151,8 @@ sx_score_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
       for (int item = pair; item < p.items && ok; item += pairs) {
-        for (int kb0 = 0; kb0 < p.num_kb && ok; kb0 += SX_SCORE_CHUNK) {
-          const int kb1 = min(p.num_kb, kb0 + SX_SCORE_CHUNK);
+        for (int kb0 = 0; kb0 < p.num_kb && ok; kb0 += SX_SCORE_CHUNK_PAIR) {
+          const int kb1 = min(p.num_kb, kb0 + SX_SCORE_CHUNK_PAIR);
           if (!mbar_wait(smem_u32(&tempty[acc]), acc_phase ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
           tc_fence_after();
           const uint32_t d_tmem = tmem_base + (uint32_t)(acc * 256);
@@ -180,7 +184,7 @@ sx_score_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
       float v[128];
 #pragma unroll
       for (int j = 0; j < 128; ++j) v[j] = 0.f;
-      for (int kb0 = 0; kb0 < p.num_kb; kb0 += SX_SCORE_CHUNK) {
+      for (int kb0 = 0; kb0 < p.num_kb; kb0 += SX_SCORE_CHUNK_PAIR) {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&tfull[acc]), acc_phase, abort_flag, p.wait_limit));
         if (!ok) break;
         tc_fence_after();
@@ -215,7 +219,7 @@ sx_score_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
       }
       if (tile < p.tiles && row < p.R) {
 #pragma unroll
-        for (int j = 0; j < 128; j += 8) sx_store8(p.sc.logits + sx_score_at(p.sc, row, n0 + j), v + j);
+        for (int j = 0; j < 128; j += 8) sx_store8<true>(p.sc.logits + sx_score_at(p.sc, row, n0 + j), v + j);
         *reinterpret_cast<float4 *>(p.sc.maxima + ((size_t)tile * p.sc.rows + row) * 4) = make_float4(gm[0], gm[1], gm[2], gm[3]);
         const float ref = mx > -INFINITY ? mx : 0.f;
         float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
