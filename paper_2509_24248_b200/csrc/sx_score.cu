@@ -325,9 +325,10 @@ __device__ __forceinline__ void score_pairs(const uint32_t *w, F f) {
 
 // The sums of a lane over its groups.  Issue slots bound this pass, so the plain way takes as few as it can: d = fma(x, c, -r),
 // r = fl(c m), with sums relative to 2^r, and a new reference only where a group is more than 2^SCORE_SLACK above the old one.
-// It has no place for -inf (0 * -inf) and none for logits so large that the rounding of r counts: the first such group
-// turns the warp over to the careful way for the rest of the row (score_pair: two more instructions an element), whose sums are
-// relative to 2^(c m).  r is off by fma(m, c, -r), exactly; the two differ by that power of two.
+// It has no place for logits so large that the rounding of r counts (a type's lowest value among them, where a row has nothing
+// else): the first such group turns the warp over to the careful way for the rest of the row (score_pair: one more
+// instruction an element), whose sums are relative to 2^(c m).  r is off by fma(m, c, -r), exactly; the two differ by that power
+// of two.
 #define SCORE_SLACK 4.f
 struct ScorePlain {
   ScoreSum a;
@@ -349,14 +350,15 @@ struct ScorePlain {
     }
     float s0 = a.s, s1 = 0.f, t0 = a.t, t1 = 0.f;
     score_pairs<E>(w, [&](float2 x) {
-      const float d0 = fmaf(x.x, scale, -r), d1 = fmaf(x.y, scale, -r), e0 = score_exp2(d0), e1 = score_exp2(d1);
+      const float d0 = score_max_nan(fmaf(x.x, scale, -r), -200.f), d1 = score_max_nan(fmaf(x.y, scale, -r), -200.f);
+      const float e0 = score_exp2(d0), e1 = score_exp2(d1);
       s0 += e0;
       s1 += e1;
       t0 = fmaf(e0, d0, t0);
       t1 = fmaf(e1, d1, t1);
     });
     t0 += t1;
-    if (!__all_sync(0xffffffffu, !on || (t0 == t0 && fabsf(r) < 1048576.f))) return false;
+    if (!__all_sync(0xffffffffu, !on || fabsf(r) < 1048576.f)) return false;
     if (on) { a.s = s0 + s1; a.t = t0; }
     return true;
   }
@@ -545,15 +547,18 @@ static sx_status score_args(int32_t T, int32_t V, int32_t n_given, const int32_t
 // Warps and CTAs per row.  An SM has room for 32 warps of this kernel.  Where there are rows enough to fill the card four warps
 // share one: the ends of a row (first loads, joining, alternatives: some 5 us in which it reads nothing, at the same time
 // for all rows that began together) weigh less the longer it takes, but more rows at a time mean more places in
-// memory that are read at once (4096 rows of 151936 in bf16 with 8, 4, 2, 1 warps: 237, 220, 297, 424 us).  Below that, as many
-// warps and then CTAs as there is room for at once.  Every warp gets two rounds of groups, where the row has as many.
+// memory that are read at once (4096 rows of 151936 in bf16 with 8, 4, 2, 1 warps: 237, 220, 297, 424 us).  Below that, eight.  Every
+// warp gets two rounds of groups, where the row has as many.  A row is spread over a cluster while that makes no more than
+// 1.75 CTAs per SM and leaves each warp a round (one row of 151936 in bf16 on 1, 2, 4, 8 CTAs: 22, 19, 15.6, 13.9 us; 74 rows: 19.3,
+// 16.4, 17.6, 22 us).
 struct ScoreSplit { int warps, cluster; };
 static ScoreSplit score_split(int64_t T, int64_t groups, int sm) {
   const int64_t room = 32ll * sm, most = groups / (2 * 32);
   ScoreSplit n = {1, 1};
   while (n.warps < 4 && n.warps * 2 <= most) n.warps *= 2;
   while (n.warps < SCORE_MAX_WARPS && n.warps * 2 <= most && T * n.warps * 2 <= room) n.warps *= 2;
-  while (n.cluster < SCORE_MAX_CLUSTER && n.warps * n.cluster * 2 <= most && T * n.warps * n.cluster * 2 <= room) n.cluster *= 2;
+  while (n.cluster < SCORE_MAX_CLUSTER && n.warps == SCORE_MAX_WARPS && groups >= 32ll * n.warps * n.cluster * 2 && 4 * T * n.cluster * 2 <= 7ll * sm)
+    n.cluster *= 2;
   return n;
 }
 
