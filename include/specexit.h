@@ -331,8 +331,8 @@ sx_status sx_kv_append(const sx_kv_shape *shape, const sx_kv *kv, int32_t T, con
  *   SX_ROPE_BANDS   f_i where n_i >= high, f_i / F where n_i <= low, between them w f_i + (1 - w) f_i / F with
  *                   w = (n_i - low) / (high - low)
  *   SX_ROPE_RAMP    (1 - w_i) f_i + w_i f_i / F; w_i rises from 0 to 1 between i = max(floor(at(high)), 0) and
- *                   i = min(ceil(at(low)), rot_dim - 1), at(n) = rot_dim ln(original_len / (2 pi n)) / (2 ln theta).  The
- *                   factor on the attention's logits that goes with it is magnitude's square
+ *                   i = min(ceil(at(low)), rot_dim - 1), at(n) = rot_dim ln(original_len / (2 pi n)) / (2 ln theta).  It
+ *                   is used with a magnitude of 0.1 ln(F) + 1
  *   SX_ROPE_LIST    f_i / divisors[i]
  * sx_rope_plan (host only) makes a plan of it, which the caller keeps and which calls copy.  head_dim: a multiple of 8 up to
  * SX_ROPE_MAX_HEAD; rot_dim and rot_start even. */
@@ -453,7 +453,7 @@ sx_status sx_set_sampling(sx_ctx *ctx, float temperature, uint64_t seed, uint32_
 
 /* Log-probabilities of given tokens, entropy and best alternatives of rows of logits: what a server returns beside the tokens,
  * and what sx_verify's argmax leaves out.  log p = log softmax(logits / temperature), natural logarithms.
- *   logits_d   [T, V] of `dtype`, `stride` elements from row to row (any, at least V)
+ *   logits_d   [T, V] of `dtype`, `stride` elements from row to row (any, at least V); on any boundary of its elements
  *   tok_d      [T, n_given] token ids, n_given 0..SX_MAX_GIVEN; -1: none, its log p is written as 0; another id outside
  *              [0, V) is reported as SX_ERR_CAPACITY and its log p is NaN
  *   top        0..SX_MAX_ALTERNATIVES: the largest logits, best first, the lower id first among equals (-0 equals 0); an

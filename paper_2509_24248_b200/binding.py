@@ -29,6 +29,7 @@ KV_BF16, KV_E4M3 = 0, 1
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_NONE, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS, ROPE_RAMP, ROPE_LIST = 0, 1, 2, 3, 4, 5
 SX_ROPE_MAX_PAIRS = 128
+SX_SCORE_MAX_PART = 1024
 SMOOTH_EWMA, SMOOTH_NONE, SMOOTH_WINDOW, SMOOTH_MOMENTUM, SMOOTH_PARAGRAPH = 0, 1, 2, 3, 4
 HIST = 16
 
@@ -656,7 +657,7 @@ class LogProbs:
 
     def sx_logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0,
                     out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
-        """Of rows of logits (bf16, fp16 or fp32 ``[T, V]``, any row stride)."""
+        """Of rows of logits (bf16, fp16 or fp32 ``[T, V]``, any row stride, on any boundary: a slice of columns will do)."""
         shape, stride, dtype = logits.shape, logits.stride(), _FLOATS.get(logits.dtype)
         if len(shape) != 2 or logits.get_device() != self._index or dtype is None or (shape[1] > 1 and stride[1] != 1):
             raise SxError(f"logits must be bf16, fp16 or fp32 [T, V] on {self.dev}, rows contiguous")
@@ -686,7 +687,9 @@ class LogProbs:
             return out
         with _guard_of(self._index):
             if self._ws_for != T:
-                need = int(self.lib.sx_head_logprobs_ws_bytes(T, self.V))
+                # sizes of powers of two rows: however T grows, all workspaces together are at most twice the largest
+                rows = -(-T // -(-T // SX_SCORE_MAX_PART))
+                need = int(self.lib.sx_head_logprobs_ws_bytes(1 << (rows - 1).bit_length(), self.V))
                 if need > self._ws_bytes:
                     self._ws.append(torch.empty(need + 256, dtype=torch.uint8, device=self.dev))
                     self._ws_at = self._ws[-1].data_ptr() + (-self._ws[-1].data_ptr()) % 256

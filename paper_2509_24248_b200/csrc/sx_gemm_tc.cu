@@ -19,6 +19,7 @@
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
+#include <atomic>
 #include <mutex>
 #include <unordered_map>
 
@@ -678,12 +679,15 @@ static size_t smem_bytes(const SxTcParams &p, size_t epi_bytes) {
   return 1024 + (size_t)p.stages * (SX_A_BYTES + (size_t)p.nmma * 128) + (size_t)(2 * p.stages + 4) * 8 + 16 + epi_bytes + 64;
 }
 
+// shared-memory opt-ins of the device, which has to be the current one; made once
 sx_status sx_gemm_init(int device) {
-  (void)device;
+  static std::atomic<bool> done[64];
+  if (device >= 0 && device < 64 && done[device].load(std::memory_order_acquire)) return SX_OK;
   if (cudaFuncSetAttribute(sx_tc_gemm_kernel<KIND_GEMM>, cudaFuncAttributeMaxDynamicSharedMemorySize, SX_SMEM_MAX) != cudaSuccess ||
       cudaFuncSetAttribute(sx_tc_gemm_kernel<KIND_HEAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, SX_SMEM_MAX) != cudaSuccess ||
       cudaFuncSetAttribute(sx_tc_gemm_kernel<KIND_SCORE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SX_SMEM_MAX) != cudaSuccess)
     return SX_ERR_CUDA;
+  if (device >= 0 && device < 64) done[device].store(true, std::memory_order_release);
   return SX_OK;
 }
 

@@ -580,7 +580,7 @@ extern "C" sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void
                                  void *stream) {
   SxScoreArgs p;
   SX_TRY(score_args(T, V, n_given, tok_d, temperature, top, out, status_d, &p));
-  if (dtype < SX_BF16 || dtype > SX_F32 || !aligned16(logits_d) || stride < V) return SX_ERR_INVALID_ARG;
+  if (dtype < SX_BF16 || dtype > SX_F32 || !logits_d || (uintptr_t)logits_d % (dtype == SX_F32 ? 4 : 2) || stride < V) return SX_ERR_INVALID_ARG;
   if (T == 0) return SX_OK;
   const int sm = sx_sm_count();
   if (!sm) return SX_ERR_CUDA;

@@ -166,6 +166,14 @@ def test_rows_past_32_bits():
     assert got["top_tok"][:-3].eq(torch.arange(5, device=DEV)).all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_slices_on_any_boundary(dtype):
+    """Rows that begin at an element of any place: the first logits of a wider matrix cut off."""
+    x = make(5, 3000, dtype, 21, 3001)
+    for cut in (1, 2, 3, 5, 8, 15, 16, 17, 31):
+        both(x[:, cut:], given(5, 3000 - cut, 2, cut), 9)
+
+
 def test_python_side_refusals():
     s = sx.LogProbs()
     x = make(3, 100, torch.bfloat16, 19)

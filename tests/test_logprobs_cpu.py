@@ -23,7 +23,7 @@ def test_calls_that_cannot_be_are_refused():
         return lib.sx_logprobs(*a)
 
     inf, nan = float("inf"), float("nan")
-    for change in (dict(_0=3), dict(_0=-1), dict(_1=-1), dict(_2=0), dict(_3=None), dict(_3=8), dict(_4=99), dict(_5=-1), dict(_6=None),
+    for change in (dict(_0=3), dict(_0=-1), dict(_1=-1), dict(_2=0), dict(_3=None), dict(_3=257), dict(_0=2, _3=258), dict(_4=99), dict(_5=-1), dict(_6=None),
                    dict(_6=258), dict(_7=0.0), dict(_7=-1.0), dict(_7=inf), dict(_7=nan), dict(_7=1e-38), dict(_8=-1), dict(_9=None), dict(_10=None)):
         assert call(**change) == INVALID, change
     for change in (dict(_5=65), dict(_8=33), dict(_2=(1 << 24) + 1, _4=1 << 25)):
