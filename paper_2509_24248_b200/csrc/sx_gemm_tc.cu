@@ -147,15 +147,13 @@ sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
         if (!mbar_wait(smem_u32(&tempty[acc]), acc_phase ^ 1u, abort_flag, p.wait_limit)) break;
         tc_fence_after();
         uint32_t d_tmem = tmem_base + (uint32_t)(acc * p.acc_cols);
-        int first = kb0;                                // KIND_SCORE: k-block that begins a chain, and chains before it in this buffer
-        int chain = 0;
-        for (int kb = kb0; kb < kb1; ++kb) {
-          if (KIND == KIND_SCORE && kb == first + SX_SCORE_CHUNK) {
-            // the chain is long enough (the accumulator truncates): go on in the columns beside it, and behind the last of
-            // them in the other buffer
-            first = kb;
-            d_tmem += (uint32_t)p.nmma;
-            if (++chain == p.chains) {
+        if constexpr (KIND == KIND_SCORE) {
+          // Chains of SX_SCORE_CHUNK k-blocks (the accumulator truncates) side by side in a buffer, and behind the last of them on in
+          // the other buffer.  Nothing of this is in the loop over the k-blocks: what this thread does per k-block is what caps
+          // a CTA's share of the bandwidth (tests there cost 7 % of the kernel).
+          int chain = 0;
+          for (int c0 = kb0; c0 < kb1 && ok; c0 += SX_SCORE_CHUNK) {
+            if (chain == p.chains) {
               chain = 0;
               tc_commit(smem_u32(&tfull[acc]));
               if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
@@ -163,16 +161,33 @@ sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
               tc_fence_after();
               d_tmem = tmem_base + (uint32_t)(acc * p.acc_cols);
             }
-          }
-          if (!mbar_wait(smem_u32(&full[stage]), phase, abort_flag, p.wait_limit)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t a = smem_u32(smem + (size_t)stage * stage_bytes);
-          const uint32_t b = a + SX_A_BYTES;
+            const int c1 = min(kb1, c0 + SX_SCORE_CHUNK);
+            for (int kb = c0; kb < c1; ++kb) {
+              if (!mbar_wait(smem_u32(&full[stage]), phase, abort_flag, p.wait_limit)) { ok = false; break; }
+              tc_fence_after();
+              const uint32_t a = smem_u32(smem + (size_t)stage * stage_bytes);
+              const uint32_t b = a + SX_A_BYTES;
 #pragma unroll
-          for (int k = 0; k < SX_BK / 16; ++k)
-            tc_mma(d_tmem, smem_desc(a + k * 32), smem_desc(b + k * 32), idesc, (kb > first || k > 0) ? 1u : 0u);
-          tc_commit(smem_u32(&empty[stage]));          // frees the stage once these MMAs have read it
-          if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+              for (int k = 0; k < SX_BK / 16; ++k)
+                tc_mma(d_tmem, smem_desc(a + k * 32), smem_desc(b + k * 32), idesc, (kb > c0 || k > 0) ? 1u : 0u);
+              tc_commit(smem_u32(&empty[stage]));
+              if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+            }
+            d_tmem += (uint32_t)p.nmma;
+            ++chain;
+          }
+        } else {
+          for (int kb = kb0; kb < kb1; ++kb) {
+            if (!mbar_wait(smem_u32(&full[stage]), phase, abort_flag, p.wait_limit)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t a = smem_u32(smem + (size_t)stage * stage_bytes);
+            const uint32_t b = a + SX_A_BYTES;
+#pragma unroll
+            for (int k = 0; k < SX_BK / 16; ++k)
+              tc_mma(d_tmem, smem_desc(a + k * 32), smem_desc(b + k * 32), idesc, (kb > kb0 || k > 0) ? 1u : 0u);
+            tc_commit(smem_u32(&empty[stage]));          // frees the stage once these MMAs have read it
+            if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+          }
         }
         if (!ok) break;
         tc_commit(smem_u32(&tfull[acc]));              // accumulator complete

@@ -81,9 +81,9 @@ struct ScoreList {
     take(sx_pack(v + 0.f, (uint32_t)id), m, top, lane);                  // -0 counts as 0
     if (lane == 0 && floor > *shared) *shared = floor;
   }
-  // Elements of groups in any order
-  __device__ __forceinline__ void offer(float v, int id, bool on, int top, int lane) {
-    const unsigned long long k = on && v > -INFINITY ? sx_pack(v + 0.f, (uint32_t)id) : 0ull;      // a NaN is not above -inf
+  // Entries in any order of ids; nothing below `least` is wanted.
+  __device__ __forceinline__ void offer(float v, int id, float least, int top, int lane) {
+    const unsigned long long k = v >= least && v > -INFINITY ? sx_pack(v + 0.f, (uint32_t)id) : 0ull;      // a NaN is not
     const unsigned long long kth = __shfl_sync(0xffffffffu, key, top - 1);
     const uint32_t m = __ballot_sync(0xffffffffu, k > kth);
     if (m) take(k, m, top, lane);
@@ -94,7 +94,7 @@ struct ScoreShared {
   unsigned long long list[SCORE_MAX_WARPS * 32];                      // the lists of the warps, or of the CTAs of a cluster
   unsigned long long group[32], best[32];                             // the best groups, the best elements
   float sum[SCORE_MAX_WARPS][3], row[3];
-  float floor;
+  volatile float floor;
 };
 static_assert(SCORE_MAX_CLUSTER <= SCORE_MAX_WARPS, "the lists of a cluster lie where those of the warps did");
 
@@ -178,10 +178,12 @@ __device__ __forceinline__ bool score_join_cluster(ScoreShared &sh, int cluster,
   return true;
 }
 
-// The best elements of the best groups -> sh.best.  element(group id, lane, &index): the lane's element, on: whether it has one.
+// The best elements of the best groups -> sh.best.  element(group id, lane, &index): the lane's element, -inf: none.  What is below the
+// maximum of the last of the groups is below `top` others.
 template <int W, typename F>
 __device__ __forceinline__ void score_best_elements(ScoreShared &sh, int top, F element) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float least = sh.group[top - 1] ? sx_pack_value(sh.group[top - 1]) : -INFINITY;
   ScoreList l;
   l.clear();
   // four groups' elements on the way at a time
@@ -189,17 +191,15 @@ __device__ __forceinline__ void score_best_elements(ScoreShared &sh, int top, F 
   for (int i = warp; i < top; i += 4 * W) {
     float v[4];
     int index[4];
-    bool on[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const unsigned long long g = i + j * W < top ? sh.group[i + j * W] : 0ull;
-      on[j] = g != 0ull;
       v[j] = -INFINITY;
       index[j] = 0;
-      if (on[j]) v[j] = element((int)sx_pack_index(g), lane, &index[j], &on[j]);
+      if (g != 0ull) v[j] = element((int)sx_pack_index(g), lane, &index[j]);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) l.offer(v[j], index[j], on[j], top, lane);
+    for (int j = 0; j < 4; ++j) l.offer(v[j], index[j], least, top, lane);
   }
   score_join_warps<W>(sh, l, top, sh.best);
 }
@@ -462,9 +462,8 @@ __global__ void __launch_bounds__(W * 32, 32 / W) sx_score_kernel(const SxScoreA
   if (p.top) score_join_warps<W>(sh, l, p.top, sh.group);
   if (cluster > 1 && !score_join_cluster<W>(sh, cluster, rank, p.top, p.scale)) return;
   if (p.top)
-    score_best_elements<W>(sh, p.top, [&](int id, int i, int *index, bool *on) {
+    score_best_elements<W>(sh, p.top, [&](int id, int i, int *index) {
       const int from = id == 0 ? 0 : lead + (id - 1) * GE, n = id == 0 ? lead : id == whole + 1 ? rest : GE;
-      *on = i < n;
       *index = from + i;
       return i < n ? ScoreElem<E>::one(x[from + i]) : -INFINITY;
     });
@@ -502,19 +501,25 @@ __global__ void __launch_bounds__(SCORE_MAX_WARPS * 32) sx_score_head_kernel(con
     l.clear();
     for (int g = first; g - lane < groups; g += 4 * step) {
       float v[4];
+      int best = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         v[j] = ahead[j];
         ahead[j] = maximum(g + (4 + j) * step);
+        if (v[j] > v[best]) best = j;
       }
+      // the best of a lane's four first: hardly any of the others is above what the list then begins with
+      const float b = v[best];
+      l.offer(b, g + best * step, sh.floor, p.top, lane);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) l.offer_group(v[j], g + j * step, p.top, lane, &sh.floor);
+      for (int j = 0; j < 4; ++j) l.offer(j == best ? -INFINITY : v[j], g + j * step, sh.floor, p.top, lane);
+      if (lane == 0 && l.floor > sh.floor) sh.floor = l.floor;
     }
     score_join_warps<W>(sh, l, p.top, sh.group);
   }
   if (cluster > 1 && !score_join_cluster<W>(sh, cluster, rank, p.top, p.scale)) return;
   if (p.top)
-    score_best_elements<W>(sh, p.top, [&](int id, int i, int *index, bool *on) {
+    score_best_elements<W>(sh, p.top, [&](int id, int i, int *index) {
       *index = id * 32 + i;
       return o.logits[sx_score_at(o, row, id * 32 + i)];
     });
