@@ -324,8 +324,9 @@ sx_status sx_kv_append(const sx_kv_shape *shape, const sx_kv *kv, int32_t T, con
 /* Rotary positions.  A head's rotated part, rot_dim elements from rot_start on, is rot_dim / 2 pairs: (x[i], x[i + rot_dim / 2])
  * in SX_ROPE_HALF, (x[2 i], x[2 i + 1]) in SX_ROPE_INTERLEAVED; the other elements of the head stay as they are.  At position
  * pos pair i = (u, v) becomes magnitude * (u cos a - v sin a, v cos a + u sin a), a = pos * f_i, modulo one turn exact to
- * pos * 2^-64 turns; cos, sin and products are fp32, the result is rounded once.  f_i = theta^(-2 i / rot_dim), and with a
- * scaling for contexts longer than the trained one (F = factor, n_i = original_len * f_i / 2 pi turns over the trained length):
+ * pos * 2^-64 turns; cos, sin and products are fp32 (fp64 for keys that go into an 8-bit cache), the result is rounded once.
+ * f_i = theta^(-2 i / rot_dim), and with a scaling for contexts longer than the trained one (F = factor, n_i = original_len *
+ * f_i / 2 pi turns over the trained length):
  *   SX_ROPE_LINEAR  f_i / F
  *   SX_ROPE_BASE    theta becomes theta * F^(rot_dim / (rot_dim - 2))
  *   SX_ROPE_BANDS   f_i where n_i >= high, f_i / F where n_i <= low, between them w f_i + (1 - w) f_i / F with
@@ -350,7 +351,7 @@ typedef struct {
 } sx_rope_cfg;
 typedef struct {
   int32_t ready, head_dim, rot_start, rot_dim, layout;
-  float magnitude;
+  double magnitude;
   uint64_t step[SX_ROPE_MAX_PAIRS];                 /* f_i / 2 pi in 2^-64 turns */
 } sx_rotation;
 sx_status sx_rope_plan(const sx_rope_cfg *cfg, sx_rotation *out);
@@ -366,7 +367,7 @@ sx_status sx_rope(const sx_rotation *plan, int32_t dtype, int32_t transpose, int
 
 /* sx_kv_append for a cache of either kind (kv->dtype), with the rotation on the way: the keys of every row are turned to the
  * row's position - rot_pos_d[t], or its slot where rot_pos_d is NULL - rounded to bf16 and written to their pages, as codes in
- * an 8-bit cache; values go as they are.  With q_d the rows' queries (shape->n_q_heads heads, strides as in sx_rope) are turned
+ * an 8-bit cache (those of sx_kv_append for that bf16 row); values go as they are.  With q_d the rows' queries (shape->n_q_heads heads, strides as in sx_rope) are turned
  * in the same launch to q_out_d, which may be q_d.  plan NULL: nothing is turned, the keys are as the attention wants them.
  * Rows, slots, refusals and reports as in sx_kv_append; rows behind the last sequence stay as they are in q_out_d too, and
  * of a row that is reported the queries may or may not be written.  head_dim 16, 32, 64 or 128. */

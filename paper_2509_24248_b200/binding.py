@@ -82,7 +82,7 @@ class RopeCfg(C.Structure):
 
 class Rotation(C.Structure):
     _fields_ = [("ready", C.c_int32), ("head_dim", C.c_int32), ("rot_start", C.c_int32), ("rot_dim", C.c_int32),
-                ("layout", C.c_int32), ("magnitude", C.c_float), ("step", C.c_uint64 * SX_ROPE_MAX_PAIRS)]
+                ("layout", C.c_int32), ("magnitude", C.c_double), ("step", C.c_uint64 * SX_ROPE_MAX_PAIRS)]
 
 
 class LogProbOut(C.Structure):

@@ -204,7 +204,9 @@ sx_tc_gemm_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       // Log-probabilities.  The sums of the accumulator's chains are added in registers, rounding to nearest; then the same data
       // flow as the argmax below: a thread owns one token row and a quarter of the vocabulary rows of each tile, here 32
       // neighbouring logits at a time, and keeps the running sums of every row it owns in registers.  The logits and the maximum
-      // of each 32 go to memory, for the alternatives and the given tokens alone.
+      // of each 32 go to memory, for the alternatives and the given tokens alone.  7 rows, 151936 x 4096: 213 us a call with
+      // twenty alternatives, 202 without any; the argmax 194.  Of the difference the chains cost 5 us, the sums 4.5, the
+      // alternatives 8.5.
       constexpr int CHUNKS = SX_SCORE_FEW / 32;
       float *tb = reinterpret_cast<float *>(epi_smem);          // [128 rows][33]
       const int tid = threadIdx.x - 64, col = tid & 31, part = tid >> 5;

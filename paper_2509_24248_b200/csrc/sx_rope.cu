@@ -6,13 +6,18 @@
 // turn: in fp32 a position of 10^5 alone costs it 0.01 rad.  The plan keeps f_i / 2 pi as a 64-bit fraction of a turn, so
 // that pos * f_i modulo one turn is one 64-bit integer product, whatever the position (off by pos * 2^-64 turns); its
 // quadrant is taken off as an integer too, and what is left, at most an eighth of a turn, is small enough for a short series.  cos,
-// sin and the products are fp32, the result is rounded once.
+// sin and the products are fp32 (fp64 for keys that become codes), the result is rounded once.
 //
 // Bound by bytes: every element is read and written once, three flops on the way.  A row (a head of a token) belongs to
 // d / 8 neighbouring lanes with 8 elements each, 16-byte accesses; the partner half comes from another lane by shuffle,
 // never a second time from memory.  A warp keeps the cos and sin of its lanes' elements in registers and takes a slice of a
 // token's rows (all of them in large calls, down to one row per lane in small ones, where the latency of a wave is all
-// there is).
+// there is).  64 registers, so that 32 warps of an SM have four rows each on the way.
+//
+// Measured (bf16, d = 128): 8192 tokens of 40 heads 29.9 us (168 MB, 5.6 TB/s; 55 us with 154 registers and the rows of all parts in
+// one loop), 32 tokens 3.7 us.  Prompts of 34k tokens into bf16 pages, 32 query and 8 KV heads, 135 us (840 MB, 6.2 TB/s); one
+// token of 32 sequences 4.5 us; 4096 tokens of keys (half of each turned) and values into an 8-bit cache 12.6 us (25 MB), bound by the
+// conversions to and from fp64, four a clock and scheduler (10.2 us with fp32).
 #include <cuda_fp16.h>
 #include <math.h>
 #include <string.h>
@@ -29,7 +34,7 @@ struct SxRopeArgs {
   int rot_start, rot_dim, half;  // half: 0 = interleaved order
   int partner;                   // where a lane finds the other half of its pairs, PARTNER_*
   int rows_per_warp, slices;
-  float magnitude;
+  double magnitude;
   int transpose;
   const int32_t *pos;            // [T] positions of the rows; append: nullptr = the row's slot
   const void *q, *k, *v;
@@ -47,7 +52,8 @@ struct SxRopeSteps { uint64_t step[SX_ROPE_MAX_PAIRS]; };
 
 // magnitude * (cos, sin) of pos * step, step in 2^-64 turns.  After the quadrant is taken off, |x| <= pi / 4 and the Taylor
 // series to x^9 and x^10 are off by 2e-9 and 1e-10 at most, below the roundings of their evaluation.
-__device__ __forceinline__ void rope_angle(uint64_t step, int pos, float magnitude, float *c, float *s) {
+__device__ __forceinline__ void rope_angle(uint64_t step, int pos, double mag, float *c, float *s) {
+  const float magnitude = (float)mag;
   const uint64_t ph = step * (uint64_t)(int64_t)pos;
   const uint32_t hi = (uint32_t)(ph >> 32), quad = (hi + (1u << 29)) >> 30;
   const float x = (float)(int32_t)(hi - (quad << 30)) * 1.4629180792671596e-9f;      // 2 pi / 2^32
@@ -62,6 +68,29 @@ __device__ __forceinline__ void rope_angle(uint64_t step, int pos, float magnitu
   cs = fmaf(z, cs, -0.5f);
   cs = fmaf(z, cs, 1.0f);
   const float u = (quad & 1) ? -sn : cs, v = (quad & 1) ? cs : sn;
+  *c = magnitude * ((quad & 2) ? -u : u);
+  *s = magnitude * ((quad & 2) ? -v : v);
+}
+
+// The same to 2^-45, for rows that are going to be rounded to codes (see rope_turn).
+__device__ __forceinline__ void rope_angle(uint64_t step, int pos, double magnitude, double *c, double *s) {
+  const uint64_t ph = step * (uint64_t)(int64_t)pos;
+  const uint32_t quad = (uint32_t)((ph + (1ull << 61)) >> 62);
+  const double x = (double)(int64_t)(ph - ((uint64_t)quad << 62)) * 3.4061215800304563e-19;      // 2 pi / 2^64
+  const double z = x * x;
+  double sn = fma(z, 1.6059043836821613e-10, -2.5052108385441720e-8);
+  sn = fma(z, sn, 2.7557319223985893e-6);
+  sn = fma(z, sn, -1.9841269841269841e-4);
+  sn = fma(z, sn, 8.3333333333333332e-3);
+  sn = fma(z, sn, -1.6666666666666666e-1);
+  sn = fma(z * x, sn, x);
+  double cs = fma(z, 2.0876756987868099e-9, -2.7557319223985888e-7);
+  cs = fma(z, cs, 2.4801587301587302e-5);
+  cs = fma(z, cs, -1.3888888888888889e-3);
+  cs = fma(z, cs, 4.1666666666666664e-2);
+  cs = fma(z, cs, -0.5);
+  cs = fma(z, cs, 1.0);
+  const double u = (quad & 1) ? -sn : cs, v = (quad & 1) ? cs : sn;
   *c = magnitude * ((quad & 2) ? -u : u);
   *s = magnitude * ((quad & 2) ? -v : v);
 }
@@ -106,18 +135,19 @@ template <> struct Rope8<float> {
 };
 
 // What a lane needs for its eight elements of every row of one position.
+template <typename F>
 struct RopeLane {
-  float c[8], s[8];              // cos, and the signed sine that the partner is multiplied by
+  F c[8], s[8];                  // cos, and the signed sine that the partner is multiplied by
   uint32_t in;                   // bit e: element e is in the rotated part
   int src;                       // PARTNER_SHUFFLE: lane of the partner's elements
 };
 
-template <int PARTNER>
-__device__ __forceinline__ void rope_lane_set(const SxRopeArgs &p, int e0, int lane, RopeLane *r) {
+template <int PARTNER, typename F>
+__device__ __forceinline__ void rope_lane_set(const SxRopeArgs &p, int e0, int lane, RopeLane<F> *r) {
   r->in = 0;
   r->src = lane;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) r->c[e] = r->s[e] = 0.f;
+  for (int e = 0; e < 8; ++e) r->c[e] = r->s[e] = F(0);
 #pragma unroll
   for (int e = 0; e < 8; ++e)
     if ((unsigned)(e0 + e - p.rot_start) < (unsigned)p.rot_dim) r->in |= 1u << e;
@@ -125,13 +155,13 @@ __device__ __forceinline__ void rope_lane_set(const SxRopeArgs &p, int e0, int l
 }
 
 // Every lane of the warp calls it (shuffles).
-template <int PARTNER>
-__device__ __forceinline__ void rope_lane_angles(const SxRopeArgs &p, const SxRopeSteps &st, int e0, int pos, RopeLane *r) {
+template <int PARTNER, typename F>
+__device__ __forceinline__ void rope_lane_angles(const SxRopeArgs &p, const SxRopeSteps &st, int e0, int pos, RopeLane<F> *r) {
   const int i0 = e0 - p.rot_start;
   if (PARTNER == PARTNER_LANE) {
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
-      float c = 0.f, s = 0.f;
+      F c = F(0), s = F(0);
       if (r->in >> e & 1) rope_angle(st.step[(i0 + e) >> 1], pos, p.magnitude, &c, &s);
       if (p.transpose) s = -s;
       r->c[e] = r->c[e + 1] = c;
@@ -142,23 +172,23 @@ __device__ __forceinline__ void rope_lane_angles(const SxRopeArgs &p, const SxRo
     // both halves of the eight pairs turn by the same angles: the lane of the first half computes four, its partner the others
     const bool first = i0 < p.half;
     const uint64_t *step = st.step + (r->in ? (first ? i0 : i0 - p.half + 4) : 0);
-    float c[4], s[4];
+    F c[4], s[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) rope_angle(step[e], pos, p.magnitude, &c[e], &s[e]);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float oc = __shfl_sync(0xffffffffu, c[e], r->src), os = __shfl_sync(0xffffffffu, s[e], r->src);
+      const F oc = __shfl_sync(0xffffffffu, c[e], r->src), os = __shfl_sync(0xffffffffu, s[e], r->src);
       r->c[e] = first ? c[e] : oc;
       r->c[e + 4] = first ? oc : c[e];
       const bool minus = first != (p.transpose != 0);
-      const float lo = first ? s[e] : os, hi = first ? os : s[e];
+      const F lo = first ? s[e] : os, hi = first ? os : s[e];
       r->s[e] = minus ? -lo : lo;
       r->s[e + 4] = minus ? -hi : hi;
     }
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      float c = 0.f, s = 0.f;
+      F c = F(0), s = F(0);
       const int i = i0 + e;
       if (r->in >> e & 1) rope_angle(st.step[i < p.half ? i : i - p.half], pos, p.magnitude, &c, &s);
       r->c[e] = c;
@@ -167,9 +197,18 @@ __device__ __forceinline__ void rope_lane_angles(const SxRopeArgs &p, const SxRo
   }
 }
 
+// To be rounded once more to fewer bits: cut off, with the last bit set if anything was lost, so that the second rounding is right.
+__device__ __forceinline__ float rope_narrow(float y) { return y; }
+__device__ __forceinline__ float rope_narrow(double y) {
+  const float f = __double2float_rz(y);                       // loses the lower 29 bits of the fraction (more only below 2^-126)
+  return (__double2loint(y) & 0x1fffffff) && fabsf(f) < INFINITY ? __uint_as_float(__float_as_uint(f) | 1u) : f;
+}
+
 // One row's words turned in place.  Every lane of the warp calls it (shuffles); row: nullptr where the lane has none.
-template <typename E, int PARTNER>
-__device__ __forceinline__ void rope_turn(const SxRopeArgs &p, const RopeLane &r, const E *row, int e0, uint32_t *w) {
+// F = double where the row goes into codes: of a value within an fp32 rounding of the border between two of them the other code, a
+// sixteenth of the value away, would be written (4096 tokens of 8 heads: some three values, 1e-4 of the result's norm).
+template <typename E, int PARTNER, typename F>
+__device__ __forceinline__ void rope_turn(const SxRopeArgs &p, const RopeLane<F> &r, const E *row, int e0, uint32_t *w) {
   constexpr int W = Rope8<E>::W;
   float x[8], o[8];
   Rope8<E>::unpack(w, x);
@@ -190,7 +229,7 @@ __device__ __forceinline__ void rope_turn(const SxRopeArgs &p, const RopeLane &r
   }
   float y[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) y[e] = fmaf(x[e], r.c[e], o[e] * r.s[e]);
+  for (int e = 0; e < 8; ++e) y[e] = rope_narrow(fma(F(x[e]), r.c[e], F(o[e]) * r.s[e]));
   // a word outside the rotated part keeps its bits (the part begins and ends between 32-bit words)
 #pragma unroll
   for (int i = 0; i < W; ++i) {
@@ -216,7 +255,7 @@ __device__ __forceinline__ void rope_store(void *dst, const uint32_t *w) {
 // Rows [h0, h1) of a token's queries or keys, G at a time, U times that on the way together.  angles() is called once the
 // first rows have been asked for.
 template <typename E, int LPR, int PARTNER, typename A>
-__device__ __forceinline__ void rope_rows(const SxRopeArgs &p, RopeLane &rl, int h0, int h1, const E *src, E *dst, int lane, A angles) {
+__device__ __forceinline__ void rope_rows(const SxRopeArgs &p, RopeLane<float> &rl, int h0, int h1, const E *src, E *dst, int lane, A angles) {
   constexpr int W = Rope8<E>::W, G = 32 / LPR, U = PARTNER == PARTNER_LOAD ? 2 : 16 / W;
   const int e0 = (lane % LPR) * 8;
 #pragma unroll 1
@@ -251,7 +290,7 @@ __global__ void __launch_bounds__(ROPE_THREADS, PARTNER == PARTNER_LOAD ? 4 : 8)
   if (t >= p.T) return;
   const int r0 = (unit - t * p.slices) * p.rows_per_warp, r1 = min(p.nq + p.nk, r0 + p.rows_per_warp);
   const int e0 = (lane % LPR) * 8, pos = p.pos[t];
-  RopeLane rl;
+  RopeLane<float> rl;
   rope_lane_set<PARTNER>(p, e0, lane, &rl);
   bool set = false;
   const auto angles = [&]() {
@@ -280,9 +319,9 @@ __device__ __forceinline__ int rope_sequence(const SxRopeArgs &p, int t, int lan
 }
 
 // Rows [h0, h1) of a token's keys (TURN) or values to their places in the pool; Q8: as e4m3 codes with one power-of-two scale
-// per row, exactly as the unrotated append writes the bf16 row that the rotation leaves.
-template <int LPR, int PARTNER, bool Q8, bool TURN, typename A>
-__device__ __forceinline__ void rope_place(const SxRopeArgs &p, RopeLane &rl, int h0, int h1, const bf16 *src, void *pool, uint8_t *scales,
+// per row, as the unrotated append writes the exact rotation's row rounded to bf16.
+template <int LPR, int PARTNER, bool Q8, bool TURN, typename F, typename A>
+__device__ __forceinline__ void rope_place(const SxRopeArgs &p, RopeLane<F> &rl, int h0, int h1, const bf16 *src, void *pool, uint8_t *scales,
                                            const int64_t &place, int lane, A angles) {
   constexpr int G = 32 / LPR, U = PARTNER == PARTNER_LOAD ? 2 : 4;
   const int e0 = (lane % LPR) * 8;
@@ -329,7 +368,7 @@ __device__ __forceinline__ void rope_place(const SxRopeArgs &p, RopeLane &rl, in
 
 // Rows of new tokens: queries and keys turned, keys and values to their pages.
 template <int LPR, int PARTNER, bool Q8>
-__global__ void __launch_bounds__(ROPE_THREADS, PARTNER == PARTNER_LOAD ? 4 : 8) sx_rope_append_kernel(const SxRopeArgs p, const __grid_constant__ SxRopeSteps st) {
+__global__ void __launch_bounds__(ROPE_THREADS, PARTNER == PARTNER_LOAD ? 4 : Q8 ? 7 : 8) sx_rope_append_kernel(const SxRopeArgs p, const __grid_constant__ SxRopeSteps st) {
   sx_pdl_wait();                              // dependents start when this kernel has completed: they may read the pages
   if (blockIdx.x == 0)
     for (int b = threadIdx.x; b < p.B; b += ROPE_THREADS) {
@@ -344,24 +383,45 @@ __global__ void __launch_bounds__(ROPE_THREADS, PARTNER == PARTNER_LOAD ? 4 : 8)
   int first = 0;
   const int b = rope_sequence(p, t, lane, &first);
   if (b < 0) return;                          // a row behind the last sequence
-  RopeLane rl;
+  RopeLane<float> rl;
   rope_lane_set<PARTNER>(p, e0, lane, &rl);
   int64_t place = -1;                         // first row of the pool for this token
+  int pos = 0;
   bool set = false;
-  const auto angles = [&]() {                 // while the first rows are on their way: the token's place and angles
+  const auto find = [&]() {                   // while the first rows are on their way: the token's place and position
     if (set) return;
     set = true;
     const int64_t slot = (int64_t)p.pos_start[b] + (t - first), lp = slot < 0 ? -1 : slot / p.page;
     int pp = -1;
     if (lp >= 0 && lp < p.max_pages) pp = p.page_table[(int64_t)b * p.max_pages + lp];
-    if (r0 < p.nq + p.nk) rope_lane_angles<PARTNER>(p, st, e0, p.pos ? p.pos[t] : (int)slot, &rl);
+    pos = p.pos ? p.pos[t] : (int)slot;
     if (pp < 0 || pp >= p.num_pages) sx_set_status(p.status, SX_ERR_CAPACITY);
     else place = (int64_t)pp * p.nk * p.page + slot % p.page;
   };
   const int k0 = p.nq, v0 = p.nq + p.nk;
-  rope_rows<bf16, LPR, PARTNER>(p, rl, r0, min(r1, k0), reinterpret_cast<const bf16 *>(p.q) + t * p.qs, reinterpret_cast<bf16 *>(p.qo) + t * p.qos, lane, angles);
-  rope_place<LPR, PARTNER, Q8, true>(p, rl, max(r0 - k0, 0), min(r1, v0) - k0, reinterpret_cast<const bf16 *>(p.k) + t * p.ks, p.kp, p.ksc, place, lane, angles);
-  rope_place<LPR, PARTNER, Q8, false>(p, rl, max(r0 - v0, 0), r1 - v0, reinterpret_cast<const bf16 *>(p.v) + t * p.vs, p.vp, p.vsc, place, lane, angles);
+  const bf16 *q = reinterpret_cast<const bf16 *>(p.q) + t * p.qs, *k = reinterpret_cast<const bf16 *>(p.k) + t * p.ks,
+             *v = reinterpret_cast<const bf16 *>(p.v) + t * p.vs;
+  bool turned = false;
+  const auto angles = [&]() {
+    find();
+    if (!turned) rope_lane_angles<PARTNER>(p, st, e0, pos, &rl);
+    turned = true;
+  };
+  rope_rows<bf16, LPR, PARTNER>(p, rl, r0, min(r1, k0), q, reinterpret_cast<bf16 *>(p.qo) + t * p.qos, lane, angles);
+  const int k_from = max(r0 - k0, 0), k_to = min(r1, v0) - k0;
+  if constexpr (Q8) {
+    RopeLane<double> wide;
+    rope_lane_set<PARTNER>(p, e0, lane, &wide);
+    bool wide_set = false;
+    rope_place<LPR, PARTNER, Q8, true>(p, wide, k_from, k_to, k, p.kp, p.ksc, place, lane, [&]() {
+      find();
+      if (!wide_set) rope_lane_angles<PARTNER>(p, st, e0, pos, &wide);
+      wide_set = true;
+    });
+  } else {
+    rope_place<LPR, PARTNER, Q8, true>(p, rl, k_from, k_to, k, p.kp, p.ksc, place, lane, angles);
+  }
+  rope_place<LPR, PARTNER, Q8, false>(p, rl, max(r0 - v0, 0), r1 - v0, v, p.vp, p.vsc, place, lane, find);
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
@@ -418,7 +478,7 @@ extern "C" sx_status sx_rope_plan(const sx_rope_cfg *cfg, sx_rotation *out) {
   out->rot_start = cfg->rot_start;
   out->rot_dim = r;
   out->layout = cfg->layout;
-  out->magnitude = (float)cfg->magnitude;
+  out->magnitude = cfg->magnitude;
   out->ready = SX_ROPE_READY;
   return SX_OK;
 }
@@ -440,6 +500,8 @@ static sx_status rope_args(const sx_rotation *plan, int head_dim, SxRopeArgs *p,
   p->magnitude = plan->magnitude;
   if (plan->layout == SX_ROPE_HALF) {
     p->half = plan->rot_dim / 2;
+    // halves that do not begin where a lane does: the partners come from memory one by one (8192 tokens of 40 heads with 120 of
+    // 128 elements turned 56 us, with 112 by shuffle 30 us)
     p->partner = (p->half % 8 == 0 && p->rot_start % 8 == 0) ? PARTNER_SHUFFLE : PARTNER_LOAD;
   }
   memcpy(st->step, plan->step, sizeof(uint64_t) * (plan->rot_dim / 2));
@@ -449,7 +511,8 @@ static sx_status rope_args(const sx_rotation *plan, int head_dim, SxRopeArgs *p,
 static int lanes_per_row(int d) { int l = 4; while (l * 8 < d) l <<= 1; return l; }
 
 // A warp takes all rows of a token where that makes 16 warps per SM; below that the rows are cut into as many slices as make
-// them, down to one row per lane.
+// them, down to one row per lane (4, 8, 16, 32, 64 warps per SM: 512 tokens of 40 heads 6.1, 5.7, 5.3, 7.4, 7.8 us; 2048 of them the same
+// within a tenth).
 static sx_status rope_grid(SxRopeArgs *p, unsigned *grid) {
   const int all = p->nq + p->nk + p->nv, G = 32 / lanes_per_row(p->D);
   const int sm = sx_sm_count();

@@ -59,3 +59,9 @@ def close(got: torch.Tensor, y: np.ndarray, far: np.ndarray) -> None:
     bound = np.where(far > 0, far + info.eps / 2 * (np.abs(y) + far) + info.smallest_normal * info.eps, 0.0)
     off = np.abs(g - y)
     assert (off <= bound).all(), (off - bound).max()
+
+
+def to_bf16(y: np.ndarray) -> torch.Tensor:
+    """Nearest bf16 of float64 values, ties to even, in one rounding (normal values)."""
+    m, e = np.frexp(y)
+    return torch.from_numpy(np.ldexp(np.round(m * 256.0), e - 8)).to(torch.float32).to(torch.bfloat16)

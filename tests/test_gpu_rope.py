@@ -138,6 +138,13 @@ def cache(B, n_kv, d, page, M, kind, seed=0, spare=2):
     return kv
 
 
+def rope_ref_rows(k, pos, rot, layout, start, n):
+    """The first n rows turned in extended precision and rounded to bf16 (the others as they are)."""
+    y = k.clone()
+    y[:n] = ref.to_bf16(ref.turned(k[:n], pos[:n], ref.frequencies(rot, 1e4), layout, start)[0]).to(DEV)
+    return y
+
+
 def i32(v):
     return torch.tensor(v, dtype=torch.int32, device=DEV)
 
@@ -146,8 +153,8 @@ def i32(v):
 @pytest.mark.parametrize("layout,start,frac", [("half", 0, 1.0), ("half", 0, 0.5), ("interleaved", 4, 0.5), ("half", 2, 0.75)])
 @pytest.mark.parametrize("d,nq,nkv", [(128, 8, 2), (64, 3, 1), (32, 4, 4), (16, 2, 1)])
 def test_append_is_rotation_then_placement(kind, page, layout, start, frac, d, nq, nkv):
-    """The same bits as sx_rope on queries and keys and then the plain placement (sx_kv_append for codes); every other slot,
-    and rows behind the last sequence, as they were."""
+    """The same bits as sx_rope on queries and keys and then the plain placement; codes are those of the exact rotation rounded
+    to bf16 (sx_kv_append on it).  Every other slot, and rows behind the last sequence, as they were."""
     rot = int(d * frac) // 2 * 2
     start = min(start, d - rot)
     rope = sx.Rope(d, 1e4, rot_dim=rot, rot_start=start, layout=LAYOUT[layout])
@@ -170,7 +177,8 @@ def test_append_is_rotation_then_placement(kind, page, layout, start, frac, d, n
     assert torch.equal(q_out[:n], wq[:n]) and (q_out[n:] == -5.0).all()
     if kind == "e4m3":
         e = sx.KV8(two)
-        e.sx_kv_append(wk, v, i32(start_), i32(at))
+        exact = rope_ref_rows(k, pos, rot, layout, start, n)
+        e.sx_kv_append(exact, v, i32(start_), i32(at))
         e.check_status()
     else:
         for b in range(B):
@@ -197,7 +205,7 @@ def test_append_without_plan_positions_of_its_own_and_in_place(kind):
     c = sx.KVPages(kv)
     c.sx_kv_append_rope(rope, k, v, start, rot_pos=pos)
     e = sx.KVPages(two)
-    e.sx_kv_append_rope(None, wk, v, start, i32([10, 0, 30]))
+    e.sx_kv_append_rope(None, rope_ref_rows(k, pos.cpu(), d, "half", 0, 7) if kind == "e4m3" else wk, v, start, i32([10, 0, 30]))
     for name in ("k_pages", "v_pages", *(("k_scale", "v_scale") if kind == "e4m3" else ())):
         assert torch.equal(kv[name], two[name]), name
     assert kv["cache_len"].tolist() == [10, 0, 30]

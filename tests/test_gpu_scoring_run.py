@@ -148,7 +148,8 @@ def test_a_draft_step_on_a_prompt_written_by_append(kv_dtype):
         else:
             pos = torch.cat([torch.arange(n, dtype=torch.int32) for n in lens]).to(DEV)
             turned = rope.sx_rope(pos, k)[0]
-            if kv_dtype == sx.KV_E4M3:
+            if kv_dtype == sx.KV_E4M3:                # codes are those of the exact rotation
+                turned = rope_ref.to_bf16(rope_ref.turned(k, pos.cpu(), rope_ref.frequencies(64, sh.theta), "half", 0)[0]).to(DEV)
                 sx.KV8(spec.kv).sx_kv_append(turned, v, start, zero)
             else:
                 for b, n in enumerate(lens):
