@@ -367,10 +367,11 @@ sx_status sx_rope(const sx_rotation *plan, int32_t dtype, int32_t transpose, int
 
 /* sx_kv_append for a cache of either kind (kv->dtype), with the rotation on the way: the keys of every row are turned to the
  * row's position - rot_pos_d[t], or its slot where rot_pos_d is NULL - rounded to bf16 and written to their pages, as codes in
- * an 8-bit cache (those of sx_kv_append for that bf16 row); values go as they are.  With q_d the rows' queries (shape->n_q_heads heads, strides as in sx_rope) are turned
- * in the same launch to q_out_d, which may be q_d.  plan NULL: nothing is turned, the keys are as the attention wants them.
- * Rows, slots, refusals and reports as in sx_kv_append; rows behind the last sequence stay as they are in q_out_d too, and
- * of a row that is reported the queries may or may not be written.  head_dim 16, 32, 64 or 128. */
+ * an 8-bit cache (those of sx_kv_append for that bf16 row); values go as they are.  With q_d the rows' queries
+ * (shape->n_q_heads heads, strides as in sx_rope) are turned in the same launch to q_out_d, which may be q_d.  plan NULL:
+ * nothing is turned, the keys are as the attention wants them.  Rows, slots, refusals and reports as in sx_kv_append; rows
+ * behind the last sequence stay as they are in q_out_d too, and of a row that is reported the queries may or may not be
+ * written.  head_dim 16, 32, 64 or 128. */
 sx_status sx_kv_append_rope(const sx_rotation *plan, const sx_kv_shape *shape, const sx_kv *kv, int32_t T,
                             const int32_t *row_start_d, const int32_t *pos_start_d, const int32_t *rot_pos_d, const void *k_d,
                             int64_t k_stride, const void *v_d, int64_t v_stride, const void *q_d, int64_t q_stride,
