@@ -39,7 +39,8 @@ def both(h, w, tok, V, top, temperature=1.0, scores=None):
 @pytest.mark.parametrize("T,V,H,extra", [
     (1, 1, 8, 0), (3, 5, 16, 0), (7, 127, 64, 3), (17, 128, 72, 3), (16, 129, 128, 0), (33, 1000, 256, 3), (64, 2049, 136, 0), (65, 3000, 64, 1),
     (128, 640, 1024, 0), (255, 1300, 64, 3), (256, 257, 64, 0), (257, 700, 64, 3), (513, 300, 40, 0), (700, 515, 264, 3), (2, 40000, 512, 3),
-    (1, 151936, 64, 3), (250, 20011, 128, 0)])
+    (1, 151936, 64, 3), (250, 20011, 128, 0), (300, 1, 8, 0), (129, 383, 1032, 3), (1025, 300, 40, 0), (2100, 130, 64, 3), (5, 200, 16384, 0),
+    (140, 260, 8200, 0)])
 def test_shapes(T, V, H, extra):
     both(*make(T, V, H, T + V, extra), V, min(20, 32))
 
@@ -59,10 +60,11 @@ def test_equal_tokens_everywhere():
     both(h, w[:100].repeat(11, 1)[:1024].contiguous(), tok, 1024, 32)
 
 
-@pytest.mark.parametrize("V,H,extra", [(300, 72, 0), (1000, 200, 3), (2048, 64, 3)])
-def test_repacked_head(V, H, extra):
+@pytest.mark.parametrize("T", [70, 300])
+@pytest.mark.parametrize("V,H,extra", [(300, 72, 0), (1000, 200, 3), (2048, 64, 3), (130, 640, 0)])
+def test_repacked_head(V, H, extra, T):
     """The layout of sx_tile_weight, rows behind the vocabulary included, gives the same bits."""
-    h, w, tok = make(70, V, H, 5, extra)
+    h, w, tok = make(T, V, H, 5, extra)
     want = both(h, w, tok, V, 8)
     got = sx.LogProbs(sx.sx_tile_weight(w), vocab=V, hidden=H).sx_head_logprobs(h, tok, top=8)
     assert all(torch.equal(want[n], got[n]) for n in want)
@@ -80,13 +82,42 @@ def test_logits_are_those_of_the_other_form():
     ref.check(got, ref.scores(x, tok, 0), x, more=more)
 
 
-def test_rows_that_are_not_finite_stay_alone():
-    h, w, tok = make(12, 900, 64, 7)
+@pytest.mark.parametrize("T", [12, 270])
+def test_rows_that_are_not_finite_stay_alone(T):
+    h, w, tok = make(T, 900, 64, 7)
     h[2, 5] = float("nan")
-    h[7, :] = float("inf")                                       # inf times a zero or signs that differ: NaN
+    h[T - 5, :] = float("inf")                                   # inf times a zero or signs that differ: NaN
     got = sx.LogProbs(w).sx_head_logprobs(h, tok, top=4)
     x = logits(h, w, 900)
     ref.check(got, ref.scores(x, tok, 4), x)
+
+
+def test_calls_in_a_row_and_beside_one_another():
+    """Calls of both kinds and several sizes without a wait between them, then on two streams at once, each with an object of its
+    own: what single calls give."""
+    V, H = 3000, 512
+    sizes = (7, 300, 1, 129, 128, 600, 33)
+    made = [make(T, V, H, 40 + T) for T in sizes]
+    w = made[0][1]
+    want = []
+    for h, _, tok in made:
+        want.append(sx.LogProbs(w).sx_head_logprobs(h, tok, top=6))
+        torch.cuda.synchronize()
+    one = sx.LogProbs(w)
+    got = [[one.sx_head_logprobs(h, tok, top=6) for h, _, tok in made] for _ in range(5)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    mine = [sx.LogProbs(w) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, o in zip(streams, mine):
+            with torch.cuda.stream(s):
+                got.append([o.sx_head_logprobs(h, tok, top=6) for h, _, tok in made])
+    torch.cuda.synchronize()
+    for run in got:
+        for a, b in zip(run, want):
+            assert all(torch.equal(a[n], b[n]) for n in b)
+    for o in (one, *mine):
+        o.check_status()
 
 
 def test_large_part_of_the_vocabulary_without_weight():
@@ -112,10 +143,11 @@ def test_a_token_outside_the_vocabulary_is_reported():
     ref.check(got, ref.scores(x, tok, 2), x)
 
 
-def test_streams_graphs_and_growing_workspaces():
+@pytest.mark.parametrize("T", [30, 200])
+def test_streams_graphs_and_growing_workspaces(T):
     """The same bits on another stream, from a captured call with new rows, and after a larger call has grown the workspace."""
-    h, w, tok = make(30, 3000, 128, 10)
-    big, _, many = make(300, 3000, 128, 11)
+    h, w, tok = make(T, 3000, 128, 10)
+    big, _, many = make(500, 3000, 128, 11)
     s = sx.LogProbs(w)
     want = s.sx_head_logprobs(h, tok, top=5)
     side = torch.cuda.Stream()
@@ -132,7 +164,7 @@ def test_streams_graphs_and_growing_workspaces():
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(want[n], out[n]) for n in want)
-    h.copy_(make(30, 3000, 128, 12)[0])
+    h.copy_(make(T, 3000, 128, 12)[0])
     graph.replay()
     torch.cuda.synchronize()
     x = logits(h, w, 3000)
