@@ -463,7 +463,9 @@ __global__ void __launch_bounds__(W * 32, 32 / W) sx_score_kernel(const SxScoreA
   }
   score_join_sums<W>(sh, a, p.scale);
   if (p.top) score_join_warps<W>(sh, l, p.top, sh.group);
-  if (cluster > 1 && !score_join_cluster<W>(sh, cluster, rank, p.top, p.scale)) return;
+  if constexpr (W == SCORE_MAX_WARPS) {
+    if (cluster > 1 && !score_join_cluster<W>(sh, cluster, rank, p.top, p.scale)) return;
+  }
   if (p.top)
     score_best_elements<W>(sh, p.top, [&](int id, int i, int *index) {
       const int from = id == 0 ? 0 : lead + (id - 1) * GE, n = id == 0 ? lead : id == whole + 1 ? rest : GE;
@@ -552,34 +554,39 @@ static sx_status score_args(int32_t T, int32_t V, int32_t n_given, const int32_t
   return SX_OK;
 }
 
-// Warps and CTAs per row.  An SM has room for 32 warps of this kernel.  Where there are rows enough to fill the card four warps
-// share one: the ends of a row (first loads, joining, alternatives: some 5 us in which it reads nothing, at the same time
-// for all rows that began together) weigh less the longer it takes, but more rows at a time mean more places in
-// memory that are read at once (4096 rows of 151936 in bf16 with 8, 4, 2, 1 warps: 237, 220, 297, 424 us).  Below that, eight.  Every
-// warp gets two rounds of groups, where the row has as many.  A row is spread over a cluster while that makes no more than
-// 1.75 CTAs per SM and leaves each warp a round (one row of 151936 in bf16 on 1, 2, 4, 8 CTAs: 22, 19, 15.6, 13.9 us; 74 rows: 19.3,
-// 16.4, 17.6, 22 us).
+// Warps and CTAs per row.  An SM has room for 32 warps of this kernel.  A row's ends (first loads, joining, alternatives: 3 to 5 us in
+// which it reads nothing) are shorter the fewer warps it has, and weigh less the longer it takes; so a row has as many warps as
+// there is room for with all rows at once (4096 rows of 32000 in bf16 with 1, 2, 4, 8: 61, 69, 76, 92 us; 2000 of 50000: 56, 52, 56,
+// 63; 1000 of 32000: 29, 25, 24, 27; 1500 of 151936: 123, 104, 100, 98; 4096 of them 219, 219, 217, 237), and every warp two rounds of
+// groups, where the row has as many.  A row is spread over a cluster while that makes no more than 1.75 CTAs per SM and leaves
+// each warp a round (one row of 151936 in bf16 on 1, 2, 4, 8 CTAs: 22, 19, 15.6, 13.9 us; 74 rows: 19.3, 16.4, 17.6, 22 us).
 struct ScoreSplit { int warps, cluster; };
 static ScoreSplit score_split(int64_t T, int64_t groups, int sm) {
   const int64_t room = 32ll * sm, most = groups / (2 * 32);
   ScoreSplit n = {1, 1};
-  while (n.warps < 4 && n.warps * 2 <= most) n.warps *= 2;
   while (n.warps < SCORE_MAX_WARPS && n.warps * 2 <= most && T * n.warps * 2 <= room) n.warps *= 2;
   while (n.cluster < SCORE_MAX_CLUSTER && n.warps == SCORE_MAX_WARPS && groups >= 32ll * n.warps * n.cluster * 2 && 4 * T * n.cluster * 2 <= 7ll * sm)
     n.cluster *= 2;
   return n;
 }
 
+template <typename E, int W>
+static sx_status launch_score_of(const SxScoreArgs &p, const E *x, int64_t stride, int cluster, cudaStream_t st) {
+  // (a cluster of one is not launched as one: that leaves room for fewer CTAs, 4096 rows of 515 in 30 instead of 12 us)
+  const dim3 grid((unsigned)(p.T * cluster)), block(W * 32);
+  if constexpr (W == SCORE_MAX_WARPS) {
+    if (cluster > 1) return sx_rc(sx_launch_cluster(sx_score_kernel<E, W>, grid, block, 0, (unsigned)cluster, st, p, x, stride, cluster));
+  }
+  return sx_rc(sx_launch(sx_score_kernel<E, W>, grid, block, 0, st, p, x, stride, 1));
+}
 template <typename E>
 static sx_status launch_score(const SxScoreArgs &p, const void *logits, int64_t stride, ScoreSplit n, cudaStream_t st) {
-  const dim3 grid((unsigned)(p.T * n.cluster)), block(n.warps * 32);
   const E *x = (const E *)logits;
-  const unsigned c = (unsigned)n.cluster;
   switch (n.warps) {
-    case 1: return sx_rc(sx_launch_cluster(sx_score_kernel<E, 1>, grid, block, 0, c, st, p, x, stride, n.cluster));
-    case 2: return sx_rc(sx_launch_cluster(sx_score_kernel<E, 2>, grid, block, 0, c, st, p, x, stride, n.cluster));
-    case 4: return sx_rc(sx_launch_cluster(sx_score_kernel<E, 4>, grid, block, 0, c, st, p, x, stride, n.cluster));
-    default: return sx_rc(sx_launch_cluster(sx_score_kernel<E, 8>, grid, block, 0, c, st, p, x, stride, n.cluster));
+    case 1: return launch_score_of<E, 1>(p, x, stride, n.cluster, st);
+    case 2: return launch_score_of<E, 2>(p, x, stride, n.cluster, st);
+    case 4: return launch_score_of<E, 4>(p, x, stride, n.cluster, st);
+    default: return launch_score_of<E, 8>(p, x, stride, n.cluster, st);
   }
 }
 
@@ -657,8 +664,9 @@ extern "C" sx_status sx_head_logprobs(const void *head_d, int32_t tiled, int32_t
     // themselves, but keep the next call's product off twice as many SMs: 7 rows 221 instead of 217 us in a row of calls.)
     int cluster = 1;
     while (cluster < SCORE_MAX_CLUSTER && R * cluster * 2 <= 4 * sm && tiles * 4 >= cluster * 2 * 4 * SCORE_MAX_WARPS * 32) cluster *= 2;
-    SX_TRY(sx_rc(sx_launch_cluster(sx_score_head_kernel, dim3(R * cluster), dim3(SCORE_MAX_WARPS * 32), 0, (unsigned)cluster, st, p, o, r0,
-                                   parts, tiles, cluster)));
+    const dim3 grid(R * cluster), block(SCORE_MAX_WARPS * 32);
+    if (cluster > 1) SX_TRY(sx_rc(sx_launch_cluster(sx_score_head_kernel, grid, block, 0, (unsigned)cluster, st, p, o, r0, parts, tiles, cluster)));
+    else SX_TRY(sx_rc(sx_launch(sx_score_head_kernel, grid, block, 0, st, p, o, r0, parts, tiles, 1)));
   }
   return SX_OK;
 }
