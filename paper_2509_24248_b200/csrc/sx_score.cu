@@ -351,7 +351,7 @@ struct ScorePlain {
       r = to;
       limit = gm + slack;
     }
-    float s0 = a.s, s1 = 0.f, t0 = a.t, t1 = 0.f;
+    float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;       // of this group: short sums of small numbers, added to the long ones once
     score_pairs<E>(w, [&](float2 x) {
       const float d0 = score_max_nan(fmaf(x.x, scale, -r), -200.f), d1 = score_max_nan(fmaf(x.y, scale, -r), -200.f);
       const float e0 = score_exp2(d0), e1 = score_exp2(d1);
@@ -360,9 +360,8 @@ struct ScorePlain {
       t0 = fmaf(e0, d0, t0);
       t1 = fmaf(e1, d1, t1);
     });
-    t0 += t1;
     if (!__all_sync(0xffffffffu, !on || fabsf(r) < 1048576.f)) return false;
-    if (on) { a.s = s0 + s1; a.t = t0; }
+    if (on) { a.s += s0 + s1; a.t += t0 + t1; }
     return true;
   }
   // relative to 2^(c m) from here on
@@ -444,10 +443,10 @@ __global__ void __launch_bounds__(W * 32, 32 / W) sx_score_kernel(const SxScoreA
     if (g < whole) {
       if (gm > a.m) a.raise(gm, p.scale);
       const float ref = a.m > -INFINITY ? a.m : 0.f;
-      float2 s2 = make_float2(a.s, 0.f), t2 = make_float2(a.t, 0.f);
+      float2 s2 = make_float2(0.f, 0.f), t2 = s2;
       score_pairs<E>(w, [&](float2 v) { score_pair(v, p.scale, ref, s2, t2); });
-      a.s = s2.x + s2.y;
-      a.t = t2.x + t2.y;
+      a.s += s2.x + s2.y;
+      a.t += t2.x + t2.y;
     }
     if (p.top) l.offer_group(gm, g + 1, p.top, lane, &sh.floor);
   }

@@ -39,8 +39,8 @@ def check(got, want, logits, temperature: float = 1.0, more: float = 0.0):
 
 The difference of a logit and the row's largest is rounded once, its product with c = log2(e) / temperature twice (c itself is
     off by 2^-24): d is off by 3 2^-24 |d|, a power that counts (d > -40) by 2^-22 + 120 2^-24 of itself at most and a mean one
-    by far less; a sum of n powers by n 2^-24 more at worst: every lane adds at most 2 n / 2048 + 64 elements in a row, some 20
-    joins follow.  ln s is then off by D = 2^-21 + (n / 1024 + 100) 2^-24, and so is t / s by D (2 + log2 n) + 20 D at most, t being
+    by far less; a sum of n powers by n 2^-24 more at worst: a lane adds its groups' sums, of 32 at most each and n / 1024 of them at
+    most, and some 20 joins follow.  ln s is then off by D = 2^-21 + (n / 1024 + 100) 2^-24, and so is t / s by D (2 + log2 n) + 20 D at most, t being
     a mean of |d| weighted by powers that sum to s (|d| above 40 does not count).  log p: D, the roundings of the difference, of its
     product and of the result, 2^-22 of their size.  `more`: what the logits themselves are off by."""
     x = logits.to(torch.float64).cpu().numpy() / temperature
