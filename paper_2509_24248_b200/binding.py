@@ -338,6 +338,14 @@ def _guard_of(index: int):
     return _NO_GUARD if torch._C._cuda_getDevice() == index else torch.cuda.device(index)
 
 
+def _on_device(index: int, call, *args) -> int:
+    """`call` with device `index` the current one."""
+    if torch._C._cuda_getDevice() == index:
+        return call(*args)
+    with torch.cuda.device(index):
+        return call(*args)
+
+
 def _heads_stride(name: str, t: torch.Tensor, dtype: torch.dtype, T: int, heads: int, d: int, index: int) -> int:
     """Row stride of ``t [T, heads, d]`` on device `index` whose heads lie side by side."""
     shape, stride = t.shape, t.stride()
@@ -399,9 +407,9 @@ class Rope:
             raise SxError("k_out without k")
         if T == 0:
             return q_out, k_out
-        with _guard_of(index):
-            code = self._call(self.plan_ref, _FLOATS[dtype], 1 if transpose else 0, T, pos.data_ptr(), nq, q.data_ptr(), qs,
-                              q_out.data_ptr(), qos, nk, k_at, ks, k_out_at, kos, torch._C._cuda_getCurrentRawStream(index))
+        code = _on_device(index, self._call, self.plan_ref, _FLOATS[dtype], 1 if transpose else 0, T, pos.data_ptr(), nq,
+                          q.data_ptr(), qs, q_out.data_ptr(), qos, nk, k_at, ks, k_out_at, kos,
+                          torch._C._cuda_getCurrentRawStream(index))
         if code:
             _check(code, "sx_rope")
         return q_out, k_out
@@ -489,11 +497,10 @@ class KVPages:
         if T == 0:
             return q_out
         self._shape.n_q_heads = nq
-        with _guard_of(index):
-            code = self._append_rope(plan, self._shape_ref, self._kv_ref, T, row_start.data_ptr(),
-                                     None if pos_start is None else pos_start.data_ptr(),
-                                     None if rot_pos is None else rot_pos.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs,
-                                     q_out_at, qos, self._status_at, torch._C._cuda_getCurrentRawStream(index))
+        code = _on_device(index, self._append_rope, plan, self._shape_ref, self._kv_ref, T, row_start.data_ptr(),
+                          None if pos_start is None else pos_start.data_ptr(), None if rot_pos is None else rot_pos.data_ptr(),
+                          k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs, q_out_at, qos, self._status_at,
+                          torch._C._cuda_getCurrentRawStream(index))
         if code:
             _check(code, "sx_kv_append_rope")
         return q_out
@@ -665,9 +672,9 @@ class LogProbs:
         n, out = self._results(T, tokens, top, out)
         if T == 0:
             return out
-        with _guard_of(self._index):
-            code = self._logprobs(dtype, T, V, logits.data_ptr(), stride[0] if T > 1 else V, n, tokens.data_ptr() if n else None,
-                                  temperature, top, self._out_ref, self._status_at, torch._C._cuda_getCurrentRawStream(self._index))
+        code = _on_device(self._index, self._logprobs, dtype, T, V, logits.data_ptr(), stride[0] if T > 1 else V, n,
+                          tokens.data_ptr() if n else None, temperature, top, self._out_ref, self._status_at,
+                          torch._C._cuda_getCurrentRawStream(self._index))
         if code:
             _check(code, "sx_logprobs")
         return out
