@@ -464,7 +464,7 @@ sx_status sx_set_sampling(sx_ctx *ctx, float temperature, uint64_t seed, uint32_
  *              of them or both; fp32
  * Logits of -inf (masked tokens) have no probability; a row of nothing else gives log p -inf and entropy 0.  A row with a NaN
  * or +inf among its logits gives NaN and ids of -1.  Sums are fp32: results are off by about 1e-6 absolute, and a log p by
- * 2^-22 of itself.  temperature > 0, and its inverse below 1e30. */
+ * 2^-22 of itself (one below fp32's range is -inf).  temperature > 0, and its inverse below 1e30. */
 #define SX_MAX_GIVEN 64
 #define SX_MAX_ALTERNATIVES 32
 #define SX_MAX_SCORE_VOCAB (1 << 24)

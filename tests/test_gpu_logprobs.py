@@ -91,6 +91,17 @@ def test_masked_rows(dtype, V):
     both(x, given(14, V, 4, 9), 20)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("temperature", [0.1, 0.7, 4.0])
+def test_lowest_values_at_other_temperatures(dtype, temperature):
+    """Masks of the type's lowest value whose log p leaves fp32's range, or not; rows of nothing else."""
+    x = make(6, 2001, dtype, 22).clone()
+    x[:3, 5:1900] = torch.finfo(dtype).min
+    x[3] = torch.finfo(dtype).min
+    x[4, 1:] = torch.finfo(dtype).min
+    both(x, given(6, 2001, 8, 23), 20, temperature)
+
+
 def test_masked_rows_of_a_cluster_where_one_part_has_everything():
     """One long row per case, over several CTAs: all parts but one masked or spoilt."""
     V = 200003
