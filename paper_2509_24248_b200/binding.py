@@ -618,8 +618,6 @@ class LogProbs:
             if not 0 < self.V <= rows or (hidden is not None and hidden != self.H):
                 raise SxError(f"head holds {rows} rows of {self.H}: it cannot have a vocabulary of {self.V} and a hidden size of {hidden or self.H}")
         self.status = torch.zeros(1, dtype=torch.int32, device=self.dev)
-        self._out = LogProbOut()
-        self._out_ref = C.byref(self._out)
         self._index, self._f32, self._status_at = self.dev.index, torch.empty(0, dtype=torch.float32, device=self.dev), self.status.data_ptr()
         self._logprobs, self._head_logprobs = self.lib.sx_logprobs, self.lib.sx_head_logprobs
         # a captured graph goes on using the workspace it was captured with, so one that became too small is kept
@@ -632,7 +630,7 @@ class LogProbs:
             _check(code, what)
 
     def _results(self, T: int, tokens: Optional[torch.Tensor], top: int, out: Optional[Dict[str, torch.Tensor]]):
-        """(number of given tokens, results), the argument block filled."""
+        """(number of given tokens, results, argument block - one of the call's own: another thread's call may come in between)."""
         index = self._index
         n = 0
         if tokens is not None:
@@ -641,7 +639,6 @@ class LogProbs:
             if (tokens.dtype is not torch.int32 or tokens.get_device() != index or not 1 <= len(shape) <= 2 or shape[0] != T
                     or not tokens.is_contiguous()):
                 raise SxError(f"tokens must be contiguous int32 [{T}, n_given] or [{T}] on {self.dev}")
-        o = self._out
         if out is None:
             if top < 0:
                 raise SxError("top must not be negative")
@@ -658,9 +655,11 @@ class LogProbs:
                         or t.get_device() != index or not t.is_contiguous()):
                     raise SxError(f"out[{name!r}] must be contiguous {list(want[name])} on {self.dev}")
             logp, entropy = out["logp"], out["entropy"]
-        o.logp_d, o.entropy_d = logp.data_ptr(), entropy.data_ptr()
-        o.top_tok_d, o.top_logp_d = (out["top_tok"].data_ptr(), out["top_logp"].data_ptr()) if top else (None, None)
-        return n, out
+        if top:
+            block = LogProbOut(logp.data_ptr(), entropy.data_ptr(), out["top_tok"].data_ptr(), out["top_logp"].data_ptr())
+        else:
+            block = LogProbOut(logp.data_ptr(), entropy.data_ptr())
+        return n, out, C.byref(block)
 
     def sx_logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0,
                     out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
@@ -669,11 +668,11 @@ class LogProbs:
         if len(shape) != 2 or logits.get_device() != self._index or dtype is None or (shape[1] > 1 and stride[1] != 1):
             raise SxError(f"logits must be bf16, fp16 or fp32 [T, V] on {self.dev}, rows contiguous")
         T, V = shape
-        n, out = self._results(T, tokens, top, out)
+        n, out, block = self._results(T, tokens, top, out)
         if T == 0:
             return out
         code = _on_device(self._index, self._logprobs, dtype, T, V, logits.data_ptr(), stride[0] if T > 1 else V, n,
-                          tokens.data_ptr() if n else None, temperature, top, self._out_ref, self._status_at,
+                          tokens.data_ptr() if n else None, temperature, top, block, self._status_at,
                           torch._C._cuda_getCurrentRawStream(self._index))
         if code:
             _check(code, "sx_logprobs")
@@ -689,7 +688,7 @@ class LogProbs:
                 or not hidden.is_contiguous()):
             raise SxError(f"hidden must be contiguous bf16 [T, {self.H}] on {self.dev}")
         T = shape[0]
-        n, out = self._results(T, tokens, top, out)
+        n, out, block = self._results(T, tokens, top, out)
         if T == 0:
             return out
         with _guard_of(self._index):
@@ -703,7 +702,7 @@ class LogProbs:
                     self._ws_bytes = need
                 self._ws_for = T
             code = self._head_logprobs(self.head.data_ptr(), 1 if self.tiled else 0, self.V, self.H, T, hidden.data_ptr(), n,
-                                       tokens.data_ptr() if n else None, temperature, top, self._out_ref, self._ws_at, self._ws_bytes,
+                                       tokens.data_ptr() if n else None, temperature, top, block, self._ws_at, self._ws_bytes,
                                        self._status_at, torch._C._cuda_getCurrentRawStream(self._index))
         if code:
             _check(code, "sx_head_logprobs")
