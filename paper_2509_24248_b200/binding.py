@@ -9,6 +9,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import os
+import threading
 from dataclasses import dataclass
 from typing import Dict, Optional
 
@@ -596,7 +597,8 @@ class LogProbs:
     two only with ``top > 0``), or fill the tensors of an ``out`` that an earlier call returned.  ``tokens`` is int32 ``[T, n_given]`` or
     ``[T]``; -1 stands for no token.  Work goes to the current stream of the device.  The object owns the workspace of
     ``sx_head_logprobs``: use one per stream, and one per captured graph that may run beside others, and keep it as long as
-    graphs captured through it."""
+    graphs captured through it.  Threads that work on one stream may share an object.  The head is read ahead of the stream's order: what writes or
+    repacks it has to be finished (a synchronisation) before a call."""
 
     def __init__(self, head: Optional[torch.Tensor] = None, vocab: Optional[int] = None, hidden: Optional[int] = None, device=None):
         self.lib = load_library()
@@ -622,6 +624,7 @@ class LogProbs:
         self._logprobs, self._head_logprobs = self.lib.sx_logprobs, self.lib.sx_head_logprobs
         # a captured graph goes on using the workspace it was captured with, so one that became too small is kept
         self._ws, self._ws_at, self._ws_bytes, self._ws_for = [], 0, 0, None
+        self._ws_lock = threading.Lock()              # both kernels of a call come before another thread's
 
     def check_status(self, what: str = "device") -> None:
         code = int(self.status.item())
@@ -691,7 +694,7 @@ class LogProbs:
         n, out, block = self._results(T, tokens, top, out)
         if T == 0:
             return out
-        with _guard_of(self._index):
+        with self._ws_lock, _guard_of(self._index):
             if self._ws_for != T:
                 # sizes of powers of two rows: however T grows, all workspaces together are at most twice the largest
                 rows = -(-T // -(-T // SX_SCORE_MAX_PART))

@@ -2,6 +2,7 @@
 the host (nothing is launched)."""
 from __future__ import annotations
 
+import threading
 import types
 
 import pytest
@@ -63,3 +64,63 @@ def test_a_call_keeps_its_own_results(on_host, monkeypatch):
     mine = s.sx_logprobs(x, tok, top=4)
     for got, want in zip(seen, (other[0], mine)):
         assert got == [want[n].data_ptr() for n in ("logp", "entropy", "top_tok", "top_logp")]
+
+
+def head_of(rows, H):
+    head = torch.zeros(rows, H, dtype=torch.bfloat16)
+    return types.SimpleNamespace(device=types.SimpleNamespace(type="cuda", index=-1), dtype=head.dtype, dim=head.dim, shape=head.shape,
+                                 is_contiguous=head.is_contiguous, data_ptr=head.data_ptr, numel=head.numel, keep=head)
+
+
+class Library:
+    """The C library with recorders for the calls that own a workspace: an entry waits until another thread is in too, or a while."""
+
+    def __init__(self, lib):
+        self.lib, self.inside, self.most, self.calls, self.guard = lib, 0, 0, [], threading.Lock()
+        self.second = threading.Event()
+
+    def __getattr__(self, name):
+        return getattr(self.lib, name)
+
+    def enter(self, call):
+        with self.guard:
+            self.inside += 1
+            self.most = max(self.most, self.inside)
+            self.calls.append(call)
+            if self.inside > 1:
+                self.second.set()
+        self.second.wait(0.3)
+        with self.guard:
+            self.inside -= 1
+        return 0
+
+    def sx_head_logprobs_ws_bytes(self, T, V):
+        return 1000 * T
+
+    def sx_head_logprobs(self, *args):
+        return self.enter((args[4], pointers(args[10]), args[11], args[12]))
+
+
+def run_all(calls):
+    threads = [threading.Thread(target=c) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(30)
+    assert not any(t.is_alive() for t in threads)
+
+
+def test_calls_through_a_head_come_one_after_the_other(on_host, monkeypatch):
+    """Both kernels of a call are on the stream before those of another thread's, since they share the object's workspace; the
+    workspace that a call is given has the size it is said to have."""
+    lib = Library(sx.load_library())
+    monkeypatch.setattr(sx, "load_library", lambda: lib)
+    s = sx.LogProbs(head_of(50, 16))
+    rows = {T: torch.zeros(T, 16, dtype=torch.bfloat16) for T in (3, 40, 7)}
+    tok = {T: torch.zeros(T, 2, dtype=torch.int32) for T in rows}
+    out = {}
+    run_all([lambda T=T: out.__setitem__(T, s.sx_head_logprobs(rows[T], tok[T], top=4)) for T in rows])
+    assert lib.most == 1 and sorted(c[0] for c in lib.calls) == sorted(rows)
+    for T, where, at, size in lib.calls:
+        assert where == [out[T][n].data_ptr() for n in ("logp", "entropy", "top_tok", "top_logp")]
+        assert size >= 1000 * T and any(w.data_ptr() <= at and at + size <= w.data_ptr() + w.numel() for w in s._ws)
