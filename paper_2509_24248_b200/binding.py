@@ -437,8 +437,8 @@ class KVPages:
         self._kv_ref = C.byref(self._kv)
         self.B = int(self._kv.batch)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.dev)
-        self._shape = KVShape(self.n_kv, self.n_kv, self.d, self.page)
-        self._shape_ref = C.byref(self._shape)
+        self._shapes = {}
+        self._shape_ref = self._shape_of(self.n_kv)
         self._append_rope, self._status_at = self.lib.sx_kv_append_rope, self.status.data_ptr()
 
     def check_status(self, what: str = "device") -> None:
@@ -465,6 +465,11 @@ class KVPages:
 
     def _guard(self):
         return _guard_of(self._index)
+
+    def _shape_of(self, n_q: int):
+        """Shape block for calls with n_q query heads, which no other call changes."""
+        ref = self._shapes.get(n_q)
+        return ref if ref is not None else self._shapes.setdefault(n_q, C.byref(KVShape(n_q, self.n_kv, self.d, self.page)))
 
     def sx_kv_append_rope(self, rope: Optional[Rope], k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor,
                           pos_start: Optional[torch.Tensor] = None, rot_pos: Optional[torch.Tensor] = None,
@@ -497,8 +502,7 @@ class KVPages:
             raise SxError("q_out without q")
         if T == 0:
             return q_out
-        self._shape.n_q_heads = nq
-        code = _on_device(index, self._append_rope, plan, self._shape_ref, self._kv_ref, T, row_start.data_ptr(),
+        code = _on_device(index, self._append_rope, plan, self._shape_of(nq), self._kv_ref, T, row_start.data_ptr(),
                           None if pos_start is None else pos_start.data_ptr(), None if rot_pos is None else rot_pos.data_ptr(),
                           k.data_ptr(), ks, v.data_ptr(), vs, q_at, qs, q_out_at, qos, self._status_at,
                           torch._C._cuda_getCurrentRawStream(index))
@@ -569,16 +573,16 @@ class KV8(KVPages):
             out = torch.empty(self.B, rows, nq, d, dtype=torch.bfloat16, device=self.dev)
         elif out.dtype is not torch.bfloat16 or out.device != self.dev or out.shape != shape or not out.is_contiguous():
             raise SxError("out must be contiguous bf16 of q's shape")
+        shape_ref = self._shape_of(nq)
         with self._guard():
-            self._shape.n_q_heads = nq
             if self._ws_for != (rows, nq):
-                need = int(self.lib.sx_attention_ws_bytes(self._shape_ref, self.B, rows, int(self._kv.n_groups)))
+                need = int(self.lib.sx_attention_ws_bytes(shape_ref, self.B, rows, int(self._kv.n_groups)))
                 if need > self._ws_bytes:
                     self._ws.append(torch.empty(need + 256, dtype=torch.uint8, device=self.dev))
                     self._ws_at = self._ws[-1].data_ptr() + (-self._ws[-1].data_ptr()) % 256
                     self._ws_bytes = need
                 self._ws_for = (rows, nq)
-            _check(self.lib.sx_attention(self._shape_ref, self._kv_ref, rows, drafted, q.data_ptr(), stride, _p(row_mask),
+            _check(self.lib.sx_attention(shape_ref, self._kv_ref, rows, drafted, q.data_ptr(), stride, _p(row_mask),
                                          d ** -0.5 if scale is None else scale, kernel, out.data_ptr(), self._ws_at,
                                          self._ws_bytes, self.status.data_ptr(), _raw_stream(self.dev)),
                    "sx_attention")

@@ -124,3 +124,31 @@ def test_calls_through_a_head_come_one_after_the_other(on_host, monkeypatch):
     for T, where, at, size in lib.calls:
         assert where == [out[T][n].data_ptr() for n in ("logp", "entropy", "top_tok", "top_logp")]
         assert size >= 1000 * T and any(w.data_ptr() <= at and at + size <= w.data_ptr() + w.numel() for w in s._ws)
+
+
+def cache(monkeypatch, kind, lib=None):
+    """A cache of 2 sequences with 2 heads of 64, its device block made without a device."""
+    if lib is not None:
+        monkeypatch.setattr(sx, "load_library", lambda: lib)
+    monkeypatch.setattr(sx, "_kv_struct", lambda kv, *_: sx.KV(2, 256, 256, 4, 8, 256, 256))
+    c = kind(dict(k_pages=torch.zeros(8, 2, 16, 64, dtype=torch.uint8), cache_len=torch.zeros(2, dtype=torch.int32)))
+    c._index = -1
+    return c
+
+
+def test_an_append_keeps_its_number_of_query_heads(on_host, monkeypatch):
+    """An append without queries that comes in while one with queries is on its way into the library."""
+    c = cache(monkeypatch, sx.KVPages)
+    qkv, start = torch.zeros(3, 10, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    seen = []
+
+    def entry(*args):
+        if not seen:
+            seen.append(None)
+            c.sx_kv_append_rope(None, qkv[:, 6:8], qkv[:, 8:], start)
+        seen.append((args[1]._obj.n_q_heads, args[11]))
+        return 0
+
+    monkeypatch.setattr(c, "_append_rope", entry)
+    c.sx_kv_append_rope(None, qkv[:, 6:8], qkv[:, 8:], start, q=qkv[:, :6])
+    assert seen[1:] == [(0, None), (6, qkv.data_ptr())]
