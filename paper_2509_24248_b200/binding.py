@@ -423,7 +423,7 @@ class KVPages:
     ``page_table`` (int32 ``[B, max_pages]``), ``cache_len`` (int32 ``[B]``) and for codes ``k_scale`` / ``v_scale`` (uint8
     ``[num_pages, n_kv, page]``): the tensors of :class:`KV8` or of :meth:`SpecExit.set_kv` (``KVPages(spec.kv)`` writes a prompt
     into a draft layer's cache).  The tensors are borrowed; what they hold may change between calls.  Work goes to the
-    current stream of their device."""
+    current stream of their device.  Threads and streams may share an object."""
 
     def __init__(self, kv: Dict[str, torch.Tensor]):
         self.lib = load_library()
@@ -519,7 +519,8 @@ class KV8(KVPages):
     ``[B]``) and, for sequences that share a prefix, ``group_start`` (int32 ``[n_groups + 1]``) with ``prefix_len``
     (int32 ``[n_groups]``).  The tensors are borrowed; what they hold may change between calls.  Work goes to the
     current stream of their device.  The object owns the attention's workspace: use one per stream, and one per captured
-    graph that may run beside others, and keep it as long as graphs captured through it."""
+    graph that may run beside others, and keep it as long as graphs captured through it.  Threads that work on one stream may
+    share an object."""
 
     def __init__(self, kv: Dict[str, torch.Tensor]):
         if kv["k_pages"].dim() != 4 or kv["k_pages"].element_size() != 1:
@@ -527,6 +528,7 @@ class KV8(KVPages):
         super().__init__(kv)
         # a captured graph goes on using the workspace it was captured with, so one that became too small is kept
         self._ws, self._ws_at, self._ws_bytes, self._ws_for = [], 0, 0, None
+        self._ws_lock = threading.Lock()              # all launches of an attention come before another thread's
 
     def sx_kv_append(self, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor,
                      pos_start: Optional[torch.Tensor] = None) -> None:
@@ -574,7 +576,7 @@ class KV8(KVPages):
         elif out.dtype is not torch.bfloat16 or out.device != self.dev or out.shape != shape or not out.is_contiguous():
             raise SxError("out must be contiguous bf16 of q's shape")
         shape_ref = self._shape_of(nq)
-        with self._guard():
+        with self._ws_lock, self._guard():
             if self._ws_for != (rows, nq):
                 need = int(self.lib.sx_attention_ws_bytes(shape_ref, self.B, rows, int(self._kv.n_groups)))
                 if need > self._ws_bytes:

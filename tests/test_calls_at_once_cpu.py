@@ -152,3 +152,24 @@ def test_an_append_keeps_its_number_of_query_heads(on_host, monkeypatch):
     monkeypatch.setattr(c, "_append_rope", entry)
     c.sx_kv_append_rope(None, qkv[:, 6:8], qkv[:, 8:], start, q=qkv[:, :6])
     assert seen[1:] == [(0, None), (6, qkv.data_ptr())]
+
+
+class Attention(Library):
+    def sx_attention_ws_bytes(self, shape, batch, rows, groups):
+        return 1000 * rows * shape._obj.n_q_heads
+
+    def sx_attention(self, *args):
+        return self.enter((args[2], args[4], args[0]._obj.n_q_heads, args[10], args[11]))
+
+
+def test_attention_calls_come_one_after_the_other(on_host, monkeypatch):
+    """The launches of an attention over the object's workspace, and its number of query heads, beside other threads' calls."""
+    lib = Attention(sx.load_library())
+    c = cache(monkeypatch, sx.KV8, lib)
+    monkeypatch.setattr(sx, "_raw_stream", lambda dev: 0)
+    q = {n: torch.zeros(2, rows, n, 64, dtype=torch.bfloat16) for rows, n in ((1, 2), (8, 16), (3, 4))}
+    run_all([lambda n=n: c.sx_attention(q[n], kernel=sx.ATTN_AUTO) for n in q])
+    assert lib.most == 1 and len(lib.calls) == 3
+    for rows, at, n, ws, size in lib.calls:
+        assert at == q[n].data_ptr() and rows == q[n].shape[1] and size >= 1000 * rows * n
+        assert any(w.data_ptr() <= ws and ws + size <= w.data_ptr() + w.numel() for w in c._ws)
