@@ -285,9 +285,11 @@ template <> struct ScoreElem<float> {
   static __device__ __forceinline__ float one(float x) { return x; }
 };
 
+// Volatile, with a clobber and on the coherent path: the kernel may start while the one that writes the logits still runs, so no load of
+// them may move before sx_pdl_wait (nor is `logits` __restrict__, which would allow the non-coherent path for the others).
 __device__ __forceinline__ void score_load32(const void *p, uint32_t *w) {
-  asm("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-      : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+  asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+      : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
 }
 
 template <typename E>
@@ -379,7 +381,7 @@ struct ScorePlain {
 // first boundary is group 0, what is behind the last whole group the last one (their elements one per lane, by the first
 // warp of the row).
 template <typename E, int W>
-__global__ void __launch_bounds__(W * 32, 32 / W) sx_score_kernel(const SxScoreArgs p, const E *__restrict__ logits, int64_t stride, int cluster) {
+__global__ void __launch_bounds__(W * 32, 32 / W) sx_score_kernel(const SxScoreArgs p, const E *logits, int64_t stride, int cluster) {
   constexpr int GE = SCORE_GROUP_BYTES / (int)sizeof(E);
   __shared__ ScoreShared sh;
   if (threadIdx.x == 0) sh.floor = -INFINITY;
