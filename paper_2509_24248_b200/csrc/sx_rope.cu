@@ -514,10 +514,11 @@ static int lanes_per_row(int d) { int l = 4; while (l * 8 < d) l <<= 1; return l
 // them, down to one row per lane (4, 8, 16, 32, 64 warps per SM: 512 tokens of 40 heads 6.1, 5.7, 5.3, 7.4, 7.8 us; 2048 of them the same
 // within a tenth).
 static sx_status rope_grid(SxRopeArgs *p, unsigned *grid) {
+  if (p->T > 0x7ffffff0) return SX_ERR_UNSUPPORTED;                    // warps are counted in 32 bits
   const int all = p->nq + p->nk + p->nv, G = 32 / lanes_per_row(p->D);
   const int sm = sx_sm_count();
   if (!sm) return SX_ERR_CUDA;
-  int slices = (16 * sm + p->T - 1) / p->T, most = (all + G - 1) / G;
+  int slices = 1 + (16 * sm - 1) / p->T, most = (all + G - 1) / G;     // 16 sm / T rounded up
   if (slices > most) slices = most;
   p->rows_per_warp = ((all + slices - 1) / slices + G - 1) / G * G;
   p->slices = (all + p->rows_per_warp - 1) / p->rows_per_warp;
