@@ -611,8 +611,8 @@ extern "C" sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void
 
 // Rows are taken SX_SCORE_MAX_PART at a time at most, in as few equal parts as that allows: every part reads the whole head.
 static int score_part(int T) {
-  const int parts = (T + SX_SCORE_MAX_PART - 1) / SX_SCORE_MAX_PART;
-  return (T + parts - 1) / parts;
+  const int parts = 1 + (T - 1) / SX_SCORE_MAX_PART;        // rounded up; T may be as large as 32 bits hold
+  return 1 + (T - 1) / parts;
 }
 
 struct ScoreWs { size_t logits, maxima, sums, total; };
@@ -656,8 +656,8 @@ extern "C" sx_status sx_head_logprobs(const void *head_d, int32_t tiled, int32_t
   const bf16 *head = (const bf16 *)head_d, *rows = (const bf16 *)hidden_d;
   const int tiles = (V + SX_TILE_M - 1) / SX_TILE_M;
   cudaStream_t st = (cudaStream_t)stream;
-  for (int r0 = 0; r0 < T; r0 += part) {
-    const int R = T - r0 < part ? T - r0 : part;
+  for (int r0 = 0, R; r0 < T; r0 += R) {
+    R = T - r0 < part ? T - r0 : part;
     int parts = 0;
     if (part <= SX_SCORE_FEW) SX_TRY(sx_launch_score_head(head, tiled != 0, V, H, rows + (size_t)r0 * H, R, o, &parts, sm, status_d, st));
     else SX_TRY(sx_launch_score_pairs(head, tiled != 0, V, H, rows + (size_t)r0 * H, R, o, &parts, status_d, st));
