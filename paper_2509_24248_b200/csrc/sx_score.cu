@@ -351,7 +351,7 @@ struct ScorePlain {
       }
       a.m = gm;
       r = to;
-      limit = gm + slack;
+      limit = fminf(gm + slack, 3.402823466e38f);     // an infinite logit is above it at any temperature
     }
     float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;       // of this group: short sums of small numbers, added to the long ones once
     score_pairs<E>(w, [&](float2 x) {
