@@ -234,7 +234,7 @@ __device__ __forceinline__ void score_write(const ScoreShared &sh, const SxScore
   const float m = sh.row[0], s = sh.row[1], t = sh.row[2], LN2 = 0.6931471805599453f, NaN = __int_as_float(0x7fffffff);
   const bool bad = !(s >= 0.f) || m == INFINITY, none = !bad && m == -INFINITY;
   const float ln = none ? 0.f : logf(s);
-  const auto log_p = [&](float x) { return fmaf(x - m, p.inverse, -ln); };
+  const auto log_p = [&](float x) { return fmaf(fmaf(x, 0.5f, -0.5f * m), 2.f * p.inverse, -ln); };      // as score_gap
 #pragma unroll
   for (int j = 0; j < ScoreGiven<W>::N; ++j) {
     const int i = threadIdx.x + j * W * 32;

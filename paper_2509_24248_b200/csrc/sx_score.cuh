@@ -15,13 +15,17 @@ __device__ __forceinline__ float score_max_nan(float a, float b) {
   return y;
 }
 
+// (a - b) * by, rounded as that is but for differences beyond fp32's range, which halves keep in it (by up to 2^100): logits at both
+// ends of it are close together at a high temperature.
+__device__ __forceinline__ float score_gap(float a, float b, float by) { return fmaf(a, 0.5f, -0.5f * b) * (2.f * by); }
+
 struct ScoreSum {
   float m, s, t;
   __device__ __forceinline__ void clear() { m = -INFINITY; s = t = 0.f; }
   // a new reference; sums of nothing have none
   __device__ __forceinline__ void raise(float to, float scale) {
     if (m > -INFINITY) {
-      const float d = fmaxf((m - to) * scale, -200.f), f = score_exp2(d);
+      const float d = fmaxf(score_gap(m, to, scale), -200.f), f = score_exp2(d);
       t = f * fmaf(s, d, t);
       s *= f;
     }
@@ -31,7 +35,7 @@ struct ScoreSum {
     if (os == 0.f) return;
     if (om > m) raise(om, scale);
     if (om == m || !(om > -INFINITY)) { s += os; t += ot; return; }         // equal references, or a NaN without one
-    const float d = fmaxf((om - m) * scale, -200.f), f = score_exp2(d);
+    const float d = fmaxf(score_gap(om, m, scale), -200.f), f = score_exp2(d);
     t += f * fmaf(os, d, ot);
     s = fmaf(os, f, s);
   }
@@ -47,7 +51,7 @@ struct ScoreSum {
 // Two more elements.  Nothing below 2^-126 of the reference counts; holding d to -200 keeps 0 * -inf out of t.  (Packed fp32
 // pairs were tried: the moves that bring the pairs together cost more than the instructions saved.)
 __device__ __forceinline__ void score_pair(float2 x, float scale, float ref, float2 &s, float2 &t) {
-  const float d0 = score_max_nan((x.x - ref) * scale, -200.f), d1 = score_max_nan((x.y - ref) * scale, -200.f);
+  const float d0 = score_max_nan(score_gap(x.x, ref, scale), -200.f), d1 = score_max_nan(score_gap(x.y, ref, scale), -200.f);
   const float e0 = score_exp2(d0), e1 = score_exp2(d1);
   s.x += e0;
   s.y += e1;
