@@ -608,7 +608,7 @@ class LogProbs:
 
     def __init__(self, head: Optional[torch.Tensor] = None, vocab: Optional[int] = None, hidden: Optional[int] = None, device=None):
         self.lib = load_library()
-        self.dev = head.device if head is not None else torch.device(device or f"cuda:{torch.cuda.current_device()}")
+        self.dev = head.device if head is not None else torch.device("cuda" if device is None else device)
         if self.dev.type != "cuda":
             raise SxError("a CUDA device is required (there is no CPU fallback)")
         if self.dev.index is None:

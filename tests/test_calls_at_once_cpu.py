@@ -173,3 +173,13 @@ def test_attention_calls_come_one_after_the_other(on_host, monkeypatch):
     for rows, at, n, ws, size in lib.calls:
         assert at == q[n].data_ptr() and rows == q[n].shape[1] and size >= 1000 * rows * n
         assert any(w.data_ptr() <= ws and ws + size <= w.data_ptr() + w.numel() for w in c._ws)
+
+
+def test_device_0_is_device_0(monkeypatch):
+    """A device given by its number, 0 among them, is not the current one."""
+    asked = []
+    monkeypatch.setattr(sx, "torch", HostTorch())
+    monkeypatch.setattr(HostTorch, "device", staticmethod(lambda *a: asked.append(a) or types.SimpleNamespace(type="cuda", index=-1)))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    sx.LogProbs(device=0)
+    assert asked == [(0,)]
