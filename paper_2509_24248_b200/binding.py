@@ -31,6 +31,8 @@ ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_NONE, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS, ROPE_RAMP, ROPE_LIST = 0, 1, 2, 3, 4, 5
 SX_ROPE_MAX_PAIRS = 128
 SX_SCORE_MAX_PART = 1024
+SX_MAX_GIVEN, SX_MAX_ALTERNATIVES = 64, 32
+INT32_MAX = 2 ** 31 - 1                  # of a size that a call takes: ctypes would cut a larger one off
 SMOOTH_EWMA, SMOOTH_NONE, SMOOTH_WINDOW, SMOOTH_MOMENTUM, SMOOTH_PARAGRAPH = 0, 1, 2, 3, 4
 HIST = 16
 
@@ -351,8 +353,8 @@ def _heads_stride(name: str, t: torch.Tensor, dtype: torch.dtype, T: int, heads:
     """Row stride of ``t [T, heads, d]`` on device `index` whose heads lie side by side."""
     shape, stride = t.shape, t.stride()
     if (t.dtype is not dtype or t.get_device() != index or shape != (T, heads, d) or (stride[2] != 1 and d > 1)
-            or (stride[1] != d and heads > 1)):
-        raise SxError(f"{name} must be {dtype} [{T}, {heads}, {d}] on cuda:{index}, rows of heads contiguous")
+            or (stride[1] != d and heads > 1) or T > INT32_MAX or heads > INT32_MAX):
+        raise SxError(f"{name} must be {dtype} [{T}, {heads}, {d}] on cuda:{index}, rows of heads contiguous, sizes of 32 bits")
     return stride[0] if T > 1 else heads * d
 
 
@@ -623,7 +625,7 @@ class LogProbs:
             self.H = int(hidden) if self.tiled else int(head.shape[1])
             self.V = int(vocab) if vocab is not None else int(head.shape[0])
             rows = head.numel() * 2 // max(1, int(self.lib.sx_tiled_weight_bytes(128, self.H))) * 128 if self.tiled else int(head.shape[0])
-            if not 0 < self.V <= rows or (hidden is not None and hidden != self.H):
+            if not 0 < self.V <= min(rows, INT32_MAX) or self.H > INT32_MAX or (hidden is not None and hidden != self.H):
                 raise SxError(f"head holds {rows} rows of {self.H}: it cannot have a vocabulary of {self.V} and a hidden size of {hidden or self.H}")
         self.status = torch.zeros(1, dtype=torch.int32, device=self.dev)
         self._index, self._f32, self._status_at = self.dev.index, torch.empty(0, dtype=torch.float32, device=self.dev), self.status.data_ptr()
@@ -648,9 +650,9 @@ class LogProbs:
             if (tokens.dtype is not torch.int32 or tokens.get_device() != index or not 1 <= len(shape) <= 2 or shape[0] != T
                     or not tokens.is_contiguous()):
                 raise SxError(f"tokens must be contiguous int32 [{T}, n_given] or [{T}] on {self.dev}")
+        if T > INT32_MAX or n > SX_MAX_GIVEN or not 0 <= top <= SX_MAX_ALTERNATIVES:
+            raise SxError(f"{T} rows, {n} tokens, {top} alternatives: at most 2^31 - 1, {SX_MAX_GIVEN} and {SX_MAX_ALTERNATIVES}")
         if out is None:
-            if top < 0:
-                raise SxError("top must not be negative")
             f, i = self._f32, self.status
             logp, entropy = f.new_empty((T, n)), f.new_empty((T,))
             out = {"logp": logp, "entropy": entropy}
@@ -677,6 +679,8 @@ class LogProbs:
         if len(shape) != 2 or logits.get_device() != self._index or dtype is None or (shape[1] > 1 and stride[1] != 1):
             raise SxError(f"logits must be bf16, fp16 or fp32 [T, V] on {self.dev}, rows contiguous")
         T, V = shape
+        if V > INT32_MAX:
+            raise SxError(f"{V} logits in a row")
         n, out, block = self._results(T, tokens, top, out)
         if T == 0:
             return out
