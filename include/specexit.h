@@ -371,7 +371,10 @@ sx_status sx_rope(const sx_rotation *plan, int32_t dtype, int32_t transpose, int
  * (shape->n_q_heads heads, strides as in sx_rope) are turned in the same launch to q_out_d, which may be q_d.  plan NULL:
  * nothing is turned, the keys are as the attention wants them.  Rows, slots, refusals and reports as in sx_kv_append; rows
  * behind the last sequence stay as they are in q_out_d too, and of a row that is reported the queries may or may not be
- * written.  head_dim 16, 32, 64 or 128. */
+ * written.  head_dim 16, 32, 64 or 128.
+ * A cache that a draft layer reads (sx_draft_step) takes one rotation alone, which this call cannot check: whole heads in
+ * SX_ROPE_HALF order, the model's rope_theta, no scaling, magnitude 1, every key at the position of its slot - that is how the
+ * draft turns its own rows. */
 sx_status sx_kv_append_rope(const sx_rotation *plan, const sx_kv_shape *shape, const sx_kv *kv, int32_t T,
                             const int32_t *row_start_d, const int32_t *pos_start_d, const int32_t *rot_pos_d, const void *k_d,
                             int64_t k_stride, const void *v_d, int64_t v_stride, const void *q_d, int64_t q_stride,

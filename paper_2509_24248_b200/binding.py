@@ -383,6 +383,14 @@ class Rope:
         _check(self.lib.sx_rope_plan(C.byref(cfg), self.plan_ref), "sx_rope_plan")
         self.d, self._call = head_dim, self.lib.sx_rope
 
+    def turns_as(self, theta: float) -> bool:
+        """Whether this is the rotation of a draft layer with that ``theta``: whole heads in the half order, no scaling that changes a
+        frequency by more than 2^-23 of itself (a context holds theta in fp32), magnitude 1."""
+        if self.plan.rot_dim != self.d or self.plan.layout != ROPE_HALF or self.plan.magnitude != 1.0:
+            return False
+        own = Rope(self.d, theta).plan.step
+        return all(abs(a - b) <= (b >> 23) + 8192 for a, b in zip(self.plan.step, own))      # 8192: 2^-20 turns at any position
+
     def sx_rope(self, pos: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
                 k_out: Optional[torch.Tensor] = None, transpose: bool = False):
         """Turns ``q [T, n_q, d]`` and, in the same launch, ``k [T, n_k, d]`` (bf16, fp16 or fp32, slices of a projection's
@@ -418,13 +426,22 @@ class Rope:
         return q_out, k_out
 
 
+class DraftCache(dict):
+    """The tensors of a draft layer's cache, and the theta that its rounds turn their rows by."""
+
+    def __init__(self, kv: Dict[str, torch.Tensor], theta: float):
+        super().__init__(kv)
+        self.theta = theta
+
+
 class KVPages:
     """A paged cache of either kind and the writing of rows into it (no draft model needed).
 
     ``kv`` holds ``k_pages`` / ``v_pages`` (bf16, or uint8 / float8_e4m3fn codes, ``[num_pages, n_kv, page, d]``),
     ``page_table`` (int32 ``[B, max_pages]``), ``cache_len`` (int32 ``[B]``) and for codes ``k_scale`` / ``v_scale`` (uint8
     ``[num_pages, n_kv, page]``): the tensors of :class:`KV8` or of :meth:`SpecExit.set_kv` (``KVPages(spec.kv)`` writes a prompt
-    into a draft layer's cache).  The tensors are borrowed; what they hold may change between calls.  Work goes to the
+    into a draft layer's cache; its rounds turn whole heads in the half order by the model's theta alone, so no other rotation is
+    taken, and the positions have to be the slots).  The tensors are borrowed; what they hold may change between calls.  Work goes to the
     current stream of their device.  Threads and streams may share an object."""
 
     def __init__(self, kv: Dict[str, torch.Tensor]):
@@ -439,6 +456,7 @@ class KVPages:
         self._kv_ref = C.byref(self._kv)
         self.B = int(self._kv.batch)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.dev)
+        self._theta, self._rope = getattr(kv, "theta", None), None      # of a draft layer's cache, and a rotation known to fit it
         self._shapes = {}
         self._shape_ref = self._shape_of(self.n_kv)
         self._append_rope, self._status_at = self.lib.sx_kv_append_rope, self.status.data_ptr()
@@ -491,6 +509,10 @@ class KVPages:
         if rope is not None:
             if rope.d != d:
                 raise SxError(f"rope is planned for heads of {rope.d}, the cache has {d}")
+            if self._theta is not None and self._rope is not rope:
+                if not rope.turns_as(self._theta):
+                    raise SxError(f"the draft layer of this cache turns whole heads in the half order by theta = {self._theta:g} alone")
+                self._rope = rope
             plan = rope.plan_ref
         nq, q_at, q_out_at, qs, qos = 0, None, None, 0, 0
         if q is not None:
@@ -796,13 +818,13 @@ class SpecExit:
         :class:`KV8` takes, shared prefixes included."""
         d = self.dev
         if "k_scale" in kv:
-            self.kv = {n: kv[n].to(d).contiguous() for n in _CACHE_NAMES if kv.get(n) is not None}
+            self.kv = DraftCache({n: kv[n].to(d).contiguous() for n in _CACHE_NAMES if kv.get(n) is not None}, self.shape.theta)
             self._kv_struct = _kv_struct(self.kv, self.shape.n_kv, self.shape.page, self.shape.d)
             self.B = int(self._kv_struct.batch)
             return
-        self.kv = {"k_pages": kv["k_pages"].to(d), "v_pages": kv["v_pages"].to(d),
-                   "page_table": kv["page_table"].to(d).contiguous(),
-                   "cache_len": kv["cache_len"].to(d).contiguous()}
+        self.kv = DraftCache({"k_pages": kv["k_pages"].to(d), "v_pages": kv["v_pages"].to(d),
+                              "page_table": kv["page_table"].to(d).contiguous(),
+                              "cache_len": kv["cache_len"].to(d).contiguous()}, self.shape.theta)
         B = int(self.kv["cache_len"].numel())
         self.B = B
         self._kv_struct = KV(B, self.kv["cache_len"].data_ptr(), self.kv["page_table"].data_ptr(),

@@ -126,12 +126,13 @@ def test_calls_through_a_head_come_one_after_the_other(on_host, monkeypatch):
         assert size >= 1000 * T and any(w.data_ptr() <= at and at + size <= w.data_ptr() + w.numel() for w in s._ws)
 
 
-def cache(monkeypatch, kind, lib=None):
-    """A cache of 2 sequences with 2 heads of 64, its device block made without a device."""
+def cache(monkeypatch, kind, lib=None, theta=None):
+    """A cache of 2 sequences with 2 heads of 64, its device block made without a device; theta: a draft layer's."""
     if lib is not None:
         monkeypatch.setattr(sx, "load_library", lambda: lib)
     monkeypatch.setattr(sx, "_kv_struct", lambda kv, *_: sx.KV(2, 256, 256, 4, 8, 256, 256))
-    c = kind(dict(k_pages=torch.zeros(8, 2, 16, 64, dtype=torch.uint8), cache_len=torch.zeros(2, dtype=torch.int32)))
+    kv = dict(k_pages=torch.zeros(8, 2, 16, 64, dtype=torch.uint8), cache_len=torch.zeros(2, dtype=torch.int32))
+    c = kind(kv if theta is None else sx.DraftCache(kv, theta))
     c._index = -1
     return c
 
