@@ -466,8 +466,9 @@ sx_status sx_set_sampling(sx_ctx *ctx, float temperature, uint64_t seed, uint32_
  *   out        logp_d [T, n_given], entropy_d [T] (sum of -p log p) or NULL, top_tok_d [T, top], top_logp_d [T, top], either
  *              of them or both; fp32
  * Logits of -inf (masked tokens) have no probability; a row of nothing else gives log p -inf and entropy 0.  A row with a NaN
- * or +inf among its logits gives NaN and ids of -1.  Sums are fp32: results are off by about 1e-6 absolute, and a log p by
- * 2^-22 of itself (one below fp32's range is -inf).  temperature > 0, and its inverse below 1e30. */
+ * or +inf among its logits gives NaN and ids of -1.  Sums are fp32: results are typically off by
+ * less than 1e-6 beside their own rounding, a log p at worst by D + 2^-22 (1 + |log p|) with D = 2^-21 + (V / 1024 + 100) 2^-24 (1.5e-5 at
+ * V = 151936) and an entropy by D (22 + log2 V); a log p below fp32's range is -inf.  temperature > 0, and its inverse below 1e30. */
 #define SX_MAX_GIVEN 64
 #define SX_MAX_ALTERNATIVES 32
 #define SX_MAX_SCORE_VOCAB (1 << 24)
@@ -481,7 +482,9 @@ sx_status sx_logprobs(int32_t dtype, int32_t T, int32_t V, const void *logits_d,
                       void *stream);
 
 /* The same from hidden states: logits = hidden . head^T are formed tile by tile on the tensor cores (fp32, in chains of
- * at most 512 products whose sums are added with rounding to nearest), their softmax sums taken on the way.  Beside sx_verify, which gives the argmax of the same product alone.
+ * at most 512 products whose sums are added with rounding to nearest: a logit is off by 7e-7 of the sum of its products' magnitudes
+ * where they have one sign, at worst by 2.5e-6 of it up to H = 8192), their softmax sums taken on the way.  Beside sx_verify, which
+ * gives the argmax of the same product alone.
  *   head_d    [V, H] bf16 row-major, or repacked by sx_tile_weight (tiled = 1; rows behind the first V, such as signal rows,
  *             may follow and are not looked at); complete and visible before the call (see the conventions)
  *   hidden_d  [T, H] bf16, contiguous; H a multiple of 8
