@@ -323,8 +323,9 @@ sx_status sx_kv_append(const sx_kv_shape *shape, const sx_kv *kv, int32_t T, con
 
 /* Rotary positions.  A head's rotated part, rot_dim elements from rot_start on, is rot_dim / 2 pairs: (x[i], x[i + rot_dim / 2])
  * in SX_ROPE_HALF, (x[2 i], x[2 i + 1]) in SX_ROPE_INTERLEAVED; the other elements of the head stay as they are.  At position
- * pos pair i = (u, v) becomes magnitude * (u cos a - v sin a, v cos a + u sin a), a = pos * f_i, modulo one turn exact to
- * pos * 2^-64 turns; cos, sin and products are fp32 (fp64 for keys that go into an 8-bit cache), the result is rounded once.
+ * pos pair i = (u, v) becomes magnitude * (u cos a - v sin a, v cos a + u sin a), a = pos * f_i modulo one turn, exact to
+ * pos * 2^-64 turns and then cut off at 2^-32 turns; cos, sin and products are fp32 (for keys that go into an 8-bit cache nothing is
+ * cut off and they are fp64), the result is rounded once.
  * f_i = theta^(-2 i / rot_dim), and with a scaling for contexts longer than the trained one (F = factor, n_i = original_len *
  * f_i / 2 pi turns over the trained length):
  *   SX_ROPE_LINEAR  f_i / F

@@ -6,7 +6,8 @@
 // turn: in fp32 a position of 10^5 alone costs it 0.01 rad.  The plan keeps f_i / 2 pi as a 64-bit fraction of a turn, so
 // that pos * f_i modulo one turn is one 64-bit integer product, whatever the position (off by pos * 2^-64 turns); its
 // quadrant is taken off as an integer too, and what is left, at most an eighth of a turn, is small enough for a short series.  cos,
-// sin and the products are fp32 (fp64 for keys that become codes), the result is rounded once.
+// sin and the products are fp32, of the angle's upper 32 bits (cut off at 2^-32 turns, 1.5e-9 rad, a fortieth of what fp32 makes of
+// a cosine); fp64, of all 64, for keys that become codes.  The result is rounded once.
 //
 // Bound by bytes: every element is read and written once, three flops on the way.  A row (a head of a token) belongs to
 // d / 8 neighbouring lanes with 8 elements each, 16-byte accesses; the partner half comes from another lane by shuffle,
@@ -72,7 +73,8 @@ __device__ __forceinline__ void rope_angle(uint64_t step, int pos, double mag, f
   *s = magnitude * ((quad & 2) ? -v : v);
 }
 
-// The same to 2^-45, for rows that are going to be rounded to codes (see rope_turn).
+// The same with all 64 bits of the angle, for rows that are going to be rounded to codes (see rope_turn): the series to x^13 and x^12 are
+// off by 2^-45 and 2^-41 at most.
 __device__ __forceinline__ void rope_angle(uint64_t step, int pos, double magnitude, double *c, double *s) {
   const uint64_t ph = step * (uint64_t)(int64_t)pos;
   const uint32_t quad = (uint32_t)((ph + (1ull << 61)) >> 62);
