@@ -715,7 +715,8 @@ class LogProbs:
 
     def sx_head_logprobs(self, hidden: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0, temperature: float = 1.0,
                          out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
-        """Of hidden states (bf16 ``[T, H]``, contiguous) through the head, without a matrix of logits in the caller's hands."""
+        """Of hidden states (bf16 ``[T, H]``, contiguous) through the head, without a matrix of logits in the caller's hands (the
+        object's workspace holds one: 4.2 bytes per row and token id, of up to 1024 rows)."""
         if self.head is None:
             raise SxError("this object was made without a head")
         shape = hidden.shape

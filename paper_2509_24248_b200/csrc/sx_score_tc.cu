@@ -11,8 +11,8 @@
 // token row and half of the tile's columns; softmax sums and maxima of groups of 32 need no exchange between threads.
 //
 // Measured, 1000 rows, H = 4096, 151936 tokens (1.24 TFLOP): 0.92 ms by itself (1.35 PFLOP/s, 0.96 of what the library's product holds
-// under the power cap, tensor pipe active 77-79 % of the cycles), 1.00-1.24 ms a call with the finishing kernel on different
-// boxes.  Chains of 256 products instead of 512 cost 5 % more, of 1024 6 % less.  Asking the L2 for weights 16 k-blocks ahead cost
+// under the power cap, tensor pipe active 77-79 % of the cycles), 0.97-1.24 ms a call with the finishing kernel on different
+// boxes.  Chains of 256 products instead of 512 cost 7 % more, of 384 2 % more, of 1024 6 % less.  Asking the L2 for weights 16 k-blocks ahead cost
 // 3-14 %.
 //
 // Per CTA 320 threads: warp 0 TMA producer, warp 1 MMA issuer (the first CTA's; both hold the TMEM allocation), warps 2-9 epilogue.
