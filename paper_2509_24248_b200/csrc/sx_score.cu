@@ -13,7 +13,7 @@
 // others are before it, and the elements of the k best groups go through lists of the same kind.  The cost does not depend on
 // the values but for the number of insertions.
 //
-// Measured: 4096 rows of 151936 in bf16 with five alternatives 217-253 us on different boxes (1.24 GB, 4.9-5.7 TB/s; 190 us at the copy
+// Measured: 4096 rows of 151936 in bf16 with five alternatives 217-256 us on different boxes (1.24 GB, 4.9-5.7 TB/s; 190 us at the copy
 // rate), one row with twenty 12.7-13.9 us, 244 rows of 32001 in fp32, half of them masked, 15.2 us.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
